@@ -292,6 +292,121 @@ int accerl_vtrace(const float* logits_original, const float* logits_smaller, con
                   float* out_vs, float* out_pg_adv, float* out_rho, void* hip_stream);
 
 /*
+ * Operators of wide policies: an action set of up to 2^20 (tokens), dense layers whose inputs have no calibrated scale.
+ *
+ * Tensors here may have rows of any stride (`ld_*`: elements from one row to the next, at least the row's length) and any
+ * alignment of whole elements, unless said otherwise; elements of a row are contiguous.
+ */
+typedef enum { ACCERL_DT_F32 = 0, ACCERL_DT_BF16 = 1, ACCERL_DT_F16 = 2 } accerl_dtype;
+
+/*
+ * Packed int8 rows: the layout in which the int8 product reads both of its operands.  Tiles of 16 rows by 64 columns of 1024 bytes,
+ * [row / 16][column / 64][(column % 64) / 16][row % 16][column % 16], rows padded to a multiple of 16 and columns with zeros to a
+ * multiple of 128.  accerl_packed_rows_bytes gives the size of the buffer (DEVICE, 16-byte aligned; negative: an accerl_status).
+ * At most 2^24 rows and 2^16 columns (ACCERL_EUNSUPPORTED above).
+ */
+int64_t accerl_packed_rows_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Quantises every row with a scale of its own (Section 2.2 "Parameter Quantization", symmetric, here with the scale found from
+ * the row itself): with m_r = max_c |x[r,c]|,
+ *     out_scale[r] = m_r / 127,    q[r,c] = rint(x[r,c] * 127 / m_r), ties to even, rounded once from the exact quotient
+ * A row of zeros has scale 0.  A row that holds an infinity or a NaN has that (or NaN) as its scale and zeros, so that a product with
+ * it is NaN.  x DEVICE [rows, cols] of x_dtype; out_scale DEVICE fp32 [rows].  Weights are quantised with the same call, a
+ * channel being a row.  rows == 0 enqueues nothing.
+ */
+int accerl_quantize_rows(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ld_x, int8_t* out_packed,
+                         float* out_scale, void* stream);
+
+/* Rows that are int8 already (q DEVICE [rows, cols]) into the packed layout, and back. */
+int accerl_pack_rows_i8(const int8_t* q, int64_t rows, int64_t cols, int64_t ld_q, int8_t* out_packed, void* stream);
+int accerl_unpack_rows_i8(const int8_t* packed, int64_t rows, int64_t cols, int8_t* out_q, int64_t ld_q, void* stream);
+
+/*
+ * Int8 dense layer with a scale for each token and each channel:
+ *     acc[m,n] = sum_k x[m,k] w[n,k] (exact int32),    y = ((float)acc * x_scale[m]) * w_scale[n] + bias[n],    ReLU if relu != 0
+ * rounded once to out_dtype.  x_packed [M, K] and w_packed [N, K] packed rows; x_scale, w_scale, bias (NULL: none) DEVICE fp32; out
+ * DEVICE [M, N].  M == 0 or N == 0 enqueues nothing.  Allocates nothing, does not synchronise.
+ */
+int accerl_dense_i8(const int8_t* x_packed, const float* x_scale, const int8_t* w_packed, const float* w_scale, const float* bias,
+                    int64_t M, int64_t N, int64_t K, int32_t relu, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
+
+/*
+ * The same layer on floating-point tokens, quantised as accerl_quantize_rows does (same results as the two calls).
+ * workspace: DEVICE, 16-byte aligned, at least accerl_dense_i8_workspace(M, K) bytes, used until the work has finished: calls that
+ * may overlap need a workspace each.  Its contents need not be kept or cleared.
+ */
+int64_t accerl_dense_i8_workspace(int64_t M, int64_t K);
+int accerl_dense_i8_dynamic(const void* x, int32_t x_dtype, int64_t ld_x, const int8_t* w_packed, const float* w_scale, const float* bias,
+                            int64_t M, int64_t N, int64_t K, int32_t relu, void* out, int32_t out_dtype, int64_t ld_out,
+                            void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Log-probabilities of actions, and the entropy of the distribution they were drawn from, for a wide action set:
+ *     out_logp[b] = log pi(a_b|x_b),    out_entropy[b] = H(pi(.|x_b))    (NULL: not wanted),    pi = softmax over the allowed actions
+ * logits DEVICE [B, A] of `dtype`, 1 <= A <= 2^20; mask DEVICE uint8 [B, A], zero = not allowed, whatever its logit (NULL: all are
+ * allowed; ld_mask == 0: one row for all); actions DEVICE int32 [B].  A logit of -inf is an action of probability 0.  An action that is not allowed
+ * has log-probability -inf, and so has every action of a row that allows none (entropy 0).  An action outside 0 .. A-1 marks a row
+ * without one: 0 and 0, and the row is not read.  workspace: DEVICE, 16-byte aligned, accerl_policy_loss_workspace() bytes (the same
+ * for all sizes), used until the work has finished: calls that may overlap need one each.  Neither call allocates or synchronises;
+ * B == 0 enqueues nothing; a call repeated gives the same bits.
+ */
+int64_t accerl_policy_loss_workspace(void);
+int accerl_action_logprob(const void* logits, int32_t dtype, int64_t ld_logits, const uint8_t* mask, int64_t ld_mask, const int32_t* actions,
+                          int64_t B, int64_t A, float* out_logp, float* out_entropy, void* workspace, int64_t workspace_bytes, void* stream);
+
+typedef enum {
+    ACCERL_KL_NONE = 0,
+    ACCERL_KL_SAMPLED = 1,   /* exp(d) - d - 1 with d = ref_logp - log pi(a): the estimate from the action taken alone */
+    ACCERL_KL_FORWARD = 2,   /* KL(pi_ref || pi) over all actions, the Monitor's and the distillation loss's */
+    ACCERL_KL_REVERSE = 3    /* KL(pi || pi_ref) over all actions */
+} accerl_kl_kind;
+
+/*
+ * Clipped policy loss with a KL term to a reference policy and an entropy term, and its gradient (the corrected actor-critic
+ * update that accerl_vtrace's out_pg_adv feeds, Section 2.3; the KL and entropy terms of Section 2.2, Eq. 1).  Per row, with
+ * pi = softmax of the allowed logits, r = exp(log pi(a) - old_logp):
+ *     loss = -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef KL - entropy_coef H(pi)
+ *     grad[b, j] = scale * weights[b] * d loss_b / d logits[b, j]
+ *     out_stats  = scale * sum_b weights[b] * {loss, KL, H, 1 if r lies outside the borders}    (summed in 64 bits)
+ * so that with scale = 1 / (number of rows that count) the first is the batch's loss and the gradient is its gradient.  A row of weight
+ * 0, or whose action lies outside 0 .. A-1, is not read: its outputs and its gradient are 0.  A KL term of coefficient 0 is reported and
+ * no part of the loss.  A row that allows no action has loss, KL,
+ * entropy and gradient 0 and log-probability -inf.  An action of probability 0 has ratio 0.  The mask applies to both policies; where
+ * the reference allows nothing, the forward KL is 0 and the reverse one infinite.  NaN and +inf among the allowed logits make the row NaN.
+ * Arithmetic is fp32 or wider, gradients are rounded once to `dtype`.  grad_logits may be NULL (value only) or the logits themselves
+ * (same stride); no other output may overlap an input.
+ */
+typedef struct {
+    int64_t B, A;
+    int32_t dtype;                 /* accerl_dtype of logits, ref_logits and grad_logits */
+    int32_t kl_kind;               /* accerl_kl_kind */
+    const void* logits;            /* DEVICE [B, A] */
+    int64_t ld_logits;
+    const void* ref_logits;        /* DEVICE [B, A] (FORWARD and REVERSE) */
+    int64_t ld_ref;
+    void* grad_logits;             /* DEVICE [B, A] or NULL */
+    int64_t ld_grad;
+    const uint8_t* mask;           /* as in accerl_action_logprob */
+    int64_t ld_mask;
+    const int32_t* actions;        /* DEVICE [B] */
+    const float* old_logp;         /* DEVICE [B]: the behaviour's log-probabilities */
+    const float* advantages;       /* DEVICE [B] */
+    const float* weights;          /* DEVICE [B] or NULL (all 1) */
+    const float* ref_logp;         /* DEVICE [B] (SAMPLED) */
+    double clip_low, clip_high, kl_coef, entropy_coef, scale;
+    float* out_loss;               /* DEVICE [B] each, or NULL */
+    float* out_logp;
+    float* out_kl;
+    float* out_entropy;
+    float* out_stats;              /* DEVICE [4] or NULL */
+    void* workspace;               /* as in accerl_action_logprob */
+    int64_t workspace_bytes;
+} accerl_policy_loss_args;
+
+int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
+
+/*
  * Measurement aids (not part of the method): the ceilings the kernels are compared with, as this machine
  * sustains them.  accerl_probe_mfma runs 2048 workgroups x 4 wavefronts, each issuing iters x 8 independent
  * 16x16 MFMAs on registers (int8 16x16x64, or bf16 16x16x32 if bf16 != 0): ops = 2048 * 4 * iters * 8 *

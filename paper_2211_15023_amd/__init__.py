@@ -8,5 +8,7 @@ from .binding import (  # noqa: F401
     accerl_policy_create, accerl_policy_destroy, accerl_actor_forward, accerl_actor_forward_teacher,
     accerl_actor_forward_recurrent, accerl_actor_forward_debug, accerl_last_error,
     accerl_profile_begin, accerl_profile_end, accerl_plan_describe, accerl_monitor_kl, accerl_monitor_kl_noalloc, accerl_vtrace, accerl_distill_loss, accerl_actor_forward_mixture, accerl_mixture_alpha, accerl_probe_mfma, accerl_probe_copy, accerl_probe_empty,
+    accerl_quantize_rows, accerl_pack_rows_i8, accerl_unpack_rows_i8, packed_rows_bytes, accerl_dense_i8, accerl_dense_i8_dynamic,
+    accerl_dense_i8_workspace, accerl_action_logprob, accerl_policy_loss, accerl_policy_loss_workspace, DenseInt8, PolicyLoss,
     INT8, FP32, BF16, TAP_ACC, TAP_ACT, TAP_ACC_A, TAP_ACT_A,
 )

@@ -34,6 +34,15 @@ class _Arch(C.Structure):
                [("layers", _Layer * MAX_LAYERS)]
 
 
+class _PolicyLossArgs(C.Structure):
+    _fields_ = [("B", C.c_int64), ("A", C.c_int64), ("dtype", C.c_int32), ("kl_kind", C.c_int32), ("logits", C.c_void_p), ("ld_logits", C.c_int64),
+                ("ref_logits", C.c_void_p), ("ld_ref", C.c_int64), ("grad_logits", C.c_void_p), ("ld_grad", C.c_int64),
+                ("mask", C.c_void_p), ("ld_mask", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ("actions", "old_logp", "advantages", "weights", "ref_logp")] + \
+               [(n, C.c_double) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef", "scale")] + \
+               [(n, C.c_void_p) for n in ("out_loss", "out_logp", "out_kl", "out_entropy", "out_stats", "workspace")] + [("workspace_bytes", C.c_int64)]
+
+
 def load_library():
     """Load libaccerl.so (after torch, so that both share one HIP runtime).  No fallback exists."""
     global _lib, torch
@@ -76,6 +85,19 @@ def load_library():
     lib.accerl_distill_loss.argtypes = [vp, vp, vp, vp, i64, i32, C.c_float, vp, vp, vp]
     lib.accerl_distill_loss.restype = C.c_int
     lib.accerl_vtrace.restype = C.c_int
+    lib.accerl_packed_rows_bytes.argtypes = [i64, i64]
+    lib.accerl_packed_rows_bytes.restype = i64
+    lib.accerl_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    lib.accerl_pack_rows_i8.argtypes = [vp, i64, i64, i64, vp, vp]
+    lib.accerl_unpack_rows_i8.argtypes = [vp, i64, i64, vp, i64, vp]
+    lib.accerl_dense_i8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, vp, i32, i64, vp]
+    lib.accerl_dense_i8_workspace.argtypes = [i64, i64]
+    lib.accerl_dense_i8_workspace.restype = i64
+    lib.accerl_dense_i8_dynamic.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, i32, vp, i32, i64, vp, i64, vp]
+    lib.accerl_policy_loss_workspace.argtypes = []
+    lib.accerl_policy_loss_workspace.restype = i64
+    lib.accerl_action_logprob.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp]
+    lib.accerl_policy_loss.argtypes = [C.POINTER(_PolicyLossArgs), vp]
     lib.accerl_last_error.restype = C.c_char_p
     for f in ("accerl_blob_sizes", "accerl_policy_create", "accerl_actor_forward", "accerl_actor_forward_teacher",
               "accerl_actor_forward_recurrent", "accerl_actor_forward_debug", "accerl_profile_begin",
@@ -354,6 +376,280 @@ def accerl_vtrace(logits_original, logits_smaller, actions, rewards, discounts, 
                                         _ptr(values, torch.float32), _ptr(bootstrap, torch.float32), T, B, A,
                                         float(rho_bar), float(c_bar), _ptr(out_vs, torch.float32),
                                         _ptr(out_pg_adv, torch.float32), _ptr(out_rho, torch.float32), _stream(stream)))
+
+
+# ---------------------------------------------------------------- operators of wide policies
+KL_KINDS = {"none": 0, "sampled": 1, "forward": 2, "reverse": 3}
+
+
+def _dtype(t):
+    try:
+        return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[t.dtype]
+    except KeyError:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}") from None
+
+
+def _rows(t, what):
+    """Pointer and row stride of a device matrix whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{what} must be a CUDA/HIP matrix")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t, dtype, n, what):
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,):
+        raise ValueError(f"{what} must be a vector of {n}")
+    return _ptr(t, dtype)
+
+
+def _packed(t, rows, cols, what):
+    if t.numel() * t.element_size() < packed_rows_bytes(rows, cols):
+        raise ValueError(f"{what} is smaller than the packed rows of {rows} x {cols}")
+    return _ptr(t, torch.int8)
+
+
+def _count(n):
+    if n < 0:
+        _check(n)
+    return n
+
+
+def packed_rows_bytes(rows, cols):
+    """Size of the buffer of accerl_quantize_rows and accerl_pack_rows_i8 (a flat int8 tensor)."""
+    return _count(load_library().accerl_packed_rows_bytes(rows, cols))
+
+
+def accerl_quantize_rows(x, out_packed, out_scale, stream=None):
+    lib = load_library()
+    p, ld = _rows(x, "x")
+    R, K = x.shape
+    _check(lib.accerl_quantize_rows(p, _dtype(x), R, K, ld, _packed(out_packed, R, K, "out_packed"), _vector(out_scale, torch.float32, R, "out_scale"),
+                                    _stream(stream)))
+
+
+def accerl_pack_rows_i8(q, out_packed, stream=None):
+    lib = load_library()
+    if q.dtype != torch.int8:
+        raise ValueError(f"expected torch.int8, got {q.dtype}")
+    p, ld = _rows(q, "q")
+    R, K = q.shape
+    _check(lib.accerl_pack_rows_i8(p, R, K, ld, _packed(out_packed, R, K, "out_packed"), _stream(stream)))
+
+
+def accerl_unpack_rows_i8(packed, out_q, stream=None):
+    lib = load_library()
+    if out_q.dtype != torch.int8:
+        raise ValueError(f"expected torch.int8, got {out_q.dtype}")
+    p, ld = _rows(out_q, "out_q")
+    R, K = out_q.shape
+    _check(lib.accerl_unpack_rows_i8(_packed(packed, R, K, "packed"), R, K, p, ld, _stream(stream)))
+
+
+def accerl_dense_i8(x_packed, x_scale, w_packed, w_scale, bias, K, out, relu=False, stream=None):
+    """out [M, N] from packed tokens [M, K] and packed features [N, K]."""
+    lib = load_library()
+    po, ld = _rows(out, "out")
+    M, N = out.shape
+    _check(lib.accerl_dense_i8(_packed(x_packed, M, K, "x_packed"), _vector(x_scale, torch.float32, M, "x_scale"), _packed(w_packed, N, K, "w_packed"),
+                               _vector(w_scale, torch.float32, N, "w_scale"), _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)),
+                               po, _dtype(out), ld, _stream(stream)))
+
+
+def accerl_dense_i8_workspace(M, K):
+    return _count(load_library().accerl_dense_i8_workspace(M, K))
+
+
+def accerl_dense_i8_dynamic(x, w_packed, w_scale, bias, out, workspace, relu=False, stream=None):
+    """out [M, N] from floating-point tokens x [M, K]; workspace: uint8 tensor of accerl_dense_i8_workspace(M, K) bytes."""
+    lib = load_library()
+    px, ldx = _rows(x, "x")
+    po, ld = _rows(out, "out")
+    (M, K), N = x.shape, out.shape[1]
+    if out.shape[0] != M:
+        raise ValueError("x and out differ in rows")
+    _check(lib.accerl_dense_i8_dynamic(px, _dtype(x), ldx, _packed(w_packed, N, K, "w_packed"), _vector(w_scale, torch.float32, N, "w_scale"),
+                                       _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)), po, _dtype(out), ld,
+                                       _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
+
+
+def accerl_policy_loss_workspace():
+    return load_library().accerl_policy_loss_workspace()
+
+
+def _mask_rows(mask, B, A):
+    """uint8 [B, A], or [1, A] for all rows."""
+    if mask is None:
+        return None, 0
+    if mask.dtype != torch.uint8:
+        raise ValueError(f"expected torch.uint8, got {mask.dtype}")
+    if mask.dim() != 2 or mask.shape[1] != A or mask.shape[0] not in (1, B):
+        raise ValueError("the mask must be [B, A] or [1, A]")
+    p, ld = _rows(mask, "mask")
+    return p, 0 if mask.shape[0] == 1 else ld
+
+
+def accerl_action_logprob(logits, mask, actions, out_logp, out_entropy, workspace, stream=None):
+    """mask: uint8 [B, A], [1, A] for all rows, or None; workspace: uint8 tensor of accerl_policy_loss_workspace() bytes."""
+    lib = load_library()
+    p, ld = _rows(logits, "logits")
+    B, A = logits.shape
+    pm, ldm = _mask_rows(mask, B, A)
+    _check(lib.accerl_action_logprob(p, _dtype(logits), ld, pm, ldm, _vector(actions, torch.int32, B, "actions"), B, A,
+                                     _vector(out_logp, torch.float32, B, "out_logp"), _vector(out_entropy, torch.float32, B, "out_entropy"),
+                                     _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
+
+
+def accerl_policy_loss(logits, actions, old_logp, advantages, workspace, mask=None, weights=None, kl="none", ref_logits=None, ref_logp=None,
+                       clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, scale=1.0, grad_logits=None, out_loss=None, out_logp=None,
+                       out_kl=None, out_entropy=None, out_stats=None, stream=None):
+    """kl: "none", "sampled" (ref_logp), "forward" or "reverse" (ref_logits).  Every output may be None."""
+    lib = load_library()
+    B, A = logits.shape
+    for t, what in ((ref_logits, "ref_logits"), (grad_logits, "grad_logits")):
+        if t is not None and (t.shape != logits.shape or t.dtype != logits.dtype):
+            raise ValueError(f"{what} differs from the logits in shape or type")
+    a = _PolicyLossArgs()
+    a.B, a.A, a.dtype, a.kl_kind = B, A, _dtype(logits), KL_KINDS[kl] if isinstance(kl, str) else int(kl)
+    a.logits, a.ld_logits = _rows(logits, "logits")
+    a.ref_logits, a.ld_ref = _rows(ref_logits, "ref_logits")
+    a.grad_logits, a.ld_grad = _rows(grad_logits, "grad_logits")
+    a.mask, a.ld_mask = _mask_rows(mask, B, A)
+    a.actions = _vector(actions, torch.int32, B, "actions")
+    for n, t in (("old_logp", old_logp), ("advantages", advantages), ("weights", weights), ("ref_logp", ref_logp), ("out_loss", out_loss),
+                 ("out_logp", out_logp), ("out_kl", out_kl), ("out_entropy", out_entropy)):
+        setattr(a, n, _vector(t, torch.float32, B, n))
+    a.out_stats = _vector(out_stats, torch.float32, 4, "out_stats")
+    a.clip_low, a.clip_high, a.kl_coef, a.entropy_coef, a.scale = clip_low, clip_high, kl_coef, entropy_coef, scale
+    a.workspace, a.workspace_bytes = _ptr(workspace, torch.uint8), workspace.numel()
+    _check(lib.accerl_policy_loss(C.byref(a), _stream(stream)))
+
+
+def _logits(t):
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError("logits must be a CUDA/HIP matrix")
+    return t.detach()
+
+
+class _Workspaces:
+    """A buffer for each stream, allocated on it: calls on different streams do not share one, and a buffer that grows is given back in
+    the order of the stream that used it."""
+
+    def __init__(self):
+        self.of = {}
+
+    def get(self, nbytes, stream, device):
+        t = self.of.get((device, stream))
+        if t is None or t.numel() < nbytes:
+            t = self.of[device, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return t
+
+
+class _On:
+    """The stream that a call runs on: what is allocated inside belongs to it."""
+
+    def __init__(self, stream, device):
+        self.other = None
+        if stream is None:
+            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
+        else:
+            s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
+            self.raw, self.other = s.cuda_stream, torch.cuda.stream(s)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        return self.raw
+
+    def __exit__(self, *e):
+        if self.other is not None:
+            self.other.__exit__(*e)
+
+
+class DenseInt8:
+    """Int8 dense layer with a scale for each token and channel: owner of packed weights, workspaces and outputs.
+
+    w: int8 [N, K] with w_scale [N], or a float matrix that is quantised here, a scale for each row; bias [N] or None.
+    """
+
+    def __init__(self, w, w_scale=None, bias=None, relu=False):
+        load_library()
+        self.N, self.K = w.shape
+        self.relu = bool(relu)
+        self.w = torch.empty(packed_rows_bytes(self.N, self.K), dtype=torch.int8, device=w.device)
+        if w.dtype == torch.int8:
+            if w_scale is None:
+                raise ValueError("int8 weights need their scales")
+            self.w_scale = w_scale.detach().to(torch.float32).contiguous().clone()
+            accerl_pack_rows_i8(w, self.w)
+        else:
+            self.w_scale = torch.empty(self.N, dtype=torch.float32, device=w.device)
+            accerl_quantize_rows(w.detach(), self.w, self.w_scale)
+        self.bias = None if bias is None else bias.detach().to(torch.float32).contiguous().clone()
+        self._work = _Workspaces()
+
+    def forward(self, x, dtype=None, out=None, stream=None):
+        """x [M, K] -> [M, N] in `dtype` (x's own if None)."""
+        if not x.is_cuda or x.dim() != 2 or x.shape[1] != self.K:
+            raise ValueError(f"x must be a CUDA/HIP matrix of {self.K} columns")
+        if out is not None and tuple(out.shape) != (x.shape[0], self.N):
+            raise ValueError(f"out must be [{x.shape[0]}, {self.N}]")
+        M = x.shape[0]
+        with _On(stream, x.device) as raw:
+            if out is None:
+                out = torch.empty((M, self.N), dtype=x.dtype if dtype is None else dtype, device=x.device)
+            ws = self._work.get(accerl_dense_i8_workspace(M, self.K), raw, x.device)
+            accerl_dense_i8_dynamic(x, self.w, self.w_scale, self.bias, out, ws, self.relu, raw)
+        return out
+
+
+class PolicyLoss:
+    """Clipped policy loss with KL and entropy terms: owner of the coefficients, workspaces and outputs.
+
+    forward returns the per-row outputs, the batch's sums and the gradient by the logits: `logits.backward(r.grad)` continues it into
+    whatever made the logits.
+    """
+
+    class Result:
+        __slots__ = ("loss", "logp", "kl", "entropy", "stats", "grad")
+
+    def __init__(self, clip_low=0.2, clip_high=0.2, kl="none", kl_coef=0.0, entropy_coef=0.0):
+        load_library()
+        self.how = dict(clip_low=clip_low, clip_high=clip_high, kl=kl, kl_coef=kl_coef, entropy_coef=entropy_coef)
+        self._bytes = accerl_policy_loss_workspace()
+        self._work = _Workspaces()
+
+    def forward(self, logits, actions, old_logp, advantages, mask=None, weights=None, scale=None, ref_logits=None, ref_logp=None,
+                grad=True, stream=None):
+        """scale: None for the mean over all rows; grad: a table to write the gradient to (the logits themselves too), True for a new one,
+        False for the value only."""
+        logits = _logits(logits)
+        B = logits.shape[0]
+        r = self.Result()
+        with _On(stream, logits.device) as raw:
+            rows = torch.empty((4, B), dtype=torch.float32, device=logits.device)
+            r.loss, r.logp, r.kl, r.entropy = rows.unbind(0)
+            r.stats = torch.empty(4, dtype=torch.float32, device=logits.device) if B else torch.zeros(4, dtype=torch.float32, device=logits.device)
+            r.grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if grad is True else None if grad is False else grad
+            accerl_policy_loss(logits, actions, old_logp, advantages, self._work.get(self._bytes, raw, logits.device), mask=mask, weights=weights,
+                               ref_logits=ref_logits, ref_logp=ref_logp, scale=1.0 / max(1, B) if scale is None else scale, grad_logits=r.grad,
+                               out_loss=r.loss, out_logp=r.logp, out_kl=r.kl, out_entropy=r.entropy, out_stats=r.stats, stream=raw, **self.how)
+        return r
+
+    def logprob(self, logits, actions, mask=None, stream=None):
+        """log pi(a) and entropy, each [B]."""
+        logits = _logits(logits)
+        with _On(stream, logits.device) as raw:
+            logp, ent = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
+            accerl_action_logprob(logits, mask, actions, logp, ent, self._work.get(self._bytes, raw, logits.device), raw)
+        return logp, ent
 
 
 STEP_KINDS = ("mlp_fused", "quant_obs", "conv", "gemm", "gemm_f32", "maxpool", "lstm_pack", "sample", "heads")

@@ -1,0 +1,211 @@
+"""Int8 dense layers with token and channel scales against the formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests import wide_reference as ref
+
+pytestmark = pytest.mark.gpu
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2211_15023_amd as A
+    A.load_library()
+    return A
+
+
+def as64(t):
+    return t.cpu().double().numpy()
+
+
+def quantized(A, x):
+    """int8 rows and scales as the library makes them; the pad bytes of the packed rows are zero."""
+    R, K = x.shape
+    packed = torch.full((A.packed_rows_bytes(R, K),), 99, dtype=torch.int8, device="cuda")
+    scale = torch.full((R,), -1.0, device="cuda")
+    A.accerl_quantize_rows(x, packed, scale)
+    q = torch.full((R, K), 55, dtype=torch.int8, device="cuda")
+    A.accerl_unpack_rows_i8(packed, q)
+    tiles = packed.view(-1, (K + 127) // 128 * 2, 4, 16, 16).permute(0, 3, 1, 2, 4).reshape(-1, (K + 127) // 128 * 128)
+    assert torch.equal(tiles[:R, :K], q)
+    assert int(tiles[R:].abs().sum()) == 0 and int(tiles[:, K:].abs().sum()) == 0
+    return q.cpu().numpy(), scale.cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,K", [(1, 1), (1, 127), (16, 128), (17, 1777), (3, 4097), (50, 20000)])
+def test_quantised_rows_are_exact(A, dtype, R, K):
+    g = torch.Generator().manual_seed(R * 1000 + K)
+    x = (torch.randn((R, K), generator=g) * torch.exp(torch.randn((R, 1), generator=g))).to(TORCH[dtype]).cuda()
+    q, scale = quantized(A, x)
+    want, want_scale = ref.quantize(as64(x))
+    assert np.array_equal(q, want)
+    assert np.array_equal(scale, want_scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_quantised_rows_at_the_middle_of_steps(A, dtype):
+    """Maxima that are multiples of 127 put elements exactly between two steps; next to them the fp32 neighbours."""
+    rows = []
+    for k in range(1, 16):
+        top = 127.0 * k
+        v = np.array([top] + [(n + 0.5) * k for n in range(127)])
+        rows.append(np.where(np.arange(128) % 2 == 0, v, -v))
+    x = torch.from_numpy(np.array(rows)).to(TORCH[dtype])
+    if dtype == "f32":
+        x = torch.cat([x, torch.nextafter(x, torch.zeros(())), torch.cat([x[:, :1], torch.nextafter(x[:, 1:], x[:, 1:] * 2)], dim=1)])
+    q, scale = quantized(A, x.cuda())
+    want, want_scale = ref.quantize(as64(x))
+    assert np.array_equal(q, want) and np.array_equal(scale, want_scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_quantised_rows_of_all_magnitudes(A, dtype):
+    """Zeros, the least and the largest values, infinities and NaN."""
+    t = TORCH[dtype]
+    f = torch.finfo(t)
+    base = torch.linspace(-1, 1, 200, dtype=torch.float64)
+    rows = [base * 0, base * f.max, base * f.smallest_normal, base * (f.smallest_normal * f.eps), base * f.max / 126.9, base * 1.0]
+    x = torch.stack(rows).to(t)
+    bad = torch.stack([base.clone() for _ in range(3)]).to(t)
+    bad[0, 7], bad[1, 9], bad[2, 199] = float("inf"), float("-inf"), float("nan")
+    q, scale = quantized(A, torch.cat([x, bad]).cuda())
+    want, want_scale = ref.quantize(as64(x))
+    assert np.array_equal(q[:6], want) and np.array_equal(scale[:6], want_scale)
+    assert np.all(q[6:] == 0) and np.all(np.isinf(scale[6:8])) and np.isnan(scale[8])
+
+
+def run_dense(A, M, K, N, x_dtype, out_dtype, bias, relu, seed, ld_x=None, ld_out=None):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((M, K), generator=g) * (1 + 7 * (torch.rand(K, generator=g) < 0.03))
+    xs = torch.full((M, ld_x or K), 3.0, dtype=TORCH[x_dtype], device="cuda")
+    xs[:, :K] = x.to(TORCH[x_dtype]).cuda()
+    wq = torch.randint(-127, 128, (N, K), generator=g, dtype=torch.int8)
+    sw = torch.rand(N, generator=g) / 127 / np.sqrt(K)
+    b = torch.randn(N, generator=g) if bias else None
+    layer = A.DenseInt8(wq.cuda(), sw.cuda(), None if b is None else b.cuda(), relu)
+    out = torch.full((M, ld_out or N), 77.0, dtype=TORCH[out_dtype], device="cuda")
+    y = layer.forward(xs[:, :K], out=out[:, :N])
+    want, prod = ref.dense(as64(xs[:, :K]), wq.numpy(), sw.numpy(), None if b is None else b.numpy(), relu)
+    # the sum to fp32, two scales (one itself rounded), the addition: five roundings of fp32, then the output's
+    tol = 5 * ref.U * (prod + np.abs(want)) + ref.HALF_STEP[out_dtype] * np.abs(want) * 1.001 + ref.TINY[out_dtype]
+    off = np.abs(as64(y) - want)
+    assert np.all(off <= tol), (np.max(off / tol), np.unravel_index(np.argmax(off / tol), off.shape))
+    if ld_out:
+        assert torch.all(out[:, N:] == 77.0)
+    return layer, xs[:, :K], y
+
+
+@pytest.mark.parametrize("M,K,N", [
+    (1, 1, 1), (1, 64, 1), (1, 4096, 4096), (2, 129, 17), (15, 100, 33), (16, 128, 16), (17, 640, 250), (24, 2048, 8192), (33, 777, 515), (64, 512, 64), (65, 1000, 4100),
+    (130, 3136, 512), (301, 3136, 512), (129, 65, 5000), (257, 300, 2049), (600, 250, 1100), (999, 1777, 2501), (1500, 384, 3000), (2100, 130, 4000), (4096, 128, 4097)])
+def test_dense_sizes(A, M, K, N):
+    run_dense(A, M, K, N, "bf16", "f32", bias=True, relu=False, seed=M + K + N)
+
+
+@pytest.mark.parametrize("x_dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("out_dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("M,K,N,bias,relu", [(5, 333, 130, True, True), (70, 500, 1001, False, False), (300, 200, 4099, True, True), (2050, 190, 4200, False, True)])
+def test_dense_types(A, x_dtype, out_dtype, M, K, N, bias, relu):
+    run_dense(A, M, K, N, x_dtype, out_dtype, bias, relu, seed=M)
+
+
+@pytest.mark.parametrize("M,K,N,ld_x,ld_out", [(3, 101, 55, 103, 57), (40, 300, 601, 333, 777), (1030, 257, 4203, 259, 4205)])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_dense_strides(A, M, K, N, ld_x, ld_out, dtype):
+    run_dense(A, M, K, N, dtype, dtype, True, False, M, ld_x, ld_out)
+
+
+def test_dense_extremes(A):
+    """Weights of -128 and tokens at both ends: sums as large as they get, exactly."""
+    M, K, N = 20, 65536, 40
+    x = torch.ones((M, K), device="cuda")
+    x[1::2] = -1
+    w = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    y = A.DenseInt8(w, torch.ones(N, device="cuda")).forward(x)
+    want = 127.0 * -128 * K / 127
+    assert torch.all((y[0::2] - want).abs() <= 5 * ref.U * abs(want)) and torch.all((y[1::2] + want).abs() <= 5 * ref.U * abs(want))
+
+
+def test_dense_rows_without_values(A):
+    """A NaN or infinite token makes its own row NaN and no other, through a ReLU too; a zero token gives the bias."""
+    for M, N in ((6, 40), (300, 5000)):
+        x = torch.randn((M, 300), device="cuda").to(torch.bfloat16)
+        x[1, 5], x[2, 299], x[3, 0], x[4] = float("nan"), float("inf"), float("-inf"), 0
+        w, b = torch.randn((N, 300), device="cuda"), torch.randn(N, device="cuda")
+        y = A.DenseInt8(w, bias=b).forward(x, dtype=torch.float32)
+        assert torch.isnan(y[1:4]).all() and torch.isfinite(y[0]).all() and torch.isfinite(y[5:]).all()
+        assert torch.equal(y[4], b)
+        assert torch.isnan(A.DenseInt8(w, bias=b, relu=True).forward(x)[1:4]).all()
+
+
+def test_dense_float_weights_are_quantised_by_channel(A):
+    w = torch.randn((70, 130), device="cuda")
+    layer = A.DenseInt8(w)
+    q = torch.empty((70, 130), dtype=torch.int8, device="cuda")
+    A.accerl_unpack_rows_i8(layer.w, q)
+    want, scale = ref.quantize(as64(w))
+    assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(layer.w_scale.cpu().numpy(), scale)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 300, 500), (7, 300, 500), (300, 512, 4096), (2048, 256, 4096)])
+def test_two_calls_give_what_one_does(A, M, K, N):
+    layer, x, y = run_dense(A, M, K, N, "f16", "f16", True, True, seed=3)
+    packed, scale = torch.empty(A.packed_rows_bytes(M, K), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    A.accerl_quantize_rows(x, packed, scale)
+    out = torch.empty_like(y)
+    A.accerl_dense_i8(packed, scale, layer.w, layer.w_scale, layer.bias, K, out, relu=True)
+    assert torch.equal(out, y)
+    # a token's result does not depend on the batch it comes in
+    assert torch.equal(layer.forward(x[:1]), y[:1])
+
+
+def test_dense_empty_batch(A):
+    layer = A.DenseInt8(torch.ones((5, 7), device="cuda"))
+    assert layer.forward(torch.empty((0, 7), device="cuda")).shape == (0, 5)
+
+
+def test_dense_refuses_tensors(A):
+    layer = A.DenseInt8(torch.randn((40, 30), device="cuda"))
+    x = torch.randn((4, 30), device="cuda")
+    for bad in (x.double(), x.cpu(), x.t().contiguous().t(), x[0]):
+        with pytest.raises((ValueError, IndexError)):
+            layer.forward(bad)
+    for columns in (29, 31, 300):                                           # not the weights' K
+        with pytest.raises(ValueError):
+            layer.forward(torch.randn((4, columns), device="cuda"))
+    with pytest.raises(ValueError):
+        layer.forward(x, out=torch.empty((3, 40), device="cuda"))
+    with pytest.raises(ValueError):
+        layer.forward(x, out=torch.empty((4, 400), device="cuda"))          # more outputs than there are weights
+    with pytest.raises(ValueError):
+        A.DenseInt8(torch.ones((4, 4), dtype=torch.int8, device="cuda"))
+
+
+def test_dense_on_another_stream_and_in_a_graph(A):
+    """Calls on two streams with one layer, and a captured call replayed between eager ones."""
+    layer = A.DenseInt8(torch.randn((1000, 500), device="cuda"), bias=torch.randn(1000, device="cuda"))
+    xs = [torch.randn((m, 500), device="cuda").to(torch.bfloat16) for m in (9, 300)]
+    want = [layer.forward(x) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            got[i].append(layer.forward(xs[i], stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i])
+    x = xs[1].clone()
+    out = torch.empty((300, 1000), dtype=torch.bfloat16, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, out=out)
+    for k in range(4):
+        x.copy_(xs[1] * (k + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, layer.forward(x))
