@@ -8,6 +8,8 @@
 // with four consecutive features of one token.
 #include <stdio.h>
 
+#include <type_traits>
+
 #include "wide_ops.h"
 
 namespace accerl {
@@ -21,6 +23,53 @@ constexpr int64_t DI_MAX_ROWS = 1 << 24, DI_MAX_K = 1 << 16;      // 2^16 * 128 
 __host__ __device__ inline int64_t di_steps(int64_t K) { return (K + 127) / 128 * 2; }
 
 // ---------------------------------------------------------------- quantising
+// Sixteen elements of a row as they lie in memory.
+template <typename T> struct Piece { u32x4 w[sizeof(T)]; };
+
+template <typename T>
+__device__ __forceinline__ void piece_load(Piece<T>& d, const T* row, int64_t k, int64_t cols) {
+    if (k + 16 <= cols) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) {
+            if constexpr (sizeof(T) == 4) d.w[i] = *(const u32x4_at4*)((const char*)(row + k) + 16 * i);
+            else d.w[i] = *(const u32x4_at2*)((const char*)(row + k) + 16 * i);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) d.w[i] = (u32x4){0, 0, 0, 0};
+    if (k >= cols) return;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (k + e < cols) {
+            const uint32_t u = sizeof(T) == 4 ? ((const uint32_t*)row)[k + e] : (uint32_t)((const uint16_t*)row)[k + e];
+            constexpr int PER = 4 / (int)sizeof(T);
+            d.w[e / (4 * PER)][e / PER % 4] |= u << (16 * (e % PER));
+        }
+}
+// Magnitudes are compared as integers, in which a NaN is larger than everything; 16-bit elements two at a time.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+template <typename T>
+__device__ __forceinline__ void piece_max(const Piece<T>& d, uint32_t& m) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) m = max(m, d.w[i][e] & 0x7fffffffu);
+            else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, d.w[i][e] & 0x7fff7fffu)));
+        }
+}
+template <typename T>
+__device__ __forceinline__ void piece_floats(const Piece<T>& d, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) v[4 * i + e] = __uint_as_float(d.w[i][e]);
+            else el_pair<T>(d.w[i][e], v[8 * i + 2 * e], v[8 * i + 2 * e + 1]);
+        }
+}
+
 // Rounded once, from the exact quotient: the product with 1 / max is off by a few parts in 2^24, so the candidate it gives may lie on the
 // wrong side of the middle of two steps; the remainder x * 127 - q * max is exact (in 32 bits for 8- and 11-bit significands, in
 // 64 for fp32) and tells the side.  Ties go to the even step.
@@ -36,78 +85,83 @@ __device__ __forceinline__ int di_quant(float x, float inv, float top) {
     }
     return (int)q;
 }
-
-// sixteen elements of a row from element k on; what lies past the row's end is zero
+// Sixteen of them.  x * inv + 1.5 * 2^23 has the rounded quotient in its low byte; only where one of the sixteen lies within 2^-15 of the
+// middle of two steps (inv's error moves a quotient by less than 2^-16), or the row's magnitude needs scaling, are they looked at one by
+// one.  That is 5 operations an element in place of 15: 8192 rows of 4096 bf16 were bound by them (31 us).
 template <typename T>
-__device__ __forceinline__ void di_load16(const T* row, int64_t k, int64_t cols, float (&v)[16]) {
-    if (k + 16 <= cols) {
-        if constexpr (__is_same(T, float)) {
+__device__ __forceinline__ v4i di_quant16(const Piece<T>& d, float inv, float top, float by) {
+    constexpr float MAGIC = 12582912.0f;
+    float v[16], off = 0.0f;
+    uint32_t u[16];
+    piece_floats(d, v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
-                const u32x4 w = *(const u32x4_at4*)(row + k + 4 * i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * i + e] = __uint_as_float(w[e]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x4 w = *(const u32x4_at2*)(row + k + 8 * i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) el_pair<T>(w[e], v[8 * i + 2 * e], v[8 * i + 2 * e + 1]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = k + e < cols ? el_f32(row[k + e]) : 0.0f;
+    for (int e = 0; e < 16; ++e) {
+        const float q = fmaf(v[e], inv, MAGIC);
+        off = fmaxf(off, fabsf(fmaf(v[e], inv, MAGIC - q)));
+        u[e] = __float_as_uint(q);
     }
+    if (off > 0.5f - 0x1p-15f || by != 1.0f) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = (uint32_t)di_quant<T>(v[e] * by, inv, top);
+    }
+    v4i o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        o[k] = (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(u[4 * k + 3], u[4 * k + 2], 0x0c0c0400), __builtin_amdgcn_perm(u[4 * k + 1], u[4 * k], 0x0c0c0400), 0x05040100);
+    return o;
 }
 
-// A workgroup quantises 16 rows, one row tile: lane l of a wavefront is row l % 16 and one of four pieces of 16 elements, so that a
-// wavefront reads 16 rows' runs of 64 elements and writes a whole KiB.  Magnitudes are compared as integers, in which a NaN is larger
-// than everything: a row that holds a NaN or an infinity gets it as its scale and zeros, so that its results are NaN.
-constexpr int QR_THREADS = 1024;
-template <typename T>
+// A workgroup quantises ROWS rows: lane l of a wavefront is row l % ROWS and one of 64 / ROWS pieces of 16 elements, so that a wavefront
+// reads runs of consecutive elements and writes runs of 16 ROWS bytes.  What a lane reads for the maximum stays in registers
+// (HOLD pieces; longer rows read the rest again).  A row that holds a NaN or an infinity gets it as its scale and zeros, so that its
+// results are NaN.
+constexpr int QR_THREADS = 256;
+// One row a workgroup up to 1024 rows (1024 x 4096 bf16 7.5 us, four rows 9.9; 2048 x 1024 6.7 / 4.7), 16 where a row is one pass of its 16
+// lanes (16384 x 256 6.0, four 9.3; 4096 x 512 6.3 / 4.9).  8192 x 4096 bf16 takes 23.5 us, 4.1 TB/s.
+constexpr int64_t QR_SINGLE = 1024, QR_SHORT = 256;
+template <typename T, int ROWS, int HOLD>
 __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t ld, v4i* out, float* scale, int steps) {
-    __shared__ uint32_t s_max[QR_THREADS / 64][16];
-    const int tid = threadIdx.x, r = tid & 15, piece = tid >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r;
-    const bool real = row < rows;
+    constexpr int LANES = QR_THREADS / ROWS;                        // lanes a row
+    __shared__ uint32_t s_max[QR_THREADS / 64][ROWS];
+    const int tid = threadIdx.x, r = tid % ROWS, piece = tid / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+    const bool real = row < rows;                                   // the rows that fill the last tile are zeros
     const T* src = x + (real ? row : rows - 1) * ld;
-    float v[16];
+    Piece<T> v[HOLD], w;
     uint32_t m = 0;
-    for (int64_t k = piece * 16; k < cols; k += QR_THREADS) {
-        di_load16(src, k, cols, v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+    for (int h = 0; h < HOLD; ++h) piece_load(v[h], src, (int64_t)(piece + h * LANES) * 16, cols);
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) piece_max(v[h], m);
+    for (int64_t k = (int64_t)(piece + HOLD * LANES) * 16; k < cols; k += LANES * 16) {
+        piece_load(w, src, k, cols);
+        piece_max(w, m);
     }
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-    if ((tid & 63) < 16) s_max[tid >> 6][r] = m;
+    if constexpr (sizeof(T) == 2) m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = ROWS; o < 64; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+    if ((tid & 63) < ROWS) s_max[tid >> 6][r] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < QR_THREADS / 64; ++w) m = max(m, s_max[w][r]);
-    float top = __uint_as_float(m);
+    for (int k = 0; k < QR_THREADS / 64; ++k) m = max(m, s_max[k][r]);
+    float top;
+    if constexpr (sizeof(T) == 4) top = __uint_as_float(m);
+    else { T t; t.u = (uint16_t)m; top = el_f32(t); }
     if (real && piece == 0) scale[row] = top / 127.0f;
     // scaled by a power of two where 127 / max or 127 * x would leave the range
-    float by = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-20f : 1.0f;
-    const bool zero = !real || !(top > 0.0f && m < 0x7f800000u);
+    const float by = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-20f : 1.0f;
+    const bool zero = !real || !(top > 0.0f && __float_as_uint(top) < 0x7f800000u);
     top *= by;
     const float inv = 127.0f / top;
-    v4i* dst = out + (int64_t)blockIdx.x * steps * 64 + r;
-    for (int p = piece; p < steps * 4; p += QR_THREADS / 16) {
-        v4i o = {0, 0, 0, 0};
-        if (!zero && (int64_t)p * 16 < cols) {
-            di_load16(src, (int64_t)p * 16, cols, v);
+    v4i* dst = out + (row >> 4) * steps * 64 + (row & 15);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t u = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) u |= ((uint32_t)di_quant<T>(v[4 * w + e] * by, inv, top) & 0xffu) << (8 * e);
-                o[w] = (int)u;
-            }
-        }
-        dst[p * 16] = o;
+    for (int h = 0; h < HOLD; ++h) {
+        const int p = piece + h * LANES;
+        if (p < steps * 4) dst[p * 16] = zero ? (v4i){0, 0, 0, 0} : di_quant16<T>(v[h], inv, top, by);
+    }
+    for (int p = piece + HOLD * LANES; p < steps * 4; p += LANES) {
+        piece_load(w, src, (int64_t)p * 16, cols);
+        dst[p * 16] = zero ? (v4i){0, 0, 0, 0} : di_quant16<T>(w, inv, top, by);
     }
 }
 
@@ -144,15 +198,16 @@ struct DenseParams {
     int dtype, relu;
 };
 
+__device__ __forceinline__ float di_result(const DenseParams& p, int acc, float sx, float sw, float b) {
+    const float y = fmaf((float)acc * sx, sw, b);
+    return p.relu && y < 0.0f ? 0.0f : y;                         // a NaN stays
+}
 // results of features n .. n + 3 of token m
 template <typename T>
 __device__ __forceinline__ void di_store(const DenseParams& p, const v4i& acc, int64_t m, int64_t n, float sx, const float (&sw)[4], const float (&b)[4]) {
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        y[e] = fmaf((float)acc[e] * sx, sw[e], b[e]);
-        if (p.relu) y[e] = y[e] < 0.0f ? 0.0f : y[e];             // a NaN stays
-    }
+    for (int e = 0; e < 4; ++e) y[e] = di_result(p, acc[e], sx, sw[e], b[e]);
     T* o = (T*)p.out + m * p.ld + n;
     if (n + 4 <= p.N) {
         if constexpr (__is_same(T, float)) {
@@ -175,104 +230,163 @@ __device__ __forceinline__ void di_channels(const DenseParams& p, int64_t n, flo
     }
 }
 
-#define DI_GLOBAL(q) ((const __attribute__((address_space(1))) void*)(q))
-#define DI_LDS(q) ((__attribute__((address_space(3))) void*)(q))
-
-// Large products.  A workgroup of WF x WT wavefronts owns (16 WF FA) features x (16 WT FB) tokens and walks K in stages of two steps
-// (128 bytes of every row).  A stage's fragments go to one of two LDS buffers while the other is multiplied from; two arrays
-// and pointers that do not alias let the compiler keep a stage's loads in flight across the reads of the other buffer.
-template <int FA, int FB>
-struct Frags { v4i a[FA], b[FB]; };
-
-template <int WF, int WT, int FA, int FB>
-__device__ __forceinline__ void di_fetch(char* __restrict__ dst, const char* const (&src)[(WF * FA + WT * FB) * 2 / (WF * WT)], int64_t at, int wave) {
-    constexpr int PER = (WF * FA + WT * FB) * 2 / (WF * WT);
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        __builtin_amdgcn_global_load_lds(DI_GLOBAL(src[i] + at), DI_LDS(dst + (wave * PER + i) * 1024), 16, 0, 0);
-}
-
-template <int WF, int WT, int FA, int FB>
-__device__ __forceinline__ void di_stage(const char* __restrict__ cur, char* __restrict__ nxt, const char* const (&src)[(WF * FA + WT * FB) * 2 / (WF * WT)],
-                                         int64_t at, bool more, int wave, int wf, int wt, int lane, v4i (&acc)[FA][FB]) {
-    if (more) di_fetch<WF, WT, FA, FB>(nxt, src, at, wave);
-    const char* pa = cur + wf * FA * 2048 + lane * 16;
-    const char* pb = cur + (WF * FA + wt * FB) * 2048 + lane * 16;
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-        Frags<FA, FB> f;
-#pragma unroll
-        for (int i = 0; i < FB; ++i) f.b[i] = *(const v4i*)(pb + (2 * i + st) * 1024);
-#pragma unroll
-        for (int i = 0; i < FA; ++i) f.a[i] = *(const v4i*)(pa + (2 * i + st) * 1024);
-#pragma unroll
-        for (int i = 0; i < FA; ++i)
-#pragma unroll
-            for (int j = 0; j < FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
-    }
-}
-
-template <typename T, int WF, int WT, int FA, int FB>
-__global__ __launch_bounds__(64 * WF * WT) void dense_i8_tile_kernel(const DenseParams p) {
-    constexpr int BF = WF * FA, BT = WT * FB;                       // row tiles of a workgroup
-    constexpr int STAGE = (BF + BT) * 2048;
-    constexpr int PER = (BF + BT) * 2 / (WF * WT);                  // fragments a wavefront fetches per stage
-    static_assert((BF + BT) * 2 % (WF * WT) == 0, "whole fragments a wavefront");
-    __shared__ __attribute__((aligned(16))) char s0[STAGE];
-    __shared__ __attribute__((aligned(16))) char s1[STAGE];
+// Large products.  A workgroup of WF x WT wavefronts owns (16 WF FA) features x (16 WT FB) tokens.  Of a step (64 bytes of every row) the
+// features, which WT wavefronts share, go from memory to registers three steps ahead, to one of three LDS buffers one step ahead, and to the
+// registers of the fragments that they replace between the matrix instructions of the step before; the tokens go to registers
+// straight from memory, two steps ahead.  (Both through LDS, a workgroup of 256 x 256 moves 128 KiB a step through it, which takes as
+// long as the step's matrix instructions; like this 80 KiB, and 48 KiB through the first-level cache.)  One barrier a step.
+//
+// LDS operations of a wavefront end in their order.  In step t - 1 a wavefront writes its fragments of step t + 1, then reads those of step t:
+// where no more than FA operations are outstanding, reads of step t - 1 all of them, its writes of step t + 1 and its reads of step
+// t - 1 (issued in step t - 2) are done.  When everybody has passed the barrier of step t like that, step t + 1 can be read and the buffer
+// of step t - 1 filled again.
+template <typename T, int WF, int WT, int FA, int FB, int KS>
+__global__ __launch_bounds__(64 * WF * WT, 2) void dense_i8_tile_kernel(const DenseParams p) {
+    constexpr int WAVES = WF * WT, BF = WF * FA, BT = WT * FB;      // row tiles of a workgroup
+    constexpr int PA = BF * KS / WAVES, BUF = BF * KS * 1024;       // fragments of features a wavefront brings per stage of KS steps
+    static_assert(BF * KS % WAVES == 0 && FA * KS < 16, "whole fragments a wavefront; the count of outstanding operations has four bits");
+    // results on their way out: 16 tokens x 16 CH features of a wavefront, rows 16 bytes apart
+    constexpr int CH = FA * 256 * (int)sizeof(T) <= 4096 ? FA : 16 / (int)sizeof(T), ROW = CH * 16 * (int)sizeof(T), PITCH = ROW + 16;
+    constexpr int OUT = WAVES * 16 * PITCH, LDS = 3 * BUF > OUT ? 3 * BUF : OUT;
+    __shared__ __attribute__((aligned(16))) char s_buf[LDS];
+    __shared__ __attribute__((aligned(16))) float s_sw[BF * 16], s_bias[BF * 16], s_sx[BT * 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wf = wave % WF, wt = wave / WF;
 
-    // Workgroup n runs on XCD n mod 8.  Every XCD takes consecutive tiles of an order that walks squares of up to 4 x 8 tiles, so
-    // that the workgroups that run together on it share rows in its cache.
+    // Workgroup n runs on XCD n mod 8.  Every XCD takes consecutive tiles of an order that walks bands of four tiles of tokens, so that
+    // the workgroups that run together on it share rows in its cache.
     const unsigned gf = (p.wt + BF - 1) / BF, gt = (p.xt + BT - 1) / BT, n = gf * gt, id = blockIdx.x, xcd = id & 7;
     const unsigned t = xcd * (n >> 3) + min(xcd, n & 7) + (id >> 3);
     constexpr unsigned GROUP = 4;
     const unsigned band = t / (GROUP * gf), first = band * GROUP, high = min(GROUP, gt - first), in = t - band * GROUP * gf;
     const int tf = (int)(in / high) * BF, tt = (int)(first + in % high) * BT;
 
-    // a tile past the end re-reads the last one; its results are not stored
-    const char* src[PER];
+    // a tile past the end re-reads the last one, a step past the end the last step; neither is used
+    const int stages = p.steps / KS;
+    const uint32_t l16 = lane * 16;
+    const char *pa[PA], *pb[FB];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int f = wave * PER + i, tile = f >> 1, st = f & 1;
-        src[i] = tile < BF ? p.w + ((int64_t)min(tf + tile, p.wt - 1) * p.steps + st) * 1024
-                           : p.x + ((int64_t)min(tt + tile - BF, p.xt - 1) * p.steps + st) * 1024;
-        src[i] += lane * 16;
+    for (int i = 0; i < PA; ++i) pa[i] = p.w + ((int64_t)min(tf + (wave * PA + i) / KS, p.wt - 1) * p.steps + (wave * PA + i) % KS) * 1024;
+#pragma unroll
+    for (int j = 0; j < FB; ++j) pb[j] = p.x + (int64_t)min(tt + wt * FB + j, p.xt - 1) * p.steps * 1024;
+    v4i r[3][PA], b[3][FB * KS], a[FA * KS], acc[FA][FB];
+    auto load_a = [&](v4i (&d)[PA], int s) {
+        const uint32_t at = min(s, stages - 1) * (KS * 1024) + l16;
+#pragma unroll
+        for (int i = 0; i < PA; ++i) d[i] = *(const v4i*)(pa[i] + at);
+    };
+    auto load_b = [&](v4i (&d)[FB * KS], int s) {
+        const uint32_t at = min(s, stages - 1) * (KS * 1024) + l16;
+#pragma unroll
+        for (int j = 0; j < FB * KS; ++j) d[j] = *(const v4i*)(pb[j % FB] + at + j / FB * 1024);
+    };
+    auto write_a = [&](const v4i (&d)[PA], int buf) {
+#pragma unroll
+        for (int i = 0; i < PA; ++i) *(v4i*)(s_buf + buf * BUF + (wave * PA + i) * 1024 + l16) = d[i];
+    };
+    load_a(r[0], 0);
+    load_b(b[0], 0);
+    load_a(r[1], 1);
+    load_b(b[1], 1);
+    load_a(r[2], 2);
+    for (int i = tid; i < BF * 16; i += 64 * WAVES) {
+        const int64_t f = min((int64_t)tf * 16 + i, p.N - 1);
+        s_sw[i] = p.sw[f];
+        s_bias[i] = p.bias ? p.bias[f] : 0.0f;
     }
-    v4i acc[FA][FB];
+    for (int i = tid; i < BT * 16; i += 64 * WAVES) s_sx[i] = p.sx[min((int64_t)tt * 16 + i, p.M - 1)];
 #pragma unroll
     for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = (v4i){0, 0, 0, 0};
-
-    const int stages = p.steps >> 1;
-    di_fetch<WF, WT, FA, FB>(s0, src, 0, wave);
+    write_a(r[0], 0);
+    load_a(r[0], 3);
+    write_a(r[1], 1);
+    load_a(r[1], 4);
     __syncthreads();
-    int s = 0;
-    for (; s + 2 <= stages; s += 2) {
-        di_stage<WF, WT, FA, FB>(s0, s1, src, (int64_t)(s + 1) * 2048, true, wave, wf, wt, lane, acc);
-        __syncthreads();
-        di_stage<WF, WT, FA, FB>(s1, s0, src, (int64_t)(s + 2) * 2048, s + 2 < stages, wave, wf, wt, lane, acc);
-        __syncthreads();
-    }
-    if (s < stages) di_stage<WF, WT, FA, FB>(s0, s1, src, 0, false, wave, wf, wt, lane, acc);
+#pragma unroll
+    for (int i = 0; i < FA * KS; ++i) a[i] = *(const v4i*)(s_buf + ((wf * FA + i % FA) * KS + i / FA) * 1024 + l16);
 
-    float sx[FB];
-    int64_t m[FB];
+    auto step = [&](int s, auto C) {
+        constexpr int c = decltype(C)::value, c1 = (c + 1) % 3, c2 = (c + 2) % 3;      // c = s % 3
+        asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(FA * KS) : "memory");
+        write_a(r[c2], c2);                                                           // step s + 2
+        load_a(r[c2], s + 5);
+        load_b(b[c2], s + 2);
+#pragma unroll
+        for (int i = 0; i < FA * KS; ++i) {
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[i % FA][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[c][i / FA * FB + j], acc[i % FA][j], 0, 0, 0);
+            a[i] = *(const v4i*)(s_buf + c1 * BUF + ((wf * FA + i % FA) * KS + i / FA) * 1024 + l16);
+        }
+        // in this order: writes and the features' loads a matrix instruction apart, then a read and a load behind every row of matrix instructions
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < FA * KS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, FB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (i * FB / FA < FB * KS) __builtin_amdgcn_sched_group_barrier(0x020, (FB + FA - 1) / FA, 0);
+        }
+    };
+    int s = 0;
+    for (; s + 3 <= stages; s += 3) {
+        step(s, std::integral_constant<int, 0>());
+        step(s + 1, std::integral_constant<int, 1>());
+        step(s + 2, std::integral_constant<int, 2>());
+    }
+    if (s < stages) step(s, std::integral_constant<int, 0>());
+    if (s + 1 < stages) step(s + 1, std::integral_constant<int, 1>());
+
+    // A lane's results are four features of a token, 16 tokens an instruction: written like that, a store covers a quarter of a line of 16
+    // rows.  They go through LDS, a wavefront's own part of it, and out in pieces of 16 bytes of consecutive features.
+    __syncthreads();
+    char* own = s_buf + wave * 16 * PITCH;
+    constexpr int EL = 16 / (int)sizeof(T), LANES = ROW / 16, ROWS = 64 / LANES;      // elements of a piece, lanes a row, rows a store
 #pragma unroll
     for (int j = 0; j < FB; ++j) {
-        m[j] = (int64_t)(tt + wt * FB + j) * 16 + (lane & 15);
-        sx[j] = p.sx[min(m[j], p.M - 1)];
-    }
+        const float sx = s_sx[(wt * FB + j) * 16 + (lane & 15)];
+        const int64_t m0 = (int64_t)(tt + wt * FB + j) * 16;
 #pragma unroll
-    for (int i = 0; i < FA; ++i) {
-        const int64_t f = (int64_t)(tf + wf * FA + i) * 16 + (lane >> 4) * 4;
-        float sw[4], b[4];
-        di_channels(p, f, sw, b);
+        for (int i0 = 0; i0 < FA; i0 += CH) {
 #pragma unroll
-        for (int j = 0; j < FB; ++j)
-            if (m[j] < p.M && f < p.N) di_store<T>(p, acc[i][j], m[j], f, sx[j], sw, b);
+            for (int i = 0; i < CH; ++i) {
+                const int f = (wf * FA + i0 + i) * 16 + (lane >> 4) * 4;
+                const v4f sw = *(const v4f*)(s_sw + f), bias = *(const v4f*)(s_bias + f);
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = di_result(p, acc[i0 + i][j][e], sx, sw[e], bias[e]);
+                char* to = own + (lane & 15) * PITCH + (i * 16 + (lane >> 4) * 4) * (int)sizeof(T);
+                if constexpr (__is_same(T, float)) *(v4f*)to = (v4f){y[0], y[1], y[2], y[3]};
+                else *(u32x2*)to = (u32x2){f32_pair<T>(y[0], y[1]), f32_pair<T>(y[2], y[3])};
+            }
+            const int64_t f = (int64_t)(tf + wf * FA + i0) * 16 + (lane % LANES) * EL;
+#pragma unroll
+            for (int k = 0; k < 16 / ROWS; ++k) {
+                const int64_t m = m0 + k * ROWS + lane / LANES;
+                const u32x4 v = *(const u32x4*)(own + (k * ROWS + lane / LANES) * PITCH + (lane % LANES) * 16);
+                if (m < p.M && f < p.N) {
+                    T* o = (T*)p.out + m * p.ld + f;
+                    if (f + EL <= p.N) {
+                        if constexpr (__is_same(T, float)) *(u32x4_at4*)o = v;
+                        else *(u32x4_at2*)o = v;
+                    } else {
+                        T part[EL];
+                        __builtin_memcpy(part, &v, 16);
+#pragma unroll
+                        for (int e = 0; e < EL; ++e) if (f + e < p.N) o[e] = part[e];
+                    }
+                }
+            }
+        }
     }
 }
 
@@ -364,18 +478,24 @@ const char* di_range(int64_t rows, int64_t cols) {
 
 int quantize(const char* who, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int8_t* out, float* scale, hipStream_t s) {
     const int steps = (int)di_steps(cols);
-    const dim3 grid((unsigned)((rows + 15) / 16)), block(QR_THREADS);
-    if (dtype == ACCERL_DT_F32) quantize_rows_kernel<float><<<grid, block, 0, s>>>((const float*)x, rows, cols, ld, (v4i*)out, scale, steps);
-    else if (dtype == ACCERL_DT_BF16) quantize_rows_kernel<BF16><<<grid, block, 0, s>>>((const BF16*)x, rows, cols, ld, (v4i*)out, scale, steps);
-    else quantize_rows_kernel<F16><<<grid, block, 0, s>>>((const F16*)x, rows, cols, ld, (v4i*)out, scale, steps);
+    auto go = [&](auto* p) {
+        typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
+        const int64_t padded = (rows + 15) / 16 * 16;
+        if (rows <= QR_SINGLE) quantize_rows_kernel<T, 1, 2><<<dim3((unsigned)padded), dim3(QR_THREADS), 0, s>>>(p, rows, cols, ld, (v4i*)out, scale, steps);
+        else if (cols > QR_SHORT) quantize_rows_kernel<T, 4, 4><<<dim3((unsigned)(padded / 4)), dim3(QR_THREADS), 0, s>>>(p, rows, cols, ld, (v4i*)out, scale, steps);
+        else quantize_rows_kernel<T, 16, 4><<<dim3((unsigned)(padded / 16)), dim3(QR_THREADS), 0, s>>>(p, rows, cols, ld, (v4i*)out, scale, steps);
+    };
+    if (dtype == ACCERL_DT_F32) go((const float*)x);
+    else if (dtype == ACCERL_DT_BF16) go((const BF16*)x);
+    else go((const F16*)x);
     return di_launched(who);
 }
 
-template <typename T, int WF, int WT, int FA, int FB>
+template <typename T, int WF, int WT, int FA, int FB, int KS>
 int tile_go(const char* who, const DenseParams& p, hipStream_t s) {
     const int64_t n = (int64_t)((p.wt + WF * FA - 1) / (WF * FA)) * ((p.xt + WT * FB - 1) / (WT * FB));
     if (n * 64 * WF * WT > MAX_LAUNCH_ITEMS) return di_fail(ACCERL_EUNSUPPORTED, who, "more outputs than one launch covers");
-    dense_i8_tile_kernel<T, WF, WT, FA, FB><<<dim3((unsigned)n), dim3(64 * WF * WT), 0, s>>>(p);
+    dense_i8_tile_kernel<T, WF, WT, FA, FB, KS><<<dim3((unsigned)n), dim3(64 * WF * WT), 0, s>>>(p);
     return di_launched(who);
 }
 template <typename T, int FT, int TT>
@@ -388,13 +508,23 @@ template <typename T>
 int product_as(const char* who, const DenseParams& p, hipStream_t s) {
     const int64_t cus = conv_num_cus();
     auto groups = [&](int bf, int bt) { return (int64_t)((p.wt + bf - 1) / bf) * ((p.xt + bt - 1) / bt); };
-    if (groups(16, 16) >= cus) return tile_go<T, 2, 4, 8, 4>(who, p, s);
-    if (groups(8, 8) >= cus) return tile_go<T, 2, 2, 4, 4>(who, p, s);
-    if (p.xt == 1) return ksplit_go<T, 1, 1>(who, p, s);
-    if (p.xt == 2) return groups(2, 2) >= cus ? ksplit_go<T, 2, 2>(who, p, s) : ksplit_go<T, 1, 2>(who, p, s);
-    if (groups(4, 4) >= 2 * cus) return tile_go<T, 2, 2, 2, 2>(who, p, s);
-    if (groups(2, 4) >= cus) return ksplit_go<T, 2, 4>(who, p, s);
-    return ksplit_go<T, 1, 2>(who, p, s);
+    // (times in us, M x K x N)
+    // 256 x 256 in one workgroup a compute unit where its rounds are nearly full, else 128 features x 256 tokens, two workgroups a compute
+    // unit, whose ends overlap the other's steps: 4096 x 4096 x 4096 55.9 / 58.2, 4096 x 16384 x 4096 199 / 217, but 6000 x 2000 x 5000
+    // 63.8 / 59.2, 8192 x 8192 x 1024 85.7 / 64.9
+    const int64_t full = groups(16, 16), rounds = (full + cus - 1) / cus;
+    if (full >= cus && 10 * full >= 9 * rounds * cus) return tile_go<T, 2, 4, 8, 4, 1>(who, p, s);
+    if (groups(8, 16) >= cus) return tile_go<T, 1, 4, 8, 4, 1>(who, p, s);
+    // 128 x 128, one workgroup a compute unit, where that is one round (64 features x 128 tokens / this: 1024 x 4096 x 4096 22.1 / 20.2,
+    // 512 x 8192 x 8192 47.0 / 40.2, 999 x 1777 x 2501 11.2 / 10.5; in a second round 1500 x 384 x 3000 7.9 / 10.9)
+    if (2 * groups(8, 8) >= cus && groups(8, 8) <= cus) return tile_go<T, 2, 4, 4, 2, 2>(who, p, s);
+    // Fewer: the wavefronts split K, with the largest of their tiles that gives every compute unit work (64 features x 128 tokens /
+    // 32 x 64 split: 512 x 2048 x 2048 8.5 / 7.4, 256 x 4096 x 4096 16.9 / 11.5, but 128 x 4096 x 16384 17.9 / 27.5, 4096 x 512 x 512 5.2 / 7.4).
+    // One or two tiles of tokens stream the weights: one tile of features a workgroup brings more of them under way (24 x 2048 x
+    // 8192: 5.3, two tiles 6.5; 32 x 8192 x 1024: one by one 4.9, two tiles of tokens 6.1).
+    if (groups(2, 4) > 2 * cus && p.xt > 2) return tile_go<T, 1, 4, 4, 2, 2>(who, p, s);
+    if (p.xt <= 2) return p.xt == 2 && p.wt >= cus ? ksplit_go<T, 1, 2>(who, p, s) : ksplit_go<T, 1, 1>(who, p, s);
+    return groups(2, 4) >= cus ? ksplit_go<T, 2, 4>(who, p, s) : ksplit_go<T, 2, 2>(who, p, s);
 }
 int product(const char* who, const DenseParams& p, hipStream_t s) {
     if (p.dtype == ACCERL_DT_F32) return product_as<float>(who, p, s);

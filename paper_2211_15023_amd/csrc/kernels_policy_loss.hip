@@ -281,7 +281,6 @@ template <typename T, int VEC>
 __device__ __forceinline__ void load_vec(const T* row, const uint8_t* mask, int i, int end, float (&v)[VEC]) {
     if (i + VEC <= end) {
         if constexpr (VEC == 4) {
-            typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
             const u32x4 w = *(const u32x4_at4*)(row + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);

@@ -7,6 +7,7 @@ namespace accerl {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // rows may start anywhere (odd widths): these vectors are aligned to one element only, which a vector load or store of the device takes
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 typedef uint32_t u32_at2 __attribute__((aligned(2)));
