@@ -2,10 +2,10 @@
 // With z the logits of a row, z' the reference policy's, p = softmax(z), l = logsumexp(z), a the action:
 //   lp = z_a - l,  r = exp(lp - old),  L = -min(r A, clip(r, 1 - lo, 1 + hi) A) + ck KL - ch H,  H = -sum p log p,
 //   KL = sum p' log(p' / p) | sum p log(p / p') | exp(lr - lp) - (lr - lp) - 1.
-// The gradient has one form for all of them, with coefficients that are the row's:
-//   dL/dz_j = p_j (c0 + c1 (z_j - m) + c2 (z_j - z'_j)) - c3 p'_j + ca [j = a].
-// One pass over a row gives the maxima m, m' and sums under them (of exp(z - m), exp(z - m) (z - m), exp(z' - m') and
-// exp(z' - m') (z' - z) or exp(z - m) (z - z')), corrected where a maximum grows; a second pass writes the gradient.
+// With m = max z, t_j = (z_j - m) log2 e, e_j = 2^t_j, s = sum e the gradient has one form for all kinds, with coefficients that are the row's:
+//   dL/dz_j = e_j (c0 + c1 t_j + c2 (z_j - z'_j)) - c3 e'_j + ca [j = a].
+// One pass over a row gives the maxima and the sums of e, e t, e' and e' (z' - z) or e (z - z'); the gradient is a second one, from registers
+// as far as they hold the row.
 #include <float.h>
 #include <stdio.h>
 
@@ -19,8 +19,12 @@ namespace {
 constexpr int64_t PL_MAX_A = 1 << 20;
 constexpr int PL_RECORDS = 2048;          // workgroups of a row pass, each leaves one record of sums
 constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is split
+constexpr int PL_LONG1 = 80, PL_LONG2 = 40;
+constexpr int PL_SCALAR = 64;             // up to this many actions lanes take single elements
 constexpr float PL_LOG2E = 1.44269504088896340736f;
+constexpr double PL_LN2 = 0.693147180559945309417;
 
+// the sums of a row or of a part of one under its maxima m and m'
 struct RowSum { float m, s, u, mr, sr, t; };
 struct Part { RowSum r; float za, pad; };      // za: the action's logit, in the piece that holds it
 struct Record { double loss, kl, ent, clipped; };
@@ -41,97 +45,125 @@ struct LossParams {
     float ck, ch, scale;
 };
 
-// what a row's gradient and outputs need
-struct Coef { float m, inv_s, mr, inv_sr, c0, c1, c2, c3, ca; int zero; };
+// A power is one multiply-add, t = z log2 e - c with c = m log2 e rounded once (what follows goes by that c), where the maximum lies within
+// -50000 .. 2^20; for others the difference comes first, so that logits of any size lose nothing.
+// A row is tried PLAIN first: all of its logits finite and both maxima in that range; masked places are at -59904, whose power is then 0,
+// and no sum needs care for 0 * inf: 12 operations and two exponentials an element with a reference, where the careful form takes 19.  What
+// is not like that gives sums that are no numbers, or a maximum out of that range, and is done again carefully: masked places at
+// -inf, and a logit counts only where its probability is not 0.
+constexpr float PL_LOW = -50000.0f, PL_HIGH = 0x1p20f;
 
-__device__ __forceinline__ float pl_exp(float d) { return __builtin_amdgcn_exp2f(d * PL_LOG2E); }   // d <= 0: results below 2^-126 may be 0
+struct Base { float c; bool far; };
+__device__ __forceinline__ bool far_off(float m) { return !(m > PL_LOW && m < PL_HIGH); }
+
+// what a row's gradient needs
+struct Coef { Base z, r; float c0, c1, c2, c3, ca; int zero, plain; };
+
+__device__ __forceinline__ float pl_exp2(float t) { return __builtin_amdgcn_exp2f(t); }     // results below 2^-126 may be 0
 __device__ __forceinline__ RowSum row_empty() { return {-FLT_MAX, 0.0f, 0.0f, -FLT_MAX, 0.0f, 0.0f}; }
+template <bool PLAIN> __device__ __forceinline__ Base base(float m) {
+    const bool far = !PLAIN && far_off(m);
+    return {far ? m : m * PL_LOG2E, far};
+}
+template <bool PLAIN> __device__ __forceinline__ float power(const Base& b, float z) {
+    const float t = fmaf(z, PL_LOG2E, -b.c);
+    return PLAIN || !b.far ? t : (z - b.c) * PL_LOG2E;
+}
 
 // Sums under a larger maximum.  The difference of maxima is kept finite so that an empty side's zeros stay zeros.
-template <int KL>
+template <bool PLAIN> __device__ __forceinline__ float moved(float from, float to) {
+    return fmaxf(PLAIN || !(far_off(from) || far_off(to)) ? from * PL_LOG2E - to * PL_LOG2E : (from - to) * PL_LOG2E, -FLT_MAX);
+}
+template <int KL, bool PLAIN>
 __device__ __forceinline__ void row_raise(RowSum& a, float m, float mr) {
-    const float d = fmaxf(a.m - m, -FLT_MAX), f = pl_exp(d);
+    const float d = moved<PLAIN>(a.m, m), f = pl_exp2(d);
     a.u = f * (a.u + a.s * d);
     a.s *= f;
     if constexpr (KL == 2) a.t *= f;
     a.m = m;
     if constexpr (KL != 0) {
-        const float fr = pl_exp(fmaxf(a.mr - mr, -FLT_MAX));
+        const float fr = pl_exp2(moved<PLAIN>(a.mr, mr));
         a.sr *= fr;
         if constexpr (KL == 1) a.t *= fr;
         a.mr = mr;
     }
 }
-template <int KL>
+template <int KL, bool PLAIN>
 __device__ __forceinline__ RowSum row_join(RowSum a, RowSum b) {
     const float m = fmaxf(a.m, b.m), mr = fmaxf(a.mr, b.mr);
-    row_raise<KL>(a, m, mr);
-    row_raise<KL>(b, m, mr);
+    row_raise<KL, PLAIN>(a, m, mr);
+    row_raise<KL, PLAIN>(b, m, mr);
     a.s += b.s; a.u += b.u; a.sr += b.sr; a.t += b.t;
     return a;
 }
-// The sums take one element.  Its probability decides whether its logit counts: masked places are -inf, and 0 * inf is no part of a sum.
-template <int KL>
-__device__ __forceinline__ void row_add(RowSum& a, float z, float zr) {
-    const float d = z - a.m, e = pl_exp(d);
+// the sums take one element; c and cr are the bases of a's maxima
+template <int KL, bool PLAIN>
+__device__ __forceinline__ void row_add(RowSum& a, const Base& c, const Base& cr, float z, float zr) {
+    const float t = power<PLAIN>(c, z), e = pl_exp2(t);
     a.s += e;
-    a.u = fmaf(e, fmaxf(d, -1000.0f), a.u);
+    a.u = fmaf(e, PLAIN ? t : fmaxf(t, -1500.0f), a.u);
     if constexpr (KL != 0) {
-        const float er = pl_exp(zr - a.mr);
+        const float er = pl_exp2(power<PLAIN>(cr, zr));
         a.sr += er;
-        if constexpr (KL == 1) a.t = fmaf(er, er > 0.0f ? zr - z : 0.0f, a.t);
-        else a.t = fmaf(e, e > 0.0f ? z - zr : 0.0f, a.t);
+        if constexpr (KL == 1) a.t = fmaf(er, PLAIN || er > 0.0f ? zr - z : 0.0f, a.t);
+        else a.t = fmaf(e, PLAIN || e > 0.0f ? z - zr : 0.0f, a.t);
     }
 }
-template <int KL>
+// whether a plain row's joined sums hold
+template <int KL, typename S>
+__device__ __forceinline__ bool row_held(const S& a) {
+    const bool z = !far_off(a.m) && fabs(a.s) < 1e30f && fabs(a.u) < 1e30f;
+    return z && (KL == 0 || (!far_off(a.mr) && fabs(a.sr) < 1e30f && fabs(a.t) < 1e30f));
+}
+template <int KL, bool PLAIN>
 __device__ __forceinline__ RowSum row_shuffle(RowSum a, int lanes) {
     for (int o = lanes >> 1; o > 0; o >>= 1) {
         RowSum b;
         b.m = __shfl_xor(a.m, o); b.s = __shfl_xor(a.s, o); b.u = __shfl_xor(a.u, o);
         b.mr = b.sr = b.t = 0.0f;
         if constexpr (KL != 0) { b.mr = __shfl_xor(a.mr, o); b.sr = __shfl_xor(a.sr, o); b.t = __shfl_xor(a.t, o); }
-        a = row_join<KL>(a, b);
+        a = row_join<KL, PLAIN>(a, b);
     }
     return a;
 }
 
 // the gradient at one element
-template <int KL>
+template <int KL, bool PLAIN>
 __device__ __forceinline__ float grad_at(const Coef& c, float z, float zr) {
-    const float d = z - c.m, p = pl_exp(d) * c.inv_s;
-    float t = fmaf(c.c1, fmaxf(d, -1000.0f), c.c0);
-    if constexpr (KL == 2) t = fmaf(c.c2, p == 0.0f ? 0.0f : fminf(z - zr, FLT_MAX), t);
-    t *= p;
-    if constexpr (KL == 1) t = fmaf(-c.c3, pl_exp(zr - c.mr) * c.inv_sr, t);
-    return t;
+    const float t = power<PLAIN>(c.z, z), e = pl_exp2(t);
+    float k = fmaf(c.c1, PLAIN ? t : fmaxf(t, -1500.0f), c.c0);
+    if constexpr (KL == 2) k = fmaf(c.c2, PLAIN ? z - zr : e == 0.0f ? 0.0f : fminf(z - zr, FLT_MAX), k);
+    k *= e;
+    if constexpr (KL == 1) k = fmaf(-c.c3, pl_exp2(power<PLAIN>(c.r, zr)), k);
+    return k;
 }
 
 struct RowOut { float loss, lp, kl, ent, clipped; };
+// A row's sums on their way to its scalars, in R.  kl: the KL where it was worked out more exactly (see loss_rows_kernel), negative: not known.
+template <typename R> struct Sums { float m, mr; R s, u, sr, t, kl; };
 
-__device__ __forceinline__ float pl_log(float x) { return logf(x); }
-__device__ __forceinline__ double pl_log(double x) { return log(x); }
-__device__ __forceinline__ float pl_log_ratio(float a, float b) {        // log(a / b), exact to its own size where a is close to b
-    const float q = a / b;
-    return q > 0.5f && q < 2.0f ? log1pf((a - b) / b) : logf(q);
-}
-__device__ __forceinline__ double pl_log_ratio(double a, double b) { return log(a / b); }
-__device__ __forceinline__ float pl_exp_full(float x) { return expf(x); }
-__device__ __forceinline__ double pl_exp_full(double x) { return exp(x); }
+__device__ __forceinline__ float pl_log2(float x) { return log2f(x); }
+__device__ __forceinline__ double pl_log2(double x) { return log2(x); }
+__device__ __forceinline__ float pl_exp(float x) { return expf(x); }
+__device__ __forceinline__ double pl_exp(double x) { return exp(x); }
 
 // Scalars of a row from its sums.  R: float where a wavefront holds many rows, double where the row is long and a wavefront does it once.
 // The ratio may be replaced (`ratio`, a double) by one that was worked out more exactly.
 template <int KL, typename R>
-__device__ __forceinline__ void row_finish(const LossParams& p, const RowSum& q, int64_t row, float za, const double* ratio, Coef& c, RowOut& o) {
-    const bool empty = q.s == 0.0f;
-    const R ls = pl_log((R)q.s), lp = ((R)za - (R)q.m) - ls, ent = ls - (R)q.u / (R)q.s;
-    c.m = q.m; c.mr = q.mr; c.inv_s = (float)((R)1 / (R)q.s); c.inv_sr = q.sr == 0.0f ? 0.0f : (float)((R)1 / (R)q.sr);
+__device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q, bool plain, int64_t row, float za, const double* ratio, Coef& c, RowOut& o) {
+    const bool empty = q.s == (R)0;
+    const R ln2 = (R)PL_LN2, l2 = pl_log2(q.s), inv = (R)1 / q.s;
+    c.z = base<false>(q.m); c.r = base<false>(q.mr); c.plain = plain;
+    // the power of the action, as the sum's terms have theirs
+    const R ta = __is_same(R, float) ? (R)power<false>(c.z, za) : c.z.far ? ((R)za - (R)c.z.c) / ln2 : (R)za * (R)PL_LOG2E - (R)c.z.c;
+    const R lp = ln2 * (ta - l2), ent = ln2 * (l2 - q.u * inv);
     c.zero = empty;
     o.lp = empty ? -INFINITY : (float)lp;
     o.ent = empty ? 0.0f : (float)ent;
     o.loss = o.kl = o.clipped = 0.0f;
     if (p.only_lp) return;
     const float w = p.w ? p.w[row] : 1.0f, adv = p.adv[row];
-    const R r = ratio ? (R)*ratio : lp == (R)-INFINITY ? (R)0 : pl_exp_full(lp - (R)p.old[row]);
+    const R r = ratio ? (R)*ratio : lp == (R)-INFINITY ? (R)0 : pl_exp(lp - (R)p.old[row]);
     const bool above = ratio ? *ratio > p.hi : r > (R)p.hi, below = ratio ? *ratio < p.lo : r < (R)p.lo;
     const bool cut = adv >= 0.0f ? above : below;
     const R pg = cut ? -(adv >= 0.0f ? (R)p.hi : (R)p.lo) * (R)adv : -r * (R)adv;
@@ -139,24 +171,29 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const RowSum& q,
     const R ck = p.ck, ch = p.ch;
     if constexpr (KL == 0) {
         if (p.kind == ACCERL_KL_SAMPLED) {
-            const R d = (R)p.ref_lp[row] - lp, e = pl_exp_full(d);
+            const R d = (R)p.ref_lp[row] - lp, e = pl_exp(d);
             kl = d == (R)INFINITY ? d : e - d - (R)1;
             if (ck != (R)0) at += ck * ((R)1 - e);
         }
     } else {
-        const R dl = ((R)q.m - (R)q.mr) + pl_log_ratio((R)q.s, (R)q.sr);       // l - l'
+        const bool none = q.sr == (R)0;
+        const bool far = c.z.far || c.r.far;                      // l - l'
+        const R dl = (far ? (R)q.m - (R)q.mr : ((R)c.z.c - (R)c.r.c) * ln2) + ln2 * pl_log2(q.s / q.sr);
         if constexpr (KL == 1) {
-            if (q.sr != 0.0f) { kl = (R)q.t / (R)q.sr + dl; c0 = ck; c3 = ck; }
+            if (!none) { kl = q.t / q.sr + dl; c0 = ck; c3 = ck / q.sr; }
         } else {
-            kl = q.sr == 0.0f ? (R)INFINITY : (R)q.t / (R)q.s - dl;
+            kl = none ? (R)INFINITY : q.t * inv - dl;
+        }
+        if (q.kl >= (R)0 && kl < (R)0.5) kl = q.kl;
+        if constexpr (KL == 2) {
             if (ck != (R)0) c0 = -ck * (dl + kl);
             c2 = ck;
         }
     }
     const R by = (R)w * (R)p.scale;
-    c.c0 = (float)(by * (c0 - at + ch * (ent - ls)));
-    c.c1 = (float)(by * ch);
-    c.c2 = (float)(by * c2);
+    c.c0 = (float)(by * inv * (c0 - at + ch * (ent - ln2 * l2)));
+    c.c1 = (float)(by * inv * ch * ln2);
+    c.c2 = (float)(by * inv * c2);
     c.c3 = (float)(by * c3);
     c.ca = (float)(by * at);
     if (empty) { o.ent = 0.0f; return; }
@@ -180,76 +217,237 @@ __device__ __forceinline__ void rec_add(const LossParams& p, Record& r, int64_t 
     r.loss += w * o.loss; r.kl += w * o.kl; r.ent += w * o.ent; r.clipped += w * o.clipped;
 }
 
-// ---------------------------------------------------------------- narrow rows: several lanes of a wavefront hold one
-// G lanes hold a row, lane j its elements j, j + G, ..  (E of them at most).  A wavefront does 64 / G rows at a time.
+// ---------------------------------------------------------------- vectors of a row
+// VEC elements of a row as they lie in memory (16 bytes, or one element of a narrow row); what is masked out, or no part of the row, is -inf.
+template <typename T, int VEC> struct Vec {
+    u32x4 w;
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else { float a, b; el_pair<T>(w[e / 2], a, b); return e & 1 ? b : a; }
+    }
+};
+template <typename T> struct Vec<T, 1> {
+    float w;
+    __device__ __forceinline__ float at(int) const { return w; }
+};
+// what stands in a masked place: -59904 of a plain row, else -inf
+template <typename T, bool PLAIN> constexpr uint32_t nothing() {
+    if (PLAIN) return __is_same(T, float) ? 0xc76a0000u : __is_same(T, BF16) ? 0xc76ac76au : 0xfb50fb50u;
+    return __is_same(T, float) ? 0xff800000u : __is_same(T, BF16) ? 0xff80ff80u : 0xfc00fc00u;
+}
+template <bool PLAIN> constexpr float nothing_f() { return PLAIN ? -59904.0f : -INFINITY; }
+
+// Between two passes over a lane's vectors: what the first made of them (floats, powers) is made again in the second and not kept, which took
+// every register of a wavefront.
+template <typename T, int VEC, int N> __device__ __forceinline__ void vec_again(Vec<T, VEC> (&v)[N]) {
+    if constexpr (VEC > 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i].w));
+    }
+}
+
+// A vector that would pass the end is moved back to end there (a row has VEC elements at least); what vectors before it have counts as
+// masked, and of one past the end that is everything.
+template <int VEC> __device__ __forceinline__ int vec_at(int i, int end) { return VEC == 1 ? i : min(i, end - VEC); }
+
+// The lane as the compiler cannot follow it: it would work out every vector's addresses and conditions before the loop over the rows and
+// keep them in registers.
+__device__ __forceinline__ int opaque(int i) { asm volatile("" : "+v"(i)); return i; }
+
+// `part` of a vector's element e in its word
+template <typename T> __device__ __forceinline__ uint32_t vec_part(int e) { return sizeof(T) == 4 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu; }
+template <bool PLAIN, typename T, int VEC>
+__device__ __forceinline__ void vec_drop(Vec<T, VEC>& v, int e) {
+    constexpr int PER = 4 / (int)sizeof(T);
+    v.w[e / PER] = (v.w[e / PER] & ~vec_part<T>(e)) | (nothing<T, PLAIN>() & vec_part<T>(e));
+}
+// FULL: the vector ends before the end.
+template <bool FULL, bool PLAIN, typename T, int VEC>
+__device__ __forceinline__ void vec_load(Vec<T, VEC>& v, const T* row, const uint8_t* mask, int i, int end) {
+    if constexpr (VEC == 1) {
+        v.w = i < end && (!mask || mask[i]) ? el_f32(row[i]) : nothing_f<PLAIN>();
+    } else {
+        const int at = FULL ? i : vec_at<VEC>(i, end);
+        if constexpr (sizeof(T) == 4) v.w = *(const u32x4_at4*)(row + at);
+        else v.w = *(const u32x4_at2*)(row + at);
+        if (mask) {
+#pragma unroll
+            for (int k = 0; k < VEC / 4; ++k) {
+                typedef uint32_t u32_at1 __attribute__((aligned(1)));
+                const uint32_t m = *(const u32_at1*)(mask + at + 4 * k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (!((m >> (8 * e)) & 0xffu)) vec_drop<PLAIN>(v, 4 * k + e);
+            }
+        }
+        if (!FULL && at != i) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) if (at + e < i) vec_drop<PLAIN>(v, e);
+        }
+    }
+}
+template <bool FULL, typename T, int VEC>
+__device__ __forceinline__ void vec_store(T* row, int i, int end, const float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        if (i < end) row[i] = f32_el<T>(v[0]);
+    } else if (FULL || i + VEC <= end) {
+        if constexpr (VEC == 4) {
+            *(u32x4_at4*)(row + i) = (u32x4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        } else {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = f32_pair<T>(v[2 * e], v[2 * e + 1]);
+            *(u32x4_at2*)(row + i) = w;
+        }
+    } else {
+        const int at = vec_at<VEC>(i, end);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) if (at + e >= i) row[at + e] = f32_el<T>(v[e]);
+    }
+}
+// the gradient of a vector's elements, to memory
+template <bool FULL, int KL, bool PLAIN, typename T, int VEC>
+__device__ __forceinline__ void vec_grad(const Coef& c, int act, const Vec<T, VEC>& z, const Vec<T, VEC>& zr, T* g, int i, int end) {
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = grad_at<KL, PLAIN>(c, z.at(e), KL ? zr.at(e) : 0.0f);
+    const int a = act - (FULL ? i : vec_at<VEC>(i, end));
+    if ((unsigned)a < (unsigned)VEC) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] += a == e ? c.ca : 0.0f;
+    }
+    vec_store<FULL>(g, i, end, v);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void zero_row(T* g, int first, int end, int lane, int lanes) {
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = 0.0f;
+    for (int i = first + lane * VEC; i < end; i += lanes * VEC) vec_store<false>(g, i, end, v);
+}
+
+// ---------------------------------------------------------------- rows that lanes of one wavefront hold
+// G lanes hold a row, lane j its vectors j, j + G, ..  (H of them at most).  A wavefront does 64 / G rows at a time.
 constexpr int NR_THREADS = 256;
-template <typename T, int KL, int E>
-__global__ __launch_bounds__(NR_THREADS) void loss_narrow_kernel(const LossParams p, int G) {
+template <typename T, int KL, int VEC, int H>
+__global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams p, int G) {
     __shared__ Record s_rec[NR_THREADS / 64];
-    const int tid = threadIdx.x, j = tid & (G - 1);
+    const int tid = threadIdx.x;
     const int rows = NR_THREADS / G;
     Record rec = {0, 0, 0, 0};
     for (int64_t row = (int64_t)blockIdx.x * rows + tid / G; row < p.B; row += (int64_t)gridDim.x * rows) {
+        const int j = opaque(tid & (G - 1));
         RowOut o = {0, 0, 0, 0, 0};
         T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
         if (row_dead(p, row)) {
-            if (g)
-                for (int i = j; i < p.A; i += G) g[i] = f32_el<T>(0.0f);
+            if (g) zero_row<T, VEC>(g, 0, p.A, j, G);
             if (j == 0) row_store(p, row, o);
             continue;
         }
         const T* z = (const T*)p.z + row * p.ldz;
         const T* zr = KL ? (const T*)p.zr + row * p.ldr : nullptr;
         const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-        float a[E], b[E];
-        RowSum q = row_empty();
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int at = j + i * G;
-            const bool in = at < p.A && (!mask || mask[at]);
-            a[i] = in ? el_f32(z[at]) : -INFINITY;
-            b[i] = KL && in ? el_f32(zr[at]) : -INFINITY;
-            q.m = fmaxf(q.m, a[i]);
-            q.mr = fmaxf(q.mr, b[i]);
-        }
-        for (int k = G >> 1; k > 0; k >>= 1) {
-            q.m = fmaxf(q.m, __shfl_xor(q.m, k));
-            if constexpr (KL != 0) q.mr = fmaxf(q.mr, __shfl_xor(q.mr, k));
-        }
-#pragma unroll
-        for (int i = 0; i < E; ++i) row_add<KL>(q, a[i], b[i]);
-        for (int k = G >> 1; k > 0; k >>= 1) {
-            q.s += __shfl_xor(q.s, k);
-            q.u += __shfl_xor(q.u, k);
-            if constexpr (KL != 0) { q.sr += __shfl_xor(q.sr, k); q.t += __shfl_xor(q.t, k); }
-        }
         const int act = p.act[row];
         const float za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
+        Vec<T, VEC> a[H], b[H];
+        RowSum q;
+        float better_kl = -1.0f;
+        auto sums = [&](auto mode) {
+            constexpr bool PLAIN = decltype(mode)::value;
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                vec_load<false, PLAIN>(a[i], z, mask, (j + i * G) * VEC, p.A);
+                if constexpr (KL != 0) vec_load<false, PLAIN>(b[i], zr, mask, (j + i * G) * VEC, p.A);
+            }
+            q = row_empty();
+#pragma unroll
+            for (int i = 0; i < H; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) { q.m = fmaxf(q.m, a[i].at(e)); if constexpr (KL != 0) q.mr = fmaxf(q.mr, b[i].at(e)); }
+            for (int k = G >> 1; k > 0; k >>= 1) {
+                q.m = fmaxf(q.m, __shfl_xor(q.m, k));
+                if constexpr (KL != 0) q.mr = fmaxf(q.mr, __shfl_xor(q.mr, k));
+            }
+            const Base c = base<PLAIN>(q.m), cr = base<PLAIN>(q.mr);
+            vec_again(a);
+            if constexpr (KL != 0) vec_again(b);
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) row_add<KL, PLAIN>(q, c, cr, a[i].at(e), KL ? b[i].at(e) : 0.0f);
+                if (VEC > 1) __builtin_amdgcn_sched_barrier(0);      // (all vectors' elements at once would take every register)
+            }
+            // A small KL is the difference of sums that are hundreds of times larger, and 32-bit sums would leave it six digits.
+            if constexpr (KL != 0 && VEC > 1) {
+                // lanes' sums joined in 64 bits
+                double ds = q.s, dsr = q.sr, dt = q.t;
+                for (int k = G >> 1; k > 0; k >>= 1) { ds += __shfl_xor(ds, k); dsr += __shfl_xor(dsr, k); dt += __shfl_xor(dt, k); q.u += __shfl_xor(q.u, k); }
+                q.s = (float)ds; q.sr = (float)dsr; q.t = (float)dt;
+                const double apart = c.far || cr.far ? ((double)q.m - q.mr) / PL_LN2 : (double)c.c - cr.c;
+                better_kl = (float)(KL == 1 ? dt / dsr + PL_LN2 * (apart + log2(ds / dsr)) : dt / ds - PL_LN2 * (apart + log2(ds / dsr)));
+                better_kl = fmaxf(better_kl, 0.0f);
+            } else {
+                for (int k = G >> 1; k > 0; k >>= 1) {
+                    q.s += __shfl_xor(q.s, k);
+                    q.u += __shfl_xor(q.u, k);
+                    if constexpr (KL != 0) { q.sr += __shfl_xor(q.sr, k); q.t += __shfl_xor(q.t, k); }
+                }
+            }
+            if constexpr (KL != 0 && VEC == 1) {
+                // With D_j the difference of logits less its mean under p' (forward) or p, KL = log E[exp(-D)] exactly, that is
+                // log1p(E[exp(-D) - 1 + D]): a sum of small terms that are none of them negative.
+                const float inv = 1.0f / (KL == 1 ? q.sr : q.s), mean = q.t * inv;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < H; ++i) {
+                    const float x = a[i].at(0), y = b[i].at(0);
+                    const float w = pl_exp2(KL == 1 ? power<PLAIN>(cr, y) : power<PLAIN>(c, x)), d = (KL == 1 ? y - x : x - y) - mean;
+                    float f = pl_exp2(-PL_LOG2E * d) - 1.0f + d;
+                    if (fabsf(d) < 0.5f)              // its series, to d^8
+                        f = d * d * fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.0f / 40320, -1.0f / 5040), 1.0f / 720), -1.0f / 120), 1.0f / 24), -1.0f / 6), 0.5f);
+                    sum = fmaf(w, w > 0.0f ? f : 0.0f, sum);
+                }
+                for (int k = G >> 1; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+                better_kl = log1pf(sum * inv);
+            }
+        };
+        sums(std::true_type());
+        const bool plain = row_held<KL>(q);
+        if (!plain) sums(std::false_type());             // (all lanes of a row alike)
         Coef c;
         double ratio;
         const double* better = nullptr;
         if (!p.only_lp && q.s > 0.0f) {
             // Next to a clipping border the side decides over the whole gradient: there the sum is taken again in 64 bits.  (All lanes of
             // a row branch alike; the 32-bit ratio is off by a few parts in 2^24.)
-            const float r = expf(za - q.m - logf(q.s) - p.old[row]);
+            const float r = expf((za - q.m) - logf(q.s) - p.old[row]);
             if (fabsf(r - (float)p.hi) < 4e-6f * r || fabsf(r - (float)p.lo) < 4e-6f * r) {
                 double s = 0.0;
-#pragma unroll
-                for (int i = 0; i < E; ++i) s += exp((double)a[i] - (double)q.m);
+#pragma unroll 1
+                for (int i = j * VEC; i < p.A; i += G * VEC)
+#pragma unroll 1
+                    for (int e = i; e < min(i + VEC, p.A); ++e)
+                        if (!mask || mask[e]) s += exp((double)el_f32(z[e]) - (double)q.m);
                 for (int k = G >> 1; k > 0; k >>= 1) s += __shfl_xor(s, k);
                 ratio = exp((double)za - (double)q.m - log(s) - (double)p.old[row]);
                 better = &ratio;
             }
         }
-        row_finish<KL, float>(p, q, row, za, better, c, o);
+        const Sums<float> joined = {q.m, q.mr, q.s, q.u, q.sr, q.t, better_kl};
+        row_finish<KL, float>(p, joined, plain, row, za, better, c, o);
         if (g) {
+            if (c.zero) zero_row<T, VEC>(g, 0, p.A, j, G);
+            else {
+                auto grads = [&](auto mode) {
+                    vec_again(a);
+                    if constexpr (KL != 0) vec_again(b);
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const int at = j + i * G;
-                if (at >= p.A) break;
-                float v = grad_at<KL>(c, a[i], b[i]);
-                if (at == act) v += c.ca;
-                g[at] = f32_el<T>(c.zero ? 0.0f : v);
+                    for (int i = 0; i < H; ++i) {
+                        if ((j + i * G) * VEC < p.A) vec_grad<false, KL, decltype(mode)::value>(c, act, a[i], b[i], g, (j + i * G) * VEC, p.A);
+                        if (VEC > 1) __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if (plain) grads(std::true_type());
+                else grads(std::false_type());
             }
         }
         if (j == 0) {
@@ -273,114 +471,155 @@ __global__ __launch_bounds__(NR_THREADS) void loss_narrow_kernel(const LossParam
 }
 
 // ---------------------------------------------------------------- wide rows: a workgroup holds one, or a piece of one
-constexpr int WR_THREADS = 512;
-constexpr int WR_WAVES = WR_THREADS / 64;
+constexpr int WR_THREADS = 256;
+constexpr int WR_WAVES = 8;               // most wavefronts of a workgroup
 
-// A vector of 16 bytes of a row from element i on as floats; past the end, and where the mask has a zero, -inf.
-template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T* row, const uint8_t* mask, int i, int end, float (&v)[VEC]) {
-    if (i + VEC <= end) {
-        if constexpr (VEC == 4) {
-            const u32x4 w = *(const u32x4_at4*)(row + i);
+// The vectors of elements first to end, U at a time, loaded together and ahead of the ones before; the last ones one by one.  f(whole,
+// vectors, vectors of the reference, first element): `whole` (a type) where no vector passes the end.
+template <typename T, int KL, int THREADS, int U, bool PLAIN, typename F>
+__device__ __forceinline__ void wide_stream(const T* z, const T* zr, const uint8_t* mask, int first, int end, F&& f) {
+    constexpr int VEC = 16 / sizeof(T), STEP = THREADS * VEC;
+    Vec<T, VEC> a[U], b[U];
+    int i = first + opaque(threadIdx.x) * VEC;
+    auto load = [&](auto whole, int at) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
-        } else {
-            const u32x4 w = *(const u32x4_at2*)(row + i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) el_pair<T>(w[e], v[2 * e], v[2 * e + 1]);
+        for (int u = 0; u < U; ++u) {
+            vec_load<decltype(whole)::value, PLAIN>(a[u], z, mask, at + u * STEP, end);
+            if constexpr (KL != 0) vec_load<decltype(whole)::value, PLAIN>(b[u], zr, mask, at + u * STEP, end);
         }
-        if (mask) {
+    };
+    const int turns = (end - first) / (U * STEP);              // whole ones
+    if (turns > 0) {
+        load(std::true_type(), i);
+        for (int k = 1; k <= turns; ++k, i += U * STEP) {
+            Vec<T, VEC> x[U], y[U];
 #pragma unroll
-            for (int k = 0; k < VEC / 4; ++k) {
-                typedef uint32_t u32_at1 __attribute__((aligned(1)));
-                const uint32_t w = *(const u32_at1*)(mask + i + 4 * k);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) if (!((w >> (8 * e)) & 0xffu)) v[4 * k + e] = -INFINITY;
-            }
+            for (int u = 0; u < U; ++u) { x[u] = a[u]; if constexpr (KL != 0) y[u] = b[u]; }
+            if (k < turns) load(std::true_type(), i + U * STEP);
+            f(std::true_type(), x, y, i);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = i + e < end && (!mask || mask[i + e]) ? el_f32(row[i + e]) : -INFINITY;
     }
+    // the rest, as many vectors as there are (the whole workgroup alike)
+    const int rest = first + turns * (U * STEP);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (rest + u * STEP < end) {
+            vec_load<false, PLAIN>(a[u], z, mask, i + u * STEP, end);
+            if constexpr (KL != 0) vec_load<false, PLAIN>(b[u], zr, mask, i + u * STEP, end);
+        }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (rest + u * STEP < end) {
+            const Vec<T, VEC> x[1] = {a[u]}, y[1] = {b[u]};
+            f(std::false_type(), x, y, i + u * STEP);
+        }
 }
-template <typename T, int VEC>
-__device__ __forceinline__ void store_vec(T* row, int i, int end, const float (&v)[VEC]) {
-    if (i + VEC <= end) {
-        if constexpr (VEC == 4) {
-            typedef v4f v4f_at4 __attribute__((aligned(4)));
-            *(v4f_at4*)(row + i) = (v4f){v[0], v[1], v[2], v[3]};
-        } else {
-            u32x4 w;
+// vectors `first` to `first + N` of an array
+template <int KL, int N, bool PLAIN, typename T, int VEC, int ALL>
+__device__ __forceinline__ void sum_vecs(RowSum& q, const Vec<T, VEC> (&x)[ALL], const Vec<T, VEC> (&y)[ALL], int first) {
+    float m = q.m, mr = q.mr;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = f32_pair<T>(v[2 * e], v[2 * e + 1]);
-            *(u32x4_at2*)(row + i) = w;
-        }
-    } else {
+    for (int u = 0; u < N; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) if (i + e < end) row[i + e] = f32_el<T>(v[e]);
-    }
+        for (int e = 0; e < VEC; ++e) { m = fmaxf(m, x[first + u].at(e)); if constexpr (KL != 0) mr = fmaxf(mr, y[first + u].at(e)); }
+    row_raise<KL, PLAIN>(q, m, mr);
+    const Base c = base<PLAIN>(m), cr = base<PLAIN>(mr);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) row_add<KL, PLAIN>(q, c, cr, x[first + u].at(e), KL ? y[first + u].at(e) : 0.0f);
 }
 
-template <typename T, int KL>
-__device__ __forceinline__ RowSum wide_sum(const T* z, const T* zr, const uint8_t* mask, int first, int end) {
-    constexpr int VEC = 16 / sizeof(T);
-    RowSum q = row_empty();
-    for (int i = first + (int)threadIdx.x * VEC; i < end; i += WR_THREADS * VEC) {
-        float a[VEC], b[VEC];
-        load_vec<T, VEC>(z, mask, i, end, a);
-        if constexpr (KL != 0) load_vec<T, VEC>(zr, mask, i, end, b);
-        float m = q.m, mr = q.mr;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) { m = fmaxf(m, a[e]); if constexpr (KL != 0) mr = fmaxf(mr, b[e]); }
-        row_raise<KL>(q, m, mr);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) row_add<KL>(q, a[e], KL ? b[e] : 0.0f);
-    }
-    return row_shuffle<KL>(q, 64);
-}
-// the sums of the workgroup's wavefronts, in wavefront 0 (all of its lanes)
+// What the workgroup of a row shares.  The row's scalars are worked out by wavefront 0 in 64 bits, in a function that is called: inside the
+// kernels its registers, and constants that the compiler keeps for the next row, would be everybody's.
+struct WideShared {
+    LossParams p;
+    RowSum sum[WR_WAVES];
+    Coef coef;
+    RowOut out;
+    int waves;
+};
 template <int KL>
-__device__ __forceinline__ RowSum wide_join(RowSum q, RowSum (&s)[WR_WAVES]) {
-    const int lane = threadIdx.x & 63;
-    if (lane == 0) s[threadIdx.x >> 6] = q;
+__device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain, int64_t row, float za) {
+    Sums<double> r = {-FLT_MAX, -FLT_MAX, 0.0, 0.0, 0.0, 0.0, -1.0};
+    for (int k = 0; k < w->waves; ++k) { r.m = fmaxf(r.m, w->sum[k].m); r.mr = fmaxf(r.mr, w->sum[k].mr); }
+    for (int k = 0; k < w->waves; ++k) {
+        const RowSum s = w->sum[k];
+        const double d = plain ? moved<true>(s.m, r.m) : moved<false>(s.m, r.m), f = pl_exp2((float)d);
+        const double fr = KL ? pl_exp2(plain ? moved<true>(s.mr, r.mr) : moved<false>(s.mr, r.mr)) : 0.0;
+        r.s += f * s.s;
+        r.u += f * (s.u + s.s * d);
+        r.sr += fr * s.sr;
+        r.t += (KL == 2 ? f : fr) * s.t;
+    }
+    Coef c;
+    RowOut o;
+    row_finish<KL, double>(w->p, r, plain, row, za, nullptr, c, o);
+    if (plain && !row_held<KL>(r)) c.plain = -1;                  // to be done again
+    if (threadIdx.x == 0) { w->coef = c; w->out = o; }
+}
+// The row's coefficients, to everybody, and its outputs, to thread 0 (`w.out`).
+template <int KL, bool PLAIN>
+__device__ __forceinline__ Coef wide_coef(WideShared& w, const RowSum& q, int64_t row, float za) {
+    if ((threadIdx.x & 63) == 0) w.sum[threadIdx.x >> 6] = q;
     __syncthreads();
-    return row_shuffle<KL>(s[lane & (WR_WAVES - 1)], WR_WAVES);
+    if (threadIdx.x < 64) wide_finish<KL>(&w, PLAIN, row, za);
+    __syncthreads();
+    return w.coef;
 }
-template <typename T>
-__device__ __forceinline__ void wide_zero(T* g, int first, int end) {
-    constexpr int VEC = 16 / sizeof(T);
-    float v[VEC] = {};
-    for (int i = first + (int)threadIdx.x * VEC; i < end; i += WR_THREADS * VEC) store_vec<T, VEC>(g, i, end, v);
+
+// The vectors tid, THREADS + tid, .. of a row, whole ones.  All are requested before anything is done with one; a mask is seen to afterwards.
+template <int THREADS, typename T, int VEC, int H>
+__device__ __forceinline__ void held_load(Vec<T, VEC> (&v)[H], const T* row, int tid) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+        const T* from = (const T*)((const char*)row + (uint32_t)((i * THREADS + tid) * 16));
+        if constexpr (sizeof(T) == 4) v[i].w = *(const u32x4_at4*)from;
+        else v[i].w = *(const u32x4_at2*)from;
+    }
 }
-template <typename T, int KL>
-__device__ __forceinline__ void wide_grad(const LossParams& p, const Coef& c, int act, const T* z, const T* zr, const uint8_t* mask, T* g, int first, int end) {
-    constexpr int VEC = 16 / sizeof(T);
-    for (int i = first + (int)threadIdx.x * VEC; i < end; i += WR_THREADS * VEC) {
-        float a[VEC], b[VEC];
-        load_vec<T, VEC>(z, mask, i, end, a);
-        if constexpr (KL != 0) load_vec<T, VEC>(zr, mask, i, end, b);
+template <bool TWO, int THREADS, typename T, int VEC, int H>
+__device__ __forceinline__ void held_mask(Vec<T, VEC> (&a)[H], Vec<T, VEC> (&b)[H], const uint8_t* mask, int tid) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) a[e] = grad_at<KL>(c, a[e], KL ? b[e] : 0.0f);
-        if ((unsigned)(act - i) < (unsigned)VEC) {
+    for (int i = 0; i < H; ++i) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) a[e] += act - i == e ? c.ca : 0.0f;
+        for (int k = 0; k < VEC / 4; ++k) {
+            typedef uint32_t u32_at1 __attribute__((aligned(1)));
+            const uint32_t m = *(const u32_at1*)(mask + (uint32_t)((i * THREADS + tid) * VEC + 4 * k));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!((m >> (8 * e)) & 0xffu)) { vec_drop<true>(a[i], 4 * k + e); if (TWO) vec_drop<true>(b[i], 4 * k + e); }
         }
-        store_vec<T, VEC>(g, i, end, a);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// Rows one after the other, each by the whole workgroup.
-template <typename T, int KL>
-__global__ __launch_bounds__(WR_THREADS) void loss_wide_kernel(const LossParams p) {
-    __shared__ RowSum s_sum[WR_WAVES];
-    __shared__ Coef s_coef;
+template <int KL, typename T, int VEC, int H>
+__device__ __forceinline__ void held_sums(RowSum& q, const Vec<T, VEC> (&a)[H], const Vec<T, VEC> (&b)[H]) {
+#pragma unroll
+    for (int i = 0; i + 2 <= H; i += 2) {
+        sum_vecs<KL, 2, true>(q, a, b, i);
+        __builtin_amdgcn_sched_barrier(0);                          // (more of them at once would take more registers)
+    }
+    if constexpr (H % 2) sum_vecs<KL, 1, true>(q, a, b, H - 1);
+}
+
+// Rows one after the other, each by the whole workgroup, four of them on a compute unit.  H vectors of a row, all of them inside it, stay in a
+// lane's registers from the sums to the gradient; the rest is read twice.  (What misses the second-level cache moves at one rate whether the
+// last-level cache has it or not, so that a second reading costs what the first did.  Twice the registers for half the wavefronts
+// lost as much as it saved: 4096 rows of 2 x 32000 bf16 228 -> 246 us, 2048 of 2 x 150000 598 / 591.)
+template <typename T, int KL, int H, int THREADS, int PER_SIMD>
+__global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const LossParams p) {
+    constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
+    __shared__ WideShared w;
+    if (threadIdx.x == 0) { w.p = p; w.waves = THREADS / 64; }
     Record rec = {0, 0, 0, 0};
     for (int64_t row = blockIdx.x; row < p.B; row += gridDim.x) {
-        RowOut o = {0, 0, 0, 0, 0};
+        const int tid = opaque(threadIdx.x);
         T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
         if (row_dead(p, row)) {
-            if (g) wide_zero<T>(g, 0, p.A);
-            if (threadIdx.x == 0) row_store(p, row, o);
+            if (g) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
+            if (tid == 0) row_store(p, row, {0, 0, 0, 0, 0});
             continue;
         }
         const T* z = (const T*)p.z + row * p.ldz;
@@ -388,37 +627,75 @@ __global__ __launch_bounds__(WR_THREADS) void loss_wide_kernel(const LossParams 
         const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
         const int act = p.act[row];
         const float za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
-        RowSum q = wide_join<KL>(wide_sum<T, KL>(z, zr, mask, 0, p.A), s_sum);
-        if (threadIdx.x < 64) {
-            Coef c;
-            row_finish<KL, double>(p, q, row, za, nullptr, c, o);
-            if (threadIdx.x == 0) {
-                s_coef = c;
-                row_store(p, row, o);
-                if (p.rec) rec_add(p, rec, row, o);
+        Vec<T, VEC> a[H], b[H];
+        held_load<THREADS>(a, z, tid);
+        if constexpr (KL != 0) held_load<THREADS>(b, zr, tid);
+        if (mask) held_mask<KL != 0, THREADS>(a, b, mask, opaque(tid));
+        RowSum q = row_empty();
+        held_sums<KL>(q, a, b);
+        wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), true>(q, x, y, 0); });
+        Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), row, za);
+        if (c.plain < 0) {                                          // (everybody)
+            q = row_empty();
+            wide_stream<T, KL, THREADS, 1, false>(z, zr, mask, 0, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), false>(q, x, y, 0); });
+            q = row_shuffle<KL, false>(q, 64);
+            __syncthreads();
+            c = wide_coef<KL, false>(w, q, row, za);
+        }
+        if (tid == 0) {
+            row_store(p, row, w.out);
+            if (p.rec) rec_add(p, rec, row, w.out);
+        }
+        if (g) {
+            auto grads = [&](auto mode, auto n, int first) {
+                constexpr int N = decltype(n)::value;
+                constexpr bool PLAIN = decltype(mode)::value;
+                wide_stream<T, KL, THREADS, N, PLAIN>(z, zr, mask, first, p.A, [&](auto full, const auto& x, const auto& y, int i) {
+#pragma unroll
+                    for (int u = 0; u < (int)(sizeof(x) / sizeof(x[0])); ++u)
+                        if (decltype(full)::value || i + u * THREADS * VEC < p.A)
+                            vec_grad<decltype(full)::value, KL, PLAIN>(c, act, x[u], y[u], g, i + u * THREADS * VEC, p.A);
+                });
+            };
+            if (c.zero) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
+            else if (c.plain) {
+                vec_again(a);
+                if constexpr (KL != 0) vec_again(b);
+                const int lane = opaque(tid);
+#pragma unroll
+                for (int i = 0; i < H; ++i) {
+                    vec_grad<true, KL, true>(c, act, a[i], b[i], g, (i * THREADS + lane) * VEC, p.A);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                grads(std::true_type(), std::integral_constant<int, U>(), HELD);
+            } else {
+                grads(std::false_type(), std::integral_constant<int, 1>(), 0);
             }
         }
-        __syncthreads();
-        if (g) {
-            const Coef c = s_coef;
-            if (c.zero) wide_zero<T>(g, 0, p.A);
-            else wide_grad<T, KL>(p, c, act, z, zr, mask, g, 0, p.A);
-        }
-        __syncthreads();                 // s_sum and s_coef are read
+        __syncthreads();                 // w.sum and w.coef are read
     }
     if (threadIdx.x == 0 && p.rec) p.rec[blockIdx.x] = rec;
 }
 
 // Few rows: pieces of rows to partial sums, then pieces again with the row's sums joined.
+constexpr int SP_THREADS = 512;
 template <typename T, int KL>
-__global__ __launch_bounds__(WR_THREADS) void loss_parts_kernel(const LossParams p) {
+__global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams p) {
+    constexpr int U = 2;
     __shared__ RowSum s_sum[WR_WAVES];
     const int64_t row = blockIdx.y;
     if (row_dead(p, row)) return;
     const int first = blockIdx.x * p.chunk, end = min(first + p.chunk, p.A);
     const T* z = (const T*)p.z + row * p.ldz;
     const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-    const RowSum q = wide_join<KL>(wide_sum<T, KL>(z, KL ? (const T*)p.zr + row * p.ldr : nullptr, mask, first, end), s_sum);
+    RowSum q = row_empty();
+    wide_stream<T, KL, SP_THREADS, U, false>(z, KL ? (const T*)p.zr + row * p.ldr : nullptr, mask, first, end,
+                          [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), false>(q, x, y, 0); });
+    q = row_shuffle<KL, false>(q, 64);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = q;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    q = row_shuffle<KL, false>(s_sum[threadIdx.x & (WR_WAVES - 1)], WR_WAVES);
     if (threadIdx.x != 0) return;
     // (the gradient may go where the logits are, so the next launch does not look the action's logit up)
     const int act = p.act[row];
@@ -427,44 +704,42 @@ __global__ __launch_bounds__(WR_THREADS) void loss_parts_kernel(const LossParams
     part.za = act >= first && act < end && (!mask || mask[act]) ? el_f32(z[act]) : -INFINITY;
 }
 template <typename T, int KL>
-__global__ __launch_bounds__(WR_THREADS) void loss_split_kernel(const LossParams p) {
-    __shared__ RowSum s_sum[WR_WAVES];
-    __shared__ Coef s_coef;
+__global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams p) {
+    constexpr int VEC = 16 / sizeof(T), U = 2;
+    __shared__ WideShared w;
     const int64_t row = blockIdx.y;
     const int first = blockIdx.x * p.chunk, end = min(first + p.chunk, p.A);
     T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
-    RowOut o = {0, 0, 0, 0, 0};
     const bool lead = blockIdx.x == 0 && threadIdx.x == 0;
     if (row_dead(p, row)) {
-        if (g) wide_zero<T>(g, first, end);
+        if (g) zero_row<T, VEC>(g, first, end, threadIdx.x, SP_THREADS);
         if (lead) {
-            row_store(p, row, o);
+            row_store(p, row, {0, 0, 0, 0, 0});
             if (p.rec) p.rec[row] = {0, 0, 0, 0};
         }
         return;
     }
+    if (threadIdx.x == 0) { w.p = p; w.waves = SP_THREADS / 64; }
     RowSum q = row_empty();
-    for (int i = threadIdx.x; i < p.splits; i += WR_THREADS) q = row_join<KL>(q, p.part[row * p.splits + i].r);
-    q = wide_join<KL>(row_shuffle<KL>(q, 64), s_sum);
-    const T* z = (const T*)p.z + row * p.ldz;
-    const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
+    for (int i = threadIdx.x; i < p.splits; i += SP_THREADS) q = row_join<KL, false>(q, p.part[row * p.splits + i].r);
     const int act = p.act[row];
-    if (threadIdx.x < 64) {
-        Coef c;
-        row_finish<KL, double>(p, q, row, p.part[row * p.splits + act / p.chunk].za, nullptr, c, o);
-        if (threadIdx.x == 0) s_coef = c;
-        if (lead) {
-            row_store(p, row, o);
-            Record rec = {0, 0, 0, 0};
-            rec_add(p, rec, row, o);
-            if (p.rec) p.rec[row] = rec;
-        }
+    const Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), row, p.part[row * p.splits + act / p.chunk].za);
+    if (lead) {
+        row_store(p, row, w.out);
+        Record rec = {0, 0, 0, 0};
+        rec_add(p, rec, row, w.out);
+        if (p.rec) p.rec[row] = rec;
     }
     if (!g) return;
-    __syncthreads();
-    const Coef c = s_coef;
-    if (c.zero) wide_zero<T>(g, first, end);
-    else wide_grad<T, KL>(p, c, act, z, KL ? (const T*)p.zr + row * p.ldr : nullptr, mask, g, first, end);
+    if (c.zero) zero_row<T, VEC>(g, first, end, threadIdx.x, SP_THREADS);
+    else
+        wide_stream<T, KL, SP_THREADS, U, false>((const T*)p.z + row * p.ldz, KL ? (const T*)p.zr + row * p.ldr : nullptr, p.mask ? p.mask + row * p.ldm : nullptr, first, end,
+                              [&](auto full, const auto& x, const auto& y, int i) {
+#pragma unroll
+                                  for (int u = 0; u < (int)(sizeof(x) / sizeof(x[0])); ++u)
+                                      if (decltype(full)::value || i + u * SP_THREADS * VEC < end)
+                                          vec_grad<decltype(full)::value, KL, false>(c, act, x[u], y[u], g, i + u * SP_THREADS * VEC, end);
+                              });
 }
 
 // the records of a pass, in their order
@@ -493,38 +768,62 @@ int pl_launched(const char* who) {
     return e == hipSuccess ? ACCERL_OK : pl_fail(ACCERL_EHIP, who, hipGetErrorString(e));
 }
 
-template <typename T, int KL, int E>
-void narrow_go(const LossParams& p, int G, int blocks, hipStream_t s) { loss_narrow_kernel<T, KL, E><<<dim3(blocks), dim3(NR_THREADS), 0, s>>>(p, G); }
+template <typename T, int KL, int VEC, int H>
+void rows_go(const LossParams& p, int G, int blocks, hipStream_t s) { loss_rows_kernel<T, KL, VEC, H><<<dim3(blocks), dim3(NR_THREADS), 0, s>>>(p, G); }
 
 template <typename T, int KL>
 int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(T);
     int records;
-    if (p.A <= 512) {
+    if (p.A <= 64 * VEC * 4) {
+        const int vec = p.A <= PL_SCALAR ? 1 : VEC, n = (p.A + vec - 1) / vec;     // vectors of a row
         int G = 4;
-        while (G * 8 < p.A) G *= 2;
+        while (G < 64 && G * (vec == 1 ? 8 : 4) < n) G *= 2;
         const int64_t want = (p.B + NR_THREADS / G - 1) / (NR_THREADS / G);
         records = (int)(want < PL_RECORDS ? want : PL_RECORDS);
-        const int E = (p.A + G - 1) / G;
-        if (E <= 2) narrow_go<T, KL, 2>(p, G, records, s);
-        else if (E <= 4) narrow_go<T, KL, 4>(p, G, records, s);
-        else if (E <= 6) narrow_go<T, KL, 6>(p, G, records, s);
-        else narrow_go<T, KL, 8>(p, G, records, s);
+        const int H = (n + G - 1) / G;
+        if (vec == 1) {
+            if (H <= 4) rows_go<T, KL, 1, 4>(p, G, records, s);
+            else if (H <= 6) rows_go<T, KL, 1, 6>(p, G, records, s);
+            else rows_go<T, KL, 1, 8>(p, G, records, s);
+        } else if (H <= 2) rows_go<T, KL, VEC, 2>(p, G, records, s);
+        else rows_go<T, KL, VEC, 4>(p, G, records, s);
     } else {
         // a row is split while there are fewer than 512 rows, into pieces of at least one vector a thread
-        const int64_t pieces = (p.A + VEC * WR_THREADS - 1) / (VEC * WR_THREADS);
+        const int64_t pieces = (p.A + VEC * SP_THREADS - 1) / (VEC * SP_THREADS);
         int64_t splits = p.B < 512 ? 1024 / p.B : 1;
         if (splits > pieces) splits = pieces;
-        p.chunk = (int)((pieces + splits - 1) / splits * VEC * WR_THREADS);
+        p.chunk = (int)((pieces + splits - 1) / splits * VEC * SP_THREADS);
         p.splits = (p.A + p.chunk - 1) / p.chunk;
         if (p.splits > 1) {
             records = (int)p.B;
-            loss_parts_kernel<T, KL><<<dim3(p.splits, (unsigned)p.B), dim3(WR_THREADS), 0, s>>>(p);
+            loss_parts_kernel<T, KL><<<dim3(p.splits, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
             if (int rc = pl_launched(who)) return rc;
-            loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(WR_THREADS), 0, s>>>(p);
+            loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
-            loss_wide_kernel<T, KL><<<dim3(records), dim3(WR_THREADS), 0, s>>>(p);
+            const int per = p.A / (VEC * WR_THREADS);
+            const auto go = [&](auto h, auto threads, auto simd) {
+                loss_wide_kernel<T, KL, decltype(h)::value, decltype(threads)::value, decltype(simd)::value><<<dim3(records), dim3(decltype(threads)::value), 0, s>>>(p);
+            };
+            typedef std::integral_constant<int, WR_THREADS> W1; typedef std::integral_constant<int, 2 * WR_THREADS> W2;
+            typedef std::integral_constant<int, 4> S4; typedef std::integral_constant<int, 2> S2;
+#define PL_HELD(n) std::integral_constant<int, n>()
+            if constexpr (KL == 0) {
+                if (p.g && per >= PL_LONG1) go(PL_HELD(40), W2(), S2());
+                else if (p.g && per >= 15) go(PL_HELD(15), W1(), S4());
+                else if (p.g && per >= 8) go(PL_HELD(8), W1(), S4());
+                else if (per >= 4) go(PL_HELD(4), W1(), S4());
+                else if (per >= 2) go(PL_HELD(2), W1(), S4());
+                else go(PL_HELD(1), W1(), S4());
+            } else {
+                if (p.g && per >= PL_LONG2) go(PL_HELD(20), W2(), S2());
+                else if (p.g && per >= 7) go(PL_HELD(7), W1(), S4());
+                else if (p.g && per >= 4) go(PL_HELD(4), W1(), S4());
+                else if (per >= 2) go(PL_HELD(2), W1(), S4());
+                else go(PL_HELD(1), W1(), S4());
+            }
+#undef PL_HELD
         }
     }
     if (int rc = pl_launched(who)) return rc;
