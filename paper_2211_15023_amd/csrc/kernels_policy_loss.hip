@@ -139,20 +139,34 @@ __device__ __forceinline__ float grad_at(const Coef& c, float z, float zr) {
 }
 
 struct RowOut { float loss, lp, kl, ent, clipped; };
+// a row's own numbers, asked for before its logits
+struct RowIn { int act; float w, adv, old, ref_lp; };
+__device__ __forceinline__ RowIn row_in(const LossParams& p, int64_t row) {
+    RowIn r = {p.act[row], 1.0f, 0.0f, 0.0f, 0.0f};
+    if (p.only_lp) return r;
+    if (p.w) r.w = p.w[row];
+    r.adv = p.adv[row];
+    r.old = p.old[row];
+    if (p.ref_lp) r.ref_lp = p.ref_lp[row];
+    return r;
+}
+__device__ __forceinline__ bool row_dead(const LossParams& p, const RowIn& r) { return r.act < 0 || r.act >= p.A || r.w == 0.0f; }
 // A row's sums on their way to its scalars, in R.  kl: the KL where it was worked out more exactly (see loss_rows_kernel), negative: not known.
 template <typename R> struct Sums { float m, mr; R s, u, sr, t, kl; };
 
-__device__ __forceinline__ float pl_log2(float x) { return log2f(x); }
+__device__ __forceinline__ float pl_log2(float x) { return __builtin_amdgcn_logf(x); }      // of sums from 1 up and their quotients; 0 gives -inf
 __device__ __forceinline__ double pl_log2(double x) { return log2(x); }
 __device__ __forceinline__ float pl_exp(float x) { return expf(x); }
 __device__ __forceinline__ double pl_exp(double x) { return exp(x); }
+__device__ __forceinline__ float pl_inverse(float x) { return __builtin_amdgcn_rcpf(x); }    // to one unit in the last place
+__device__ __forceinline__ double pl_inverse(double x) { return 1.0 / x; }
 
 // Scalars of a row from its sums.  R: float where a wavefront holds many rows, double where the row is long and a wavefront does it once.
 // The ratio may be replaced (`ratio`, a double) by one that was worked out more exactly.
 template <int KL, typename R>
-__device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q, bool plain, int64_t row, float za, const double* ratio, Coef& c, RowOut& o) {
+__device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q, bool plain, const RowIn& in, float za, const double* ratio, Coef& c, RowOut& o) {
     const bool empty = q.s == (R)0;
-    const R ln2 = (R)PL_LN2, l2 = pl_log2(q.s), inv = (R)1 / q.s;
+    const R ln2 = (R)PL_LN2, l2 = pl_log2(q.s), inv = pl_inverse(q.s);
     c.z = base<false>(q.m); c.r = base<false>(q.mr); c.plain = plain;
     // the power of the action, as the sum's terms have theirs
     const R ta = __is_same(R, float) ? (R)power<false>(c.z, za) : c.z.far ? ((R)za - (R)c.z.c) / ln2 : (R)za * (R)PL_LOG2E - (R)c.z.c;
@@ -162,8 +176,8 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     o.ent = empty ? 0.0f : (float)ent;
     o.loss = o.kl = o.clipped = 0.0f;
     if (p.only_lp) return;
-    const float w = p.w ? p.w[row] : 1.0f, adv = p.adv[row];
-    const R r = ratio ? (R)*ratio : lp == (R)-INFINITY ? (R)0 : pl_exp(lp - (R)p.old[row]);
+    const float w = in.w, adv = in.adv;
+    const R r = ratio ? (R)*ratio : lp == (R)-INFINITY ? (R)0 : pl_exp(lp - (R)in.old);
     const bool above = ratio ? *ratio > p.hi : r > (R)p.hi, below = ratio ? *ratio < p.lo : r < (R)p.lo;
     const bool cut = adv >= 0.0f ? above : below;
     const R pg = cut ? -(adv >= 0.0f ? (R)p.hi : (R)p.lo) * (R)adv : -r * (R)adv;
@@ -171,16 +185,17 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     const R ck = p.ck, ch = p.ch;
     if constexpr (KL == 0) {
         if (p.kind == ACCERL_KL_SAMPLED) {
-            const R d = (R)p.ref_lp[row] - lp, e = pl_exp(d);
+            const R d = (R)in.ref_lp - lp, e = pl_exp(d);
             kl = d == (R)INFINITY ? d : e - d - (R)1;
             if (ck != (R)0) at += ck * ((R)1 - e);
         }
     } else {
         const bool none = q.sr == (R)0;
+        const R inv_r = pl_inverse(q.sr);
         const bool far = c.z.far || c.r.far;                      // l - l'
-        const R dl = (far ? (R)q.m - (R)q.mr : ((R)c.z.c - (R)c.r.c) * ln2) + ln2 * pl_log2(q.s / q.sr);
+        const R dl = (far ? (R)q.m - (R)q.mr : ((R)c.z.c - (R)c.r.c) * ln2) + ln2 * pl_log2(q.s * inv_r);
         if constexpr (KL == 1) {
-            if (!none) { kl = q.t / q.sr + dl; c0 = ck; c3 = ck / q.sr; }
+            if (!none) { kl = q.t * inv_r + dl; c0 = ck; c3 = ck * inv_r; }
         } else {
             kl = none ? (R)INFINITY : q.t * inv - dl;
         }
@@ -202,18 +217,14 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     o.clipped = above || below ? 1.0f : 0.0f;
 }
 
-__device__ __forceinline__ bool row_dead(const LossParams& p, int64_t row) {
-    const int a = p.act[row];
-    return a < 0 || a >= p.A || (!p.only_lp && p.w && p.w[row] == 0.0f);
-}
 __device__ __forceinline__ void row_store(const LossParams& p, int64_t row, const RowOut& o) {
     if (p.loss) p.loss[row] = o.loss;
     if (p.lp) p.lp[row] = o.lp;
     if (p.kl) p.kl[row] = o.kl;
     if (p.ent) p.ent[row] = o.ent;
 }
-__device__ __forceinline__ void rec_add(const LossParams& p, Record& r, int64_t row, const RowOut& o) {
-    const double w = p.w ? p.w[row] : 1.0;
+__device__ __forceinline__ void rec_add(Record& r, float weight, const RowOut& o) {
+    const double w = weight;
     r.loss += w * o.loss; r.kl += w * o.kl; r.ent += w * o.ent; r.clipped += w * o.clipped;
 }
 
@@ -325,6 +336,23 @@ __device__ __forceinline__ void zero_row(T* g, int first, int end, int lane, int
     for (int i = first + lane * VEC; i < end; i += lanes * VEC) vec_store<false>(g, i, end, v);
 }
 
+// log2 of a quotient, off by a unit in the last place of a 32-bit logarithm: of a quotient near 1 that is far below 32 bits' step at 1
+__device__ __forceinline__ double log2_close(double x) {
+    const float y = (float)x;
+    return (double)__builtin_amdgcn_logf(y) + (x - y) / y * 1.44269504088896340736;
+}
+// The ratio in 64 bits, from memory, by the lanes of a row.  A function that is called: it is hardly ever, and its registers would be every
+// row's.
+template <typename T>
+__device__ __attribute__((noinline)) double exact_ratio(const T* z, const uint8_t* mask, int A, int j, int G, int step, float m, float za, float old) {
+    double s = 0.0;
+    for (int i = j * step; i < A; i += G * step)
+        for (int e = i; e < min(i + step, A); ++e)
+            if (!mask || mask[e]) s += exp((double)el_f32(z[e]) - (double)m);
+    for (int k = G >> 1; k > 0; k >>= 1) s += __shfl_xor(s, k);
+    return exp((double)za - (double)m - log(s) - (double)old);
+}
+
 // ---------------------------------------------------------------- rows that lanes of one wavefront hold
 // G lanes hold a row, lane j its vectors j, j + G, ..  (H of them at most).  A wavefront does 64 / G rows at a time.
 constexpr int NR_THREADS = 256;
@@ -334,11 +362,15 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
     const int tid = threadIdx.x;
     const int rows = NR_THREADS / G;
     Record rec = {0, 0, 0, 0};
-    for (int64_t row = (int64_t)blockIdx.x * rows + tid / G; row < p.B; row += (int64_t)gridDim.x * rows) {
+    int64_t row = (int64_t)blockIdx.x * rows + tid / G;
+    RowIn next = row_in(p, row < p.B ? row : p.B - 1);
+    for (const int64_t stride = (int64_t)gridDim.x * rows; row < p.B; row += stride) {
         const int j = opaque(tid & (G - 1));
+        const RowIn in = next;
+        if (row + stride < p.B) next = row_in(p, row + stride);
         RowOut o = {0, 0, 0, 0, 0};
         T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
-        if (row_dead(p, row)) {
+        if (row_dead(p, in)) {
             if (g) zero_row<T, VEC>(g, 0, p.A, j, G);
             if (j == 0) row_store(p, row, o);
             continue;
@@ -346,7 +378,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         const T* z = (const T*)p.z + row * p.ldz;
         const T* zr = KL ? (const T*)p.zr + row * p.ldr : nullptr;
         const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-        const int act = p.act[row];
+        const int act = in.act;
         const float za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
         Vec<T, VEC> a[H], b[H];
         RowSum q;
@@ -383,7 +415,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
                 for (int k = G >> 1; k > 0; k >>= 1) { ds += __shfl_xor(ds, k); dsr += __shfl_xor(dsr, k); dt += __shfl_xor(dt, k); q.u += __shfl_xor(q.u, k); }
                 q.s = (float)ds; q.sr = (float)dsr; q.t = (float)dt;
                 const double apart = c.far || cr.far ? ((double)q.m - q.mr) / PL_LN2 : (double)c.c - cr.c;
-                better_kl = (float)(KL == 1 ? dt / dsr + PL_LN2 * (apart + log2(ds / dsr)) : dt / ds - PL_LN2 * (apart + log2(ds / dsr)));
+                better_kl = (float)(KL == 1 ? dt / dsr + PL_LN2 * (apart + log2_close(ds / dsr)) : dt / ds - PL_LN2 * (apart + log2_close(ds / dsr)));
                 better_kl = fmaxf(better_kl, 0.0f);
             } else {
                 for (int k = G >> 1; k > 0; k >>= 1) {
@@ -395,7 +427,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
             if constexpr (KL != 0 && VEC == 1) {
                 // With D_j the difference of logits less its mean under p' (forward) or p, KL = log E[exp(-D)] exactly, that is
                 // log1p(E[exp(-D) - 1 + D]): a sum of small terms that are none of them negative.
-                const float inv = 1.0f / (KL == 1 ? q.sr : q.s), mean = q.t * inv;
+                const float inv = pl_inverse(KL == 1 ? q.sr : q.s), mean = q.t * inv;
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < H; ++i) {
@@ -407,7 +439,8 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
                     sum = fmaf(w, w > 0.0f ? f : 0.0f, sum);
                 }
                 for (int k = G >> 1; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-                better_kl = log1pf(sum * inv);
+                const float v = sum * inv, y = 1.0f + v;         // log(1 + v) = v log(y) / (y - 1), y as rounded
+                better_kl = y == 1.0f ? v : (float)PL_LN2 * __builtin_amdgcn_logf(y) * v * __builtin_amdgcn_rcpf(y - 1.0f);
             }
         };
         sums(std::true_type());
@@ -419,21 +452,14 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         if (!p.only_lp && q.s > 0.0f) {
             // Next to a clipping border the side decides over the whole gradient: there the sum is taken again in 64 bits.  (All lanes of
             // a row branch alike; the 32-bit ratio is off by a few parts in 2^24.)
-            const float r = expf((za - q.m) - logf(q.s) - p.old[row]);
+            const float r = expf((za - q.m) - logf(q.s) - in.old);
             if (fabsf(r - (float)p.hi) < 4e-6f * r || fabsf(r - (float)p.lo) < 4e-6f * r) {
-                double s = 0.0;
-#pragma unroll 1
-                for (int i = j * VEC; i < p.A; i += G * VEC)
-#pragma unroll 1
-                    for (int e = i; e < min(i + VEC, p.A); ++e)
-                        if (!mask || mask[e]) s += exp((double)el_f32(z[e]) - (double)q.m);
-                for (int k = G >> 1; k > 0; k >>= 1) s += __shfl_xor(s, k);
-                ratio = exp((double)za - (double)q.m - log(s) - (double)p.old[row]);
+                ratio = exact_ratio<T>(z, mask, p.A, j, G, VEC, q.m, za, in.old);
                 better = &ratio;
             }
         }
         const Sums<float> joined = {q.m, q.mr, q.s, q.u, q.sr, q.t, better_kl};
-        row_finish<KL, float>(p, joined, plain, row, za, better, c, o);
+        row_finish<KL, float>(p, joined, plain, in, za, better, c, o);
         if (g) {
             if (c.zero) zero_row<T, VEC>(g, 0, p.A, j, G);
             else {
@@ -452,7 +478,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         }
         if (j == 0) {
             row_store(p, row, o);
-            if (p.rec) rec_add(p, rec, row, o);
+            if (p.rec) rec_add(rec, in.w, o);
         }
     }
     if (!p.rec) return;
@@ -540,7 +566,7 @@ struct WideShared {
     int waves;
 };
 template <int KL>
-__device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain, int64_t row, float za) {
+__device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain, RowIn in, float za) {
     Sums<double> r = {-FLT_MAX, -FLT_MAX, 0.0, 0.0, 0.0, 0.0, -1.0};
     for (int k = 0; k < w->waves; ++k) { r.m = fmaxf(r.m, w->sum[k].m); r.mr = fmaxf(r.mr, w->sum[k].mr); }
     for (int k = 0; k < w->waves; ++k) {
@@ -554,16 +580,16 @@ __device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain,
     }
     Coef c;
     RowOut o;
-    row_finish<KL, double>(w->p, r, plain, row, za, nullptr, c, o);
+    row_finish<KL, double>(w->p, r, plain, in, za, nullptr, c, o);
     if (plain && !row_held<KL>(r)) c.plain = -1;                  // to be done again
     if (threadIdx.x == 0) { w->coef = c; w->out = o; }
 }
 // The row's coefficients, to everybody, and its outputs, to thread 0 (`w.out`).
 template <int KL, bool PLAIN>
-__device__ __forceinline__ Coef wide_coef(WideShared& w, const RowSum& q, int64_t row, float za) {
+__device__ __forceinline__ Coef wide_coef(WideShared& w, const RowSum& q, const RowIn& in, float za) {
     if ((threadIdx.x & 63) == 0) w.sum[threadIdx.x >> 6] = q;
     __syncthreads();
-    if (threadIdx.x < 64) wide_finish<KL>(&w, PLAIN, row, za);
+    if (threadIdx.x < 64) wide_finish<KL>(&w, PLAIN, in, za);
     __syncthreads();
     return w.coef;
 }
@@ -617,7 +643,8 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
     for (int64_t row = blockIdx.x; row < p.B; row += gridDim.x) {
         const int tid = opaque(threadIdx.x);
         T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
-        if (row_dead(p, row)) {
+        const RowIn in = row_in(p, row);
+        if (row_dead(p, in)) {
             if (g) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
             if (tid == 0) row_store(p, row, {0, 0, 0, 0, 0});
             continue;
@@ -625,7 +652,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         const T* z = (const T*)p.z + row * p.ldz;
         const T* zr = KL ? (const T*)p.zr + row * p.ldr : nullptr;
         const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-        const int act = p.act[row];
+        const int act = in.act;
         const float za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
         Vec<T, VEC> a[H], b[H];
         held_load<THREADS>(a, z, tid);
@@ -634,17 +661,17 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         RowSum q = row_empty();
         held_sums<KL>(q, a, b);
         wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), true>(q, x, y, 0); });
-        Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), row, za);
+        Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), in, za);
         if (c.plain < 0) {                                          // (everybody)
             q = row_empty();
             wide_stream<T, KL, THREADS, 1, false>(z, zr, mask, 0, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), false>(q, x, y, 0); });
             q = row_shuffle<KL, false>(q, 64);
             __syncthreads();
-            c = wide_coef<KL, false>(w, q, row, za);
+            c = wide_coef<KL, false>(w, q, in, za);
         }
         if (tid == 0) {
             row_store(p, row, w.out);
-            if (p.rec) rec_add(p, rec, row, w.out);
+            if (p.rec) rec_add(rec, in.w, w.out);
         }
         if (g) {
             auto grads = [&](auto mode, auto n, int first) {
@@ -684,7 +711,8 @@ __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams
     constexpr int U = 2;
     __shared__ RowSum s_sum[WR_WAVES];
     const int64_t row = blockIdx.y;
-    if (row_dead(p, row)) return;
+    const RowIn in = row_in(p, row);
+    if (row_dead(p, in)) return;
     const int first = blockIdx.x * p.chunk, end = min(first + p.chunk, p.A);
     const T* z = (const T*)p.z + row * p.ldz;
     const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
@@ -698,7 +726,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams
     q = row_shuffle<KL, false>(s_sum[threadIdx.x & (WR_WAVES - 1)], WR_WAVES);
     if (threadIdx.x != 0) return;
     // (the gradient may go where the logits are, so the next launch does not look the action's logit up)
-    const int act = p.act[row];
+    const int act = in.act;
     Part& part = p.part[row * p.splits + blockIdx.x];
     part.r = q;
     part.za = act >= first && act < end && (!mask || mask[act]) ? el_f32(z[act]) : -INFINITY;
@@ -711,7 +739,8 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     const int first = blockIdx.x * p.chunk, end = min(first + p.chunk, p.A);
     T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
     const bool lead = blockIdx.x == 0 && threadIdx.x == 0;
-    if (row_dead(p, row)) {
+    const RowIn in = row_in(p, row);
+    if (row_dead(p, in)) {
         if (g) zero_row<T, VEC>(g, first, end, threadIdx.x, SP_THREADS);
         if (lead) {
             row_store(p, row, {0, 0, 0, 0, 0});
@@ -722,12 +751,12 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     if (threadIdx.x == 0) { w.p = p; w.waves = SP_THREADS / 64; }
     RowSum q = row_empty();
     for (int i = threadIdx.x; i < p.splits; i += SP_THREADS) q = row_join<KL, false>(q, p.part[row * p.splits + i].r);
-    const int act = p.act[row];
-    const Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), row, p.part[row * p.splits + act / p.chunk].za);
+    const int act = in.act;
+    const Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), in, p.part[row * p.splits + act / p.chunk].za);
     if (lead) {
         row_store(p, row, w.out);
         Record rec = {0, 0, 0, 0};
-        rec_add(p, rec, row, w.out);
+        rec_add(rec, in.w, w.out);
         if (p.rec) p.rec[row] = rec;
     }
     if (!g) return;
