@@ -50,6 +50,7 @@ def load_library():
         return _lib
     import torch as _torch  # brings in the HIP runtime the library links against
     torch = _torch
+    _CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
     if not os.path.exists(_SO):
         raise ImportError(f"{_SO} is missing: {_BUILD}; there is no CPU fallback")
     lib = C.CDLL(_SO)
@@ -223,7 +224,8 @@ def accerl_policy_destroy(handle):
 # Marshalling is most of what a small call costs the host (32 states of the 64-unit MLP, time between calls: 5.8 us through ctypes from
 # the code below, 3.6 through accerl_args; the kernel takes 2.5).  A policy's forwards, V-trace and the KL indicators go through
 # accerl_args and come here where it returns None, because an argument is not a plain tensor: an error to raise, a subclass of torch.Tensor,
-# a stream object.  The mixture and the distillation loss always come here.
+# a stream object.  The mixture and the distillation loss always come here.  DenseInt8 and PolicyLoss go through accerl_args, which makes their
+# outputs too, on the current stream.
 def _ptr(t, dtype=None):
     if t is None:
         return None
@@ -532,6 +534,9 @@ def accerl_policy_loss(logits, actions, old_logp, advantages, workspace, mask=No
     _check(lib.accerl_policy_loss(C.byref(a), _stream(stream)))
 
 
+_CODES = {None: -1}         # output types of accerl_args, filled by load_library
+
+
 def _logits(t):
     if not t.is_cuda or t.dim() != 2:
         raise ValueError("logits must be a CUDA/HIP matrix")
@@ -583,6 +588,7 @@ class DenseInt8:
         load_library()
         self.N, self.K = w.shape
         self.relu = bool(relu)
+        self._relu = int(self.relu)
         self.w = torch.empty(packed_rows_bytes(self.N, self.K), dtype=torch.int8, device=w.device)
         if w.dtype == torch.int8:
             if w_scale is None:
@@ -597,6 +603,15 @@ class DenseInt8:
 
     def forward(self, x, dtype=None, out=None, stream=None):
         """x [M, K] -> [M, N] in `dtype` (x's own if None)."""
+        if stream is None and out is None and x.is_cuda:
+            raw = torch._C._cuda_getCurrentRawStream(x.device.index)
+            ws = self._work.of.get((x.device, raw))
+            r = None if ws is None else (_args or _loaded()).dense_dynamic(x, self.w, self.w_scale, self.bias, self.N, self.K, self._relu, _CODES.get(dtype, 3),
+                                                                           ws, raw)
+            if r is not None:
+                if r[0]:
+                    _check(r[0])
+                return r[1]
         if not x.is_cuda or x.dim() != 2 or x.shape[1] != self.K:
             raise ValueError(f"x must be a CUDA/HIP matrix of {self.K} columns")
         if out is not None and tuple(out.shape) != (x.shape[0], self.N):
@@ -623,6 +638,7 @@ class PolicyLoss:
     def __init__(self, clip_low=0.2, clip_high=0.2, kl="none", kl_coef=0.0, entropy_coef=0.0):
         load_library()
         self.how = dict(clip_low=clip_low, clip_high=clip_high, kl=kl, kl_coef=kl_coef, entropy_coef=entropy_coef)
+        self._how = (KL_KINDS[kl], float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef))
         self._bytes = accerl_policy_loss_workspace()
         self._work = _Workspaces()
 
@@ -630,6 +646,17 @@ class PolicyLoss:
                 grad=True, stream=None):
         """scale: None for the mean over all rows; grad: a table to write the gradient to (the logits themselves too), True for a new one,
         False for the value only."""
+        if stream is None and (grad is True or grad is False) and logits.is_cuda:
+            raw = torch._C._cuda_getCurrentRawStream(logits.device.index)
+            t = (_args or _loaded()).policy_loss(logits, actions, old_logp, advantages, mask, weights, ref_logits, ref_logp, int(grad), *self._how,
+                                                 1.0 / max(1, logits.shape[0]) if scale is None else float(scale), self._work.get(self._bytes, raw, logits.device), raw)
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                r = self.Result()
+                _, r.loss, r.logp, r.kl, r.entropy, r.stats, *g = t
+                r.grad = g[0] if grad else None
+                return r
         logits = _logits(logits)
         B = logits.shape[0]
         r = self.Result()
@@ -645,6 +672,13 @@ class PolicyLoss:
 
     def logprob(self, logits, actions, mask=None, stream=None):
         """log pi(a) and entropy, each [B]."""
+        if stream is None and logits.is_cuda:
+            raw = torch._C._cuda_getCurrentRawStream(logits.device.index)
+            t = (_args or _loaded()).action_logprob(logits, actions, mask, self._work.get(self._bytes, raw, logits.device), raw)
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                return t[1], t[2]
         logits = _logits(logits)
         with _On(stream, logits.device) as raw:
             logp, ent = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)

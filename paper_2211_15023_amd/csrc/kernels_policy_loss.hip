@@ -20,7 +20,7 @@ constexpr int64_t PL_MAX_A = 1 << 20;
 constexpr int PL_RECORDS = 2048;          // workgroups of a row pass, each leaves one record of sums
 constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is split
 constexpr int PL_LONG1 = 80, PL_LONG2 = 40;
-constexpr int PL_SCALAR = 64;             // up to this many actions lanes take single elements
+constexpr int PL_SCALAR = 32;             // up to this many actions lanes take single elements
 constexpr float PL_LOG2E = 1.44269504088896340736f;
 constexpr double PL_LN2 = 0.693147180559945309417;
 
@@ -806,15 +806,16 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     int records;
     if (p.A <= 64 * VEC * 4) {
         const int vec = p.A <= PL_SCALAR ? 1 : VEC, n = (p.A + vec - 1) / vec;     // vectors of a row
-        int G = 4;
-        while (G < 64 && G * (vec == 1 ? 8 : 4) < n) G *= 2;
+        int G = 1;
+        while (G < 64 && G * (vec == 1 ? 10 : 4) < n) G *= 2;
         const int64_t want = (p.B + NR_THREADS / G - 1) / (NR_THREADS / G);
         records = (int)(want < PL_RECORDS ? want : PL_RECORDS);
         const int H = (n + G - 1) / G;
         if (vec == 1) {
             if (H <= 4) rows_go<T, KL, 1, 4>(p, G, records, s);
             else if (H <= 6) rows_go<T, KL, 1, 6>(p, G, records, s);
-            else rows_go<T, KL, 1, 8>(p, G, records, s);
+            else if (H <= 8) rows_go<T, KL, 1, 8>(p, G, records, s);
+            else rows_go<T, KL, 1, 10>(p, G, records, s);
         } else if (H <= 2) rows_go<T, KL, VEC, 2>(p, G, records, s);
         else rows_go<T, KL, VEC, 4>(p, G, records, s);
     } else {

@@ -313,7 +313,7 @@ def test_loss_refuses_tensors(A):
         with pytest.raises((ValueError, A.AccerlError)):
             how.forward(z, a, o, v, ref_logits=z)
     with pytest.raises(KeyError):
-        A.PolicyLoss(kl="other").forward(x.z, act, v, v)
+        A.PolicyLoss(kl="other")
 
 
 def test_loss_empty_batch(A):
