@@ -275,9 +275,8 @@ __device__ __forceinline__ void vec_drop(Vec<T, VEC>& v, int e) {
 // FULL: the vector ends before the end.
 template <bool FULL, bool PLAIN, typename T, int VEC>
 __device__ __forceinline__ void vec_load(Vec<T, VEC>& v, const T* row, const uint8_t* mask, int i, int end) {
-    if constexpr (VEC == 1) {
-        v.w = i < end && (!mask || mask[i]) ? el_f32(row[i]) : nothing_f<PLAIN>();
-    } else {
+    static_assert(VEC > 1, "whole vectors");
+    {
         const int at = FULL ? i : vec_at<VEC>(i, end);
         if constexpr (sizeof(T) == 4) v.w = *(const u32x4_at4*)(row + at);
         else v.w = *(const u32x4_at2*)(row + at);
@@ -315,6 +314,21 @@ __device__ __forceinline__ void vec_store(T* row, int i, int end, const float (&
         for (int e = 0; e < VEC; ++e) if (at + e >= i) row[at + e] = f32_el<T>(v[e]);
     }
 }
+// Elements j, j + G, .. of a narrow row; bit i of `allowed`: the i-th is part of the row.
+template <bool PLAIN, typename T, int H>
+__device__ __forceinline__ void single_load(Vec<T, 1> (&v)[H], const T* row, uint32_t allowed, int j, int G) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) v[i].w = (allowed >> i) & 1 ? el_f32(row[j + i * G]) : nothing_f<PLAIN>();
+}
+template <int H>
+__device__ __forceinline__ uint32_t single_allowed(const uint8_t* mask, int j, int G, int end) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+        if (j + i * G < end && (!mask || mask[j + i * G])) bits |= 1u << i;
+    return bits;
+}
+
 // the gradient of a vector's elements, to memory
 template <bool FULL, int KL, bool PLAIN, typename T, int VEC>
 __device__ __forceinline__ void vec_grad(const Coef& c, int act, const Vec<T, VEC>& z, const Vec<T, VEC>& zr, T* g, int i, int end) {
@@ -360,7 +374,7 @@ template <typename T, int KL, int VEC, int H>
 __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams p, int G) {
     __shared__ Record s_rec[NR_THREADS / 64];
     const int tid = threadIdx.x;
-    const int rows = NR_THREADS / G;
+    const int rows = NR_THREADS / G, shift = __builtin_ctz(G);
     Record rec = {0, 0, 0, 0};
     int64_t row = (int64_t)blockIdx.x * rows + tid / G;
     RowIn next = row_in(p, row < p.B ? row : p.B - 1);
@@ -379,16 +393,23 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         const T* zr = KL ? (const T*)p.zr + row * p.ldr : nullptr;
         const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
         const int act = in.act;
-        const float za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
         Vec<T, VEC> a[H], b[H];
         RowSum q;
-        float better_kl = -1.0f;
+        float better_kl = -1.0f, za;
+        uint32_t allowed = 0;                            // VEC == 1: this lane's elements; else whether the row has any, as far as the lane sees
+        if constexpr (VEC == 1) allowed = single_allowed<H>(mask, j, G, p.A);
+        else za = mask && !mask[act] ? -INFINITY : el_f32(z[act]);
         auto sums = [&](auto mode) {
             constexpr bool PLAIN = decltype(mode)::value;
+            if constexpr (VEC == 1) {
+                single_load<PLAIN>(a, z, allowed, j, G);
+                if constexpr (KL != 0) single_load<PLAIN>(b, zr, allowed, j, G);
+            } else {
 #pragma unroll
-            for (int i = 0; i < H; ++i) {
-                vec_load<false, PLAIN>(a[i], z, mask, (j + i * G) * VEC, p.A);
-                if constexpr (KL != 0) vec_load<false, PLAIN>(b[i], zr, mask, (j + i * G) * VEC, p.A);
+                for (int i = 0; i < H; ++i) {
+                    vec_load<false, PLAIN>(a[i], z, mask, (j + i * G) * VEC, p.A);
+                    if constexpr (KL != 0) vec_load<false, PLAIN>(b[i], zr, mask, (j + i * G) * VEC, p.A);
+                }
             }
             q = row_empty();
 #pragma unroll
@@ -444,8 +465,25 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
             }
         };
         sums(std::true_type());
-        const bool plain = row_held<KL>(q);
+        bool plain = row_held<KL>(q);
+        if (!plain && mask && q.m == nothing_f<true>()) {
+            // a row that the mask leaves empty, most likely: not to be done again
+            uint32_t any = allowed;
+            if constexpr (VEC > 1)
+                for (int i = j; i < p.A; i += G) any |= mask[i];
+            for (int k = G >> 1; k > 0; k >>= 1) any |= (uint32_t)__shfl_xor((int)any, k);
+            if (!any) { q = row_empty(); plain = true; }
+        }
         if (!plain) sums(std::false_type());             // (all lanes of a row alike)
+        if constexpr (VEC == 1) {
+            // the action's logit from the lane that holds it
+            const int held = act >> shift;
+            float v = a[0].w;
+#pragma unroll
+            for (int i = 1; i < H; ++i) v = held == i ? a[i].w : v;
+            v = (allowed >> held) & 1 ? v : -INFINITY;
+            za = __shfl(v, (tid & 63 & ~(G - 1)) | (act & (G - 1)));
+        }
         Coef c;
         double ratio;
         const double* better = nullptr;
