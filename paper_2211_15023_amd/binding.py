@@ -590,16 +590,24 @@ class DenseInt8:
         self.relu = bool(relu)
         self._relu = int(self.relu)
         self.w = torch.empty(packed_rows_bytes(self.N, self.K), dtype=torch.int8, device=w.device)
+        self.w_scale = torch.empty(self.N, dtype=torch.float32, device=w.device)
+        self.bias = None if bias is None else bias.detach().to(torch.float32).contiguous().clone()
+        self._work = _Workspaces()
+        self.update(w, w_scale)
+
+    def update(self, w, w_scale=None, bias=None):
+        """New weights of the same shape (a learner's, after its step), and bias if given, on the current stream."""
+        if tuple(w.shape) != (self.N, self.K) or (bias is not None and (self.bias is None or bias.shape != self.bias.shape)):
+            raise ValueError("the weights or the bias differ in shape from the layer's")
         if w.dtype == torch.int8:
             if w_scale is None:
                 raise ValueError("int8 weights need their scales")
-            self.w_scale = w_scale.detach().to(torch.float32).contiguous().clone()
+            self.w_scale.copy_(w_scale.detach())
             accerl_pack_rows_i8(w, self.w)
         else:
-            self.w_scale = torch.empty(self.N, dtype=torch.float32, device=w.device)
             accerl_quantize_rows(w.detach(), self.w, self.w_scale)
-        self.bias = None if bias is None else bias.detach().to(torch.float32).contiguous().clone()
-        self._work = _Workspaces()
+        if bias is not None:
+            self.bias.copy_(bias.detach())
 
     def forward(self, x, dtype=None, out=None, stream=None):
         """x [M, K] -> [M, N] in `dtype` (x's own if None)."""

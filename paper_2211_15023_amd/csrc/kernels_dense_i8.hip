@@ -85,6 +85,8 @@ __device__ __forceinline__ int di_quant(float x, float inv, float top) {
     }
     return (int)q;
 }
+// the power of two by which a row is scaled where 127 / max or 127 * x would leave the range
+__device__ __forceinline__ float di_by(float top) { return top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-20f : 1.0f; }
 // Sixteen of them.  x * inv + 1.5 * 2^23 has the rounded quotient in its low byte; only where one of the sixteen lies within 2^-15 of the
 // middle of two steps (inv's error moves a quotient by less than 2^-16), or the row's magnitude needs scaling, are they looked at one by
 // one.  That is 5 operations an element in place of 15: 8192 rows of 4096 bf16 were bound by them (31 us).
@@ -148,8 +150,7 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const T* x, i
     if constexpr (sizeof(T) == 4) top = __uint_as_float(m);
     else { T t; t.u = (uint16_t)m; top = el_f32(t); }
     if (real && piece == 0) scale[row] = top / 127.0f;
-    // scaled by a power of two where 127 / max or 127 * x would leave the range
-    const float by = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-20f : 1.0f;
+    const float by = di_by(top);
     const bool zero = !real || !(top > 0.0f && __float_as_uint(top) < 0x7f800000u);
     top *= by;
     const float inv = 127.0f / top;
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void dense_i8_tile_kernel(const De
 
 // Few tokens or few tiles: the eight wavefronts of a workgroup split K, each multiplies straight from memory (a weight is read once, by
 // one wavefront), and their sums meet in LDS.
-constexpr int KS_WAVES = 8;
+constexpr int KS_WAVES = 8, KS_AHEAD = 8;     // fragments a wavefront has on their way
 template <typename T, int FT, int TT>
 __global__ __launch_bounds__(64 * KS_WAVES) void dense_i8_ksplit_kernel(const DenseParams p) {
     __shared__ v4i s_acc[KS_WAVES][FT * TT][64];
@@ -410,34 +411,38 @@ __global__ __launch_bounds__(64 * KS_WAVES) void dense_i8_ksplit_kernel(const De
     for (int i = 0; i < FT; ++i)
 #pragma unroll
         for (int j = 0; j < TT; ++j) acc[i][j] = (v4i){0, 0, 0, 0};
-    constexpr int U = 4;
-    int s = first;
-    for (; s + U <= last; s += U) {
-        v4i w[U][FT], x[U][TT];
+    // U steps are on their way while the U before them are multiplied; steps past the last one load the operands' last step
+    constexpr int U = KS_AHEAD / (FT + TT);
+    v4i w[U][FT], x[U][TT];
+    auto load = [&](int s) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = (int64_t)min(s + u, p.steps - 1) * 1024;
+#pragma unroll
+            for (int i = 0; i < FT; ++i) w[u][i] = *(const v4i*)(pw[i] + at);
+#pragma unroll
+            for (int j = 0; j < TT; ++j) x[u][j] = *(const v4i*)(px[j] + at);
+        }
+    };
+    load(first);
+    for (int s = first; s < last; s += U) {
+        v4i cw[U][FT], cx[U][TT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int i = 0; i < FT; ++i) w[u][i] = *(const v4i*)(pw[i] + (int64_t)(s + u) * 1024);
+            for (int i = 0; i < FT; ++i) cw[u][i] = w[u][i];
 #pragma unroll
-            for (int j = 0; j < TT; ++j) x[u][j] = *(const v4i*)(px[j] + (int64_t)(s + u) * 1024);
+            for (int j = 0; j < TT; ++j) cx[u][j] = x[u][j];
         }
+        if (s + U < last) load(s + U);
 #pragma unroll
         for (int u = 0; u < U; ++u)
+            if (s + u < last) {
 #pragma unroll
-            for (int i = 0; i < FT; ++i)
+                for (int i = 0; i < FT; ++i)
 #pragma unroll
-                for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][i], x[u][j], acc[i][j], 0, 0, 0);
-    }
-    for (; s < last; ++s) {
-        v4i w[FT], x[TT];
-#pragma unroll
-        for (int i = 0; i < FT; ++i) w[i] = *(const v4i*)(pw[i] + (int64_t)s * 1024);
-#pragma unroll
-        for (int j = 0; j < TT; ++j) x[j] = *(const v4i*)(px[j] + (int64_t)s * 1024);
-#pragma unroll
-        for (int i = 0; i < FT; ++i)
-#pragma unroll
-            for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw[u][i], cx[u][j], acc[i][j], 0, 0, 0);
+            }
     }
 #pragma unroll
     for (int i = 0; i < FT; ++i)
@@ -453,6 +458,106 @@ __global__ __launch_bounds__(64 * KS_WAVES) void dense_i8_ksplit_kernel(const De
             float sw[4], b[4];
             di_channels(p, f, sw, b);
             di_store<T>(p, sum, m, f, p.sx[m], sw, b);
+        }
+    }
+}
+
+// One or two floating-point tokens in one launch: every workgroup quantises them for itself (32 elements a thread at most), into LDS, while
+// its first weights are on their way, and goes on as the kernel above.
+constexpr int TK_ELEMENTS = 16384;          // tokens x padded K
+constexpr int TK_TOKENS = 2;
+template <typename X, typename T, int FT>
+__global__ __launch_bounds__(64 * KS_WAVES) void dense_i8_tokens_kernel(const DenseParams p, const X* x, int64_t ldx, int K) {
+    constexpr int THREADS = 64 * KS_WAVES, U = 4;
+    __shared__ __attribute__((aligned(16))) char s_x[TK_ELEMENTS];         // [token][16-byte piece]
+    __shared__ v4i s_acc[KS_WAVES][FT][64];
+    __shared__ uint32_t s_top[TK_TOKENS];
+    const int tid = threadIdx.x, lane = tid & 63, M = (int)p.M;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tf = blockIdx.x * FT, pieces = p.steps * 4;                  // of a token
+    const int first = (int)((int64_t)wave * p.steps / KS_WAVES), last = (int)((int64_t)(wave + 1) * p.steps / KS_WAVES);
+    const char* pw[FT];
+#pragma unroll
+    for (int i = 0; i < FT; ++i) pw[i] = p.w + (int64_t)min(tf + i, p.wt - 1) * p.steps * 1024 + lane * 16;
+    v4i w[U][FT];
+    auto load = [&](int s) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < FT; ++i) w[u][i] = *(const v4i*)(pw[i] + (int64_t)min(s + u, p.steps - 1) * 1024);
+    };
+    // the tokens' pieces, two a thread at most, their tokens' largest magnitudes in LDS
+    Piece<X> v[2];
+    int row[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = tid + h * THREADS;
+        row[h] = i < M * pieces ? i / pieces : -1;
+        if (row[h] >= 0) piece_load(v[h], x + row[h] * ldx, (int64_t)(i - row[h] * pieces) * 16, (int64_t)K);
+    }
+    load(first);
+    if (tid < TK_TOKENS) s_top[tid] = 0;
+    __syncthreads();
+    uint32_t m[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (row[h] >= 0) {
+            piece_max(v[h], m[h]);
+            if constexpr (sizeof(X) == 2) m[h] = max(m[h] & 0xffffu, m[h] >> 16);
+        }
+    for (int r = 0; r < M; ++r) {
+        uint32_t t = max(row[0] == r ? m[0] : 0u, row[1] == r ? m[1] : 0u);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
+        if (lane == 0 && t) atomicMax(&s_top[r], t);                       // (the largest, whatever the order)
+    }
+    __syncthreads();
+    auto top_of = [&](int r) {
+        if constexpr (sizeof(X) == 4) return __uint_as_float(s_top[r]);
+        else { X t; t.u = (uint16_t)s_top[r]; return el_f32(t); }
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (row[h] >= 0) {
+            float top = top_of(row[h]);
+            const bool zero = !(top > 0.0f && __float_as_uint(top) < 0x7f800000u);
+            const float by = di_by(top);
+            top *= by;
+            *(v4i*)(s_x + (tid + h * THREADS) * 16) = zero ? (v4i){0, 0, 0, 0} : di_quant16<X>(v[h], 127.0f / top, top, by);
+        }
+    __syncthreads();
+
+    v4i acc[FT];
+#pragma unroll
+    for (int i = 0; i < FT; ++i) acc[i] = (v4i){0, 0, 0, 0};
+    const char* px = s_x + (min(lane & 15, M - 1) * pieces + (lane >> 4)) * 16;      // columns behind the last token repeat it
+    for (int s = first; s < last; s += U) {
+        v4i c[U][FT];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < FT; ++i) c[u][i] = w[u][i];
+        if (s + U < last) load(s + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (s + u < last) {
+                const v4i b = *(const v4i*)(px + (s + u) * 64);
+#pragma unroll
+                for (int i = 0; i < FT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(c[u][i], b, acc[i], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < FT; ++i) s_acc[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave < FT) {
+        v4i sum = s_acc[0][wave][lane];
+#pragma unroll
+        for (int k = 1; k < KS_WAVES; ++k) sum += s_acc[k][wave][lane];
+        const int64_t r = lane & 15, f = (int64_t)(tf + wave) * 16 + (lane >> 4) * 4;
+        if (r < M && f < p.N) {
+            float sw[4], b[4];
+            di_channels(p, f, sw, b);
+            di_store<T>(p, sum, r, f, top_of((int)r) / 127.0f, sw, b);
         }
     }
 }
@@ -509,26 +614,44 @@ int product_as(const char* who, const DenseParams& p, hipStream_t s) {
     const int64_t cus = conv_num_cus();
     auto groups = [&](int bf, int bt) { return (int64_t)((p.wt + bf - 1) / bf) * ((p.xt + bt - 1) / bt); };
     // (times in us, M x K x N)
-    // 256 x 256 in one workgroup a compute unit where its rounds are nearly full, else 128 features x 256 tokens, two workgroups a compute
-    // unit, whose ends overlap the other's steps: 4096 x 4096 x 4096 55.9 / 58.2, 4096 x 16384 x 4096 199 / 217, but 6000 x 2000 x 5000
-    // 63.8 / 59.2, 8192 x 8192 x 1024 85.7 / 64.9
-    const int64_t full = groups(16, 16), rounds = (full + cus - 1) / cus;
-    if (full >= cus && 10 * full >= 9 * rounds * cus) return tile_go<T, 2, 4, 8, 4, 1>(who, p, s);
-    if (groups(8, 16) >= cus) return tile_go<T, 1, 4, 8, 4, 1>(who, p, s);
-    // 128 x 128, one workgroup a compute unit, where that is one round (64 features x 128 tokens / this: 1024 x 4096 x 4096 22.1 / 20.2,
-    // 512 x 8192 x 8192 47.0 / 40.2, 999 x 1777 x 2501 11.2 / 10.5; in a second round 1500 x 384 x 3000 7.9 / 10.9)
-    if (2 * groups(8, 8) >= cus && groups(8, 8) <= cus) return tile_go<T, 2, 4, 4, 2, 2>(who, p, s);
+    // One or two tiles of tokens stream the weights: one tile of features a workgroup brings more of them under way (24 x 2048 x 8192 5.3, two
+    // tiles 6.5; 32 x 8192 x 1024 one by one 4.9, two tiles of tokens 6.1; 8 x 4096 x 16384 in tiles 24.3).
+    if (p.xt <= 2) return p.xt == 2 && p.wt >= cus ? ksplit_go<T, 1, 2>(who, p, s) : ksplit_go<T, 1, 1>(who, p, s);
+    if (p.xt > 8) {
+        // 256 x 256 in one workgroup a compute unit where its rounds are nearly full, else 128 features x 256 tokens, two workgroups a
+        // compute unit, whose ends overlap the other's steps: 4096 x 4096 x 4096 55.9 / 58.2, 4096 x 16384 x 4096 199 / 217, but 6000 x 2000
+        // x 5000 63.8 / 59.2, 8192 x 8192 x 1024 85.7 / 64.9
+        const int64_t full = groups(16, 16), rounds = (full + cus - 1) / cus;
+        if (full >= cus && 10 * full >= 9 * rounds * cus) return tile_go<T, 2, 4, 8, 4, 1>(who, p, s);
+        if (groups(8, 16) >= cus) return tile_go<T, 1, 4, 8, 4, 1>(who, p, s);
+        // 128 x 128, one workgroup a compute unit, where that is one round (64 features x 128 tokens / this: 1024 x 4096 x 4096 22.1 / 20.2,
+        // 512 x 8192 x 8192 47.0 / 40.2, 999 x 1777 x 2501 11.2 / 10.5; in a second round 1500 x 384 x 3000 7.9 / 10.9)
+        if (2 * groups(8, 8) >= cus && groups(8, 8) <= cus) return tile_go<T, 2, 4, 4, 2, 2>(who, p, s);
+    }
     // Fewer: the wavefronts split K, with the largest of their tiles that gives every compute unit work (64 features x 128 tokens /
     // 32 x 64 split: 512 x 2048 x 2048 8.5 / 7.4, 256 x 4096 x 4096 16.9 / 11.5, but 128 x 4096 x 16384 17.9 / 27.5, 4096 x 512 x 512 5.2 / 7.4).
-    // One or two tiles of tokens stream the weights: one tile of features a workgroup brings more of them under way (24 x 2048 x
-    // 8192: 5.3, two tiles 6.5; 32 x 8192 x 1024: one by one 4.9, two tiles of tokens 6.1).
-    if (groups(2, 4) > 2 * cus && p.xt > 2) return tile_go<T, 1, 4, 4, 2, 2>(who, p, s);
-    if (p.xt <= 2) return p.xt == 2 && p.wt >= cus ? ksplit_go<T, 1, 2>(who, p, s) : ksplit_go<T, 1, 1>(who, p, s);
+    if (groups(2, 4) > 2 * cus) return tile_go<T, 1, 4, 4, 2, 2>(who, p, s);
     return groups(2, 4) >= cus ? ksplit_go<T, 2, 4>(who, p, s) : ksplit_go<T, 2, 2>(who, p, s);
 }
 int product(const char* who, const DenseParams& p, hipStream_t s) {
     if (p.dtype == ACCERL_DT_F32) return product_as<float>(who, p, s);
     return p.dtype == ACCERL_DT_BF16 ? product_as<BF16>(who, p, s) : product_as<F16>(who, p, s);
+}
+
+// One or two tokens: one launch (us, two launches / one: 1 x 4096 x 4096 9.7 / 7.1, 2 x 4096 x 4096 9.6 / 7.6, but 4 tokens 9.5 / 10.1, 8 x
+// 2048 x 2048 7.2 / 9.4); two tiles of features a workgroup from 1024 on (1 x 512 x 32000 12.8 / 10.8, 1 x 4096 x 4096 7.1 / 7.9).
+bool tokens_fit(int64_t M, int64_t K) { return M <= TK_TOKENS && M * di_steps(K) * 64 <= TK_ELEMENTS; }
+template <typename X>
+int tokens(const char* who, const X* x, int64_t ldx, int64_t K, const DenseParams& p, hipStream_t s) {
+    const auto go = [&](auto type) {
+        typedef decltype(type) T;
+        if (p.wt < 1024) dense_i8_tokens_kernel<X, T, 1><<<dim3((unsigned)p.wt), dim3(64 * KS_WAVES), 0, s>>>(p, x, ldx, (int)K);
+        else dense_i8_tokens_kernel<X, T, 2><<<dim3((unsigned)((p.wt + 1) / 2)), dim3(64 * KS_WAVES), 0, s>>>(p, x, ldx, (int)K);
+    };
+    if (p.dtype == ACCERL_DT_F32) go(0.0f);
+    else if (p.dtype == ACCERL_DT_BF16) go(BF16());
+    else go(F16());
+    return di_launched(who);
 }
 
 // what both forms of the layer check; `done` is set where nothing is to be done
@@ -641,6 +764,11 @@ int accerl_dense_i8_dynamic(const void* x, int32_t x_dtype, int64_t ld_x, const 
     if (!x || !workspace) return di_fail(ACCERL_EINVAL, who, "NULL argument (only bias may be NULL)");
     if (!di_aligned(x, dtype_bytes(x_dtype)) || !di_aligned(workspace, 16)) return di_fail(ACCERL_EINVAL, who, "misaligned argument");
     if (workspace_bytes < accerl_dense_i8_workspace(M, K)) return di_fail(ACCERL_EINVAL, who, "workspace smaller than accerl_dense_i8_workspace says");
+    if (tokens_fit(M, K)) {
+        const DenseParams p = dense_params(nullptr, nullptr, w_packed, w_scale, bias, M, N, K, relu, out, out_dtype, ld_out);
+        if (x_dtype == ACCERL_DT_F32) return tokens(who, (const float*)x, ld_x, K, p, (hipStream_t)stream);
+        return x_dtype == ACCERL_DT_BF16 ? tokens(who, (const BF16*)x, ld_x, K, p, (hipStream_t)stream) : tokens(who, (const F16*)x, ld_x, K, p, (hipStream_t)stream);
+    }
     int8_t* xq = (int8_t*)workspace;
     float* sx = (float*)((char*)workspace + scales_at(M, K));
     if (int rc = quantize(who, x, x_dtype, M, K, ld_x, xq, sx, (hipStream_t)stream)) return rc;

@@ -19,7 +19,7 @@ namespace {
 constexpr int64_t PL_MAX_A = 1 << 20;
 constexpr int PL_RECORDS = 2048;          // workgroups of a row pass, each leaves one record of sums
 constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is split
-constexpr int PL_LONG1 = 80, PL_LONG2 = 40;
+constexpr int PL_LONG1 = 80, PL_LONG2 = 56;             // times 256 vectors: what registers, and LDS with a reference, hold of a long row
 constexpr int PL_SCALAR = 32;             // up to this many actions lanes take single elements
 constexpr float PL_LOG2E = 1.44269504088896340736f;
 constexpr double PL_LN2 = 0.693147180559945309417;
@@ -43,6 +43,7 @@ struct LossParams {
     int splits, chunk;       // pieces of a row, elements of a piece
     double lo, hi;           // the clipping borders themselves
     float ck, ch, scale;
+    float* stats;            // out_stats where one workgroup does the pass (rec is then only a flag)
 };
 
 // A power is one multiply-add, t = z log2 e - c with c = m log2 e rounded once (what follows goes by that c), where the maximum lies within
@@ -115,14 +116,19 @@ __device__ __forceinline__ bool row_held(const S& a) {
     const bool z = !far_off(a.m) && fabs(a.s) < 1e30f && fabs(a.u) < 1e30f;
     return z && (KL == 0 || (!far_off(a.mr) && fabs(a.sr) < 1e30f && fabs(a.t) < 1e30f));
 }
+// the sums of neighbouring lanes joined, in all of them: under the common maxima first, so that a lane's sums are corrected once
 template <int KL, bool PLAIN>
 __device__ __forceinline__ RowSum row_shuffle(RowSum a, int lanes) {
+    float m = a.m, mr = a.mr;
     for (int o = lanes >> 1; o > 0; o >>= 1) {
-        RowSum b;
-        b.m = __shfl_xor(a.m, o); b.s = __shfl_xor(a.s, o); b.u = __shfl_xor(a.u, o);
-        b.mr = b.sr = b.t = 0.0f;
-        if constexpr (KL != 0) { b.mr = __shfl_xor(a.mr, o); b.sr = __shfl_xor(a.sr, o); b.t = __shfl_xor(a.t, o); }
-        a = row_join<KL, PLAIN>(a, b);
+        m = fmaxf(m, __shfl_xor(m, o));
+        if constexpr (KL != 0) mr = fmaxf(mr, __shfl_xor(mr, o));
+    }
+    row_raise<KL, PLAIN>(a, m, mr);
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+        a.s += __shfl_xor(a.s, o);
+        a.u += __shfl_xor(a.u, o);
+        if constexpr (KL != 0) { a.sr += __shfl_xor(a.sr, o); a.t += __shfl_xor(a.t, o); }
     }
     return a;
 }
@@ -222,6 +228,9 @@ __device__ __forceinline__ void row_store(const LossParams& p, int64_t row, cons
     if (p.lp) p.lp[row] = o.lp;
     if (p.kl) p.kl[row] = o.kl;
     if (p.ent) p.ent[row] = o.ent;
+}
+__device__ __forceinline__ void rec_stats(const Record& r, float scale, float* out) {
+    out[0] = (float)(scale * r.loss); out[1] = (float)(scale * r.kl); out[2] = (float)(scale * r.ent); out[3] = (float)(scale * r.clipped);
 }
 __device__ __forceinline__ void rec_add(Record& r, float weight, const RowOut& o) {
     const double w = weight;
@@ -530,7 +539,8 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         for (int k = 1; k < NR_THREADS / 64; ++k) {
             rec.loss += s_rec[k].loss; rec.kl += s_rec[k].kl; rec.ent += s_rec[k].ent; rec.clipped += s_rec[k].clipped;
         }
-        p.rec[blockIdx.x] = rec;
+        if (p.stats) rec_stats(rec, p.scale, p.stats);
+        else p.rec[blockIdx.x] = rec;
     }
 }
 
@@ -672,10 +682,11 @@ __device__ __forceinline__ void held_sums(RowSum& q, const Vec<T, VEC> (&a)[H], 
 // lane's registers from the sums to the gradient; the rest is read twice.  (What misses the second-level cache moves at one rate whether the
 // last-level cache has it or not, so that a second reading costs what the first did.  Twice the registers for half the wavefronts
 // lost as much as it saved: 4096 rows of 2 x 32000 bf16 228 -> 246 us, 2048 of 2 x 150000 598 / 591.)
-template <typename T, int KL, int H, int THREADS, int PER_SIMD>
+template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
 __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
     __shared__ WideShared w;
+    __shared__ u32x4 s_row[LDS > 0 ? LDS * (KL ? 2 : 1) : 1][LDS > 0 ? THREADS : 1];     // vectors behind those in registers, a lane's own
     if (threadIdx.x == 0) { w.p = p; w.waves = THREADS / 64; }
     Record rec = {0, 0, 0, 0};
     for (int64_t row = blockIdx.x; row < p.B; row += gridDim.x) {
@@ -698,7 +709,19 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         if (mask) held_mask<KL != 0, THREADS>(a, b, mask, opaque(tid));
         RowSum q = row_empty();
         held_sums<KL>(q, a, b);
-        wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), true>(q, x, y, 0); });
+        wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, [&](auto, const auto& x, const auto& y, int at) {
+            constexpr int N = sizeof(x) / sizeof(x[0]);
+            if constexpr (LDS > 0) {
+                const int slot = (at - HELD) / (THREADS * VEC);
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+                    if (slot + u < LDS) {
+                        s_row[slot + u][tid] = x[u].w;
+                        if constexpr (KL != 0) s_row[LDS + slot + u][tid] = y[u].w;
+                    }
+            }
+            sum_vecs<KL, N, true>(q, x, y, 0);
+        });
         Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), in, za);
         if (c.plain < 0) {                                          // (everybody)
             q = row_empty();
@@ -732,7 +755,17 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
                     vec_grad<true, KL, true>(c, act, a[i], b[i], g, (i * THREADS + lane) * VEC, p.A);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                grads(std::true_type(), std::integral_constant<int, U>(), HELD);
+                if constexpr (LDS > 0) {
+                    // (long rows: LDS is full)
+#pragma unroll 1
+                    for (int i = 0; i < LDS; ++i) {
+                        Vec<T, VEC> x, y;
+                        x.w = s_row[i][lane];
+                        if constexpr (KL != 0) y.w = s_row[LDS + i][lane];
+                        vec_grad<true, KL, true>(c, act, x, y, g, ((H + i) * THREADS + lane) * VEC, p.A);
+                    }
+                }
+                grads(std::true_type(), std::integral_constant<int, U>(), HELD + LDS * THREADS * VEC);
             } else {
                 grads(std::false_type(), std::integral_constant<int, 1>(), 0);
             }
@@ -813,15 +846,15 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
 __global__ __launch_bounds__(1024) void loss_stats_kernel(const Record* rec, int n, float scale, float* out) {
     __shared__ Record s_rec[16];
     Record r = {0, 0, 0, 0};
-    for (int i = threadIdx.x; i < n; i += 1024) { r.loss += rec[i].loss; r.kl += rec[i].kl; r.ent += rec[i].ent; r.clipped += rec[i].clipped; }
+    for (int i = threadIdx.x; i < n; i += (int)blockDim.x) { r.loss += rec[i].loss; r.kl += rec[i].kl; r.ent += rec[i].ent; r.clipped += rec[i].clipped; }
     for (int k = 32; k > 0; k >>= 1) {
         r.loss += __shfl_xor(r.loss, k); r.kl += __shfl_xor(r.kl, k); r.ent += __shfl_xor(r.ent, k); r.clipped += __shfl_xor(r.clipped, k);
     }
     if ((threadIdx.x & 63) == 0) s_rec[threadIdx.x >> 6] = r;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int k = 1; k < 16; ++k) { r.loss += s_rec[k].loss; r.kl += s_rec[k].kl; r.ent += s_rec[k].ent; r.clipped += s_rec[k].clipped; }
-        out[0] = (float)(scale * r.loss); out[1] = (float)(scale * r.kl); out[2] = (float)(scale * r.ent); out[3] = (float)(scale * r.clipped);
+        for (int k = 1; k < (int)blockDim.x / 64; ++k) { r.loss += s_rec[k].loss; r.kl += s_rec[k].kl; r.ent += s_rec[k].ent; r.clipped += s_rec[k].clipped; }
+        rec_stats(r, scale, out);
     }
 }
 
@@ -849,6 +882,7 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
         const int64_t want = (p.B + NR_THREADS / G - 1) / (NR_THREADS / G);
         records = (int)(want < PL_RECORDS ? want : PL_RECORDS);
         const int H = (n + G - 1) / G;
+        if (records == 1) { p.stats = out_stats; out_stats = nullptr; }
         if (vec == 1) {
             if (H <= 4) rows_go<T, KL, 1, 4>(p, G, records, s);
             else if (H <= 6) rows_go<T, KL, 1, 6>(p, G, records, s);
@@ -857,9 +891,11 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
         } else if (H <= 2) rows_go<T, KL, VEC, 2>(p, G, records, s);
         else rows_go<T, KL, VEC, 4>(p, G, records, s);
     } else {
-        // a row is split while there are fewer than 512 rows, into pieces of at least one vector a thread
+        // Few long rows are split, into pieces of at least one vector a lane; a row that one workgroup gets through in about the time of
+        // another launch is not (bf16, log-probabilities, split / not: 16 x 20000 11.5 / 7.9 us, x 100000 12.5 / 14.7, 256 x 100000 24.3 /
+        // 21.6; the loss with the forward KL: 16 x 20000 20.6 / 17.8, x 100000 24.5 / 33.9, 256 x 100000 69.9 / 45.4).
         const int64_t pieces = (p.A + VEC * SP_THREADS - 1) / (VEC * SP_THREADS);
-        int64_t splits = p.B < 512 ? 1024 / p.B : 1;
+        int64_t splits = p.B < 256 && (int64_t)p.A * (KL ? 2 : 1) > 32 * VEC * WR_THREADS ? 512 / p.B : 1;
         if (splits > pieces) splits = pieces;
         p.chunk = (int)((pieces + splits - 1) / splits * VEC * SP_THREADS);
         p.splits = (p.A + p.chunk - 1) / p.chunk;
@@ -872,7 +908,7 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
             const int per = p.A / (VEC * WR_THREADS);
             const auto go = [&](auto h, auto threads, auto simd) {
-                loss_wide_kernel<T, KL, decltype(h)::value, decltype(threads)::value, decltype(simd)::value><<<dim3(records), dim3(decltype(threads)::value), 0, s>>>(p);
+                loss_wide_kernel<T, KL, decltype(h)::value, decltype(threads)::value, decltype(simd)::value, decltype(simd)::value == 2 && KL ? 8 : 0><<<dim3(records), dim3(decltype(threads)::value), 0, s>>>(p);
             };
             typedef std::integral_constant<int, WR_THREADS> W1; typedef std::integral_constant<int, 2 * WR_THREADS> W2;
             typedef std::integral_constant<int, 4> S4; typedef std::integral_constant<int, 2> S2;
@@ -896,7 +932,7 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     }
     if (int rc = pl_launched(who)) return rc;
     if (!out_stats) return ACCERL_OK;
-    loss_stats_kernel<<<dim3(1), dim3(1024), 0, s>>>(p.rec, records, p.scale, out_stats);
+    loss_stats_kernel<<<dim3(1), dim3(records <= 256 ? 64 : 1024), 0, s>>>(p.rec, records, p.scale, out_stats);
     return pl_launched(who);
 }
 template <typename T>

@@ -118,6 +118,42 @@ def test_dense_strides(A, M, K, N, ld_x, ld_out, dtype):
     run_dense(A, M, K, N, dtype, dtype, True, False, M, ld_x, ld_out)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3])
+@pytest.mark.parametrize("x_dtype,K,N,bias", [("bf16", 4096, 300, True), ("f32", 1001, 16500, False), ("f16", 77, 40, True), ("f32", 8192, 20, True), ("bf16", 16384, 33, False)])
+def test_dense_few_tokens(A, M, x_dtype, K, N, bias):
+    """One or two tokens in one launch, three in two."""
+    run_dense(A, M, K, N, x_dtype, "f32", bias, True, seed=K)
+
+
+def test_dense_few_tokens_without_values(A):
+    """The forms of few tokens and of many agree on zeros, infinities, NaN and the ends of the types' ranges."""
+    w, b = torch.randn((60, 200), device="cuda"), torch.randn(60, device="cuda")
+    layer = A.DenseInt8(w, bias=b)
+    for t in (torch.float32, torch.bfloat16, torch.float16):
+        f = torch.finfo(t)
+        x = torch.linspace(-1, 1, 200, device="cuda").repeat(20, 1).to(t)
+        x[1], x[2], x[3], x[4, 7], x[5, 8], x[6, 9] = 0, x[2] * f.smallest_normal, x[3] * (f.max / 2), float("nan"), float("inf"), float("-inf")
+        many = layer.forward(x, dtype=torch.float32)
+        for i in range(0, 8, 2):
+            few = layer.forward(x[i:i + 2], dtype=torch.float32)
+            assert torch.equal(few.view(torch.int32), many[i:i + 2].view(torch.int32)) or torch.equal(few.isnan(), many[i:i + 2].isnan())
+            ok = ~few.isnan()
+            assert torch.equal(few[ok], many[i:i + 2][ok])
+
+
+def test_dense_update(A):
+    """New weights and bias in place: what a layer made from them gives."""
+    w = [torch.randn((130, 90), device="cuda") for _ in range(2)]
+    b = [torch.randn(130, device="cuda") for _ in range(2)]
+    x = torch.randn((40, 90), device="cuda")
+    layer = A.DenseInt8(w[0], bias=b[0])
+    layer.update(w[1], bias=b[1])
+    assert torch.equal(layer.forward(x), A.DenseInt8(w[1], bias=b[1]).forward(x))
+    for bad in ((w[0][:100], None), (w[0], b[0][:5])):
+        with pytest.raises(ValueError):
+            layer.update(bad[0], bias=bad[1])
+
+
 def test_dense_extremes(A):
     """Weights of -128 and tokens at both ends: sums as large as they get, exactly."""
     M, K, N = 20, 65536, 40

@@ -119,6 +119,72 @@ def test_loss_strides(A, B, n, ld, dtype, kl):
     assert torch.all(g[:, n:] == 9.0)
 
 
+class Sparse(Inputs):
+    """Many rows, of which few count: the others are not read, and only those few are worked out in 64 bits."""
+
+    def __init__(self, B, A, dtype, kl, mask, seed, live=5):
+        super().__init__(live, A, dtype, kl, mask, seed)
+        self.live = torch.randperm(B, generator=torch.Generator().manual_seed(seed))[:live]
+        few = {k: getattr(self, k) for k in ("z", "zr", "mask", "act", "old", "ref_lp", "adv", "w")}
+        few["w"] = few["w"] + 0.25
+        self.few, self.B = few, B
+
+        def spread(t, fill):
+            out = torch.full((B, *t.shape[1:]), fill, dtype=t.dtype, device=t.device)
+            out[self.live.to(t.device)] = t
+            return out
+
+        self.z, self.zr = spread(few["z"], float("nan")), spread(few["zr"], float("nan"))
+        if mask == "rows":
+            self.mask = spread(few["mask"], 1)
+        self.act, self.old, self.ref_lp, self.adv = (spread(few[k], 0) for k in ("act", "old", "ref_lp", "adv"))
+        self.w = spread(few["w"], 0)
+
+    def check(self, got):
+        where = self.live.cuda()
+        dead = torch.ones(self.B, dtype=torch.bool, device="cuda")
+        dead[where] = False
+        assert not got.grad[dead].any() and not got.loss[dead].any() and not got.logp[dead].any()
+        part = type(got)()
+        part.stats = got.stats
+        for k in ("loss", "logp", "kl", "entropy", "grad"):
+            setattr(part, k, getattr(got, k)[where])
+        for k, v in self.few.items():
+            setattr(self, k, v)
+        super().check(part)
+
+
+@pytest.mark.parametrize("n", [5003, 9000, 17001, 33333, 60001, 130001, 190003])
+@pytest.mark.parametrize("dtype,kl,mask", [("f32", "forward", "none"), ("bf16", "reverse", "rows"), ("f16", "none", "shared"), ("bf16", "forward", "none"), ("f32", "sampled", "none")])
+def test_loss_long_rows(A, n, dtype, kl, mask):
+    """Every number of vectors that stay in registers, what LDS holds behind them, and what is read twice."""
+    x = Sparse(300, n, dtype, kl, mask, seed=n)
+    x.check(x.run(A))
+
+
+@pytest.mark.parametrize("n", [40001, 130001])
+@pytest.mark.parametrize("dtype,kl", [("f32", "forward"), ("bf16", "reverse"), ("f16", "sampled"), ("bf16", "none")])
+@pytest.mark.parametrize("B", [1, 3, 40])
+def test_loss_long_rows_in_pieces(A, B, n, dtype, kl):
+    x = Sparse(B, n, dtype, kl, "none", seed=n, live=min(B, 4))
+    x.check(x.run(A))
+
+
+@pytest.mark.parametrize("n", [9000, 130001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kl", KLS)
+def test_loss_long_rows_with_infinities(A, n, dtype, kl):
+    """Logits of -inf and of the type's lowest value in long rows, which are then summed the careful way."""
+    x = Sparse(300, n, dtype, kl, "none", seed=n)
+    for t, k in ((x.z, "z"), (x.zr, "zr")):
+        t[:, 1::3] = float("-inf")
+        t[:, 2::3] = torch.finfo(TORCH[dtype]).min
+        x.few[k] = t[x.live.cuda()]
+    x.act[x.live] = 0
+    x.few["act"] = x.act[x.live]
+    x.check(x.run(A))
+
+
 @pytest.mark.parametrize("B,n", [(40, 18), (3, 9001), (513, 1000)])
 @pytest.mark.parametrize("kl", ["sampled", "reverse"])
 def test_loss_gradient_in_place_and_without(A, B, n, kl):
