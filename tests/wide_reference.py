@@ -92,9 +92,9 @@ def policy_loss(z, act, old, adv, mask=None, w=None, kl="none", zr=None, ref_lp=
 
 def sum_error(A):
     """Relative error of the sums under the maximum.  A term is off by 3 u |d| + 2 u (difference, product and exponential; d = z - max), in
-    the mean over the distribution at most 3 u (ln A + 1) + 2 u; a lane adds at most A / 512 + 8 terms, and 16 joins follow that each
+    the mean over the distribution at most 3 u (ln A + 1) + 2 u; a lane adds at most A / 256 + 32 terms, and 16 joins follow that each
     correct a sum by two roundings and an exponential of its own (6 u)."""
-    return U * (3 * (np.log(A) + 1) + 2 + A / 512 + 8 + 16 * 6)
+    return U * (3 * (np.log(A) + 1) + 2 + A / 256 + 32 + 16 * 6)
 
 
 def tolerances(ref, z, mask, dtype, kl, adv, ck, ch, scale):
