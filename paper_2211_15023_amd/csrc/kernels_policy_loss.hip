@@ -19,6 +19,9 @@ namespace {
 constexpr int64_t PL_MAX_A = 1 << 20;
 constexpr int PL_RECORDS = 2048;          // workgroups of a row pass, each leaves one record of sums
 constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is split
+// Vectors of a row that a lane of a wavefront holds at most; longer rows are a workgroup's (a workgroup each / a wavefront each, us: 10000 x 3000
+// bf16 forward 104 / 78, 10000 x 2000 fp32 reverse 84.5 / 70.5, log-probabilities of 32827 x 1305 fp32 140 / 80).
+constexpr int PL_HELD = 8;
 constexpr int PL_LONG1 = 80, PL_LONG2 = 56;             // times 256 vectors: what registers, and LDS with a reference, hold of a long row
 constexpr int PL_SCALAR = 32;             // up to this many actions lanes take single elements
 constexpr float PL_LOG2E = 1.44269504088896340736f;
@@ -167,6 +170,19 @@ __device__ __forceinline__ double pl_exp(double x) { return exp(x); }
 __device__ __forceinline__ float pl_inverse(float x) { return __builtin_amdgcn_rcpf(x); }    // to one unit in the last place
 __device__ __forceinline__ double pl_inverse(double x) { return 1.0 / x; }
 
+// exp(d) - d - 1, exact to its own size (in 32 bits the difference would leave a small one few digits): a series to d^8 below 1/2
+__device__ __forceinline__ float exp_rest(float d) {
+    if (fabsf(d) < 0.5f)
+        return d * d * fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.0f / 40320, 1.0f / 5040), 1.0f / 720), 1.0f / 120), 1.0f / 24), 1.0f / 6), 0.5f);
+    return d == INFINITY ? d : expf(d) - d - 1.0f;
+}
+__device__ __forceinline__ double exp_rest(double d) { return d == INFINITY ? d : exp(d) - d - 1.0; }
+// log pi(a) in 64 bits from a row's 32-bit sum: what is subtracted from a reference's log-probability must not be rounded where that is.
+// A function that is called, for its registers.
+__device__ __attribute__((noinline)) double exact_logp(float za, float c, bool far, float s) {
+    return PL_LN2 * ((far ? ((double)za - c) / PL_LN2 : (double)za * PL_LOG2E - c) - log2((double)s));
+}
+
 // Scalars of a row from its sums.  R: float where a wavefront holds many rows, double where the row is long and a wavefront does it once.
 // The ratio may be replaced (`ratio`, a double) by one that was worked out more exactly.
 template <int KL, typename R>
@@ -176,13 +192,23 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     c.z = base<false>(q.m); c.r = base<false>(q.mr); c.plain = plain;
     // the power of the action, as the sum's terms have theirs
     const R ta = __is_same(R, float) ? (R)power<false>(c.z, za) : c.z.far ? ((R)za - (R)c.z.c) / ln2 : (R)za * (R)PL_LOG2E - (R)c.z.c;
-    const R lp = ln2 * (ta - l2), ent = ln2 * (l2 - q.u * inv);
+    R lp = ln2 * (ta - l2);
+    const R ent = ln2 * (l2 - q.u * inv);
     c.zero = empty;
     o.lp = empty ? -INFINITY : (float)lp;
     o.ent = empty ? 0.0f : (float)ent;
     o.loss = o.kl = o.clipped = 0.0f;
     if (p.only_lp) return;
     const float w = in.w, adv = in.adv;
+    R away = (R)in.ref_lp - lp;
+    if constexpr (__is_same(R, float) && KL == 0) {
+        if (p.kind == ACCERL_KL_SAMPLED && !empty) {
+            const double l = exact_logp(za, c.z.c, c.z.far, q.s);
+            lp = (float)l;
+            o.lp = lp;
+            away = (float)(in.ref_lp - l);
+        }
+    }
     const R r = ratio ? (R)*ratio : lp == (R)-INFINITY ? (R)0 : pl_exp(lp - (R)in.old);
     const bool above = ratio ? *ratio > p.hi : r > (R)p.hi, below = ratio ? *ratio < p.lo : r < (R)p.lo;
     const bool cut = adv >= 0.0f ? above : below;
@@ -191,9 +217,8 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     const R ck = p.ck, ch = p.ch;
     if constexpr (KL == 0) {
         if (p.kind == ACCERL_KL_SAMPLED) {
-            const R d = (R)in.ref_lp - lp, e = pl_exp(d);
-            kl = d == (R)INFINITY ? d : e - d - (R)1;
-            if (ck != (R)0) at += ck * ((R)1 - e);
+            kl = exp_rest(away);
+            if (ck != (R)0) at -= ck * (kl + away);                // 1 - exp(d)
         }
     } else {
         const bool none = q.sr == (R)0;
@@ -463,9 +488,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
                 for (int i = 0; i < H; ++i) {
                     const float x = a[i].at(0), y = b[i].at(0);
                     const float w = pl_exp2(KL == 1 ? power<PLAIN>(cr, y) : power<PLAIN>(c, x)), d = (KL == 1 ? y - x : x - y) - mean;
-                    float f = pl_exp2(-PL_LOG2E * d) - 1.0f + d;
-                    if (fabsf(d) < 0.5f)              // its series, to d^8
-                        f = d * d * fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.0f / 40320, -1.0f / 5040), 1.0f / 720), -1.0f / 120), 1.0f / 24), -1.0f / 6), 0.5f);
+                    const float f = exp_rest(-d);
                     sum = fmaf(w, w > 0.0f ? f : 0.0f, sum);
                 }
                 for (int k = G >> 1; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
@@ -875,7 +898,7 @@ template <typename T, int KL>
 int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(T);
     int records;
-    if (p.A <= 64 * VEC * 4) {
+    if (p.A <= 64 * VEC * PL_HELD) {
         const int vec = p.A <= PL_SCALAR ? 1 : VEC, n = (p.A + vec - 1) / vec;     // vectors of a row
         int G = 1;
         while (G < 64 && G * (vec == 1 ? 10 : 4) < n) G *= 2;
@@ -889,7 +912,8 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             else if (H <= 8) rows_go<T, KL, 1, 8>(p, G, records, s);
             else rows_go<T, KL, 1, 10>(p, G, records, s);
         } else if (H <= 2) rows_go<T, KL, VEC, 2>(p, G, records, s);
-        else rows_go<T, KL, VEC, 4>(p, G, records, s);
+        else if (H <= 4) rows_go<T, KL, VEC, 4>(p, G, records, s);
+        else rows_go<T, KL, VEC, PL_HELD>(p, G, records, s);
     } else {
         // Few long rows are split, into pieces of at least one vector a lane; a row that one workgroup gets through in about the time of
         // another launch is not (bf16, log-probabilities, split / not: 16 x 20000 11.5 / 7.9 us, x 100000 12.5 / 14.7, 256 x 100000 24.3 /
@@ -906,28 +930,26 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
-            const int per = p.A / (VEC * WR_THREADS);
+            const int per = p.A / (VEC * WR_THREADS);            // at least 2
             const auto go = [&](auto h, auto threads, auto simd) {
                 loss_wide_kernel<T, KL, decltype(h)::value, decltype(threads)::value, decltype(simd)::value, decltype(simd)::value == 2 && KL ? 8 : 0><<<dim3(records), dim3(decltype(threads)::value), 0, s>>>(p);
             };
             typedef std::integral_constant<int, WR_THREADS> W1; typedef std::integral_constant<int, 2 * WR_THREADS> W2;
             typedef std::integral_constant<int, 4> S4; typedef std::integral_constant<int, 2> S2;
-#define PL_HELD(n) std::integral_constant<int, n>()
+#define PL_KEPT(n) std::integral_constant<int, n>()
             if constexpr (KL == 0) {
-                if (p.g && per >= PL_LONG1) go(PL_HELD(40), W2(), S2());
-                else if (p.g && per >= 15) go(PL_HELD(15), W1(), S4());
-                else if (p.g && per >= 8) go(PL_HELD(8), W1(), S4());
-                else if (per >= 4) go(PL_HELD(4), W1(), S4());
-                else if (per >= 2) go(PL_HELD(2), W1(), S4());
-                else go(PL_HELD(1), W1(), S4());
+                if (p.g && per >= PL_LONG1) go(PL_KEPT(40), W2(), S2());
+                else if (p.g && per >= 15) go(PL_KEPT(15), W1(), S4());
+                else if (p.g && per >= 8) go(PL_KEPT(8), W1(), S4());
+                else if (per >= 4) go(PL_KEPT(4), W1(), S4());
+                else go(PL_KEPT(2), W1(), S4());
             } else {
-                if (p.g && per >= PL_LONG2) go(PL_HELD(20), W2(), S2());
-                else if (p.g && per >= 7) go(PL_HELD(7), W1(), S4());
-                else if (p.g && per >= 4) go(PL_HELD(4), W1(), S4());
-                else if (per >= 2) go(PL_HELD(2), W1(), S4());
-                else go(PL_HELD(1), W1(), S4());
+                if (p.g && per >= PL_LONG2) go(PL_KEPT(20), W2(), S2());
+                else if (p.g && per >= 7) go(PL_KEPT(7), W1(), S4());
+                else if (p.g && per >= 4) go(PL_KEPT(4), W1(), S4());
+                else go(PL_KEPT(2), W1(), S4());
             }
-#undef PL_HELD
+#undef PL_KEPT
         }
     }
     if (int rc = pl_launched(who)) return rc;

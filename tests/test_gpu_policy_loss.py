@@ -411,3 +411,21 @@ def test_loss_on_another_stream_and_in_a_graph(A, B, n):
         eager = how.forward(z, act, old, adv, weights=w, scale=1.0, ref_logits=x.zr)
         for name in ("loss", "logp", "kl", "entropy", "stats", "grad"):
             assert torch.equal(getattr(r, name), getattr(eager, name)), (k, name)
+
+
+@pytest.mark.parametrize("B,n", [(300, 18), (300, 130), (40, 2000), (600, 5003)])
+@pytest.mark.parametrize("apart", [0.3, 1e-2, 1e-3])
+def test_loss_small_sampled_kl(A, B, n, apart):
+    """A reference close to the policy: its KL is a small number, and keeps six digits of it."""
+    x = Inputs(B, n, "f32", "sampled", "none", seed=81, spread=1.0)
+    x.w[:] = 1.0
+    x.act = torch.randint(0, n, (B,), dtype=torch.int32, generator=torch.Generator().manual_seed(2))
+    lp = ref.softmax_rows(as64(x.z), np.ones((B, n), bool))[0][np.arange(B), x.act.numpy()]
+    x.ref_lp = torch.from_numpy(lp + apart * np.random.default_rng(3).uniform(0.5, 1, B)).float()
+    got = x.run(A)
+    r, _ = x.want()
+    d = as64(x.ref_lp) - r["logp"]
+    # off by the slope exp(d) - 1 times the sum's error (terms within 2 u, exponents of at most 8: 8 u; the joins of a lane's terms), and by 8 u
+    tol = np.expm1(d) * (16 * ref.U + 4 * ref.U * np.sqrt(n / 64 + 32)) + 16 * ref.U * r["kl"]
+    off = np.abs(as64(got.kl) - r["kl"])
+    assert (off <= tol).all(), np.max(off / tol)
