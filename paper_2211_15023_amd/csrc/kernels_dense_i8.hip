@@ -312,6 +312,7 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void dense_i8_tile_kernel(const De
         constexpr int c = decltype(C)::value, c1 = (c + 1) % 3, c2 = (c + 2) % 3;      // c = s % 3
         asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(FA * KS) : "memory");
         write_a(r[c2], c2);                                                           // step s + 2
+        asm volatile("" ::: "memory");                                                // (the barriers count on writes before reads)
         load_a(r[c2], s + 5);
         load_b(b[c2], s + 2);
 #pragma unroll
