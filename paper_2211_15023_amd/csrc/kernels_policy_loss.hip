@@ -306,14 +306,18 @@ __device__ __forceinline__ void vec_drop(Vec<T, VEC>& v, int e) {
     constexpr int PER = 4 / (int)sizeof(T);
     v.w[e / PER] = (v.w[e / PER] & ~vec_part<T>(e)) | (nothing<T, PLAIN>() & vec_part<T>(e));
 }
+// 16 bytes of any alignment of elements; ONCE: nobody reads them again, they pass the caches by
+template <bool ONCE, typename T> __device__ __forceinline__ u32x4 load16(const T* from) {
+    if constexpr (sizeof(T) == 4) return ONCE ? __builtin_nontemporal_load((const u32x4_at4*)from) : *(const u32x4_at4*)from;
+    else return ONCE ? __builtin_nontemporal_load((const u32x4_at2*)from) : *(const u32x4_at2*)from;
+}
 // FULL: the vector ends before the end.
-template <bool FULL, bool PLAIN, typename T, int VEC>
+template <bool FULL, bool PLAIN, bool ONCE = false, typename T, int VEC>
 __device__ __forceinline__ void vec_load(Vec<T, VEC>& v, const T* row, const uint8_t* mask, int i, int end) {
     static_assert(VEC > 1, "whole vectors");
     {
         const int at = FULL ? i : vec_at<VEC>(i, end);
-        if constexpr (sizeof(T) == 4) v.w = *(const u32x4_at4*)(row + at);
-        else v.w = *(const u32x4_at2*)(row + at);
+        v.w = load16<ONCE>(row + at);
         if (mask) {
 #pragma unroll
             for (int k = 0; k < VEC / 4; ++k) {
@@ -329,18 +333,21 @@ __device__ __forceinline__ void vec_load(Vec<T, VEC>& v, const T* row, const uin
         }
     }
 }
+// Results are not read again here: they pass the caches by (2048 x 150000 bf16 with the forward KL 538 -> 496 us, 16000 x 6003 fp16 152 -> 123,
+// 100000 x 300 fp32 163 -> 128).
 template <bool FULL, typename T, int VEC>
 __device__ __forceinline__ void vec_store(T* row, int i, int end, const float (&v)[VEC]) {
     if constexpr (VEC == 1) {
         if (i < end) row[i] = f32_el<T>(v[0]);
     } else if (FULL || i + VEC <= end) {
         if constexpr (VEC == 4) {
-            *(u32x4_at4*)(row + i) = (u32x4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            const u32x4 w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            __builtin_nontemporal_store(w, (u32x4_at4*)(row + i));
         } else {
             u32x4 w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = f32_pair<T>(v[2 * e], v[2 * e + 1]);
-            *(u32x4_at2*)(row + i) = w;
+            __builtin_nontemporal_store(w, (u32x4_at2*)(row + i));
         }
     } else {
         const int at = vec_at<VEC>(i, end);
@@ -573,7 +580,7 @@ constexpr int WR_WAVES = 8;               // most wavefronts of a workgroup
 
 // The vectors of elements first to end, U at a time, loaded together and ahead of the ones before; the last ones one by one.  f(whole,
 // vectors, vectors of the reference, first element): `whole` (a type) where no vector passes the end.
-template <typename T, int KL, int THREADS, int U, bool PLAIN, typename F>
+template <typename T, int KL, int THREADS, int U, bool PLAIN, bool ONCE = false, typename F>
 __device__ __forceinline__ void wide_stream(const T* z, const T* zr, const uint8_t* mask, int first, int end, F&& f) {
     constexpr int VEC = 16 / sizeof(T), STEP = THREADS * VEC;
     Vec<T, VEC> a[U], b[U];
@@ -581,8 +588,8 @@ __device__ __forceinline__ void wide_stream(const T* z, const T* zr, const uint8
     auto load = [&](auto whole, int at) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            vec_load<decltype(whole)::value, PLAIN>(a[u], z, mask, at + u * STEP, end);
-            if constexpr (KL != 0) vec_load<decltype(whole)::value, PLAIN>(b[u], zr, mask, at + u * STEP, end);
+            vec_load<decltype(whole)::value, PLAIN, ONCE>(a[u], z, mask, at + u * STEP, end);
+            if constexpr (KL != 0) vec_load<decltype(whole)::value, PLAIN, ONCE>(b[u], zr, mask, at + u * STEP, end);
         }
     };
     const int turns = (end - first) / (U * STEP);              // whole ones
@@ -601,8 +608,8 @@ __device__ __forceinline__ void wide_stream(const T* z, const T* zr, const uint8
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (rest + u * STEP < end) {
-            vec_load<false, PLAIN>(a[u], z, mask, i + u * STEP, end);
-            if constexpr (KL != 0) vec_load<false, PLAIN>(b[u], zr, mask, i + u * STEP, end);
+            vec_load<false, PLAIN, ONCE>(a[u], z, mask, i + u * STEP, end);
+            if constexpr (KL != 0) vec_load<false, PLAIN, ONCE>(b[u], zr, mask, i + u * STEP, end);
         }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -670,9 +677,9 @@ template <int THREADS, typename T, int VEC, int H>
 __device__ __forceinline__ void held_load(Vec<T, VEC> (&v)[H], const T* row, int tid) {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-        const T* from = (const T*)((const char*)row + (uint32_t)((i * THREADS + tid) * 16));
-        if constexpr (sizeof(T) == 4) v[i].w = *(const u32x4_at4*)from;
-        else v[i].w = *(const u32x4_at2*)from;
+        // (past the caches where registers hold most of a row: 8192 x 32000 bf16 222 -> 209 us, 8192 x 2 x 16000 245 -> 224, but with two of
+        // three vectors held 16000 x 6003 fp16 123 -> 139)
+        v[i].w = load16<(H >= 7)>((const T*)((const char*)row + (uint32_t)((i * THREADS + tid) * 16)));
     }
 }
 template <bool TWO, int THREADS, typename T, int VEC, int H>
@@ -732,7 +739,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         if (mask) held_mask<KL != 0, THREADS>(a, b, mask, opaque(tid));
         RowSum q = row_empty();
         held_sums<KL>(q, a, b);
-        wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, [&](auto, const auto& x, const auto& y, int at) {
+        const auto take = [&](auto, const auto& x, const auto& y, int at) {
             constexpr int N = sizeof(x) / sizeof(x[0]);
             if constexpr (LDS > 0) {
                 const int slot = (at - HELD) / (THREADS * VEC);
@@ -744,7 +751,10 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
                     }
             }
             sum_vecs<KL, N, true>(q, x, y, 0);
-        });
+        };
+        // (without a gradient nothing is read twice: log-probabilities of 4096 x 32768 fp32 105 -> 95 us)
+        if (H <= 4 && !p.g) wide_stream<T, KL, THREADS, U, true, true>(z, zr, mask, HELD, p.A, take);
+        else wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, take);
         Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), in, za);
         if (c.plain < 0) {                                          // (everybody)
             q = row_empty();
