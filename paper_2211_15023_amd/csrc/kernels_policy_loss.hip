@@ -22,7 +22,6 @@ constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is spli
 // Vectors of a row that a lane of a wavefront holds at most; longer rows are a workgroup's (a workgroup each / a wavefront each, us: 10000 x 3000
 // bf16 forward 104 / 78, 10000 x 2000 fp32 reverse 84.5 / 70.5, log-probabilities of 32827 x 1305 fp32 140 / 80).
 constexpr int PL_HELD = 8;
-constexpr int PL_LONG1 = 80, PL_LONG2 = 56;             // times 256 vectors: what registers, and LDS with a reference, hold of a long row
 constexpr int PL_SCALAR = 32;             // up to this many actions lanes take single elements
 constexpr float PL_LOG2E = 1.44269504088896340736f;
 constexpr double PL_LN2 = 0.693147180559945309417;
@@ -708,10 +707,12 @@ __device__ __forceinline__ void held_sums(RowSum& q, const Vec<T, VEC> (&a)[H], 
     if constexpr (H % 2) sum_vecs<KL, 1, true>(q, a, b, H - 1);
 }
 
-// Rows one after the other, each by the whole workgroup, four of them on a compute unit.  H vectors of a row, all of them inside it, stay in a
-// lane's registers from the sums to the gradient; the rest is read twice.  (What misses the second-level cache moves at one rate whether the
-// last-level cache has it or not, so that a second reading costs what the first did.  Twice the registers for half the wavefronts
-// lost as much as it saved: 4096 rows of 2 x 32000 bf16 228 -> 246 us, 2048 of 2 x 150000 598 / 591.)
+// Rows one after the other, each by the whole workgroup.  H vectors of a row, all of them inside it, stay in a lane's registers from the sums
+// to the gradient, and up to LDS more (of each table) in LDS, a lane's own; the rest is read twice.  Bound by memory, a row's two to three
+// tables once where all of it is held: what misses the second-level cache moves at one rate whether the last-level cache has it or not, so
+// that a second reading costs what the first did.  Four workgroups of 256 a compute unit hold 15 vectors (seven of each table), two hold 56 (28)
+// and one of 512 112 (56): fewer wavefronts hide less, but what they save is more from rows of 15 to 20 vectors a lane on (with the figures
+// at the rule).  8192 x 32000 bf16, no reference: 206 us, 5.1 TB/s of once read and once written, 2048 x 2 x 150000 480 us, 3.8 TB/s.
 template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
 __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
@@ -788,17 +789,17 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
                     vec_grad<true, KL, true>(c, act, a[i], b[i], g, (i * THREADS + lane) * VEC, p.A);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                const int rest = (p.A - HELD) / (THREADS * VEC), kept = rest < LDS ? rest : LDS;      // whole vectors in LDS
                 if constexpr (LDS > 0) {
-                    // (long rows: LDS is full)
 #pragma unroll 1
-                    for (int i = 0; i < LDS; ++i) {
+                    for (int i = 0; i < kept; ++i) {
                         Vec<T, VEC> x, y;
                         x.w = s_row[i][lane];
                         if constexpr (KL != 0) y.w = s_row[LDS + i][lane];
                         vec_grad<true, KL, true>(c, act, x, y, g, ((H + i) * THREADS + lane) * VEC, p.A);
                     }
                 }
-                grads(std::true_type(), std::integral_constant<int, U>(), HELD + LDS * THREADS * VEC);
+                grads(std::true_type(), std::integral_constant<int, U>(), HELD + kept * THREADS * VEC);
             } else {
                 grads(std::false_type(), std::integral_constant<int, 1>(), 0);
             }
@@ -904,6 +905,9 @@ int pl_launched(const char* who) {
 template <typename T, int KL, int VEC, int H>
 void rows_go(const LossParams& p, int G, int blocks, hipStream_t s) { loss_rows_kernel<T, KL, VEC, H><<<dim3(blocks), dim3(NR_THREADS), 0, s>>>(p, G); }
 
+template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
+void wide_go(const LossParams& p, int blocks, hipStream_t s) { loss_wide_kernel<T, KL, H, THREADS, PER_SIMD, LDS><<<dim3(blocks), dim3(THREADS), 0, s>>>(p); }
+
 template <typename T, int KL>
 int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(T);
@@ -940,26 +944,24 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
-            const int per = p.A / (VEC * WR_THREADS);            // at least 2
-            const auto go = [&](auto h, auto threads, auto simd) {
-                loss_wide_kernel<T, KL, decltype(h)::value, decltype(threads)::value, decltype(simd)::value, decltype(simd)::value == 2 && KL ? 8 : 0><<<dim3(records), dim3(decltype(threads)::value), 0, s>>>(p);
-            };
-            typedef std::integral_constant<int, WR_THREADS> W1; typedef std::integral_constant<int, 2 * WR_THREADS> W2;
-            typedef std::integral_constant<int, 4> S4; typedef std::integral_constant<int, 2> S2;
-#define PL_KEPT(n) std::integral_constant<int, n>()
+            const int per = p.A / (VEC * WR_THREADS);            // whole vectors a thread of 256: at least 2, and at least what the forms below hold in registers
+            // With a gradient, the form that holds the most of the row (times in us, this line's form / the line's below, bf16).
             if constexpr (KL == 0) {
-                if (p.g && per >= PL_LONG1) go(PL_KEPT(40), W2(), S2());
-                else if (p.g && per >= 15) go(PL_KEPT(15), W1(), S4());
-                else if (p.g && per >= 8) go(PL_KEPT(8), W1(), S4());
-                else if (per >= 4) go(PL_KEPT(4), W1(), S4());
-                else go(PL_KEPT(2), W1(), S4());
+                if (p.g && per >= 96) wide_go<T, KL, 40, 512, 2, 16>(p, records, s);         // 887 x 225285 219 / 231, but 1148 x 174085 219 / 210
+                else if (p.g && per >= 48) wide_go<T, KL, 40, 256, 2, 16>(p, records, s);    // 1953 x 102405 192 / 194, but 2325 x 86021 198 / 194
+                else if (p.g && per >= 20) wide_go<T, KL, 20, 256, 2, 16>(p, records, s);    // 4649 x 43013 200 / 208, 2441 x 81925 187 / 212
+                else if (p.g && per >= 15) wide_go<T, KL, 15, 256, 4, 0>(p, records, s);
+                else if (p.g && per >= 8) wide_go<T, KL, 8, 256, 4, 0>(p, records, s);
+                else if (per >= 4) wide_go<T, KL, 4, 256, 4, 0>(p, records, s);
+                else wide_go<T, KL, 2, 256, 4, 0>(p, records, s);
             } else {
-                if (p.g && per >= PL_LONG2) go(PL_KEPT(20), W2(), S2());
-                else if (p.g && per >= 7) go(PL_KEPT(7), W1(), S4());
-                else if (p.g && per >= 4) go(PL_KEPT(4), W1(), S4());
-                else go(PL_KEPT(2), W1(), S4());
+                if (p.g && per >= 44) wide_go<T, KL, 20, 512, 2, 8>(p, records, s);          // 1992 x 100357 forward 341 / 370, but 2325 x 86021 377 / 375
+                else if (p.g && per >= 20) wide_go<T, KL, 20, 256, 2, 8>(p, records, s);     // 4438 x 45061 reverse 318 / 363 (seven vectors)
+                else if (p.g && per >= 15) wide_go<T, KL, 12, 256, 2, 8>(p, records, s);     // 6259 x 31953 forward 342 / 401, but fp32 3000 x 14000 159 / 144
+                else if (p.g && per >= 7) wide_go<T, KL, 7, 256, 4, 0>(p, records, s);
+                else if (p.g && per >= 4) wide_go<T, KL, 4, 256, 4, 0>(p, records, s);
+                else wide_go<T, KL, 2, 256, 4, 0>(p, records, s);
             }
-#undef PL_KEPT
         }
     }
     if (int rc = pl_launched(who)) return rc;
