@@ -408,7 +408,11 @@ __device__ __attribute__((noinline)) double exact_ratio(const T* z, const uint8_
 }
 
 // ---------------------------------------------------------------- rows that lanes of one wavefront hold
-// G lanes hold a row, lane j its vectors j, j + G, ..  (H of them at most).  A wavefront does 64 / G rows at a time.
+// G lanes hold a row, lane j its vectors j, j + G, ..  (H of them at most), read once.  A wavefront does 64 / G rows at a time.  Long batches
+// of short rows are bound by instructions and the latency of a row's chain of sums, logarithm and gradient more than by memory: 262144 x 18
+// fp32 with the forward KL and masks 35 us, of 14 that their bytes take at a copy's rate (a row a lane, through LDS, was
+// faster from 9 to 18 actions by up to a sixth, and slower elsewhere by as much); 32 x 18 5.4 us in one launch, of which 4 is any launch that
+// waits for memory.
 constexpr int NR_THREADS = 256;
 template <typename T, int KL, int VEC, int H>
 __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams p, int G) {
@@ -676,9 +680,9 @@ template <int THREADS, typename T, int VEC, int H>
 __device__ __forceinline__ void held_load(Vec<T, VEC> (&v)[H], const T* row, int tid) {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-        // (past the caches where registers hold most of a row: 8192 x 32000 bf16 222 -> 209 us, 8192 x 2 x 16000 245 -> 224, but with two of
-        // three vectors held 16000 x 6003 fp16 123 -> 139)
-        v[i].w = load16<(H >= 7)>((const T*)((const char*)row + (uint32_t)((i * THREADS + tid) * 16)));
+        // (past the caches: 8192 x 32000 bf16 222 -> 209 us, 12500 x 2 x 16000 295 -> 285, but with two of three vectors held 16000 x 6003 fp16
+        // 123 -> 139)
+        v[i].w = load16<(H >= 4)>((const T*)((const char*)row + (uint32_t)((i * THREADS + tid) * 16)));
     }
 }
 template <bool TWO, int THREADS, typename T, int VEC, int H>
@@ -710,9 +714,9 @@ __device__ __forceinline__ void held_sums(RowSum& q, const Vec<T, VEC> (&a)[H], 
 // Rows one after the other, each by the whole workgroup.  H vectors of a row, all of them inside it, stay in a lane's registers from the sums
 // to the gradient, and up to LDS more (of each table) in LDS, a lane's own; the rest is read twice.  Bound by memory, a row's two to three
 // tables once where all of it is held: what misses the second-level cache moves at one rate whether the last-level cache has it or not, so
-// that a second reading costs what the first did.  Four workgroups of 256 a compute unit hold 15 vectors (seven of each table), two hold 56 (28)
-// and one of 512 112 (56): fewer wavefronts hide less, but what they save is more from rows of 15 to 20 vectors a lane on (with the figures
-// at the rule).  8192 x 32000 bf16, no reference: 206 us, 5.1 TB/s of once read and once written, 2048 x 2 x 150000 480 us, 3.8 TB/s.
+// that a second reading costs what the first did.  Four workgroups of 256 a compute unit hold 15 vectors (eight of each table: more registers
+// would spill, and seven did), two hold 56 (28) and one of 512 112 (56): fewer wavefronts hide less, but what they save is more from rows of
+// 15 to 30 vectors a lane on.  8192 x 32000 bf16, no reference: 206 us, 5.1 TB/s of once read and once written; 2048 x 2 x 150000 486, 3.8.
 template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
 __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
@@ -809,7 +813,8 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
     if (threadIdx.x == 0 && p.rec) p.rec[blockIdx.x] = rec;
 }
 
-// Few rows: pieces of rows to partial sums, then pieces again with the row's sums joined.
+// Few rows: pieces of rows to partial sums, then pieces again with the row's sums joined.  Two dependent launches, latency: 16 x 100000
+// bf16 log-probabilities 4.8 + 6.0 us.  (One launch would need its workgroups to wait for each other or memory that is cleared between calls.)
 constexpr int SP_THREADS = 512;
 template <typename T, int KL>
 __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams p) {
@@ -876,7 +881,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
                               });
 }
 
-// the records of a pass, in their order
+// the records of a pass, in their order, so that sums repeat: 2048 of them 5 us, a launch and two round trips
 __global__ __launch_bounds__(1024) void loss_stats_kernel(const Record* rec, int n, float scale, float* out) {
     __shared__ Record s_rec[16];
     Record r = {0, 0, 0, 0};
@@ -914,8 +919,10 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
     int records;
     if (p.A <= 64 * VEC * PL_HELD) {
         const int vec = p.A <= PL_SCALAR ? 1 : VEC, n = (p.A + vec - 1) / vec;     // vectors of a row
+        // Lanes of a row, with up to 8 single elements or 4 vectors each (us; half as many / these / twice: 200000 x 32 fp32 41 / 34, 10 elements
+        // 262144 x 18 42 / 40; 100000 x 300 fp32 176 / 129 / 133, 50000 x 100 bf16 27 / 26 / 33, 20000 x 1000 60 / 49 / 49).
         int G = 1;
-        while (G < 64 && G * (vec == 1 ? 10 : 4) < n) G *= 2;
+        while (G < 64 && G * (vec == 1 ? 8 : 4) < n) G *= 2;
         const int64_t want = (p.B + NR_THREADS / G - 1) / (NR_THREADS / G);
         records = (int)(want < PL_RECORDS ? want : PL_RECORDS);
         const int H = (n + G - 1) / G;
@@ -923,8 +930,7 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
         if (vec == 1) {
             if (H <= 4) rows_go<T, KL, 1, 4>(p, G, records, s);
             else if (H <= 6) rows_go<T, KL, 1, 6>(p, G, records, s);
-            else if (H <= 8) rows_go<T, KL, 1, 8>(p, G, records, s);
-            else rows_go<T, KL, 1, 10>(p, G, records, s);
+            else rows_go<T, KL, 1, 8>(p, G, records, s);
         } else if (H <= 2) rows_go<T, KL, VEC, 2>(p, G, records, s);
         else if (H <= 4) rows_go<T, KL, VEC, 4>(p, G, records, s);
         else rows_go<T, KL, VEC, PL_HELD>(p, G, records, s);
@@ -945,21 +951,22 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
             const int per = p.A / (VEC * WR_THREADS);            // whole vectors a thread of 256: at least 2, and at least what the forms below hold in registers
-            // With a gradient, the form that holds the most of the row (times in us, this line's form / the line's below, bf16).
+            // With a gradient, the form that holds the most of the row (times in us, this line's form / the line's below, bf16; with a
+            // reference the forward KL, with masks of each row's own four workgroups for longer: 6250 x 32000 478 / 393, 4000 x 50000 fp16 491 / 420).
+            const bool own = p.mask && p.ldm;
             if constexpr (KL == 0) {
                 if (p.g && per >= 96) wide_go<T, KL, 40, 512, 2, 16>(p, records, s);         // 887 x 225285 219 / 231, but 1148 x 174085 219 / 210
                 else if (p.g && per >= 48) wide_go<T, KL, 40, 256, 2, 16>(p, records, s);    // 1953 x 102405 192 / 194, but 2325 x 86021 198 / 194
-                else if (p.g && per >= 20) wide_go<T, KL, 20, 256, 2, 16>(p, records, s);    // 4649 x 43013 200 / 208, 2441 x 81925 187 / 212
-                else if (p.g && per >= 15) wide_go<T, KL, 15, 256, 4, 0>(p, records, s);
-                else if (p.g && per >= 8) wide_go<T, KL, 8, 256, 4, 0>(p, records, s);
+                else if (p.g && per >= 30) wide_go<T, KL, 20, 256, 2, 16>(p, records, s);    // 2500 x 80000 184 / 212, but 4000 x 50000 186 / 177
+                else if (p.g && per >= 15) wide_go<T, KL, 15, 256, 4, 0>(p, records, s);     // 8192 x 32000 224 / 247, eight in registers and nine in LDS
+                else if (p.g && per >= 8) wide_go<T, KL, 8, 256, 4, 0>(p, records, s);       // 8192 x 28000 181 / 215, but 8192 x 14000 105 / 104
                 else if (per >= 4) wide_go<T, KL, 4, 256, 4, 0>(p, records, s);
                 else wide_go<T, KL, 2, 256, 4, 0>(p, records, s);
             } else {
                 if (p.g && per >= 44) wide_go<T, KL, 20, 512, 2, 8>(p, records, s);          // 1992 x 100357 forward 341 / 370, but 2325 x 86021 377 / 375
-                else if (p.g && per >= 20) wide_go<T, KL, 20, 256, 2, 8>(p, records, s);     // 4438 x 45061 reverse 318 / 363 (seven vectors)
-                else if (p.g && per >= 15) wide_go<T, KL, 12, 256, 2, 8>(p, records, s);     // 6259 x 31953 forward 342 / 401, but fp32 3000 x 14000 159 / 144
-                else if (p.g && per >= 7) wide_go<T, KL, 7, 256, 4, 0>(p, records, s);
-                else if (p.g && per >= 4) wide_go<T, KL, 4, 256, 4, 0>(p, records, s);
+                else if (p.g && per >= (own ? 28 : 20)) wide_go<T, KL, 20, 256, 2, 8>(p, records, s);    // 4347 x 46000 277 / 316
+                else if (p.g && per >= (own ? 28 : 15)) wide_go<T, KL, 12, 256, 2, 8>(p, records, s);    // 6259 x 31953 342 / 401, but 8000 x 25000 315 / 294
+                else if (p.g && per >= 4) wide_go<T, KL, 4, 256, 4, 4>(p, records, s);       // 9523 x 21000 forward 294 / 338, 8192 x 8200 120 / 128
                 else wide_go<T, KL, 2, 256, 4, 0>(p, records, s);
             }
         }

@@ -162,13 +162,20 @@ def test_loss_long_rows(A, n, dtype, kl, mask):
     x.check(x.run(A))
 
 
-@pytest.mark.parametrize("vectors", [15, 20, 28, 36, 44, 48, 56, 96, 112])
+@pytest.mark.parametrize("vectors", [4, 8, 15, 17, 20, 28, 30, 36, 44, 48, 56, 96, 112])
 @pytest.mark.parametrize("more", [-1, 0, 1, 1027])
 @pytest.mark.parametrize("dtype,kl", [("bf16", "forward"), ("f16", "sampled"), ("f32", "reverse"), ("bf16", "none")])
 def test_loss_long_rows_at_whole_vectors(A, vectors, more, dtype, kl):
     """Rows of a whole number of vectors for 256 threads, and a little less or more, where one form takes over from another and where what
     registers and LDS hold just ends."""
     x = Sparse(257, vectors * 256 * (4 if dtype == "f32" else 8) + more, dtype, kl, "shared" if vectors % 8 else "none", seed=vectors)
+    x.check(x.run(A))
+
+
+@pytest.mark.parametrize("vectors", [8, 15, 20, 27, 28, 44])
+@pytest.mark.parametrize("dtype,kl", [("bf16", "forward"), ("f16", "reverse"), ("f32", "none")])
+def test_loss_long_rows_with_masks_of_their_own(A, vectors, dtype, kl):
+    x = Sparse(257, vectors * 256 * (4 if dtype == "f32" else 8) + 5, dtype, kl, "rows", seed=vectors)
     x.check(x.run(A))
 
 
