@@ -587,11 +587,13 @@ class DenseInt8:
     def __init__(self, w, w_scale=None, bias=None, relu=False):
         load_library()
         self.N, self.K = w.shape
+        if bias is not None and tuple(bias.shape) != (self.N,):
+            raise ValueError(f"the bias must be a vector of {self.N}")
         self.relu = bool(relu)
         self._relu = int(self.relu)
         self.w = torch.empty(packed_rows_bytes(self.N, self.K), dtype=torch.int8, device=w.device)
         self.w_scale = torch.empty(self.N, dtype=torch.float32, device=w.device)
-        self.bias = None if bias is None else bias.detach().to(torch.float32).contiguous().clone()
+        self.bias = None if bias is None else bias.detach().to(w.device, torch.float32, copy=True).contiguous()
         self._work = _Workspaces()
         self.update(w, w_scale)
 
@@ -614,7 +616,7 @@ class DenseInt8:
         if stream is None and out is None and x.is_cuda:
             raw = torch._C._cuda_getCurrentRawStream(x.device.index)
             ws = self._work.of.get((x.device, raw))
-            r = None if ws is None else (_args or _loaded()).dense_dynamic(x, self.w, self.w_scale, self.bias, self.N, self.K, self._relu, _CODES.get(dtype, 3),
+            r = None if ws is None else (_args or _loaded()).dense_dynamic(x, self.N, self.K, self.w, self.w_scale, self.bias, self._relu, _CODES.get(dtype, 3),
                                                                            ws, raw)
             if r is not None:
                 if r[0]:

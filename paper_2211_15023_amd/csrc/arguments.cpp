@@ -231,21 +231,24 @@ PyObject* call_out(PyObject* const* argv, Py_ssize_t given, Py_ssize_t count, Pa
     }
 }
 
-// (x, w_packed, w_scale, bias, N, K, relu, type of the output or -1 for x's, workspace, stream) -> (status, out)
+// (x, N, K, w_packed, w_scale, bias, relu, type of the output or -1 for x's, workspace, stream) -> (status, out)
 PyObject* dense_dynamic(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return call_out(argv, n, 10, [](Args& a, std::vector<at::Tensor>& outs) {
         c10::ScalarType type = c10::ScalarType::Undefined;
         int64_t M = -1, Kx = -1, ldx = 0, bytes = 0;
         const void* x = a.rows(&type, &M, &Kx, &ldx);
         const int code = dtype_code(type);
-        const int8_t* w = (const int8_t*)a.pointer(c10::kChar);
-        const float *sw = a.f32(), *bias = a.f32();
-        const int64_t N = a.integer(), K = a.integer(), relu = a.integer();
+        const int64_t N = a.integer(), K = a.integer();
+        const at::Tensor* w = a.tensor();
+        const float *sw = (const float*)a.vector(c10::kFloat, N), *bias = (const float*)a.vector(c10::kFloat, N);
+        const int64_t relu = a.integer();
         int64_t out = a.integer();
         const at::Tensor* ws = a.tensor();
         void* s = a.stream();
         if (out < 0) out = code;
-        if (code < 0 || out > 2 || Kx != K) a.plain = false;
+        if (code < 0 || out > 2 || Kx != K || !sw) a.plain = false;
+        if (a.plain && (w->scalar_type() != c10::kChar || w->numel() < accerl_packed_rows_bytes(N, K))) a.plain = false;
+        const int8_t* pw = a.plain ? (const int8_t*)w->data_ptr() : nullptr;
         void *po = nullptr, *pws = nullptr;
         if (a.plain) {
             bytes = ws->numel();
@@ -256,7 +259,7 @@ PyObject* dense_dynamic(PyObject*, PyObject* const* argv, Py_ssize_t n) {
                 po = outs[0].data_ptr();
             }
         }
-        return [=] { return accerl_dense_i8_dynamic(x, code, ldx, w, sw, bias, M, N, K, (int32_t)relu, po, (int32_t)out, N, pws, bytes, s); };
+        return [=] { return accerl_dense_i8_dynamic(x, code, ldx, pw, sw, bias, M, N, K, (int32_t)relu, po, (int32_t)out, N, pws, bytes, s); };
     });
 }
 
