@@ -602,8 +602,8 @@ class DenseInt8:
         if tuple(w.shape) != (self.N, self.K) or (bias is not None and (self.bias is None or bias.shape != self.bias.shape)):
             raise ValueError("the weights or the bias differ in shape from the layer's")
         if w.dtype == torch.int8:
-            if w_scale is None:
-                raise ValueError("int8 weights need their scales")
+            if w_scale is None or tuple(w_scale.shape) != (self.N,):
+                raise ValueError(f"int8 weights need a vector of {self.N} scales")
             self.w_scale.copy_(w_scale.detach())
             accerl_pack_rows_i8(w, self.w)
         else:
