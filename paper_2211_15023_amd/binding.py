@@ -606,6 +606,8 @@ class DenseInt8:
                 raise ValueError(f"int8 weights need a vector of {self.N} scales")
             self.w_scale.copy_(w_scale.detach())
             accerl_pack_rows_i8(w, self.w)
+        elif w_scale is not None:
+            raise ValueError("scales belong to int8 weights; a float matrix is quantised with scales of its own")
         else:
             accerl_quantize_rows(w.detach(), self.w, self.w_scale)
         if bias is not None:

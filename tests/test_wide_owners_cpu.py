@@ -25,3 +25,10 @@ def test_scales_of_another_length_are_refused(A, shape):
         w, w_scale = torch.empty((40, 30), dtype=torch.int8, device="cuda"), torch.empty(shape, device="cuda")
         with pytest.raises(ValueError, match="scales"):
             A.DenseInt8(w, w_scale)
+
+
+def test_scales_of_a_float_matrix_are_refused(A):
+    with FakeTensorMode():
+        w, w_scale = torch.empty((40, 30), device="cuda"), torch.empty(40, device="cuda")
+        with pytest.raises(ValueError, match="scales"):
+            A.DenseInt8(w, w_scale)
