@@ -1,6 +1,7 @@
 """Binding of include/accerl.h (ctypes; forwards, V-trace and the KL indicators through the compiled accerl_args): same names, argument marshalling only."""
 import ctypes as C
 import os
+import threading
 
 import numpy as np
 
@@ -544,16 +545,22 @@ def _logits(t):
 
 
 class _Workspaces:
-    """A buffer for each stream, allocated on it: calls on different streams do not share one, and a buffer that grows is given back in
-    the order of the stream that used it."""
+    """A buffer for each thread and stream, allocated on the stream: a call is several launches that meet in it, and another thread's may come
+    between them.  A buffer that grows is given back in the order of the stream that used it, and so are a thread's when it ends."""
 
     def __init__(self):
-        self.of = {}
+        self._own = threading.local()
+
+    def __reduce__(self):
+        return _Workspaces, ()                # a copy begins with none
+
+    def kept(self, stream, device):
+        return self._own.__dict__.get((device, stream))
 
     def get(self, nbytes, stream, device):
-        t = self.of.get((device, stream))
+        t = self.kept(stream, device)
         if t is None or t.numel() < nbytes:
-            t = self.of[device, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            t = self._own.__dict__[device, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return t
 
 
@@ -581,7 +588,8 @@ class _On:
 class DenseInt8:
     """Int8 dense layer with a scale for each token and channel: owner of packed weights, workspaces and outputs.
 
-    w: int8 [N, K] with w_scale [N], or a float matrix that is quantised here, a scale for each row; bias [N] or None.
+    w: int8 [N, K] with w_scale [N], or a float matrix that is quantised here, a scale for each row; bias [N] or None.  Threads and streams may
+    share a layer: each has a workspace of its own in it (accerl_dense_i8_workspace bytes, for as long as the thread and the layer live).
     """
 
     def __init__(self, w, w_scale=None, bias=None, relu=False):
@@ -598,7 +606,8 @@ class DenseInt8:
         self.update(w, w_scale)
 
     def update(self, w, w_scale=None, bias=None):
-        """New weights of the same shape (a learner's, after its step), and bias if given, on the current stream."""
+        """New weights of the same shape (a learner's, after its step), and bias if given, on the current stream.  Forwards of other streams or
+        threads that are not ordered with it may see some of both."""
         if tuple(w.shape) != (self.N, self.K) or (bias is not None and (self.bias is None or bias.shape != self.bias.shape)):
             raise ValueError("the weights or the bias differ in shape from the layer's")
         if w.dtype == torch.int8:
@@ -617,7 +626,7 @@ class DenseInt8:
         """x [M, K] -> [M, N] in `dtype` (x's own if None)."""
         if stream is None and out is None and x.is_cuda:
             raw = torch._C._cuda_getCurrentRawStream(x.device.index)
-            ws = self._work.of.get((x.device, raw))
+            ws = self._work.kept(raw, x.device)
             r = None if ws is None else (_args or _loaded()).dense_dynamic(x, self.N, self.K, self.w, self.w_scale, self.bias, self._relu, _CODES.get(dtype, 3),
                                                                            ws, raw)
             if r is not None:
@@ -641,7 +650,7 @@ class PolicyLoss:
     """Clipped policy loss with KL and entropy terms: owner of the coefficients, workspaces and outputs.
 
     forward returns the per-row outputs, the batch's sums and the gradient by the logits: `logits.backward(r.grad)` continues it into
-    whatever made the logits.
+    whatever made the logits.  Threads and streams may share one, as they may a DenseInt8.
     """
 
     class Result:

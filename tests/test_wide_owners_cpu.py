@@ -1,4 +1,8 @@
 """DenseInt8 and PolicyLoss without a GPU: what they refuse before anything is enqueued, on tensors that claim to lie on one."""
+import copy
+import pickle
+import threading
+
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -32,3 +36,31 @@ def test_scales_of_a_float_matrix_are_refused(A):
         w, w_scale = torch.empty((40, 30), device="cuda"), torch.empty(40, device="cuda")
         with pytest.raises(ValueError, match="scales"):
             A.DenseInt8(w, w_scale)
+
+
+def _in_thread(f):
+    out = []
+    t = threading.Thread(target=lambda: out.append(f()))
+    t.start()
+    t.join()
+    return out[0]
+
+
+def test_a_workspace_belongs_to_one_thread_and_stream(A):
+    """Calls of one thread on one stream share a buffer; a call of another thread may come between the launches of this one's."""
+    from paper_2211_15023_amd import binding
+    w, cpu = binding._Workspaces(), torch.device("cpu")
+    mine = w.get(100, 0, cpu)
+    assert w.get(64, 0, cpu) is mine and w.kept(0, cpu) is mine and w.get(101, 0, cpu) is not mine
+    mine = w.kept(0, cpu)
+    other = _in_thread(lambda: (w.kept(0, cpu), w.get(100, 0, cpu)))
+    assert other[0] is None and other[1].data_ptr() != mine.data_ptr()
+    assert w.get(100, 7, cpu).data_ptr() != mine.data_ptr() and w.kept(0, cpu) is mine
+
+
+def test_owners_are_copied_without_their_workspaces(A):
+    from paper_2211_15023_amd import binding
+    w, cpu = binding._Workspaces(), torch.device("cpu")
+    w.get(100, 0, cpu)
+    for c in (copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
+        assert c.kept(0, cpu) is None and w.kept(0, cpu) is not None
