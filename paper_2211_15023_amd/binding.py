@@ -544,9 +544,16 @@ def _logits(t):
     return t.detach()
 
 
+def _captured(stream):
+    """Whether what the current stream, this one, is given now goes into a graph (0.3 us; the default stream, 0, cannot be captured)."""
+    return stream != 0 and torch._C._cuda_isCurrentStreamCapturing()
+
+
 class _Workspaces:
     """A buffer for each thread and stream, allocated on the stream: a call is several launches that meet in it, and another thread's may come
-    between them.  A buffer that grows is given back in the order of the stream that used it, and so are a thread's when it ends."""
+    between them.  A buffer that grows is given back in the order of the stream that used it, and so are a thread's when it ends.  A call that
+    torch.cuda.graph captures gets one of the graph's own memory, as its outputs do: no other graph, no eager call and nothing that is allocated
+    later has it."""
 
     def __init__(self):
         self._own = threading.local()
@@ -555,12 +562,14 @@ class _Workspaces:
         return _Workspaces, ()                # a copy begins with none
 
     def kept(self, stream, device):
-        return self._own.__dict__.get((device, stream))
+        return None if _captured(stream) else self._own.__dict__.get((device, stream))
 
     def get(self, nbytes, stream, device):
         t = self.kept(stream, device)
         if t is None or t.numel() < nbytes:
-            t = self._own.__dict__[device, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            if not _captured(stream):
+                self._own.__dict__[device, stream] = t
         return t
 
 

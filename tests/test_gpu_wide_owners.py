@@ -85,3 +85,69 @@ def test_two_threads_share_a_loss(A, B, n):
     for i in range(2):
         for r in got[i]:
             assert torch.equal(r.stats, want[i].stats) and torch.equal(r.grad, want[i].grad), i
+
+
+def _replays(graphs, outs, want, rounds=4):
+    for _ in range(rounds):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+
+
+def test_a_layer_outgrows_what_a_graph_has_seen(A):
+    """Captured at 64 tokens on the user's stream, then called there with more, then memory of that stream is taken: the replays give the
+    captured call's results and leave that memory alone."""
+    layer = A.DenseInt8(torch.randn((300, 200), device="cuda"))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        x, many = torch.randn((64, 200), device="cuda"), torch.randn((4096, 200), device="cuda")
+        want = layer.forward(x)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = layer.forward(x)
+        layer.forward(many)
+        taken = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in (512, 2048, 16384, 16896, 20480, 65536) for _ in range(20)]
+        _replays([graph], [out], [want])
+        assert all(bool((t == 7).all()) for t in taken)
+        assert torch.equal(layer.forward(x), want)
+
+
+@pytest.mark.parametrize("side", ["layer", "loss"])
+def test_two_graphs_of_one_owner_replayed_at_once(A, side):
+    """Captured one after the other on torch's capture stream, replayed on two streams."""
+    if side == "layer":
+        layer = A.DenseInt8(torch.randn((1000, 500), device="cuda"))
+        x = [torch.randn((300, 500), device="cuda") * 10 ** i for i in range(2)]
+        call = lambda i: [layer.forward(x[i])]
+    else:
+        how, v = A.PolicyLoss(entropy_coef=0.1), torch.full((3,), -1.0, device="cuda")
+        x, act = [torch.randn((3, 60001), device="cuda") * (i + 1) for i in range(2)], torch.zeros(3, dtype=torch.int32, device="cuda")
+
+        def call(i):
+            r = how.forward(x[i], act, v, v)
+            return [r.grad, r.stats]
+    want = [call(i) for i in range(2)]
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], [None, None]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            outs[i] = call(i)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for i in range(2):
+            for o in outs[i]:
+                o.zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        call(0)                                                   # an eager call between them
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(o, w) for o, w in zip(outs[i], want[i])), i

@@ -38,6 +38,15 @@ def test_scales_of_a_float_matrix_are_refused(A):
             A.DenseInt8(w, w_scale)
 
 
+@pytest.fixture
+def capture(monkeypatch):
+    """Says whether the current stream captures: none does here."""
+    from paper_2211_15023_amd import binding
+    now = [False]
+    monkeypatch.setattr(binding, "_captured", lambda stream: now[0], raising=False)
+    return now
+
+
 def _in_thread(f):
     out = []
     t = threading.Thread(target=lambda: out.append(f()))
@@ -46,7 +55,7 @@ def _in_thread(f):
     return out[0]
 
 
-def test_a_workspace_belongs_to_one_thread_and_stream(A):
+def test_a_workspace_belongs_to_one_thread_and_stream(A, capture):
     """Calls of one thread on one stream share a buffer; a call of another thread may come between the launches of this one's."""
     from paper_2211_15023_amd import binding
     w, cpu = binding._Workspaces(), torch.device("cpu")
@@ -58,9 +67,21 @@ def test_a_workspace_belongs_to_one_thread_and_stream(A):
     assert w.get(100, 7, cpu).data_ptr() != mine.data_ptr() and w.kept(0, cpu) is mine
 
 
-def test_owners_are_copied_without_their_workspaces(A):
+def test_owners_are_copied_without_their_workspaces(A, capture):
     from paper_2211_15023_amd import binding
     w, cpu = binding._Workspaces(), torch.device("cpu")
     w.get(100, 0, cpu)
     for c in (copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
         assert c.kept(0, cpu) is None and w.kept(0, cpu) is not None
+
+
+def test_a_captured_call_has_a_workspace_of_its_own(A, capture):
+    """A graph keeps the address: no later call on its stream, captured or not, gets it from the owner, and none replaces it there."""
+    from paper_2211_15023_amd import binding
+    w, cpu = binding._Workspaces(), torch.device("cpu")
+    eager = w.get(100, 0, cpu)
+    capture[0] = True
+    captured = [w.get(100, 0, cpu) for _ in range(2)]
+    assert len({t.data_ptr() for t in (eager, *captured)}) == 3 and w.kept(0, cpu) is None
+    capture[0] = False
+    assert w.get(100, 0, cpu) is eager
