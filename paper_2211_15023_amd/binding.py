@@ -1,4 +1,5 @@
 """Binding of include/accerl.h (ctypes; forwards, V-trace and the KL indicators through the compiled accerl_args): same names, argument marshalling only."""
+import contextlib
 import ctypes as C
 import os
 import threading
@@ -392,6 +393,18 @@ def _dtype(t):
         raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}") from None
 
 
+_SAME = contextlib.nullcontext()
+
+
+def _device_of(*tensors):
+    """The device that all of them lie on (the first is no None), as a context: kernels are launched on the current one."""
+    at = tensors[0].get_device()                     # (-1 on the host)
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors of one call lie on different devices: {tensors[0].device} and {t.device}")
+    return _SAME if at < 0 or at == torch._C._cuda_getDevice() else torch.cuda.device(at)
+
+
 def _rows(t, what):
     """Pointer and row stride of a device matrix whose rows are contiguous."""
     if t is None:
@@ -434,8 +447,9 @@ def accerl_quantize_rows(x, out_packed, out_scale, stream=None):
     lib = load_library()
     p, ld = _rows(x, "x")
     R, K = x.shape
-    _check(lib.accerl_quantize_rows(p, _dtype(x), R, K, ld, _packed(out_packed, R, K, "out_packed"), _vector(out_scale, torch.float32, R, "out_scale"),
-                                    _stream(stream)))
+    with _device_of(x, out_packed, out_scale):
+        _check(lib.accerl_quantize_rows(p, _dtype(x), R, K, ld, _packed(out_packed, R, K, "out_packed"), _vector(out_scale, torch.float32, R, "out_scale"),
+                                        _stream(stream)))
 
 
 def accerl_pack_rows_i8(q, out_packed, stream=None):
@@ -444,7 +458,8 @@ def accerl_pack_rows_i8(q, out_packed, stream=None):
         raise ValueError(f"expected torch.int8, got {q.dtype}")
     p, ld = _rows(q, "q")
     R, K = q.shape
-    _check(lib.accerl_pack_rows_i8(p, R, K, ld, _packed(out_packed, R, K, "out_packed"), _stream(stream)))
+    with _device_of(q, out_packed):
+        _check(lib.accerl_pack_rows_i8(p, R, K, ld, _packed(out_packed, R, K, "out_packed"), _stream(stream)))
 
 
 def accerl_unpack_rows_i8(packed, out_q, stream=None):
@@ -453,7 +468,8 @@ def accerl_unpack_rows_i8(packed, out_q, stream=None):
         raise ValueError(f"expected torch.int8, got {out_q.dtype}")
     p, ld = _rows(out_q, "out_q")
     R, K = out_q.shape
-    _check(lib.accerl_unpack_rows_i8(_packed(packed, R, K, "packed"), R, K, p, ld, _stream(stream)))
+    with _device_of(packed, out_q):
+        _check(lib.accerl_unpack_rows_i8(_packed(packed, R, K, "packed"), R, K, p, ld, _stream(stream)))
 
 
 def accerl_dense_i8(x_packed, x_scale, w_packed, w_scale, bias, K, out, relu=False, stream=None):
@@ -461,9 +477,10 @@ def accerl_dense_i8(x_packed, x_scale, w_packed, w_scale, bias, K, out, relu=Fal
     lib = load_library()
     po, ld = _rows(out, "out")
     M, N = out.shape
-    _check(lib.accerl_dense_i8(_packed(x_packed, M, K, "x_packed"), _vector(x_scale, torch.float32, M, "x_scale"), _packed(w_packed, N, K, "w_packed"),
-                               _vector(w_scale, torch.float32, N, "w_scale"), _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)),
-                               po, _dtype(out), ld, _stream(stream)))
+    with _device_of(x_packed, x_scale, w_packed, w_scale, bias, out):
+        _check(lib.accerl_dense_i8(_packed(x_packed, M, K, "x_packed"), _vector(x_scale, torch.float32, M, "x_scale"), _packed(w_packed, N, K, "w_packed"),
+                                   _vector(w_scale, torch.float32, N, "w_scale"), _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)),
+                                   po, _dtype(out), ld, _stream(stream)))
 
 
 def accerl_dense_i8_workspace(M, K):
@@ -478,9 +495,10 @@ def accerl_dense_i8_dynamic(x, w_packed, w_scale, bias, out, workspace, relu=Fal
     (M, K), N = x.shape, out.shape[1]
     if out.shape[0] != M:
         raise ValueError("x and out differ in rows")
-    _check(lib.accerl_dense_i8_dynamic(px, _dtype(x), ldx, _packed(w_packed, N, K, "w_packed"), _vector(w_scale, torch.float32, N, "w_scale"),
-                                       _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)), po, _dtype(out), ld,
-                                       _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
+    with _device_of(x, w_packed, w_scale, bias, out, workspace):
+        _check(lib.accerl_dense_i8_dynamic(px, _dtype(x), ldx, _packed(w_packed, N, K, "w_packed"), _vector(w_scale, torch.float32, N, "w_scale"),
+                                           _vector(bias, torch.float32, N, "bias"), M, N, K, int(bool(relu)), po, _dtype(out), ld,
+                                           _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
 
 
 def accerl_policy_loss_workspace():
@@ -505,9 +523,10 @@ def accerl_action_logprob(logits, mask, actions, out_logp, out_entropy, workspac
     p, ld = _rows(logits, "logits")
     B, A = logits.shape
     pm, ldm = _mask_rows(mask, B, A)
-    _check(lib.accerl_action_logprob(p, _dtype(logits), ld, pm, ldm, _vector(actions, torch.int32, B, "actions"), B, A,
-                                     _vector(out_logp, torch.float32, B, "out_logp"), _vector(out_entropy, torch.float32, B, "out_entropy"),
-                                     _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
+    with _device_of(logits, mask, actions, out_logp, out_entropy, workspace):
+        _check(lib.accerl_action_logprob(p, _dtype(logits), ld, pm, ldm, _vector(actions, torch.int32, B, "actions"), B, A,
+                                         _vector(out_logp, torch.float32, B, "out_logp"), _vector(out_entropy, torch.float32, B, "out_entropy"),
+                                         _ptr(workspace, torch.uint8), workspace.numel(), _stream(stream)))
 
 
 def accerl_policy_loss(logits, actions, old_logp, advantages, workspace, mask=None, weights=None, kl="none", ref_logits=None, ref_logp=None,
@@ -532,7 +551,8 @@ def accerl_policy_loss(logits, actions, old_logp, advantages, workspace, mask=No
     a.out_stats = _vector(out_stats, torch.float32, 4, "out_stats")
     a.clip_low, a.clip_high, a.kl_coef, a.entropy_coef, a.scale = clip_low, clip_high, kl_coef, entropy_coef, scale
     a.workspace, a.workspace_bytes = _ptr(workspace, torch.uint8), workspace.numel()
-    _check(lib.accerl_policy_loss(C.byref(a), _stream(stream)))
+    with _device_of(logits, actions, old_logp, advantages, workspace, mask, weights, ref_logits, ref_logp, grad_logits, out_loss, out_logp, out_kl, out_entropy, out_stats):
+        _check(lib.accerl_policy_loss(C.byref(a), _stream(stream)))
 
 
 _CODES = {None: -1}         # output types of accerl_args, filled by load_library
@@ -561,27 +581,32 @@ class _Workspaces:
     def __reduce__(self):
         return _Workspaces, ()                # a copy begins with none
 
-    def kept(self, stream, device):
-        return None if _captured(stream) else self._own.__dict__.get((device, stream))
+    def kept(self, stream, index):
+        """What this thread has on a stream of the device of this index, or None."""
+        return self._own.__dict__.get((index, stream)) if stream == 0 or not _captured(stream) else None
 
     def get(self, nbytes, stream, device):
-        t = self.kept(stream, device)
+        t = self.kept(stream, device.index)
         if t is None or t.numel() < nbytes:
             t = torch.empty(nbytes, dtype=torch.uint8, device=device)
             if not _captured(stream):
-                self._own.__dict__[device, stream] = t
+                self._own.__dict__[device.index, stream] = t
         return t
 
 
 class _On:
-    """The stream that a call runs on: what is allocated inside belongs to it."""
+    """The stream that a call runs on, and its device: what is allocated inside belongs to it."""
 
     def __init__(self, stream, device):
         self.other = None
         if stream is None:
             self.raw = torch._C._cuda_getCurrentRawStream(device.index)
+            if device.index != torch._C._cuda_getDevice():
+                self.other = torch.cuda.device(device)
         else:
             s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
+            if s.device != device:
+                raise ValueError(f"the stream is one of {s.device}, the tensors lie on {device}")
             self.raw, self.other = s.cuda_stream, torch.cuda.stream(s)
 
     def __enter__(self):
@@ -634,8 +659,9 @@ class DenseInt8:
     def forward(self, x, dtype=None, out=None, stream=None):
         """x [M, K] -> [M, N] in `dtype` (x's own if None)."""
         if stream is None and out is None and x.is_cuda:
-            raw = torch._C._cuda_getCurrentRawStream(x.device.index)
-            ws = self._work.kept(raw, x.device)
+            at = x.get_device()
+            raw = torch._C._cuda_getCurrentRawStream(at)
+            ws = self._work.kept(raw, at)
             r = None if ws is None else (_args or _loaded()).dense_dynamic(x, self.N, self.K, self.w, self.w_scale, self.bias, self._relu, _CODES.get(dtype, 3),
                                                                            ws, raw)
             if r is not None:
@@ -677,9 +703,12 @@ class PolicyLoss:
         """scale: None for the mean over all rows; grad: a table to write the gradient to (the logits themselves too), True for a new one,
         False for the value only."""
         if stream is None and (grad is True or grad is False) and logits.is_cuda:
-            raw = torch._C._cuda_getCurrentRawStream(logits.device.index)
+            at = logits.get_device()
+            raw = torch._C._cuda_getCurrentRawStream(at)
+            ws = self._work.kept(raw, at)
             t = (_args or _loaded()).policy_loss(logits, actions, old_logp, advantages, mask, weights, ref_logits, ref_logp, int(grad), *self._how,
-                                                 1.0 / max(1, logits.shape[0]) if scale is None else float(scale), self._work.get(self._bytes, raw, logits.device), raw)
+                                                 1.0 / max(1, logits.shape[0]) if scale is None else float(scale),
+                                                 self._work.get(self._bytes, raw, logits.device) if ws is None else ws, raw)
             if t is not None:
                 if t[0]:
                     _check(t[0])
@@ -703,8 +732,10 @@ class PolicyLoss:
     def logprob(self, logits, actions, mask=None, stream=None):
         """log pi(a) and entropy, each [B]."""
         if stream is None and logits.is_cuda:
-            raw = torch._C._cuda_getCurrentRawStream(logits.device.index)
-            t = (_args or _loaded()).action_logprob(logits, actions, mask, self._work.get(self._bytes, raw, logits.device), raw)
+            at = logits.get_device()
+            raw = torch._C._cuda_getCurrentRawStream(at)
+            ws = self._work.kept(raw, at)
+            t = (_args or _loaded()).action_logprob(logits, actions, mask, self._work.get(self._bytes, raw, logits.device) if ws is None else ws, raw)
             if t is not None:
                 if t[0]:
                     _check(t[0])

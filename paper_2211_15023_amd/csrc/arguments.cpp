@@ -12,6 +12,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -28,14 +29,17 @@ PyObject* value_name = nullptr;
 struct Args {
     PyObject* const* at;
     bool plain;
+    int device;                               // where all tensors lie; negative: anywhere
 
-    explicit Args(PyObject* const* a) : at(a), plain(!at::impl::torch_function_mode_enabled()) {}
+    explicit Args(PyObject* const* a, int device = -1) : at(a), plain(!at::impl::torch_function_mode_enabled()), device(device) {}
+
+    bool here(const at::Tensor& t) const { return t.is_cuda() && (device < 0 || t.device().index() == device); }
 
     const at::Tensor* tensor() {
         PyObject* o = *at++;
         if (!plain || Py_TYPE(o) != (PyTypeObject*)THPVariableClass) { plain = false; return nullptr; }
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || !t.is_contiguous()) plain = false;
+        if (!here(t) || !t.is_contiguous()) plain = false;
         return &t;
     }
     void* pointer(c10::ScalarType type) {
@@ -72,7 +76,7 @@ struct Args {
         PyObject* o = *at++;
         if (!plain || Py_TYPE(o) != (PyTypeObject*)THPVariableClass) { plain = false; return nullptr; }
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || t.dim() != 2 || (*type != c10::ScalarType::Undefined && t.scalar_type() != *type) || (*B >= 0 && t.size(0) != *B) ||
+        if (!here(t) || t.dim() != 2 || (*type != c10::ScalarType::Undefined && t.scalar_type() != *type) || (*B >= 0 && t.size(0) != *B) ||
             (*A >= 0 && t.size(1) != *A)) { plain = false; return nullptr; }
         *type = t.scalar_type();
         *B = t.size(0);
@@ -204,12 +208,13 @@ constexpr c10::ScalarType CODES[3] = {c10::kFloat, c10::kBFloat16, c10::kHalf};
 
 at::Tensor made(c10::IntArrayRef shape, c10::ScalarType type) { return at::empty(shape, c10::TensorOptions(c10::kCUDA).dtype(type)); }
 
-// Like call(), for functions that make their outputs: parse(args, outputs) reads the arguments, appends the outputs and returns the call.
+// Like call(), for functions that make their outputs: parse(args, outputs) reads the arguments, appends the outputs and returns the call.  Outputs are made
+// on the current device, where the call's tensors must lie.
 template <class Parse>
 PyObject* call_out(PyObject* const* argv, Py_ssize_t given, Py_ssize_t count, Parse&& parse) {
     if (given != count) { PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", count, given); return nullptr; }
     try {
-        Args a(argv);
+        Args a(argv, c10::hip::current_device());
         std::vector<at::Tensor> outs;
         auto run = parse(a, outs);
         if (PyErr_Occurred()) { PyErr_Clear(); a.plain = false; }

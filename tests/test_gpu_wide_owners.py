@@ -151,3 +151,21 @@ def test_two_graphs_of_one_owner_replayed_at_once(A, side):
         torch.cuda.synchronize()
         for i in range(2):
             assert all(torch.equal(o, w) for o, w in zip(outs[i], want[i])), i
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_outputs_lie_where_the_inputs_do(A):
+    """Inputs of the device that is not the current one: outputs, workspaces and launches are that device's, in every call."""
+    layer = A.DenseInt8(torch.randn((40, 30), device="cuda:1"), bias=torch.randn(40, device="cuda:1"))
+    how = A.PolicyLoss()
+    x, act, v = torch.randn((4, 30), device="cuda:1"), torch.zeros(4, dtype=torch.int32, device="cuda:1"), torch.zeros(4, device="cuda:1")
+    with torch.cuda.device(1):
+        want = layer.forward(x)
+        loss = how.forward(want, act, v, v)
+        torch.cuda.synchronize()
+    for _ in range(3):
+        y = layer.forward(x)
+        r, lp = how.forward(y, act, v, v), how.logprob(y, act)
+        torch.cuda.synchronize(1)
+        assert all(t.device == x.device for t in (y, r.loss, r.grad, r.stats, *lp))
+        assert torch.equal(y, want) and torch.equal(r.grad, loss.grad) and torch.equal(lp[0], loss.logp)
