@@ -326,7 +326,7 @@ int accerl_unpack_rows_i8(const int8_t* packed, int64_t rows, int64_t cols, int8
  * Int8 dense layer with a scale for each token and each channel:
  *     acc[m,n] = sum_k x[m,k] w[n,k] (exact int32),    y = ((float)acc * x_scale[m]) * w_scale[n] + bias[n],    ReLU if relu != 0
  * rounded once to out_dtype.  x_packed [M, K] and w_packed [N, K] packed rows; x_scale, w_scale, bias (NULL: none) DEVICE fp32; out
- * DEVICE [M, N].  M == 0 or N == 0 enqueues nothing.  Allocates nothing, does not synchronise.
+ * DEVICE [M, N], overlapping none of them (ACCERL_EINVAL).  M == 0 or N == 0 enqueues nothing.  Allocates nothing, does not synchronise.
  */
 int accerl_dense_i8(const int8_t* x_packed, const float* x_scale, const int8_t* w_packed, const float* w_scale, const float* bias,
                     int64_t M, int64_t N, int64_t K, int32_t relu, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
@@ -334,7 +334,8 @@ int accerl_dense_i8(const int8_t* x_packed, const float* x_scale, const int8_t* 
 /*
  * The same layer on floating-point tokens, quantised as accerl_quantize_rows does (same results as the two calls).
  * workspace: DEVICE, 16-byte aligned, at least accerl_dense_i8_workspace(M, K) bytes, used until the work has finished: calls that
- * may overlap need a workspace each.  Its contents need not be kept or cleared.
+ * may overlap need a workspace each.  Its contents need not be kept or cleared.  out may lie over x, whose tokens are quantised before it is
+ * written, and over nothing else; the workspace over neither (ACCERL_EINVAL).
  */
 int64_t accerl_dense_i8_workspace(int64_t M, int64_t K);
 int accerl_dense_i8_dynamic(const void* x, int32_t x_dtype, int64_t ld_x, const int8_t* w_packed, const float* w_scale, const float* bias,

@@ -579,6 +579,8 @@ int di_launched(const char* who) {
 }
 bool di_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+int64_t packed_bytes(int64_t rows, int64_t cols) { return (rows + 15) / 16 * di_steps(cols) * 1024; }
+
 const char* di_sizes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1) return "need rows >= 0 and at least one column";
     return nullptr;
@@ -673,6 +675,9 @@ int check_product(const char* who, const int8_t* w, const float* w_scale, const 
     if (!w || !w_scale || !out) return di_fail(ACCERL_EINVAL, who, "NULL argument (only bias may be NULL)");
     if (!di_aligned(w, 16)) return di_fail(ACCERL_EINVAL, who, "packed rows must be 16-byte aligned");
     if (!di_aligned(w_scale, 4) || !di_aligned(bias, 4) || !di_aligned(out, dtype_bytes(out_dtype))) return di_fail(ACCERL_EINVAL, who, "misaligned argument");
+    const Table to = table(out, M, ld_out, N, dtype_bytes(out_dtype));
+    if (share(to, table(w, packed_bytes(N, K))) || share(to, table(w_scale, N * 4)) || share(to, table(bias, N * 4)))
+        return di_fail(ACCERL_EINVAL, who, "the output overlaps the layer's weights, scales or bias");
     return ACCERL_OK;
 }
 DenseParams dense_params(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale, const float* bias, int64_t M, int64_t N, int64_t K,
@@ -684,7 +689,6 @@ DenseParams dense_params(const int8_t* x, const float* x_scale, const int8_t* w,
     p.dtype = out_dtype; p.relu = relu != 0;
     return p;
 }
-int64_t packed_bytes(int64_t rows, int64_t cols) { return (rows + 15) / 16 * di_steps(cols) * 1024; }
 }  // namespace
 }  // namespace accerl
 
@@ -746,6 +750,8 @@ int accerl_dense_i8(const int8_t* x_packed, const float* x_scale, const int8_t* 
     if (done) return ACCERL_OK;
     if (!x_packed || !x_scale) return di_fail(ACCERL_EINVAL, who, "NULL argument (only bias may be NULL)");
     if (!di_aligned(x_packed, 16) || !di_aligned(x_scale, 4)) return di_fail(ACCERL_EINVAL, who, "misaligned argument");
+    const Table to = table(out, M, ld_out, N, dtype_bytes(out_dtype));
+    if (share(to, table(x_packed, packed_bytes(M, K))) || share(to, table(x_scale, M * 4))) return di_fail(ACCERL_EINVAL, who, "the output overlaps the tokens or their scales");
     return product(who, dense_params(x_packed, x_scale, w_packed, w_scale, bias, M, N, K, relu, out, out_dtype, ld_out), (hipStream_t)stream);
 }
 
@@ -770,7 +776,11 @@ int accerl_dense_i8_dynamic(const void* x, int32_t x_dtype, int64_t ld_x, const 
     if (!x || !workspace) return di_fail(ACCERL_EINVAL, who, "NULL argument (only bias may be NULL)");
     if (!di_aligned(x, dtype_bytes(x_dtype)) || !di_aligned(workspace, 16)) return di_fail(ACCERL_EINVAL, who, "misaligned argument");
     if (workspace_bytes < accerl_dense_i8_workspace(M, K)) return di_fail(ACCERL_EINVAL, who, "workspace smaller than accerl_dense_i8_workspace says");
-    if (tokens_fit(M, K)) {
+    const int64_t used = accerl_dense_i8_workspace(M, K);
+    const Table from = table(x, M, ld_x, K, dtype_bytes(x_dtype)), to = table(out, M, ld_out, N, dtype_bytes(out_dtype));
+    if (share(table(workspace, used), from) || share(table(workspace, used), to)) return di_fail(ACCERL_EINVAL, who, "the workspace overlaps the input or the output");
+    // (every workgroup of the one launch reads the tokens: where the output lies over them they are quantised first)
+    if (tokens_fit(M, K) && !share(from, to)) {
         const DenseParams p = dense_params(nullptr, nullptr, w_packed, w_scale, bias, M, N, K, relu, out, out_dtype, ld_out);
         if (x_dtype == ACCERL_DT_F32) return tokens(who, (const float*)x, ld_x, K, p, (hipStream_t)stream);
         return x_dtype == ACCERL_DT_BF16 ? tokens(who, (const BF16*)x, ld_x, K, p, (hipStream_t)stream) : tokens(who, (const F16*)x, ld_x, K, p, (hipStream_t)stream);

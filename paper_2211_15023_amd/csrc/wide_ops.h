@@ -1,6 +1,7 @@
 // What the operators of wide policies share: element types and their conversions, loads of any alignment.
 #pragma once
 #include "accerl_internal.h"
+#include "tables.h"
 
 namespace accerl {
 

@@ -169,3 +169,28 @@ def test_outputs_lie_where_the_inputs_do(A):
         torch.cuda.synchronize(1)
         assert all(t.device == x.device for t in (y, r.loss, r.grad, r.stats, *lp))
         assert torch.equal(y, want) and torch.equal(r.grad, loss.grad) and torch.equal(lp[0], loss.logp)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 200])
+@pytest.mark.parametrize("shift", [0, 1, -3])
+def test_a_layer_writes_over_its_input(A, M, shift):
+    """Whole, and shifted by some elements: all tokens are read before a result is written."""
+    n = 900
+    layer = A.DenseInt8(torch.randn((n, n), device="cuda"), bias=torch.randn(n, device="cuda"))
+    table = torch.randn(M * n + 16, device="cuda")
+    x, out = (table[8 + s:8 + s + M * n].view(M, n) for s in (0, shift))
+    want = layer.forward(x.clone())
+    assert layer.forward(x, out=out) is out
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("M", [2, 40])
+def test_a_layer_writes_beside_its_input(A, M):
+    """Input and output are columns of one table: rows that lie between each other's, which share nothing."""
+    layer = A.DenseInt8(torch.randn((300, 500), device="cuda"))
+    table = torch.randn((M, 1000), device="cuda")
+    x, out = table[:, 100:600], table[:, 600:900]
+    rest, want = table.clone(), layer.forward(x.contiguous())
+    layer.forward(x, out=out)
+    rest[:, 600:900] = want
+    assert torch.equal(table, rest)
