@@ -1009,9 +1009,6 @@ void table_params(LossParams& p, int64_t B, int64_t A, const void* z, int64_t ld
     p.rec = (Record*)workspace;
     p.part = (Part*)((char*)workspace + PL_RECORDS * sizeof(Record));
 }
-bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
-}
 }  // namespace
 }  // namespace accerl
 
@@ -1050,17 +1047,17 @@ int accerl_policy_loss(const accerl_policy_loss_args* a, void* stream) {
     if (done) return ACCERL_OK;
     if (!a->old_logp || !a->advantages || (ref && !a->ref_logits) || (a->kl_kind == ACCERL_KL_SAMPLED && !a->ref_logp))
         return pl_fail(ACCERL_EINVAL, who, "NULL input");
-    const uintptr_t es = dtype_bytes(a->dtype);
+    const int es = dtype_bytes(a->dtype);
     if (!pl_aligned(a->old_logp, 4) || !pl_aligned(a->advantages, 4) || !pl_aligned(a->weights, 4) || !pl_aligned(a->ref_logp, 4) ||
         !pl_aligned(a->out_loss, 4) || !pl_aligned(a->out_logp, 4) || !pl_aligned(a->out_kl, 4) || !pl_aligned(a->out_entropy, 4) ||
         !pl_aligned(a->out_stats, 4) || !pl_aligned(a->grad_logits, es) || (ref && !pl_aligned(a->ref_logits, es)))
         return pl_fail(ACCERL_EINVAL, who, "misaligned argument");
     if (a->grad_logits) {
-        const int64_t n = ((a->B - 1) * a->ld_grad + a->A) * (int64_t)es, nz = ((a->B - 1) * a->ld_logits + a->A) * (int64_t)es;
+        const Table g = table(a->grad_logits, a->B, a->ld_grad, a->A, es);
         const bool in_place = a->grad_logits == a->logits && a->ld_grad == a->ld_logits;
-        if (!in_place && overlap(a->grad_logits, n, a->logits, nz)) return pl_fail(ACCERL_EINVAL, who, "the gradient overlaps the logits and is not the same table");
-        if (ref && overlap(a->grad_logits, n, a->ref_logits, ((a->B - 1) * a->ld_ref + a->A) * (int64_t)es))
-            return pl_fail(ACCERL_EINVAL, who, "the gradient overlaps the reference's logits");
+        if (!in_place && share(g, table(a->logits, a->B, a->ld_logits, a->A, es)))
+            return pl_fail(ACCERL_EINVAL, who, "the gradient overlaps the logits and is not the same table");
+        if (ref && share(g, table(a->ref_logits, a->B, a->ld_ref, a->A, es))) return pl_fail(ACCERL_EINVAL, who, "the gradient overlaps the reference's logits");
     }
     LossParams p{};
     table_params(p, a->B, a->A, a->logits, a->ld_logits, a->mask, a->ld_mask, a->actions, a->workspace);

@@ -194,3 +194,17 @@ def test_a_layer_writes_beside_its_input(A, M):
     layer.forward(x, out=out)
     rest[:, 600:900] = want
     assert torch.equal(table, rest)
+
+
+@pytest.mark.parametrize("B,n", [(50, 18), (300, 130), (520, 5003), (3, 60001)])
+def test_a_gradient_beside_the_logits(A, B, n):
+    """Logits, the reference's and the gradient are columns of one table."""
+    how = A.PolicyLoss(kl="forward", kl_coef=0.1, entropy_coef=0.1)
+    table = torch.randn((B, 3 * n), device="cuda")
+    z, zr, g = table[:, n:2 * n], table[:, 2 * n:], table[:, :n]
+    act, v = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.full((B,), -1.0, device="cuda")
+    want = how.forward(z.contiguous(), act, v, v, ref_logits=zr.contiguous())
+    rest = table.clone()
+    got = how.forward(z, act, v, v, ref_logits=zr, grad=g)
+    rest[:, :n] = want.grad
+    assert torch.equal(table, rest) and torch.equal(got.stats, want.stats) and torch.equal(got.loss, want.loss)
