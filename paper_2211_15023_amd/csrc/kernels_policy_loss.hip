@@ -176,6 +176,8 @@ __device__ __forceinline__ float exp_rest(float d) {
     return d == INFINITY ? d : expf(d) - d - 1.0f;
 }
 __device__ __forceinline__ double exp_rest(double d) { return d == INFINITY ? d : exp(d) - d - 1.0; }
+// its slope, exp(d) - 1: from 1/2 on not from the value, whose d takes the 1's digits (at -1e8 all of them) and whose -inf leaves no number
+template <typename R> __device__ __forceinline__ R exp_slope(R d, R rest) { return fabs(d) < (R)0.5 ? rest + d : pl_exp(d) - (R)1; }
 // log pi(a) in 64 bits from a row's 32-bit sum: what is subtracted from a reference's log-probability must not be rounded where that is.
 // A function that is called, for its registers.
 __device__ __attribute__((noinline)) double exact_logp(float za, float c, bool far, float s) {
@@ -217,7 +219,7 @@ __device__ __forceinline__ void row_finish(const LossParams& p, const Sums<R>& q
     if constexpr (KL == 0) {
         if (p.kind == ACCERL_KL_SAMPLED) {
             kl = exp_rest(away);
-            if (ck != (R)0) at -= ck * (kl + away);                // 1 - exp(d)
+            if (ck != (R)0) at -= ck * exp_slope(away, kl);
         }
     } else {
         const bool none = q.sr == (R)0;

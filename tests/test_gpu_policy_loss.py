@@ -446,3 +446,22 @@ def test_loss_small_sampled_kl(A, B, n, apart):
     tol = np.expm1(d) * (16 * ref.U + 4 * ref.U * np.sqrt(n / 64 + 32)) + 16 * ref.U * r["kl"]
     off = np.abs(as64(got.kl) - r["kl"])
     assert (off <= tol).all(), np.max(off / tol)
+
+
+@pytest.mark.parametrize("B,n", [(9, 18), (9, 400), (300, 5003), (3, 60001)])
+@pytest.mark.parametrize("far", [float("-inf"), -1e9, -3e5])
+def test_loss_sampled_kl_of_an_action_the_reference_forbids(A, B, n, far):
+    """A reference's log-probability of -inf (which logprob gives for an action that its mask forbids), or far down: the KL is infinite or large, its slope
+    1 - exp(d) is 1, and the gradient is a number."""
+    x = Inputs(B, n, "f32", "sampled", "none", seed=91)
+    x.w[:] = 1.0
+    x.ref_lp[:] = far
+    got = x.run(A)
+    r, _ = x.want()
+    live = (x.act.numpy() >= 0) & (x.act.numpy() < n)
+    assert np.array_equal(np.isinf(as64(got.kl)), np.isinf(r["kl"])) and np.array_equal(np.isinf(as64(got.loss)), np.isinf(r["loss"]))
+    assert np.isfinite(r["grad"]).all() and live.any()
+    # a slope that does not depend on the sums: the tolerance is the one of a KL of 0
+    t = ref.tolerances(dict(r, kl=np.zeros(B), loss=np.zeros(B)), as64(x.z), None, "f32", "sampled", as64(x.adv), x.ck, x.ch, x.scale)
+    off = np.abs(as64(got.grad) - r["grad"])
+    assert (off <= t["grad"]).all(), np.nanmax(off / t["grad"])
