@@ -159,6 +159,13 @@ __device__ __forceinline__ RowIn row_in(const LossParams& p, int64_t row) {
     return r;
 }
 __device__ __forceinline__ bool row_dead(const LossParams& p, const RowIn& r) { return r.act < 0 || r.act >= p.A || r.w == 0.0f; }
+// Next to a clipping border the side decides over a row's whole gradient: there the ratio is worked out in 64 bits.  "Next" is what the ratio
+// may be off by, relative: half a step of 32 bits for each of the n terms that a lane adds up, 64 for terms, joins and logarithm, and for the
+// roundings of log pi(a) four of its own steps.  (Near a border old is log pi(a) but for a fraction.)
+__device__ __forceinline__ bool near_border(const LossParams& p, float lp, float old, int n) {
+    const float r = expf(lp - old), by = 0x1p-24f * (64.0f + 0.5f * (float)n + 4.0f * fabsf(lp)) * r;
+    return fabsf(r - (float)p.hi) < by || fabsf(r - (float)p.lo) < by;
+}
 // A row's sums on their way to its scalars, in R.  kl: the KL where it was worked out more exactly (see loss_rows_kernel), negative: not known.
 template <typename R> struct Sums { float m, mr; R s, u, sr, t, kl; };
 
@@ -532,10 +539,9 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         double ratio;
         const double* better = nullptr;
         if (!p.only_lp && q.s > 0.0f) {
-            // Next to a clipping border the side decides over the whole gradient: there the sum is taken again in 64 bits.  (All lanes of
-            // a row branch alike; the 32-bit ratio is off by a few parts in 2^24.)
-            const float r = expf((za - q.m) - logf(q.s) - in.old);
-            if (fabsf(r - (float)p.hi) < 4e-6f * r || fabsf(r - (float)p.lo) < 4e-6f * r) {
+            // (all lanes of a row branch alike)
+            const float lp = (float)PL_LN2 * (power<false>(base<false>(q.m), za) - pl_log2(q.s));
+            if (near_border(p, lp, in.old, H * VEC)) {
                 ratio = exact_ratio<T>(z, mask, p.A, j, G, VEC, q.m, za, in.old);
                 better = &ratio;
             }

@@ -465,3 +465,27 @@ def test_loss_sampled_kl_of_an_action_the_reference_forbids(A, B, n, far):
     t = ref.tolerances(dict(r, kl=np.zeros(B), loss=np.zeros(B)), as64(x.z), None, "f32", "sampled", as64(x.adv), x.ck, x.ch, x.scale)
     off = np.abs(as64(got.grad) - r["grad"])
     assert (off <= t["grad"]).all(), np.nanmax(off / t["grad"])
+
+
+def _at_the_border(x):
+    """Ratios within a few parts in 2^24 of a border, on both sides of it, for advantages of both signs."""
+    B, n = len(x.act), x.z.shape[1]
+    lp = ref.softmax_rows(as64(x.z), np.ones((B, n), bool))[0][np.arange(B), x.act.numpy()]
+    border = np.where(np.arange(B) % 2 == 0, np.log(1.25), np.log(0.8))
+    x.adv = torch.from_numpy(np.where(np.arange(B) % 4 < 2, 1.0, -1.0)).float()
+    x.old = torch.from_numpy(lp - border).float()
+
+
+@pytest.mark.parametrize("B,n", [(2000, 18), (2000, 400), (500, 2000)])
+@pytest.mark.parametrize("kl", ["none", "forward"])
+@pytest.mark.parametrize("down,up", [(0, 0), (40, 0), (85, 0), (3, 1000), (40, 20000)])
+def test_loss_next_to_the_clipping_border_of_improbable_actions(A, B, n, kl, down, up):
+    """What 32 bits leave of log pi(a) grows with it; where the logits lie makes no difference."""
+    x = Inputs(B, n, "f32", kl, "none", seed=52)
+    x.w[:] = 1.0
+    x.act = torch.randint(0, n, (B,), dtype=torch.int32, generator=torch.Generator().manual_seed(1))
+    x.z[torch.arange(B, device="cuda"), x.act.cuda().long()] -= down
+    x.z += up
+    x.zr += up
+    _at_the_border(x)
+    x.check(x.run(A))
