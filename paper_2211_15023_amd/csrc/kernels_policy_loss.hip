@@ -44,6 +44,7 @@ struct LossParams {
     int only_lp;             // log-probabilities and entropies only
     int splits, chunk;       // pieces of a row, elements of a piece
     double lo, hi;           // the clipping borders themselves
+    float log_lo, log_hi;    // their logarithms
     float ck, ch, scale;
     float* stats;            // out_stats where one workgroup does the pass (rec is then only a flag)
 };
@@ -159,12 +160,12 @@ __device__ __forceinline__ RowIn row_in(const LossParams& p, int64_t row) {
     return r;
 }
 __device__ __forceinline__ bool row_dead(const LossParams& p, const RowIn& r) { return r.act < 0 || r.act >= p.A || r.w == 0.0f; }
-// Next to a clipping border the side decides over a row's whole gradient: there the ratio is worked out in 64 bits.  "Next" is what the ratio
-// may be off by, relative: half a step of 32 bits for each of the n terms that a lane adds up, 64 for terms, joins and logarithm, and for the
-// roundings of log pi(a) four of its own steps.  (Near a border old is log pi(a) but for a fraction.)
-__device__ __forceinline__ bool near_border(const LossParams& p, float lp, float old, int n) {
-    const float r = expf(lp - old), by = 0x1p-24f * (64.0f + 0.5f * (float)n + 4.0f * fabsf(lp)) * r;
-    return fabsf(r - (float)p.hi) < by || fabsf(r - (float)p.lo) < by;
+// Next to a clipping border the side decides over a row's whole gradient: there the ratio is worked out in 64 bits.  "Next" is what 32 bits may
+// be off by, which is relative for the ratio and absolute for its logarithm.  In half steps of 32 bits: `terms` for the sum (a few dozen for its powers and
+// joins, and up to a half for each term that a lane adds up), `steps` of |log pi(a)| for its own roundings.
+__device__ __forceinline__ bool near_border(const LossParams& p, float lp, float old, float terms, float steps) {
+    const float r = lp - old, by = 0x1p-24f * fmaf(steps, fabsf(lp), terms);
+    return fabsf(r - p.log_hi) < by || fabsf(r - p.log_lo) < by;
 }
 // A row's sums on their way to its scalars, in R.  kl: the KL where it was worked out more exactly (see loss_rows_kernel), negative: not known.
 template <typename R> struct Sums { float m, mr; R s, u, sr, t, kl; };
@@ -541,7 +542,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         if (!p.only_lp && q.s > 0.0f) {
             // (all lanes of a row branch alike)
             const float lp = (float)PL_LN2 * (power<false>(base<false>(q.m), za) - pl_log2(q.s));
-            if (near_border(p, lp, in.old, H * VEC)) {
+            if (near_border(p, lp, in.old, 64.0f + 0.5f * H * VEC, 4.0f)) {
                 ratio = exact_ratio<T>(z, mask, p.A, j, G, VEC, q.m, za, in.old);
                 better = &ratio;
             }
@@ -653,8 +654,11 @@ struct WideShared {
     Coef coef;
     RowOut out;
     int waves;
+    float m;                 // the row's maximum
+    double exact[WR_WAVES];
 };
-template <int KL>
+// EXACT: with the ratio of the sum in `exact`.
+template <int KL, bool EXACT>
 __device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain, RowIn in, float za) {
     Sums<double> r = {-FLT_MAX, -FLT_MAX, 0.0, 0.0, 0.0, 0.0, -1.0};
     for (int k = 0; k < w->waves; ++k) { r.m = fmaxf(r.m, w->sum[k].m); r.mr = fmaxf(r.mr, w->sum[k].mr); }
@@ -669,16 +673,48 @@ __device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain,
     }
     Coef c;
     RowOut o;
-    row_finish<KL, double>(w->p, r, plain, in, za, nullptr, c, o);
+    double ratio = 0.0;
+    if constexpr (EXACT) {
+        for (int k = 0; k < w->waves; ++k) ratio += w->exact[k];
+        ratio = exp((double)za - (double)r.m - log(ratio) - (double)in.old);
+    }
+    row_finish<KL, double>(w->p, r, plain, in, za, EXACT ? &ratio : nullptr, c, o);
     if (plain && !row_held<KL>(r)) c.plain = -1;                  // to be done again
-    if (threadIdx.x == 0) { w->coef = c; w->out = o; }
+    if (threadIdx.x == 0) { w->coef = c; w->out = o; w->m = r.m; }
+}
+// The row's sum in 64 bits, from memory, by the whole workgroup: the wavefronts' parts go to `w->exact`.  A function that is called, like the one
+// above; eight elements a lane are on their way while eight are summed (one after the other a row of 50000 took 150 us).
+template <int THREADS, typename T>
+__device__ __attribute__((noinline)) void exact_sum(WideShared* w, const T* z, const uint8_t* mask) {
+    const int A = w->p.A;
+    const double m = w->m;
+    double s = 0.0;
+    float v[8], next[8];
+    const auto load = [&](float (&d)[8], int i) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[k] = el_f32(z[min(i + k * THREADS, A - 1)]);
+        if (mask) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) if (!mask[min(i + k * THREADS, A - 1)]) d[k] = -INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (i + k * THREADS >= A) d[k] = -INFINITY;
+    };
+    load(v, threadIdx.x);
+    for (int i = threadIdx.x; i < A; i += 8 * THREADS) {
+        load(next, i + 8 * THREADS);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { s += exp((double)v[k] - m); v[k] = next[k]; }
+    }
+    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+    if ((threadIdx.x & 63) == 0) w->exact[threadIdx.x >> 6] = s;
 }
 // The row's coefficients, to everybody, and its outputs, to thread 0 (`w.out`).
 template <int KL, bool PLAIN>
 __device__ __forceinline__ Coef wide_coef(WideShared& w, const RowSum& q, const RowIn& in, float za) {
     if ((threadIdx.x & 63) == 0) w.sum[threadIdx.x >> 6] = q;
     __syncthreads();
-    if (threadIdx.x < 64) wide_finish<KL>(&w, PLAIN, in, za);
+    if (threadIdx.x < 64) wide_finish<KL, false>(&w, PLAIN, in, za);
     __syncthreads();
     return w.coef;
 }
@@ -769,52 +805,73 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         if (H <= 4 && !p.g) wide_stream<T, KL, THREADS, U, true, true>(z, zr, mask, HELD, p.A, take);
         else wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, take);
         Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), in, za);
+        const auto put = [&] {
+            if (tid == 0) {
+                row_store(p, row, w.out);
+                if (p.rec) rec_add(rec, in.w, w.out);
+            }
+        };
+        // (terms of one size round the same way within one power of two only, so that a quarter of a half step each is as far as their sum goes)
+        const auto near = [&] { return !p.only_lp && near_border(p, w.out.lp, in.old, 24.0f + 0.25f / THREADS * (float)p.A, 2.0f); };
+        const auto exact = [&] {
+            exact_sum<THREADS>(&w, z, mask);
+            __syncthreads();
+            if (threadIdx.x < 64) wide_finish<KL, true>(&w, c.plain, in, za);
+            __syncthreads();
+            c = w.coef;
+        };
+        const auto grads = [&](auto mode, auto n, int first) {
+            constexpr int N = decltype(n)::value;
+            constexpr bool PLAIN = decltype(mode)::value;
+            wide_stream<T, KL, THREADS, N, PLAIN>(z, zr, mask, first, p.A, [&](auto full, const auto& x, const auto& y, int i) {
+#pragma unroll
+                for (int u = 0; u < (int)(sizeof(x) / sizeof(x[0])); ++u)
+                    if (decltype(full)::value || i + u * THREADS * VEC < p.A)
+                        vec_grad<decltype(full)::value, KL, PLAIN>(c, act, x[u], y[u], g, i + u * THREADS * VEC, p.A);
+            });
+        };
         if (c.plain < 0) {                                          // (everybody)
             q = row_empty();
             wide_stream<T, KL, THREADS, 1, false>(z, zr, mask, 0, p.A, [&](auto, const auto& x, const auto& y, int) { sum_vecs<KL, sizeof(x) / sizeof(x[0]), false>(q, x, y, 0); });
             q = row_shuffle<KL, false>(q, 64);
             __syncthreads();
             c = wide_coef<KL, false>(w, q, in, za);
-        }
-        if (tid == 0) {
-            row_store(p, row, w.out);
-            if (p.rec) rec_add(rec, in.w, w.out);
-        }
-        if (g) {
-            auto grads = [&](auto mode, auto n, int first) {
-                constexpr int N = decltype(n)::value;
-                constexpr bool PLAIN = decltype(mode)::value;
-                wide_stream<T, KL, THREADS, N, PLAIN>(z, zr, mask, first, p.A, [&](auto full, const auto& x, const auto& y, int i) {
-#pragma unroll
-                    for (int u = 0; u < (int)(sizeof(x) / sizeof(x[0])); ++u)
-                        if (decltype(full)::value || i + u * THREADS * VEC < p.A)
-                            vec_grad<decltype(full)::value, KL, PLAIN>(c, act, x[u], y[u], g, i + u * THREADS * VEC, p.A);
-                });
-            };
-            if (c.zero) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
-            else if (c.plain) {
-                vec_again(a);
-                if constexpr (KL != 0) vec_again(b);
-                const int lane = opaque(tid);
-#pragma unroll
-                for (int i = 0; i < H; ++i) {
-                    vec_grad<true, KL, true>(c, act, a[i], b[i], g, (i * THREADS + lane) * VEC, p.A);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                const int rest = (p.A - HELD) / (THREADS * VEC), kept = rest < LDS ? rest : LDS;      // whole vectors in LDS
-                if constexpr (LDS > 0) {
-#pragma unroll 1
-                    for (int i = 0; i < kept; ++i) {
-                        Vec<T, VEC> x, y;
-                        x.w = s_row[i][lane];
-                        if constexpr (KL != 0) y.w = s_row[LDS + i][lane];
-                        vec_grad<true, KL, true>(c, act, x, y, g, ((H + i) * THREADS + lane) * VEC, p.A);
-                    }
-                }
-                grads(std::true_type(), std::integral_constant<int, U>(), HELD + kept * THREADS * VEC);
-            } else {
-                grads(std::false_type(), std::integral_constant<int, 1>(), 0);
+            if (near()) exact();
+            put();
+            if (g) {
+                if (c.zero) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
+                else grads(std::false_type(), std::integral_constant<int, 1>(), 0);
             }
+        } else {
+            int first = 0;                                          // where the part of the row begins that is read again
+            if (near()) {                                           // (everybody) all of it: what is held would take registers over the calls
+                exact();
+                put();
+            } else {
+                put();
+                if (g) {
+                    vec_again(a);
+                    if constexpr (KL != 0) vec_again(b);
+                    const int lane = opaque(tid);
+#pragma unroll
+                    for (int i = 0; i < H; ++i) {
+                        vec_grad<true, KL, true>(c, act, a[i], b[i], g, (i * THREADS + lane) * VEC, p.A);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    const int rest = (p.A - HELD) / (THREADS * VEC), kept = rest < LDS ? rest : LDS;      // whole vectors in LDS
+                    if constexpr (LDS > 0) {
+#pragma unroll 1
+                        for (int i = 0; i < kept; ++i) {
+                            Vec<T, VEC> x, y;
+                            x.w = s_row[i][lane];
+                            if constexpr (KL != 0) y.w = s_row[LDS + i][lane];
+                            vec_grad<true, KL, true>(c, act, x, y, g, ((H + i) * THREADS + lane) * VEC, p.A);
+                        }
+                    }
+                    first = HELD + kept * THREADS * VEC;
+                }
+            }
+            if (g) grads(std::true_type(), std::integral_constant<int, U>(), first);
         }
         __syncthreads();                 // w.sum and w.coef are read
     }
@@ -1075,6 +1132,7 @@ int accerl_policy_loss(const accerl_policy_loss_args* a, void* stream) {
     p.loss = a->out_loss; p.lp = a->out_logp; p.kl = a->out_kl; p.ent = a->out_entropy;
     p.kind = a->kl_kind;
     p.lo = 1.0 - a->clip_low; p.hi = 1.0 + a->clip_high;
+    p.log_lo = (float)log(p.lo); p.log_hi = (float)log(p.hi);
     p.ck = (float)a->kl_coef; p.ch = (float)a->entropy_coef; p.scale = (float)a->scale;
     if (!a->out_stats) p.rec = nullptr;
     return loss_run(who, a->dtype, p, a->out_stats, (hipStream_t)stream);

@@ -489,3 +489,26 @@ def test_loss_next_to_the_clipping_border_of_improbable_actions(A, B, n, kl, dow
     x.zr += up
     _at_the_border(x)
     x.check(x.run(A))
+
+
+@pytest.mark.parametrize("n,dtype,kl", [(5003, "f32", "none"), (5003, "f32", "forward"), (9001, "bf16", "reverse"), (33333, "bf16", "none"), (33333, "f16", "forward"),
+                                        (70001, "f32", "sampled")])
+@pytest.mark.parametrize("down,up,holes", [(0, 0, False), (30, 0, False), (3, 1000, False), (3, 0, True)])
+def test_loss_next_to_the_clipping_border_of_long_rows(A, n, dtype, kl, down, up, holes):
+    """Rows of a workgroup each; with holes of -inf they are summed the careful way."""
+    B = 257
+    x = Inputs(B, n, dtype, kl, "none", seed=53)
+    x.w[:] = 1.0
+    x.act = torch.randint(0, n // 4, (B,), dtype=torch.int32, generator=torch.Generator().manual_seed(1)) * 4
+    if holes:
+        x.z[:, 1::4] = float("-inf")
+        x.zr[:, 1::4] = float("-inf")
+    x.z[torch.arange(B, device="cuda"), x.act.cuda().long()] -= down
+    x.z += up
+    x.zr += up
+    _at_the_border(x)
+    x.ref_lp = x.old + 0.1
+    x.check(x.run(A))
+    kept = x.z.clone()
+    got, again = x.run(A), x.run(A, grad=x.z)                                   # and in place
+    assert torch.equal(got.grad, again.grad) and torch.equal(got.stats, again.stats) and not torch.equal(kept, x.z)
