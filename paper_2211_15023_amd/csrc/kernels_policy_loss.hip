@@ -19,6 +19,7 @@ namespace {
 constexpr int64_t PL_MAX_A = 1 << 20;
 constexpr int PL_RECORDS = 2048;          // workgroups of a row pass, each leaves one record of sums
 constexpr int PL_PARTS = 2048;            // pieces of rows, where a row is split
+constexpr int PL_SPLIT = 256;             // rows below which one may be
 // Vectors of a row that a lane of a wavefront holds at most; longer rows are a workgroup's (a workgroup each / a wavefront each, us: 10000 x 3000
 // bf16 forward 104 / 78, 10000 x 2000 fp32 reverse 84.5 / 70.5, log-probabilities of 32827 x 1305 fp32 140 / 80).
 constexpr int PL_HELD = 8;
@@ -39,6 +40,7 @@ struct LossParams {
     float *loss, *lp, *kl, *ent;
     Record* rec;
     Part* part;
+    double* exact;           // split rows whose gradient goes where the logits are: a row's sum in 64 bits, or 0 where it is not next to a border
     int64_t B, ldz, ldr, ldg, ldm;
     int A, kind;             // accerl_kl_kind
     int only_lp;             // log-probabilities and entropies only
@@ -906,6 +908,29 @@ __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams
     part.r = q;
     part.za = act >= first && act < end && (!mask || mask[act]) ? el_f32(z[act]) : -INFINITY;
 }
+// whether a row of pieces is next to a border
+__device__ __forceinline__ bool split_near(const LossParams& p, const WideShared& w, const RowIn& in) {
+    return !p.only_lp && near_border(p, w.out.lp, in.old, 40.0f + 0.25f / SP_THREADS * (float)p.chunk, 2.0f);
+}
+// Between the two, where the gradient goes where the logits are: a row next to a border is summed in 64 bits before any of it is overwritten.
+template <typename T>
+__global__ __launch_bounds__(SP_THREADS) void loss_border_kernel(const LossParams p) {
+    __shared__ WideShared w;
+    const int64_t row = blockIdx.x;
+    const RowIn in = row_in(p, row);
+    if (row_dead(p, in)) return;
+    if (threadIdx.x == 0) { w.p = p; w.waves = SP_THREADS / 64; }
+    RowSum q = row_empty();
+    for (int i = threadIdx.x; i < p.splits; i += SP_THREADS) q = row_join<0, false>(q, p.part[row * p.splits + i].r);
+    wide_coef<0, false>(w, row_shuffle<0, false>(q, 64), in, p.part[row * p.splits + in.act / p.chunk].za);
+    const bool near = split_near(p, w, in);                         // (everybody)
+    if (near) exact_sum<SP_THREADS>(&w, (const T*)p.z + row * p.ldz, p.mask ? p.mask + row * p.ldm : nullptr);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    double s = 0.0;
+    if (near) for (int k = 0; k < w.waves; ++k) s += w.exact[k];
+    p.exact[row] = s;
+}
 template <typename T, int KL>
 __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = 2;
@@ -927,7 +952,18 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     RowSum q = row_empty();
     for (int i = threadIdx.x; i < p.splits; i += SP_THREADS) q = row_join<KL, false>(q, p.part[row * p.splits + i].r);
     const int act = in.act;
-    const Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), in, p.part[row * p.splits + act / p.chunk].za);
+    const float za = p.part[row * p.splits + act / p.chunk].za;
+    Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), in, za);
+    const T* z = (const T*)p.z + row * p.ldz;
+    const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
+    if (p.exact ? p.exact[row] != 0.0 : split_near(p, w, in)) {     // (everybody)
+        if (!p.exact) exact_sum<SP_THREADS>(&w, z, mask);
+        else if (threadIdx.x < SP_THREADS / 64) w.exact[threadIdx.x] = threadIdx.x == 0 ? p.exact[row] : 0.0;
+        __syncthreads();
+        if (threadIdx.x < 64) wide_finish<KL, true>(&w, false, in, za);
+        __syncthreads();
+        c = w.coef;
+    }
     if (lead) {
         row_store(p, row, w.out);
         Record rec = {0, 0, 0, 0};
@@ -937,7 +973,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     if (!g) return;
     if (c.zero) zero_row<T, VEC>(g, first, end, threadIdx.x, SP_THREADS);
     else
-        wide_stream<T, KL, SP_THREADS, U, false>((const T*)p.z + row * p.ldz, KL ? (const T*)p.zr + row * p.ldr : nullptr, p.mask ? p.mask + row * p.ldm : nullptr, first, end,
+        wide_stream<T, KL, SP_THREADS, U, false>(z, KL ? (const T*)p.zr + row * p.ldr : nullptr, mask, first, end,
                               [&](auto full, const auto& x, const auto& y, int i) {
 #pragma unroll
                                   for (int u = 0; u < (int)(sizeof(x) / sizeof(x[0])); ++u)
@@ -1004,7 +1040,7 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
         // another launch is not (bf16, log-probabilities, split / not: 16 x 20000 11.5 / 7.9 us, x 100000 12.5 / 14.7, 256 x 100000 24.3 /
         // 21.6; the loss with the forward KL: 16 x 20000 20.6 / 17.8, x 100000 24.5 / 33.9, 256 x 100000 69.9 / 45.4).
         const int64_t pieces = (p.A + VEC * SP_THREADS - 1) / (VEC * SP_THREADS);
-        int64_t splits = p.B < 256 && (int64_t)p.A * (KL ? 2 : 1) > 32 * VEC * WR_THREADS ? 512 / p.B : 1;
+        int64_t splits = p.B < PL_SPLIT && (int64_t)p.A * (KL ? 2 : 1) > 32 * VEC * WR_THREADS ? 512 / p.B : 1;
         if (splits > pieces) splits = pieces;
         p.chunk = (int)((pieces + splits - 1) / splits * VEC * SP_THREADS);
         p.splits = (p.A + p.chunk - 1) / p.chunk;
@@ -1012,6 +1048,12 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             records = (int)p.B;
             loss_parts_kernel<T, KL><<<dim3(p.splits, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
             if (int rc = pl_launched(who)) return rc;
+            if (p.g == p.z) {
+                loss_border_kernel<T><<<dim3((unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
+                if (int rc = pl_launched(who)) return rc;
+            } else {
+                p.exact = nullptr;
+            }
             loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
@@ -1051,7 +1093,7 @@ int loss_run(const char* who, int dtype, LossParams& p, float* out_stats, hipStr
     return dtype == ACCERL_DT_BF16 ? loss_kl<BF16>(who, p, out_stats, s) : loss_kl<F16>(who, p, out_stats, s);
 }
 
-constexpr int64_t PL_WORKSPACE = PL_RECORDS * (int64_t)sizeof(Record) + PL_PARTS * (int64_t)sizeof(Part);
+constexpr int64_t PL_WORKSPACE = PL_RECORDS * (int64_t)sizeof(Record) + PL_PARTS * (int64_t)sizeof(Part) + PL_SPLIT * (int64_t)sizeof(double);
 bool pl_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // what every call checks; `done` is set where nothing is to be done
@@ -1073,6 +1115,7 @@ void table_params(LossParams& p, int64_t B, int64_t A, const void* z, int64_t ld
     p.B = B; p.A = (int)A; p.z = z; p.ldz = ldz; p.mask = mask; p.ldm = ldm; p.act = act;
     p.rec = (Record*)workspace;
     p.part = (Part*)((char*)workspace + PL_RECORDS * sizeof(Record));
+    p.exact = (double*)(p.part + PL_PARTS);
 }
 }  // namespace
 }  // namespace accerl

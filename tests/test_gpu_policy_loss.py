@@ -512,3 +512,37 @@ def test_loss_next_to_the_clipping_border_of_long_rows(A, n, dtype, kl, down, up
     kept = x.z.clone()
     got, again = x.run(A), x.run(A, grad=x.z)                                   # and in place
     assert torch.equal(got.grad, again.grad) and torch.equal(got.stats, again.stats) and not torch.equal(kept, x.z)
+
+
+@pytest.mark.parametrize("B,n", [(1, 40001), (40, 40001), (3, 300001)])
+@pytest.mark.parametrize("dtype,kl", [("f32", "none"), ("bf16", "forward"), ("f16", "reverse")])
+@pytest.mark.parametrize("down,up", [(0, 0), (30, 0), (3, 1000)])
+def test_loss_next_to_the_clipping_border_of_rows_in_pieces(A, B, n, dtype, kl, down, up):
+    """With the gradient beside the logits and over them, and without one; the border is tried at several hundred distances."""
+    x = Inputs(B, n, dtype, kl, "shared", seed=54)
+    x.w[:] = 1.0
+    x.act = torch.from_numpy(np.flatnonzero(x.mask[0].numpy())[np.random.default_rng(1).integers(0, n // 2, B)]).to(torch.int32)
+    x.z[torch.arange(B, device="cuda"), x.act.cuda().long()] -= down
+    x.z += up
+    x.zr += up
+    mask = x.mask.numpy() != 0
+    lp = ref.softmax_rows(as64(x.z), np.broadcast_to(mask, (B, n)))[0][np.arange(B), x.act.numpy()]
+    kept, rng = x.z.clone(), np.random.default_rng(2)
+    how = A.PolicyLoss(x.lo, x.hi, kl, x.ck, x.ch)
+    wide = dict(ref_logits=x.zr) if kl != "none" else {}
+    outside = lambda old, adv, **k: how.forward(x.z, x.act.cuda(), old.cuda(), adv.cuda(), mask=x.mask.cuda(), scale=1.0, **wide, **k)
+    for turn in range(max(4, 120 // B)):
+        border = np.log(rng.choice([x.hi + 1, 1 - x.lo], B))
+        old = torch.from_numpy(lp - border).float() + 0.0
+        # whole steps of fp32 to either side of what is next to the border
+        old = torch.from_numpy(old.numpy() + rng.integers(-3, 4, B).astype(np.float32) * np.spacing(np.abs(old.numpy())))
+        adv = torch.from_numpy(rng.choice([1.0, -1.0], B)).float()
+        r = np.exp(lp - as64(old))
+        want = ((r < 1 - x.lo) | (r > 1 + x.hi)).sum()
+        a, b = outside(old, adv), outside(old, adv, grad=False)
+        assert float(a.stats[3]) == want == float(b.stats[3]), turn
+        c = outside(old, adv, grad=x.z)
+        assert torch.equal(a.grad, c.grad) and torch.equal(a.stats, c.stats) and torch.equal(a.loss, b.loss)
+        x.z.copy_(kept)
+    x.old, x.adv = old, adv
+    x.check(a)
