@@ -655,6 +655,7 @@ struct WideShared {
     RowSum sum[WR_WAVES];
     Coef coef;
     RowOut out;
+    Record rec;              // the sums of the workgroup's rows, thread 0's: in registers they would be everybody's
     int waves;
     float m;                 // the row's maximum
     double exact[WR_WAVES];
@@ -691,22 +692,22 @@ __device__ __attribute__((noinline)) void exact_sum(WideShared* w, const T* z, c
     const int A = w->p.A;
     const double m = w->m;
     double s = 0.0;
-    float v[8], next[8];
-    const auto load = [&](float (&d)[8], int i) {
+    float v[4], next[4];
+    const auto load = [&](float (&d)[4], int i) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = el_f32(z[min(i + k * THREADS, A - 1)]);
+        for (int k = 0; k < 4; ++k) d[k] = el_f32(z[min(i + k * THREADS, A - 1)]);
         if (mask) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (!mask[min(i + k * THREADS, A - 1)]) d[k] = -INFINITY;
+            for (int k = 0; k < 4; ++k) if (!mask[min(i + k * THREADS, A - 1)]) d[k] = -INFINITY;
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) if (i + k * THREADS >= A) d[k] = -INFINITY;
+        for (int k = 0; k < 4; ++k) if (i + k * THREADS >= A) d[k] = -INFINITY;
     };
     load(v, threadIdx.x);
-    for (int i = threadIdx.x; i < A; i += 8 * THREADS) {
-        load(next, i + 8 * THREADS);
+    for (int i = threadIdx.x; i < A; i += 4 * THREADS) {
+        load(next, i + 4 * THREADS);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { s += exp((double)v[k] - m); v[k] = next[k]; }
+        for (int k = 0; k < 4; ++k) { s += exp((double)v[k] - m); v[k] = next[k]; }
     }
     for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
     if ((threadIdx.x & 63) == 0) w->exact[threadIdx.x >> 6] = s;
@@ -768,8 +769,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
     constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
     __shared__ WideShared w;
     __shared__ u32x4 s_row[LDS > 0 ? LDS * (KL ? 2 : 1) : 1][LDS > 0 ? THREADS : 1];     // vectors behind those in registers, a lane's own
-    if (threadIdx.x == 0) { w.p = p; w.waves = THREADS / 64; }
-    Record rec = {0, 0, 0, 0};
+    if (threadIdx.x == 0) { w.p = p; w.rec = {0, 0, 0, 0}; w.waves = THREADS / 64; }
     for (int64_t row = blockIdx.x; row < p.B; row += gridDim.x) {
         const int tid = opaque(threadIdx.x);
         T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
@@ -810,7 +810,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         const auto put = [&] {
             if (tid == 0) {
                 row_store(p, row, w.out);
-                if (p.rec) rec_add(rec, in.w, w.out);
+                if (p.rec) rec_add(w.rec, in.w, w.out);
             }
         };
         // (terms of one size round the same way within one power of two only, so that a quarter of a half step each is as far as their sum goes)
@@ -877,7 +877,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
         }
         __syncthreads();                 // w.sum and w.coef are read
     }
-    if (threadIdx.x == 0 && p.rec) p.rec[blockIdx.x] = rec;
+    if (threadIdx.x == 0 && p.rec) p.rec[blockIdx.x] = w.rec;
 }
 
 // Few rows: pieces of rows to partial sums, then pieces again with the row's sums joined.  Two dependent launches, latency: 16 x 100000
@@ -910,7 +910,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams
 }
 // whether a row of pieces is next to a border
 __device__ __forceinline__ bool split_near(const LossParams& p, const WideShared& w, const RowIn& in) {
-    return !p.only_lp && near_border(p, w.out.lp, in.old, 40.0f + 0.25f / SP_THREADS * (float)p.chunk, 2.0f);
+    return near_border(p, w.out.lp, in.old, 40.0f + 0.25f / SP_THREADS * (float)p.chunk, 2.0f);
 }
 // Between the two, where the gradient goes where the logits are: a row next to a border is summed in 64 bits before any of it is overwritten.
 template <typename T>
@@ -931,7 +931,8 @@ __global__ __launch_bounds__(SP_THREADS) void loss_border_kernel(const LossParam
     if (near) for (int k = 0; k < w.waves; ++k) s += w.exact[k];
     p.exact[row] = s;
 }
-template <typename T, int KL>
+// LOSS: not log-probabilities alone, which have no border to be next to (what that takes costs their 10 us half a one).
+template <typename T, int KL, bool LOSS>
 __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = 2;
     __shared__ WideShared w;
@@ -956,7 +957,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), in, za);
     const T* z = (const T*)p.z + row * p.ldz;
     const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-    if (p.exact ? p.exact[row] != 0.0 : split_near(p, w, in)) {     // (everybody)
+    if (LOSS && (p.exact ? p.exact[row] != 0.0 : split_near(p, w, in))) {     // (everybody)
         if (!p.exact) exact_sum<SP_THREADS>(&w, z, mask);
         else if (threadIdx.x < SP_THREADS / 64) w.exact[threadIdx.x] = threadIdx.x == 0 ? p.exact[row] : 0.0;
         __syncthreads();
@@ -1054,7 +1055,8 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             } else {
                 p.exact = nullptr;
             }
-            loss_split_kernel<T, KL><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
+            if (KL == 0 && p.only_lp) loss_split_kernel<T, 0, false><<<dim3(1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
+            else loss_split_kernel<T, KL, true><<<dim3(p.g ? p.splits : 1, (unsigned)p.B), dim3(SP_THREADS), 0, s>>>(p);
         } else {
             records = (int)(p.B < PL_RECORDS ? p.B : PL_RECORDS);
             const int per = p.A / (VEC * WR_THREADS);            // whole vectors a thread of 256: at least 2, and at least what the forms below hold in registers
