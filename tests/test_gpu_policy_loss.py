@@ -546,3 +546,61 @@ def test_loss_next_to_the_clipping_border_of_rows_in_pieces(A, B, n, dtype, kl, 
         x.z.copy_(kept)
     x.old, x.adv = old, adv
     x.check(a)
+
+
+def _softmax_64(z):
+    """(log p, p) of logits in 64 bits on the GPU, in elementary operations."""
+    z = z.double()
+    z = z - z.amax(dim=1, keepdim=True)
+    e = z.exp()
+    s = e.sum(dim=1, keepdim=True)
+    return z - s.log(), e / s
+
+
+@pytest.mark.parametrize("vectors", [2, 4, 8, 15, 20, 28, 30, 44, 48, 96, 112])
+@pytest.mark.parametrize("more", [0, 1027])
+@pytest.mark.parametrize("dtype,kl", [("bf16", "forward"), ("f16", "reverse"), ("f32", "none"), ("bf16", "none"), ("f32", "forward")])
+@pytest.mark.parametrize("B", [300, 40])
+def test_loss_long_rows_see_every_vector(A, B, vectors, more, dtype, kl):
+    """Each row has most of its probability in one place, next to where a lane's vectors, registers, LDS, stream or pieces may end: the place tried moves on
+    from row to row, the reference's backwards.  Whoever leaves a vector out, or takes one twice, is off by far more than 32-bit sums of 2^17 terms."""
+    vec = 4 if dtype == "f32" else 8
+    n = vectors * 256 * vec + more
+    spots = sorted({min(max(k * 256 * vec + o, 1), n - 1) for k in range(vectors + 1) for o in (-1, 0)} | {n - 1, n - vec, n - vec - 1})
+    g = torch.Generator(device="cuda").manual_seed(vectors)
+    table = lambda: torch.randn((B, n), generator=g, device="cuda").to(TORCH[dtype])
+    z, zr = table(), table()
+    tried = [b % len(spots) if len(spots) <= B else b * len(spots) // B for b in range(B)]      # (all of them by 300 rows)
+    at, at_ref = (torch.tensor([spots[i] for i in t], device="cuda") for t in (tried, [-1 - i for i in tried]))
+    rows = torch.arange(B, device="cuda")
+    z[rows, at] = 16.0
+    zr[rows, at_ref] = 16.0
+    act = torch.zeros(B, dtype=torch.int32, device="cuda")
+    logp, p = _softmax_64(z)
+    lp = logp[:, 0]
+    old = (lp + 0.1).float()                                                    # a ratio of exp(-0.1), inside the borders
+    adv = torch.where(rows % 2 == 0, 1.0, -1.0)
+    out = torch.full((B, n), 9.0, dtype=TORCH[dtype], device="cuda")
+    ck = 0.25 if kl != "none" else 0.0
+    got = A.PolicyLoss(0.2, 0.2, kl, ck).forward(z, act, old, adv, scale=1.0, ref_logits=zr if ck else None, grad=out)
+    at_grad = -(lp - old.double()).exp() * adv
+    want = -at_grad[:, None] * p
+    want[:, 0] += at_grad
+    e, far = ref.sum_error(n), 40.0                                             # 16 + 16 and the spread of normal numbers between any two logits' differences
+    size = at_grad.abs()[:, None] * p
+    if ck:
+        logr, pr = _softmax_64(zr)
+        if kl == "forward":
+            k = (pr * (logr - logp)).sum(dim=1)
+            want += ck * (p - pr)
+            size = size + ck * (p + pr)
+        else:
+            k = (p * (logp - logr)).sum(dim=1)
+            want += ck * p * (logp - logr - k[:, None])
+            size = size + ck * p * 2 * far
+        assert ((got.kl.double() - k).abs() <= 2 * e * (1 + far + np.log(n))).all()
+    size[:, 0] += at_grad.abs()
+    assert ((got.logp.double() - lp).abs() <= e + 4 * ref.U * (lp.abs() + 1)).all()
+    off = (got.grad.double() - want).abs()
+    tol = size * (4 * e + 64 * ref.U) + ref.HALF_STEP[dtype] * want.abs() * 1.001 + ref.TINY[dtype]
+    assert (off <= tol).all(), (off / tol).max()
