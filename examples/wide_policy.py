@@ -2,8 +2,9 @@
 
 The actor's head is an int8 dense layer that quantises its inputs with a scale for each state (DenseInt8); it samples from the logits and
 stores the log-probabilities of what it took (PolicyLoss.logprob).  The learner computes the logits again with its own weights, takes the
-clipped loss with a KL term to the policy it started from (PolicyLoss.forward), continues the gradient into the weights, and hands the
-actor the new ones, quantised anew (DenseInt8.update).  The task: every state has its own best actions out of 2000, found by trying.
+clipped loss with a KL term to the policy it started from (PolicyLoss.forward; the advantages are the round's rewards, normalised), continues
+the gradient into the weights, and hands the actor the new ones, quantised anew (DenseInt8.update).  The task: every state has its own best
+actions out of 2000, found by trying.
 
     python examples/wide_policy.py
 """

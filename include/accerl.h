@@ -333,8 +333,8 @@ int accerl_dense_i8(const int8_t* x_packed, const float* x_scale, const int8_t* 
 
 /*
  * The same layer on floating-point tokens, quantised as accerl_quantize_rows does (same results as the two calls).
- * workspace: DEVICE, 16-byte aligned, at least accerl_dense_i8_workspace(M, K) bytes, used until the work has finished: calls that
- * may overlap need a workspace each.  Its contents need not be kept or cleared.  out may lie over x, whose tokens are quantised before it is
+ * workspace: DEVICE, 16-byte aligned, at least accerl_dense_i8_workspace(M, K) bytes, used until the work has finished, and by a graph that
+ * captured the call as long as it is replayed: calls that may overlap, of several threads on one stream too, need a workspace each.  Its contents need not be kept or cleared.  out may lie over x, whose tokens are quantised before it is
  * written, and over nothing else; the workspace over neither (ACCERL_EINVAL).
  */
 int64_t accerl_dense_i8_workspace(int64_t M, int64_t K);
@@ -349,7 +349,7 @@ int accerl_dense_i8_dynamic(const void* x, int32_t x_dtype, int64_t ld_x, const 
  * allowed; ld_mask == 0: one row for all); actions DEVICE int32 [B].  A logit of -inf is an action of probability 0.  An action that is not allowed
  * has log-probability -inf, and so has every action of a row that allows none (entropy 0).  An action outside 0 .. A-1 marks a row
  * without one: 0 and 0, and the row is not read.  workspace: DEVICE, 16-byte aligned, accerl_policy_loss_workspace() bytes (the same
- * for all sizes), used until the work has finished: calls that may overlap need one each.  Neither call allocates or synchronises;
+ * for all sizes), used as accerl_dense_i8_dynamic's: calls that may overlap need one each.  Neither call allocates or synchronises;
  * B == 0 enqueues nothing; a call repeated gives the same bits.
  */
 int64_t accerl_policy_loss_workspace(void);

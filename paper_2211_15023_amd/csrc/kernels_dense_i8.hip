@@ -166,7 +166,8 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const T* x, i
     }
 }
 
-// int8 rows to tiles and back, a 16-byte piece a thread (done once for weights, bound by its byte loads)
+// int8 rows to tiles and back, a 16-byte piece a thread: with every update of int8 weights.  Bound by its byte loads and stores: 16384 x 4096 116 us
+// (back 120), 1.2 TB/s; 2501 x 1777 8.9 (12.8).
 __global__ __launch_bounds__(256) void pack_rows_kernel(const int8_t* q, int64_t rows, int64_t cols, int64_t ld, v4i* out, int64_t steps, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t tile = i / (steps * 64), p = i - tile * steps * 64, row = tile * 16 + (p & 15), k = (p >> 4) * 16;

@@ -660,7 +660,7 @@ struct WideShared {
     float m;                 // the row's maximum
     double exact[WR_WAVES];
 };
-// EXACT: with the ratio of the sum in `exact`.
+// EXACT: with the ratio that the sum in `exact` gives.
 template <int KL, bool EXACT>
 __device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain, RowIn in, float za) {
     Sums<double> r = {-FLT_MAX, -FLT_MAX, 0.0, 0.0, 0.0, 0.0, -1.0};
@@ -686,7 +686,8 @@ __device__ __attribute__((noinline)) void wide_finish(WideShared* w, bool plain,
     if (threadIdx.x == 0) { w->coef = c; w->out = o; w->m = r.m; }
 }
 // The row's sum in 64 bits, from memory, by the whole workgroup: the wavefronts' parts go to `w->exact`.  A function that is called, like the one
-// above; eight elements a lane are on their way while eight are summed (one after the other a row of 50000 took 150 us).
+// above; four elements a lane are on their way while four are summed (one after the other a masked row of 50000 took 150 us, like this, its
+// gradient read again, 38; eight take more registers than some of the kernels have).
 template <int THREADS, typename T>
 __device__ __attribute__((noinline)) void exact_sum(WideShared* w, const T* z, const uint8_t* mask) {
     const int A = w->p.A;
@@ -813,7 +814,8 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
                 if (p.rec) rec_add(w.rec, in.w, w.out);
             }
         };
-        // (terms of one size round the same way within one power of two only, so that a quarter of a half step each is as far as their sum goes)
+        // (A lane adds A / THREADS terms: in the worst case, equal ones, those of the sum's last power of two are half of them, round the same way, and
+        // are half of the sum on average.)
         const auto near = [&] { return !p.only_lp && near_border(p, w.out.lp, in.old, 24.0f + 0.25f / THREADS * (float)p.A, 2.0f); };
         const auto exact = [&] {
             exact_sum<THREADS>(&w, z, mask);

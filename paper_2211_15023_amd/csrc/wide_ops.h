@@ -11,7 +11,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
-typedef uint32_t u32_at2 __attribute__((aligned(2)));
 
 struct BF16 { uint16_t u; };
 struct F16 { uint16_t u; };
