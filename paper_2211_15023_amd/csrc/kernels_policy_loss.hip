@@ -163,8 +163,8 @@ __device__ __forceinline__ RowIn row_in(const LossParams& p, int64_t row) {
 }
 __device__ __forceinline__ bool row_dead(const LossParams& p, const RowIn& r) { return r.act < 0 || r.act >= p.A || r.w == 0.0f; }
 // Next to a clipping border the side decides over a row's whole gradient: there the ratio is worked out in 64 bits.  "Next" is what 32 bits may
-// be off by, which is relative for the ratio and absolute for its logarithm.  In half steps of 32 bits: `terms` for the sum (a few dozen for its powers and
-// joins, and up to a half for each term that a lane adds up), `steps` of |log pi(a)| for its own roundings.
+// be off by, which is relative for the ratio and absolute for its logarithm.  In half steps of 32 bits: `terms` for the sum (two or three dozen for its
+// powers and joins, and one for each term that a lane adds up, all of which may be rounded the same way), `steps` of |log pi(a)| for its own roundings.
 __device__ __forceinline__ bool near_border(const LossParams& p, float lp, float old, float terms, float steps) {
     const float r = lp - old, by = 0x1p-24f * fmaf(steps, fabsf(lp), terms);
     return fabsf(r - p.log_hi) < by || fabsf(r - p.log_lo) < by;
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(NR_THREADS) void loss_rows_kernel(const LossParams 
         if (!p.only_lp && q.s > 0.0f) {
             // (all lanes of a row branch alike)
             const float lp = (float)PL_LN2 * (power<false>(base<false>(q.m), za) - pl_log2(q.s));
-            if (near_border(p, lp, in.old, 64.0f + 0.5f * H * VEC, 4.0f)) {
+            if (near_border(p, lp, in.old, 40.0f + H * VEC, 4.0f)) {
                 ratio = exact_ratio<T>(z, mask, p.A, j, G, VEC, q.m, za, in.old);
                 better = &ratio;
             }
@@ -642,10 +642,19 @@ __device__ __forceinline__ void sum_vecs(RowSum& q, const Vec<T, VEC> (&x)[ALL],
         for (int e = 0; e < VEC; ++e) { m = fmaxf(m, x[first + u].at(e)); if constexpr (KL != 0) mr = fmaxf(mr, y[first + u].at(e)); }
     row_raise<KL, PLAIN>(q, m, mr);
     const Base c = base<PLAIN>(m), cr = base<PLAIN>(mr);
+    // (among themselves first: a lane's sum is then rounded once for all of them)
+    RowSum own = {m, 0.0f, 0.0f, mr, 0.0f, 0.0f};
 #pragma unroll
     for (int u = 0; u < N; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) row_add<KL, PLAIN>(q, c, cr, x[first + u].at(e), KL ? y[first + u].at(e) : 0.0f);
+        for (int e = 0; e < VEC; ++e) row_add<KL, PLAIN>(own, c, cr, x[first + u].at(e), KL ? y[first + u].at(e) : 0.0f);
+    q.s += own.s; q.u += own.u; q.sr += own.sr; q.t += own.t;
+}
+
+// Terms of a lane's sum, as near_border counts them: those of up to four vectors among themselves, then two vectors a time, each time once more and three
+// where the maximum rises.
+template <int VEC> __device__ __forceinline__ float wide_terms(int elements, int threads) {
+    return 24.0f + 4 * VEC + 4.0f * (2.0f + (float)elements / (float)(2 * VEC * threads));
 }
 
 // What the workgroup of a row shares.  The row's scalars are worked out by wavefront 0 in 64 bits, in a function that is called: inside the
@@ -765,7 +774,8 @@ __device__ __forceinline__ void held_sums(RowSum& q, const Vec<T, VEC> (&a)[H], 
 // that a second reading costs what the first did.  Four workgroups of 256 a compute unit hold 15 vectors (eight of each table: more registers
 // would spill, and seven did), two hold 56 (28) and one of 512 112 (56): fewer wavefronts hide less, but what they save is more from rows of
 // 15 to 30 vectors a lane on.  8192 x 32000 bf16, no reference: 206 us, 5.1 TB/s of once read and once written; 2048 x 2 x 150000 486, 3.8.
-template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
+// LOSS: not log-probabilities alone, which have no gradient and no border to be next to, and need not have these' registers.
+template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS, bool LOSS>
 __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = KL ? 2 : 4, HELD = H * THREADS * VEC;
     __shared__ WideShared w;
@@ -773,7 +783,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
     if (threadIdx.x == 0) { w.p = p; w.rec = {0, 0, 0, 0}; w.waves = THREADS / 64; }
     for (int64_t row = blockIdx.x; row < p.B; row += gridDim.x) {
         const int tid = opaque(threadIdx.x);
-        T* g = p.g ? (T*)p.g + row * p.ldg : nullptr;
+        T* g = LOSS && p.g ? (T*)p.g + row * p.ldg : nullptr;
         const RowIn in = row_in(p, row);
         if (row_dead(p, in)) {
             if (g) zero_row<T, VEC>(g, 0, p.A, tid, THREADS);
@@ -805,7 +815,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
             sum_vecs<KL, N, true>(q, x, y, 0);
         };
         // (without a gradient nothing is read twice: log-probabilities of 4096 x 32768 fp32 105 -> 95 us)
-        if (H <= 4 && !p.g) wide_stream<T, KL, THREADS, U, true, true>(z, zr, mask, HELD, p.A, take);
+        if (H <= 4 && !g) wide_stream<T, KL, THREADS, U, true, true>(z, zr, mask, HELD, p.A, take);
         else wide_stream<T, KL, THREADS, U, true>(z, zr, mask, HELD, p.A, take);
         Coef c = wide_coef<KL, true>(w, row_shuffle<KL, true>(q, 64), in, za);
         const auto put = [&] {
@@ -814,9 +824,7 @@ __global__ __launch_bounds__(THREADS, PER_SIMD) void loss_wide_kernel(const Loss
                 if (p.rec) rec_add(w.rec, in.w, w.out);
             }
         };
-        // (A lane adds A / THREADS terms: in the worst case, equal ones, those of the sum's last power of two are half of them, round the same way, and
-        // are half of the sum on average.)
-        const auto near = [&] { return !p.only_lp && near_border(p, w.out.lp, in.old, 24.0f + 0.25f / THREADS * (float)p.A, 2.0f); };
+        const auto near = [&] { return LOSS && near_border(p, w.out.lp, in.old, wide_terms<VEC>(p.A, THREADS), 2.0f); };
         const auto exact = [&] {
             exact_sum<THREADS>(&w, z, mask);
             __syncthreads();
@@ -910,9 +918,9 @@ __global__ __launch_bounds__(SP_THREADS) void loss_parts_kernel(const LossParams
     part.r = q;
     part.za = act >= first && act < end && (!mask || mask[act]) ? el_f32(z[act]) : -INFINITY;
 }
-// whether a row of pieces is next to a border
-__device__ __forceinline__ bool split_near(const LossParams& p, const WideShared& w, const RowIn& in) {
-    return near_border(p, w.out.lp, in.old, 40.0f + 0.25f / SP_THREADS * (float)p.chunk, 2.0f);
+// whether a row of pieces is next to a border (three a level for the joins of pieces)
+template <int VEC> __device__ __forceinline__ bool split_near(const LossParams& p, const WideShared& w, const RowIn& in) {
+    return near_border(p, w.out.lp, in.old, 24.0f + wide_terms<VEC>(p.chunk, SP_THREADS), 2.0f);
 }
 // Between the two, where the gradient goes where the logits are: a row next to a border is summed in 64 bits before any of it is overwritten.
 template <typename T>
@@ -925,7 +933,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_border_kernel(const LossParam
     RowSum q = row_empty();
     for (int i = threadIdx.x; i < p.splits; i += SP_THREADS) q = row_join<0, false>(q, p.part[row * p.splits + i].r);
     wide_coef<0, false>(w, row_shuffle<0, false>(q, 64), in, p.part[row * p.splits + in.act / p.chunk].za);
-    const bool near = split_near(p, w, in);                         // (everybody)
+    const bool near = split_near<16 / (int)sizeof(T)>(p, w, in);                         // (everybody)
     if (near) exact_sum<SP_THREADS>(&w, (const T*)p.z + row * p.ldz, p.mask ? p.mask + row * p.ldm : nullptr);
     __syncthreads();
     if (threadIdx.x != 0) return;
@@ -933,7 +941,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_border_kernel(const LossParam
     if (near) for (int k = 0; k < w.waves; ++k) s += w.exact[k];
     p.exact[row] = s;
 }
-// LOSS: not log-probabilities alone, which have no border to be next to (what that takes costs their 10 us half a one).
+// LOSS: as above; what the border takes costs the 10 us of few rows' log-probabilities half a one.
 template <typename T, int KL, bool LOSS>
 __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams p) {
     constexpr int VEC = 16 / sizeof(T), U = 2;
@@ -959,7 +967,7 @@ __global__ __launch_bounds__(SP_THREADS) void loss_split_kernel(const LossParams
     Coef c = wide_coef<KL, false>(w, row_shuffle<KL, false>(q, 64), in, za);
     const T* z = (const T*)p.z + row * p.ldz;
     const uint8_t* mask = p.mask ? p.mask + row * p.ldm : nullptr;
-    if (LOSS && (p.exact ? p.exact[row] != 0.0 : split_near(p, w, in))) {     // (everybody)
+    if (LOSS && (p.exact ? p.exact[row] != 0.0 : split_near<VEC>(p, w, in))) {     // (everybody)
         if (!p.exact) exact_sum<SP_THREADS>(&w, z, mask);
         else if (threadIdx.x < SP_THREADS / 64) w.exact[threadIdx.x] = threadIdx.x == 0 ? p.exact[row] : 0.0;
         __syncthreads();
@@ -1014,8 +1022,8 @@ int pl_launched(const char* who) {
 template <typename T, int KL, int VEC, int H>
 void rows_go(const LossParams& p, int G, int blocks, hipStream_t s) { loss_rows_kernel<T, KL, VEC, H><<<dim3(blocks), dim3(NR_THREADS), 0, s>>>(p, G); }
 
-template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS>
-void wide_go(const LossParams& p, int blocks, hipStream_t s) { loss_wide_kernel<T, KL, H, THREADS, PER_SIMD, LDS><<<dim3(blocks), dim3(THREADS), 0, s>>>(p); }
+template <typename T, int KL, int H, int THREADS, int PER_SIMD, int LDS, bool LOSS = true>
+void wide_go(const LossParams& p, int blocks, hipStream_t s) { loss_wide_kernel<T, KL, H, THREADS, PER_SIMD, LDS, LOSS><<<dim3(blocks), dim3(THREADS), 0, s>>>(p); }
 
 template <typename T, int KL>
 int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
@@ -1066,7 +1074,12 @@ int loss_as(const char* who, LossParams& p, float* out_stats, hipStream_t s) {
             // reference the forward KL, with masks of each row's own four workgroups for longer: 6250 x 32000 478 / 393, 4000 x 50000 fp16 491 / 420).
             const bool own = p.mask && p.ldm;
             if constexpr (KL == 0) {
-                if (p.g && per >= 96) wide_go<T, KL, 40, 512, 2, 16>(p, records, s);         // 887 x 225285 219 / 231, but 1148 x 174085 219 / 210
+                // Log-probabilities: eight workgroups a compute unit, all 2048 of a pass at once (4096 x 32768 fp32 seven, whose second round is a few / eight
+                // 94.5 / 85.6, 2000 x 150000 211 / 191, 10000 x 6000 fp16 49 / 38); bf16's take more registers than that leaves (8192 x 32000 110 / 133).
+                constexpr int SIMD = __is_same(T, BF16) ? 4 : 8;
+                if (p.only_lp && per >= 4) wide_go<T, KL, 4, 256, SIMD, 0, false>(p, records, s);
+                else if (p.only_lp) wide_go<T, KL, 2, 256, SIMD, 0, false>(p, records, s);
+                else if (p.g && per >= 96) wide_go<T, KL, 40, 512, 2, 16>(p, records, s);         // 887 x 225285 219 / 231, but 1148 x 174085 219 / 210
                 else if (p.g && per >= 48) wide_go<T, KL, 40, 256, 2, 16>(p, records, s);    // 1953 x 102405 192 / 194, but 2325 x 86021 198 / 194
                 else if (p.g && per >= 30) wide_go<T, KL, 20, 256, 2, 16>(p, records, s);    // 2500 x 80000 184 / 212, but 4000 x 50000 186 / 177
                 else if (p.g && per >= 15) wide_go<T, KL, 15, 256, 4, 0>(p, records, s);     // 8192 x 32000 224 / 247, eight in registers and nine in LDS

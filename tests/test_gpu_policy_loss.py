@@ -604,3 +604,35 @@ def test_loss_long_rows_see_every_vector(A, B, vectors, more, dtype, kl):
     off = (got.grad.double() - want).abs()
     tol = size * (4 * e + 64 * ref.U) + ref.HALF_STEP[dtype] * want.abs() * 1.001 + ref.TINY[dtype]
     assert (off <= tol).all(), (off / tol).max()
+
+
+@pytest.mark.parametrize("B,n", [(300, 17), (300, 2000), (300, 5003), (300, 20001), (300, 60001), (300, 260001), (40, 60001), (3, 1 << 20)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", ["two", "one", "rising"])
+def test_loss_next_to_the_clipping_border_whatever_the_roundings(A, B, n, dtype, shape):
+    """Rows whose sums are off by roundings that all go one way: of two logits only, of one large logit and many equal small ones, of logits that
+    rise.  The side is the one that a sum in 64 bits gives."""
+    rng = np.random.default_rng(n)
+    place = torch.arange(n, device="cuda")[None]
+    column = lambda v: torch.from_numpy(v).cuda()[:, None]
+    if shape == "two":
+        z = torch.where(place < column(rng.integers(1, n, B)), 0.0, column(-rng.uniform(0.1, 6.0, B)))
+    elif shape == "one":
+        z = torch.where(place == column(rng.integers(0, n, B)), 0.0, column(-rng.uniform(0.5, 1.5, B) * np.log(n) - rng.uniform(0, 4, B)))
+    else:
+        z = (place / n - 0.5) * column(rng.uniform(0.01, 20.0, B))
+    z = z.to(TORCH[dtype])
+    act = torch.from_numpy(np.where(rng.random(B) < 0.5, 0, n - 1)).to(torch.int32)
+    lp = np.array([float(_softmax_64(z[b:b + 1])[0][0, int(act[b])]) for b in range(B)])
+    for turn in range(6):
+        up = rng.random(B) < 0.5
+        old = (lp - np.where(up, np.log(1.25), np.log(0.8))).astype(np.float32)
+        old += rng.integers(-2, 3, B).astype(np.float32) * np.spacing(np.abs(old))
+        adv = np.where(rng.random(B) < 0.5, 1.0, -1.0).astype(np.float32)
+        r = np.exp(lp - old.astype(np.float64))
+        assert (np.abs(r / np.where(up, 1.25, 0.8) - 1) > 1e-13).all()          # (the definition itself tells the sides apart)
+        cut = np.where(adv > 0, r > 1.25, r < 0.8)
+        got = A.PolicyLoss(0.2, 0.25).forward(z, act.cuda(), torch.from_numpy(old).cuda(), torch.from_numpy(adv).cuda(), scale=1.0)
+        wrong = np.flatnonzero((got.grad == 0).all(dim=1).cpu().numpy() != cut)
+        assert wrong.size == 0, (turn, wrong[:5], (r / np.where(up, 1.25, 0.8) - 1)[wrong[:5]])
+        assert float(got.stats[3]) == ((r > 1.25) | (r < 0.8)).sum(), turn
