@@ -648,7 +648,8 @@ __device__ __forceinline__ void sum_vecs(RowSum& q, const Vec<T, VEC> (&x)[ALL],
     for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) row_add<KL, PLAIN>(own, c, cr, x[first + u].at(e), KL ? y[first + u].at(e) : 0.0f);
-    q.s += own.s; q.u += own.u; q.sr += own.sr; q.t += own.t;
+    q.s += own.s; q.u += own.u;
+    if constexpr (KL != 0) { q.sr += own.sr; q.t += own.t; }
 }
 
 // Terms of a lane's sum, as near_border counts them: those of up to four vectors among themselves, then two vectors a time, each time once more and three
