@@ -408,6 +408,105 @@ typedef struct {
 int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
 
 /*
+ * Operators of policies with a memory: linear attention with a decay for each head, and the norms around a block.  An actor carries the
+ * memory from step to step, as it does the state of accerl_actor_forward_recurrent; a learner unrolls it over many steps and takes gradients.
+ *
+ * For a head h of decay g = exp(log_decay[h]) and its queries, keys and values, tokens in their order t = 0 .. n - 1:
+ *     S_t = g S_{t-1} + k_t v_t^T,    o_t = scale q_t S_t        (S: [Dk, Dv]; S_{-1} = state, or zeros)
+ * where reset[t] != 0 the token begins an episode: the state before it counts as zeros, whatever it holds.  H heads of queries share H / Hk heads
+ * each: head h reads k and v of head h Hk / H (H is a multiple of Hk), and has a state of its own.  lengths[b] = n (taken as 0 .. T; NULL: T): the
+ * tokens from n on are not read, their outputs and gradients are 0, and the state is that after n tokens.
+ *
+ * Tensors of tokens are [B, T, heads, D] with strides (elements) of their own for batch, token and head, of any alignment of whole elements;
+ * elements of a head are contiguous: time-major tensors and parts of wider rows are taken as they are.  States are DEVICE fp32 [B, H, Dk, Dv], dense, 16-byte
+ * aligned.  1 <= Dk, Dv <= 256.  log_decay holds numbers <= 0 or -inf.  State and sums are fp32.  With bf16 tokens the weights of
+ * pairs of tokens and the state's copy that queries are multiplied with are rounded to bf16, as their partners are; the state itself is kept to 2^-16.
+ * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others.
+ * out_state may be the state; otherwise outputs overlap neither inputs nor each other.
+ */
+typedef struct { int64_t batch, token, head; } accerl_token_stride;
+
+typedef struct {
+    int64_t B, T;
+    int32_t H, Hk, Dk, Dv;
+    int32_t dtype;                 /* accerl_dtype of the tokens, and of their outputs and gradients */
+    const void *q, *k, *v;         /* DEVICE [B, T, H, Dk], [B, T, Hk, Dk], [B, T, Hk, Dv] */
+    accerl_token_stride q_stride, k_stride, v_stride;
+    const float* log_decay;        /* DEVICE [H] */
+    double scale;
+    const uint8_t* reset;          /* DEVICE [B, T] with strides, or NULL (no token resets) */
+    int64_t reset_batch, reset_token;
+    const int32_t* lengths;        /* DEVICE [B] or NULL */
+    const float* state;            /* DEVICE [B, H, Dk, Dv] or NULL (zeros) */
+    void* out;                     /* DEVICE [B, T, H, Dv] */
+    accerl_token_stride out_stride;
+    float* out_state;              /* DEVICE [B, H, Dk, Dv] or NULL (not wanted) */
+    /* gradients (accerl_linear_attention_grad; out and out_state are not looked at) */
+    const void* grad_out;          /* DEVICE [B, T, H, Dv] */
+    accerl_token_stride grad_out_stride;
+    const float* grad_out_state;   /* DEVICE [B, H, Dk, Dv] or NULL (zeros) */
+    void *grad_q, *grad_k, *grad_v;    /* shapes of q, k, v */
+    accerl_token_stride grad_q_stride, grad_k_stride, grad_v_stride;
+    float* grad_state;             /* DEVICE [B, H, Dk, Dv] or NULL (not wanted) */
+    void* workspace;               /* DEVICE, 16-byte aligned, of accerl_linear_attention_workspace's size; used as accerl_dense_i8_dynamic's */
+    int64_t workspace_bytes;
+} accerl_linear_attention_args;
+
+/* Bytes of the workspace of an unroll (grad == 0) or of its gradients; negative: an accerl_status. */
+int64_t accerl_linear_attention_workspace(int64_t B, int64_t T, int32_t H, int32_t Hk, int32_t Dk, int32_t Dv, int32_t grad);
+/* The unroll: out, and out_state behind the last token.  B == 0 enqueues nothing. */
+int accerl_linear_attention(const accerl_linear_attention_args* args, void* stream);
+/* The gradients of sum(grad_out . out) + sum(grad_out_state . out_state) by q, k, v and state; the decay is a constant. */
+int accerl_linear_attention_grad(const accerl_linear_attention_args* args, void* stream);
+/* One token for each of B environments: T, lengths, token strides and the workspace are not looked at, state and out_state are needed (they may be the
+ * same).  All arithmetic is fp32. */
+int accerl_linear_attention_step(const accerl_linear_attention_args* args, void* stream);
+
+typedef enum { ACCERL_NORM_RMS = 0, ACCERL_NORM_LAYER = 1 } accerl_norm_kind;             /* LAYER: the mean is taken off first */
+typedef enum { ACCERL_GATE_NONE = 0, ACCERL_GATE_SIGMOID = 1, ACCERL_GATE_SILU = 2 } accerl_gate_kind;
+
+/*
+ * The end of a block and the beginning of the next one, in one pass over the rows: the norm behind the block, its gate, the residual with
+ * its scales, and the norm before the next block.  For a row of D channels, y being the block's output and x the residual stream,
+ *     u = skip x + branch act(gate) after(y),    h = before(u)
+ *     norm(z)_i = weight_i (z_i - m) / sqrt(mean_j (z_j - m)^2 + eps),    m = 0 (RMS) or mean_j z_j (LAYER)
+ * `after` works on each of `groups` equal parts of a row by itself (the heads of an attention); `before` on the whole row, and with it
+ * groups is 1.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the gate.  1 <= D <= 16384.
+ * y, gate, h and their gradients have `dtype`; x, u and theirs `stream_dtype`, which is `dtype` or fp32.  Weights and their
+ * gradients are DEVICE fp32 [D].  Arithmetic is fp32; h is taken from u before u is rounded; results are rounded once.  Rows do not
+ * touch each other: a NaN stays in its row (and in the weights' gradients).  An output may lie over an input of the same type and stride, whole, and
+ * overlaps nothing else.
+ * Gradients: of sum(grad_u . u) + sum(grad_h . h), by y, x, gate and both weights (a pointer of NULL: not wanted; grad_u or grad_h NULL: zeros).
+ * They start from the forward's inputs: nothing is kept from the forward.  The weights' sums over rows have a fixed order.
+ * workspace: of accerl_block_norm_workspace's bytes, needed where gradients of weights are asked for; used as accerl_dense_i8_dynamic's.
+ */
+typedef struct {
+    int64_t N;                     /* rows */
+    int32_t D, groups;
+    int32_t kind, gate_kind;
+    int32_t dtype, stream_dtype;
+    double eps, skip, branch;
+    const void* y; int64_t ld_y;               /* DEVICE [N, D] each, rows `ld` elements apart */
+    const void* x; int64_t ld_x;
+    const void* gate; int64_t ld_gate;
+    const float *after, *before;
+    void* out_u; int64_t ld_u;                 /* NULL: not wanted */
+    void* out_h; int64_t ld_h;
+    const void* grad_u; int64_t ld_grad_u;
+    const void* grad_h; int64_t ld_grad_h;
+    void* grad_y; int64_t ld_grad_y;
+    void* grad_x; int64_t ld_grad_x;
+    void* grad_gate; int64_t ld_grad_gate;
+    float *grad_after, *grad_before;           /* [D] */
+    void* workspace;
+    int64_t workspace_bytes;
+} accerl_block_norm_args;
+
+int64_t accerl_block_norm_workspace(int64_t N, int32_t D, int32_t groups);
+int accerl_block_norm(const accerl_block_norm_args* args, void* stream);
+int accerl_block_norm_grad(const accerl_block_norm_args* args, void* stream);
+
+/*
  * Measurement aids (not part of the method): the ceilings the kernels are compared with, as this machine
  * sustains them.  accerl_probe_mfma runs 2048 workgroups x 4 wavefronts, each issuing iters x 8 independent
  * 16x16 MFMAs on registers (int8 16x16x64, or bf16 16x16x32 if bf16 != 0): ops = 2048 * 4 * iters * 8 *

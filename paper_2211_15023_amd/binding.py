@@ -1,6 +1,7 @@
 """Binding of include/accerl.h (ctypes; forwards, V-trace and the KL indicators through the compiled accerl_args): same names, argument marshalling only."""
 import contextlib
 import ctypes as C
+import math
 import os
 import threading
 
@@ -43,6 +44,29 @@ class _PolicyLossArgs(C.Structure):
                [(n, C.c_void_p) for n in ("actions", "old_logp", "advantages", "weights", "ref_logp")] + \
                [(n, C.c_double) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef", "scale")] + \
                [(n, C.c_void_p) for n in ("out_loss", "out_logp", "out_kl", "out_entropy", "out_stats", "workspace")] + [("workspace_bytes", C.c_int64)]
+
+
+class _TokenStride(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch", "token", "head")]
+
+
+class _LinearAttentionArgs(C.Structure):
+    _fields_ = [("B", C.c_int64), ("T", C.c_int64)] + [(n, C.c_int32) for n in ("H", "Hk", "Dk", "Dv", "dtype")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, _TokenStride) for n in ("q_stride", "k_stride", "v_stride")] + \
+               [("log_decay", C.c_void_p), ("scale", C.c_double), ("reset", C.c_void_p), ("reset_batch", C.c_int64), ("reset_token", C.c_int64),
+                ("lengths", C.c_void_p), ("state", C.c_void_p), ("out", C.c_void_p), ("out_stride", _TokenStride), ("out_state", C.c_void_p),
+                ("grad_out", C.c_void_p), ("grad_out_stride", _TokenStride), ("grad_out_state", C.c_void_p)] + \
+               [(n, C.c_void_p) for n in ("grad_q", "grad_k", "grad_v")] + [(n, _TokenStride) for n in ("grad_q_stride", "grad_k_stride", "grad_v_stride")] + \
+               [("grad_state", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class _BlockNormArgs(C.Structure):
+    _fields_ = [("N", C.c_int64)] + [(n, C.c_int32) for n in ("D", "groups", "kind", "gate_kind", "dtype", "stream_dtype")] + \
+               [(n, C.c_double) for n in ("eps", "skip", "branch")] + \
+               [f for n in ("y", "x", "gate") for f in ((n, C.c_void_p), (f"ld_{n}", C.c_int64))] + [("after", C.c_void_p), ("before", C.c_void_p)] + \
+               [f for n in ("u", "h") for f in ((f"out_{n}", C.c_void_p), (f"ld_{n}", C.c_int64))] + \
+               [f for n in ("grad_u", "grad_h", "grad_y", "grad_x", "grad_gate") for f in ((n, C.c_void_p), (f"ld_{n}", C.c_int64))] + \
+               [("grad_after", C.c_void_p), ("grad_before", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
 def load_library():
@@ -101,6 +125,14 @@ def load_library():
     lib.accerl_policy_loss_workspace.restype = i64
     lib.accerl_action_logprob.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp]
     lib.accerl_policy_loss.argtypes = [C.POINTER(_PolicyLossArgs), vp]
+    lib.accerl_linear_attention_workspace.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+    lib.accerl_linear_attention_workspace.restype = i64
+    for f in (lib.accerl_linear_attention, lib.accerl_linear_attention_grad, lib.accerl_linear_attention_step):
+        f.argtypes = [C.POINTER(_LinearAttentionArgs), vp]
+    lib.accerl_block_norm_workspace.argtypes = [i64, i32, i32]
+    lib.accerl_block_norm_workspace.restype = i64
+    for f in (lib.accerl_block_norm, lib.accerl_block_norm_grad):
+        f.argtypes = [C.POINTER(_BlockNormArgs), vp]
     lib.accerl_last_error.restype = C.c_char_p
     for f in ("accerl_blob_sizes", "accerl_policy_create", "accerl_actor_forward", "accerl_actor_forward_teacher",
               "accerl_actor_forward_recurrent", "accerl_actor_forward_debug", "accerl_profile_begin",
@@ -555,6 +587,159 @@ def accerl_policy_loss(logits, actions, old_logp, advantages, workspace, mask=No
         _check(lib.accerl_policy_loss(C.byref(a), _stream(stream)))
 
 
+# ---------------------------------------------------------------- operators of policies with a memory
+def _tokens(t, shape, dtype, what):
+    """Pointer and strides of a device tensor [B, T, heads, D] of this shape and type whose heads are contiguous."""
+    if t is None:
+        return None, _TokenStride()
+    if not t.is_cuda or t.dim() != 4 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} must be a CUDA/HIP tensor [B, T, heads, D]" + ("" if shape is None else f" of {tuple(shape)}"))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError(f"the heads of {what} must be contiguous")
+    return t.data_ptr(), _TokenStride(*(0 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()[:3])))
+
+
+def _state_of(t, shape, what):
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {tuple(shape)}")
+    return _ptr(t, torch.float32)
+
+
+def _attention(q, k, v, log_decay, scale, state, reset, lengths):
+    """The arguments that all calls share; tokens are [B, T, heads, D]."""
+    a = _LinearAttentionArgs()
+    a.q, a.q_stride = _tokens(q, None, None, "q")
+    a.dtype = _dtype(q)
+    a.B, a.T, a.H, a.Dk = q.shape
+    if k.dim() != 4 or v.dim() != 4 or k.shape[2] != v.shape[2]:
+        raise ValueError("k and v must be [B, T, heads, D] of as many heads")
+    a.Hk, a.Dv = k.shape[2], v.shape[3]
+    a.k, a.k_stride = _tokens(k, (a.B, a.T, a.Hk, a.Dk), q.dtype, "k")
+    a.v, a.v_stride = _tokens(v, (a.B, a.T, a.Hk, a.Dv), q.dtype, "v")
+    a.log_decay, a.scale = _vector(log_decay, torch.float32, a.H, "log_decay"), scale
+    if reset is not None:
+        if not reset.is_cuda or reset.dtype != torch.uint8 or tuple(reset.shape) != (a.B, a.T):
+            raise ValueError(f"reset must be a CUDA/HIP tensor of bytes [{a.B}, {a.T}]")
+        a.reset, a.reset_batch, a.reset_token = reset.data_ptr(), reset.stride(0), reset.stride(1)
+    a.lengths = _vector(lengths, torch.int32, a.B, "lengths")
+    a.state = _state_of(state, (a.B, a.H, a.Dk, a.Dv), "state")
+    return a
+
+
+def accerl_linear_attention_workspace(B, T, H, Hk, Dk, Dv, grad=False):
+    return _count(load_library().accerl_linear_attention_workspace(B, T, H, Hk, Dk, Dv, int(bool(grad))))
+
+
+def accerl_linear_attention(q, k, v, log_decay, out, workspace, scale=1.0, reset=None, lengths=None, state=None, out_state=None, stream=None):
+    """q [B, T, H, Dk], k [B, T, Hk, Dk], v [B, T, Hk, Dv] -> out [B, T, H, Dv]; workspace: uint8 tensor of accerl_linear_attention_workspace's bytes, or None
+    where that is 0."""
+    lib = load_library()
+    a = _attention(q, k, v, log_decay, scale, state, reset, lengths)
+    a.out, a.out_stride = _tokens(out, (a.B, a.T, a.H, a.Dv), q.dtype, "out")
+    a.out_state = _state_of(out_state, (a.B, a.H, a.Dk, a.Dv), "out_state")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _ptr(workspace, torch.uint8), workspace.numel()
+    with _device_of(q, k, v, log_decay, out, workspace, reset, lengths, state, out_state):
+        _check(lib.accerl_linear_attention(C.byref(a), _stream(stream)))
+
+
+def accerl_linear_attention_grad(grad_out, q, k, v, log_decay, grad_q, grad_k, grad_v, workspace, scale=1.0, reset=None, lengths=None, state=None,
+                                 grad_out_state=None, grad_state=None, stream=None):
+    lib = load_library()
+    a = _attention(q, k, v, log_decay, scale, state, reset, lengths)
+    a.grad_out, a.grad_out_stride = _tokens(grad_out, (a.B, a.T, a.H, a.Dv), q.dtype, "grad_out")
+    a.grad_q, a.grad_q_stride = _tokens(grad_q, q.shape, q.dtype, "grad_q")
+    a.grad_k, a.grad_k_stride = _tokens(grad_k, k.shape, q.dtype, "grad_k")
+    a.grad_v, a.grad_v_stride = _tokens(grad_v, v.shape, q.dtype, "grad_v")
+    a.grad_out_state = _state_of(grad_out_state, (a.B, a.H, a.Dk, a.Dv), "grad_out_state")
+    a.grad_state = _state_of(grad_state, (a.B, a.H, a.Dk, a.Dv), "grad_state")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _ptr(workspace, torch.uint8), workspace.numel()
+    with _device_of(q, k, v, log_decay, grad_out, grad_q, grad_k, grad_v, workspace, reset, lengths, state, grad_out_state, grad_state):
+        _check(lib.accerl_linear_attention_grad(C.byref(a), _stream(stream)))
+
+
+def accerl_linear_attention_step(q, k, v, log_decay, state, out, out_state, scale=1.0, reset=None, stream=None):
+    """One token: q [B, H, Dk], k [B, Hk, Dk], v [B, Hk, Dv] -> out [B, H, Dv]; reset [B]; out_state may be the state."""
+    lib = load_library()
+    a = _attention(*(_one_token(t, n) for t, n in ((q, "q"), (k, "k"), (v, "v"))), log_decay, scale, state, None if reset is None else reset.unsqueeze(1), None)
+    a.out, a.out_stride = _tokens(_one_token(out, "out"), (a.B, 1, a.H, a.Dv), q.dtype, "out")
+    a.out_state = _state_of(out_state, (a.B, a.H, a.Dk, a.Dv), "out_state")
+    with _device_of(q, k, v, log_decay, out, reset, state, out_state):
+        _check(lib.accerl_linear_attention_step(C.byref(a), _stream(stream)))
+
+
+def _one_token(t, what):
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [B, heads, D]")
+    return t.unsqueeze(1)
+
+
+NORM_KINDS = {"rms": 0, "layer": 1}
+GATE_KINDS = {None: 0, "sigmoid": 1, "silu": 2}
+
+
+def _block_norm(y, x, gate, after, before, kind, gate_kind, groups, eps, skip, branch):
+    a = _BlockNormArgs()
+    a.y, a.ld_y = _rows(y, "y")
+    a.N, a.D = y.shape
+    a.groups, a.kind, a.gate_kind = groups, NORM_KINDS[kind], GATE_KINDS[gate_kind]
+    a.dtype = _dtype(y)
+    a.stream_dtype = a.dtype if x is None else _dtype(x)
+    if (gate is None) != (gate_kind is None):
+        raise ValueError("a gate belongs to a kind of gate, and the other way round")
+    for n, t, dtype in (("x", x, None), ("gate", gate, y.dtype)):
+        p, ld = _rows_like(t, y, dtype, n)
+        setattr(a, n, p), setattr(a, f"ld_{n}", ld)
+    a.after, a.before = _vector(after, torch.float32, a.D, "after"), _vector(before, torch.float32, a.D, "before")
+    a.eps, a.skip, a.branch = eps, skip, branch
+    return a
+
+
+def _rows_like(t, y, dtype, what):
+    if t is not None and (t.shape != y.shape or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"{what} differs from the rows in shape or type")
+    return _rows(t, what)
+
+
+def accerl_block_norm_workspace(N, D, groups=1):
+    return _count(load_library().accerl_block_norm_workspace(N, D, groups))
+
+
+def accerl_block_norm(y, out_u, out_h, x=None, gate=None, after=None, before=None, kind="rms", gate_kind=None, groups=1, eps=1e-6, skip=1.0, branch=1.0, stream=None):
+    """u = skip x + branch act(gate) after(y) into out_u (or None), before(u) into out_h (with `before`)."""
+    lib = load_library()
+    a = _block_norm(y, x, gate, after, before, kind, gate_kind, groups, eps, skip, branch)
+    if x is None and out_u is not None:
+        a.stream_dtype = _dtype(out_u)
+    a.out_u, a.ld_u = _rows_like(out_u, y, None if x is None else x.dtype, "out_u")
+    a.out_h, a.ld_h = _rows_like(out_h, y, y.dtype, "out_h")
+    with _device_of(y, x, gate, after, before, out_u, out_h):
+        _check(lib.accerl_block_norm(C.byref(a), _stream(stream)))
+
+
+def accerl_block_norm_grad(y, workspace, x=None, gate=None, after=None, before=None, grad_u=None, grad_h=None, grad_y=None, grad_x=None, grad_gate=None,
+                           grad_after=None, grad_before=None, kind="rms", gate_kind=None, groups=1, eps=1e-6, skip=1.0, branch=1.0, stream=None):
+    """workspace: uint8 tensor of accerl_block_norm_workspace's bytes, or None where no gradient of a weight is asked for."""
+    lib = load_library()
+    a = _block_norm(y, x, gate, after, before, kind, gate_kind, groups, eps, skip, branch)
+    if x is None and grad_u is not None:
+        a.stream_dtype = _dtype(grad_u)
+    flow = None if x is None else x.dtype
+    for n, t, dtype in (("grad_u", grad_u, flow), ("grad_h", grad_h, y.dtype), ("grad_y", grad_y, y.dtype), ("grad_x", grad_x, flow), ("grad_gate", grad_gate, y.dtype)):
+        p, ld = _rows_like(t, y, dtype, n)
+        setattr(a, n, p), setattr(a, f"ld_{n}", ld)
+    a.grad_after, a.grad_before = _vector(grad_after, torch.float32, a.D, "grad_after"), _vector(grad_before, torch.float32, a.D, "grad_before")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _ptr(workspace, torch.uint8), workspace.numel()
+    with _device_of(y, x, gate, after, before, grad_u, grad_h, grad_y, grad_x, grad_gate, grad_after, grad_before, workspace):
+        _check(lib.accerl_block_norm_grad(C.byref(a), _stream(stream)))
+
+
 _CODES = {None: -1}         # output types of accerl_args, filled by load_library
 
 
@@ -745,6 +930,146 @@ class PolicyLoss:
             logp, ent = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
             accerl_action_logprob(logits, mask, actions, logp, ent, self._work.get(self._bytes, raw, logits.device), raw)
         return logp, ent
+
+
+class LinearAttention:
+    """Linear attention with a decay for each head, a memory for policies: owner of the decays, workspaces and outputs.
+
+    decay: a number in 0 .. 1 for each head of queries, a constant (it has no gradient).  An actor carries the state with `step`; a learner
+    unrolls the same tokens with `forward`, from the actor's state on, and takes gradients with `backward`.  Threads and streams may share one, as they may a DenseInt8.
+    """
+
+    class Result:
+        __slots__ = ("q", "k", "v", "state")
+
+    def __init__(self, decay, scale=1.0, device=None):
+        load_library()
+        if isinstance(decay, torch.Tensor):
+            device = decay.device if device is None and decay.is_cuda else device
+            decay = decay.detach().tolist()
+        decay = [float(d) for d in decay]
+        if not decay or not all(0.0 <= d <= 1.0 for d in decay):
+            raise ValueError("decays are numbers in 0 .. 1, one for each head")
+        self.H, self.scale = len(decay), float(scale)
+        self.log_decay = torch.tensor([math.log(d) if d else -math.inf for d in decay], dtype=torch.float32, device="cuda" if device is None else device)
+        self._work = _Workspaces()
+
+    def _heads(self, q, k, v, dims):
+        if not q.is_cuda or q.dim() != dims or k.dim() != dims or v.dim() != dims or q.shape[-2] != self.H:
+            raise ValueError(f"q, k and v must be CUDA/HIP tensors of {dims} dimensions, q of {self.H} heads")
+
+    def _workspace(self, q, k, v, grad, raw):
+        n = accerl_linear_attention_workspace(q.shape[0], q.shape[1], self.H, k.shape[2], q.shape[3], v.shape[3], grad)
+        return self._work.get(n, raw, q.device) if n else None
+
+    def forward(self, q, k, v, state=None, reset=None, lengths=None, out=None, out_state=None, stream=None):
+        """q [B, T, H, Dk], k [B, T, Hk, Dk], v [B, T, Hk, Dv] -> (out [B, T, H, Dv], state [B, H, Dk, Dv] behind the last token).
+
+        state: the one before the first token (None: zeros); reset: bytes [B, T], not 0 where a token begins an episode; lengths: int32 [B], tokens a
+        sequence has; out_state: where the state goes, the given one too (None: a new tensor)."""
+        self._heads(q, k, v, 4)
+        q, k, v = q.detach(), k.detach(), v.detach()
+        with _On(stream, q.device) as raw:
+            if out is None:
+                out = torch.empty((*q.shape[:3], v.shape[3]), dtype=q.dtype, device=q.device)
+            if out_state is None:
+                out_state = torch.empty((q.shape[0], self.H, q.shape[3], v.shape[3]), dtype=torch.float32, device=q.device)
+            accerl_linear_attention(q, k, v, self.log_decay, out, self._workspace(q, k, v, False, raw), self.scale, reset, lengths, state, out_state, raw)
+        return out, out_state
+
+    def backward(self, grad_out, q, k, v, state=None, reset=None, lengths=None, grad_state=None, stream=None):
+        """Gradients by q, k, v and (if it was given) the state, of what `forward` of these arguments returns: grad_out by its output, grad_state by
+        the state it returns (None: zeros).  `torch.autograd.backward([q, k, v], [r.q, r.k, r.v])` continues them."""
+        self._heads(q, k, v, 4)
+        q, k, v = q.detach(), k.detach(), v.detach()
+        r = self.Result()
+        with _On(stream, q.device) as raw:
+            r.q, r.k, r.v = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+            r.state = None if state is None else torch.empty(state.shape, dtype=torch.float32, device=q.device)
+            accerl_linear_attention_grad(grad_out, q, k, v, self.log_decay, r.q, r.k, r.v, self._workspace(q, k, v, True, raw), self.scale, reset, lengths, state,
+                                         grad_state, r.state, raw)
+        return r
+
+    def step(self, q, k, v, state, reset=None, out=None, out_state=None, stream=None):
+        """One token of each environment: q [B, H, Dk], k [B, Hk, Dk], v [B, Hk, Dv] -> out [B, H, Dv].  The state is updated in place, or goes to out_state."""
+        self._heads(q, k, v, 3)
+        q, k, v = q.detach(), k.detach(), v.detach()
+        with _On(stream, q.device) as raw:
+            if out is None:
+                out = torch.empty((*q.shape[:2], v.shape[2]), dtype=q.dtype, device=q.device)
+            accerl_linear_attention_step(q, k, v, self.log_decay, state, out, state if out_state is None else out_state, self.scale, reset, raw)
+        return out
+
+
+class BlockNorm:
+    """The end of a block and the beginning of the next one, u = skip x + branch act(gate) after(y) and h = before(u): owner of the norms' weights,
+    workspaces and outputs.
+
+    D: channels; after, before: the weights [D] of the norm behind the block and of the one before the next block (None: without that norm), which are copied;
+    kind: "rms" or "layer" (the mean is taken off first); gate: None, "sigmoid" or "silu"; groups: equal parts of a row that `after` norms each by itself.
+    Threads and streams may share one, as they may a DenseInt8.
+    """
+
+    class Result:
+        __slots__ = ("y", "x", "gate", "after", "before")
+
+    def __init__(self, D, after=None, before=None, kind="rms", gate=None, groups=1, eps=1e-6, skip=1.0, branch=1.0):
+        load_library()
+        accerl_block_norm_workspace(0, D, groups)             # (refuses what no call can take)
+        if groups > 1 and before is not None:
+            raise ValueError("groups are for calls without the norm before the next block")
+        if kind not in NORM_KINDS or gate not in GATE_KINDS:
+            raise ValueError("unknown kind of norm or gate")
+        self.D = D
+        self.how = dict(kind=kind, gate_kind=gate, groups=groups, eps=float(eps), skip=float(skip), branch=float(branch))
+        for n, w in (("after", after), ("before", before)):
+            if w is not None and tuple(w.shape) != (D,):
+                raise ValueError(f"{n} must be a vector of {D}")
+            setattr(self, n, None if w is None else w.detach().to(w.device if w.is_cuda else "cuda", torch.float32, copy=True).contiguous())
+        self._work = _Workspaces()
+
+    def update(self, after=None, before=None):
+        """New weights (a learner's, after its step), on the current stream; calls of other streams or threads that are not ordered with it may see some of both."""
+        for n, w in (("after", after), ("before", before)):
+            if w is not None and (getattr(self, n) is None or tuple(w.shape) != (self.D,)):
+                raise ValueError(f"{n} differs in shape from the owner's")
+        for n, w in (("after", after), ("before", before)):
+            if w is not None:
+                getattr(self, n).copy_(w.detach())
+
+    def _input(self, y):
+        if not y.is_cuda or y.dim() != 2 or y.shape[1] != self.D:
+            raise ValueError(f"y must be a CUDA/HIP matrix of {self.D} columns")
+        return y.detach()
+
+    def forward(self, y, x=None, gate=None, u=None, h=None, stream=None):
+        """y, x, gate [N, D] -> (u, h): u of x's type (of y's without x), h of y's, None without `before`.  u, h: tables to write to, x and y themselves too."""
+        y = self._input(y)
+        x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
+        with _On(stream, y.device) as raw:
+            if u is None:
+                u = torch.empty(y.shape, dtype=y.dtype if x is None else x.dtype, device=y.device)
+            if h is None and self.before is not None:
+                h = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+            accerl_block_norm(y, u, h if self.before is not None else None, x, gate, self.after, self.before, stream=raw, **self.how)
+        return u, h if self.before is not None else None
+
+    def backward(self, y, x=None, gate=None, grad_u=None, grad_h=None, stream=None):
+        """Gradients of what `forward` of these arguments returns, by y, x, gate and the weights (fp32), None where there is nothing to have one; grad_u by
+        u, grad_h by h (None: zeros)."""
+        y = self._input(y)
+        x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
+        if grad_h is not None and self.before is None:
+            raise ValueError("grad_h belongs to the norm before the next block")
+        r = self.Result()
+        with _On(stream, y.device) as raw:
+            like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+            r.y, r.x, r.gate, r.after, r.before = like(y), like(x), like(gate), like(self.after), like(self.before)
+            ws = None
+            if r.after is not None or r.before is not None:
+                ws = self._work.get(accerl_block_norm_workspace(y.shape[0], self.D, self.how["groups"]), raw, y.device)
+            accerl_block_norm_grad(y, ws, x, gate, self.after, self.before, grad_u, grad_h, r.y, r.x, r.gate, r.after, r.before, stream=raw, **self.how)
+        return r
 
 
 STEP_KINDS = ("mlp_fused", "quant_obs", "conv", "gemm", "gemm_f32", "maxpool", "lstm_pack", "sample", "heads")
