@@ -10,6 +10,7 @@
 // and the chunk's last state is g^64 E_before + sum_s g^{63-s} b_s c_s^T: four matrix products.
 #include <algorithm>
 #include <cstdio>
+#include <type_traits>
 
 #include "wide_ops.h"
 
@@ -51,13 +52,12 @@ struct LaParams {
     uint32_t groups;                      // B H segs
 };
 
-// The element types of the matrix products: bf16 tokens as they are, others as fp32.
-template <typename T> struct LaCompute { typedef float E; static constexpr bool HALF = false; };
-template <> struct LaCompute<BF16> { typedef BF16 E; static constexpr bool HALF = true; };
-
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 // g^n of lg = log2 g, which may be -inf
 __device__ __forceinline__ float decay_pow(float lg, int n) { return n == 0 ? 1.0f : pow2(lg * (float)n); }
+
+// the same number of all lanes, in a scalar register
+__device__ __forceinline__ float everywhere(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 // 16 bytes of a row of which `left` elements are inside; the others are zeros
 template <typename T> __device__ __forceinline__ u32x4 row_vec(const T* p, int left) {
@@ -78,381 +78,786 @@ template <typename T> __device__ __forceinline__ u32x4 row_vec(const T* p, int l
     return v;
 }
 
-// largest magnitude so far, as bits: halves of a word (bf16) or words
-template <bool HALF> __device__ __forceinline__ void keep_top(uint32_t& top, uint32_t w) {
-    if constexpr (HALF) {
-        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-        top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, top), __builtin_bit_cast(us2, w & 0x7fff7fffu)));
-    } else {
-        top = max(top, w & 0x7fffffffu);
+// Which work a workgroup has.  Workgroups go round the eight XCDs: the slices of a sequence, which read the same a and b, lie eight apart.
+struct LaPlace { bool mine; uint32_t which, slice, seg, bh; };
+__device__ __forceinline__ LaPlace la_place(const LaParams& p) {
+    LaPlace a;
+    const uint32_t id = blockIdx.x, slices = p.role[0].slices + p.role[1].slices + p.role[2].slices, grp = id / (8 * slices) * 8 + id % 8;
+    a.mine = grp < p.groups;
+    a.slice = id / 8 % slices;
+    a.which = 0;
+    while (a.slice >= (uint32_t)p.role[a.which].slices) a.slice -= p.role[a.which++].slices;
+    a.seg = grp % p.segs;
+    a.bh = grp / p.segs;
+    return a;
+}
+// A lane's part of a state: rows x + 16 ta + i, columns y0 + y + the tile's first, which is 16 d or, dealt out by fours (STEP 4), 64 (d / 4) + 4 (d % 4).
+template <int STEP> __device__ __forceinline__ constexpr int la_column(int d) { return STEP == 4 ? 64 * (d / 4) + 4 * (d % 4) : STEP * d; }
+template <int NA, int ND, int STEP, bool FULL>
+__device__ __forceinline__ void la_state_in(const LaRole& q, uint32_t seg, uint32_t bh, int x, int y0, int y, int X, int yw, v4f (&S)[NA][ND]) {
+#pragma unroll
+    for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+    if (!q.enter) return;
+    const float* e = q.enter + seg * q.eseg + (int64_t)bh * q.X * q.Y + x * q.ex + (y0 + y) * q.ey;
+#pragma unroll
+    for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (FULL || (x + 16 * ta + i < X && y + la_column<STEP>(d) < yw)) S[ta][d][i] = e[(16 * ta + i) * q.ex + la_column<STEP>(d) * q.ey];
+}
+template <int NA, int ND, int STEP, bool FULL>
+__device__ __forceinline__ void la_state_out(const LaRole& q, uint32_t seg, uint32_t bh, int x, int y0, int y, int X, int yw, bool gone, const v4f (&S)[NA][ND]) {
+    float* e = q.last + seg * q.lseg + (int64_t)bh * q.X * q.Y + x * q.lx + (y0 + y) * q.ly;
+#pragma unroll
+    for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (FULL || (x + 16 * ta + i < X && y + la_column<STEP>(d) < yw)) e[(16 * ta + i) * q.lx + la_column<STEP>(d) * q.ly] = gone ? 0.0f : S[ta][d][i];
+}
+
+// outputs of tokens behind the sequence's end
+template <typename T, int NW> __device__ __forceinline__ void la_behind(const LaParams& p, const LaRole& q, const LaPlace& at, int64_t n, int64_t i0, int y0, int yw) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t i = max(i0, n) + (threadIdx.x >> 6); i < min(p.T, i0 + p.seg_len); i += NW) {
+        const int64_t o = (at.bh / p.H) * q.ob + (int64_t)(at.bh % p.H) * q.oh + i * q.ot + y0;
+        for (int y = lane; y < yw; y += 64) {
+            if (q.out_f32) ((float*)q.out)[o + y] = 0.0f;
+            else ((T*)q.out)[o + y] = T{};
+        }
     }
 }
-template <bool HALF> __device__ __forceinline__ bool not_finite(uint32_t top) {
-    return HALF ? (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u : top >= 0x7f800000u;
-}
 
-template <typename T, int DX>
-struct LaTile {
-    typedef typename LaCompute<T>::E E;
-    static constexpr bool HALF = LaCompute<T>::HALF;
-    // rows 16 bytes further on in the banks: a quarter wavefront's 16-byte reads of 16 rows meet no bank twice.  c is only read down its columns
-    // (bf16: transposing reads of four rows, which 32 bytes keep apart)
-    static constexpr int BP = DX + 16 / (int)sizeof(E);
-    static constexpr int CP = HALF ? LY + 16 : LY + 4;
-    static constexpr int VE = 16 / (int)sizeof(T);            // elements of a vector in memory
-    static constexpr int BV = LC * DX / VE / 256, CV = LC * LY / VE / 256;
-    static constexpr int FR = HALF ? 32 : 16;                 // depth of a fragment
-    static constexpr int KX = DX / FR;
+// ---------------------------------------------------------------- tokens of 16 bits
+// bf16 tokens are operands as they are.  fp16 tokens are split into two bf16 parts where fp16 could not hold what they meet (weights of pairs, the state: any
+// size), and the first and second order products taken.
+template <typename T, int DX, int NW>
+struct LaHalf {
+    static constexpr bool SPLIT = __is_same(T, F16);
+    static constexpr int PARTS = SPLIT ? 2 : 1;
+    static constexpr uint32_t INF = SPLIT ? 0x7c00u : 0x7f80u;
+    // rows 16 bytes further on in the banks: a quarter wavefront's 16-byte reads of 16 rows meet no bank twice; and c's rows 8 bytes, for reads down its columns
+    static constexpr int YW = 16 * NW;                        // columns of a workgroup
+    static constexpr int BP = DX + 8, CP = YW + 4;
+    static constexpr int BV = DX / 8 / NW, CV = YW / 8 / NW;  // vectors of a lane
+    static constexpr int NA = DX / 16 / NW, ND = NW;          // tiles of 16 rows and 16 columns of the state for a wavefront
+    static constexpr int KX = DX / 32;                        // depth of the products over X in matrix instructions
+    static constexpr int WAVES = NW == 8 ? 2 : SPLIT ? (DX == 256 ? 1 : 2) : DX == 64 ? 3 : DX == 128 ? 2 : 1;      // of a SIMD
+    static constexpr int CT = LC * CP, SF = DX * YW;          // elements of a part of c's tile and of the state's fragments
 };
 
-template <typename T, int DX, bool OUT>
-__global__ __launch_bounds__(256, LaCompute<T>::HALF ? 2 : 1) void la_chunks_kernel(const LaParams p) {
-    typedef LaTile<T, DX> L;
-    typedef typename L::E E;
-    constexpr bool HALF = L::HALF;
-    constexpr int NA = DX / 64;                               // tiles of 16 rows of the state for a wavefront
-
-    __shared__ __attribute__((aligned(16))) E sb[LC * L::BP];
-    __shared__ __attribute__((aligned(16))) E sc[LC * L::CP];
-    // the state as the fragments that the product with a reads: [column tile][depth][lane]
-    __shared__ __attribute__((aligned(16))) E ss[OUT ? DX * LY : 16];
-    __shared__ int odd[4];                                    // whether a wavefront has seen a NaN or an infinity in b or c
-    __shared__ float red[4][LY];
-
-    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, g = lane >> 4, r = lane & 15;
-    // workgroups go round the eight XCDs: the slices of a sequence, which read the same a and b, lie eight apart
-    uint32_t id = blockIdx.x, which = 0, slice = 0;
-    int slices = 0;
+__device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+__device__ __forceinline__ float cut16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+// eight values as the sum of N bf16 parts, each cut off behind 8 bits (N = 3: exactly) and the last of two rounded
+template <int N> __device__ __forceinline__ void parts8(const float* x, v8bf* to) {
+    u32x4 p[N];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) slices += p.role[i].slices;
-    const uint32_t grp = id / (8 * slices) * 8 + id % 8;
-    slice = id / 8 % slices;
-    if (grp >= p.groups) return;
-    while (slice >= (uint32_t)p.role[which].slices) slice -= p.role[which++].slices;
-    const LaRole& q = p.role[which];
-    const int X = q.X, Y = q.Y, y0 = slice * LY;
-    const uint32_t seg = grp % p.segs, bh = grp / p.segs;
-    const uint32_t b = bh / p.H, h = bh % p.H;
-    const int back = q.back;
+    for (int j = 0; j < 4; ++j) {
+        float a = x[2 * j], b = x[2 * j + 1];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            p[k][j] = k == 1 && N == 2 ? f32_pair<BF16>(a, b) : high_halves(a, b);
+            a -= cut16(a);
+            b -= cut16(b);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) to[k] = __builtin_bit_cast(v8bf, p[k]);
+}
+template <typename T> __device__ __forceinline__ void unpack8(u32x4 w, float* x) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) el_pair<T>(w[j], x[2 * j], x[2 * j + 1]);
+}
+__device__ __forceinline__ v4f mma(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+template <typename T> __device__ __forceinline__ v4f mma_as(u32x4 a, u32x4 b, v4f c) {
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    if constexpr (__is_same(T, BF16)) return mma(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
 
+// FULL: heads of exactly DX and slices of exactly LY elements, whose loads need no look at where a row ends.  OUT: the mixing; else the state behind the
+// segment alone.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its end) and the tables hold for all.
+template <typename T, int DX, int NW, bool OUT, bool FULL>
+__global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_kernel(const LaParams p) {
+    typedef LaHalf<T, DX, NW> L;
+    constexpr int NA = L::NA, ND = L::ND;
+
+    __shared__ __attribute__((aligned(16))) uint16_t sb[LC * L::BP];
+    __shared__ __attribute__((aligned(16))) uint16_t sc[L::PARTS * L::CT];
+    // the state as the fragments that the product with a reads: [part][column tile][depth][lane][8]
+    __shared__ __attribute__((aligned(16))) uint16_t ss[OUT ? L::PARTS * L::SF : 8];
+    __shared__ int odd[NW];                                   // whether a wavefront has seen a NaN or an infinity in b or c
+    __shared__ float red[NW][L::YW];
+
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const LaPlace at = la_place(p);
+    if (!at.mine) return;
+    const LaRole& q = p.role[at.which];
+    const int X = FULL ? DX : q.X, Y = q.Y, y0 = at.slice * L::YW, yw = FULL ? L::YW : min(Y - y0, L::YW), back = q.back;
+    const uint32_t seg = at.seg, bh = at.bh, b = bh / p.H, h = bh % p.H;
     int64_t n = p.T;
     if (p.lengths) n = min(max((int64_t)p.lengths[b], (int64_t)0), n);
     const int64_t i0 = seg * p.seg_len, i1 = min(n, i0 + p.seg_len);
+    const int chunks = i1 > i0 ? (int)((i1 - i0 + LC - 1) / LC) : 0;
+    const int64_t base0 = i1 - (int64_t)chunks * LC;          // of the first chunk; its tokens from `gap` on are there
+    const int gap = (int)(i0 - base0);
     const float lg = p.log_decay[h] * LOG2E;
-    const T* pa = (const T*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh;
-    const T* pb = (const T*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh;
-    const T* pc = (const T*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + y0;
-    const int yw = min(Y - y0, LY);                           // columns of the slice
+    // tokens in this order: token i lies i strides behind the first
+    const int64_t tb = back ? -q.b.st : q.b.st, tc = back ? -q.c.st : q.c.st, ta_ = back ? -q.a.st : q.a.st, to = back ? -q.ot : q.ot;
+    const int64_t t0 = back ? n - 1 : 0;
+    const T* pb = (const T*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh + t0 * q.b.st + base0 * tb;
+    const T* pc = (const T*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + t0 * q.c.st + base0 * tc + y0;
+    const T* pa = (const T*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh + t0 * q.a.st + base0 * ta_;
+    const int64_t po = b * q.ob + (int64_t)h * q.oh + t0 * q.ot + base0 * to + y0;
 
-    // the state: rows 16 (NA w + ta) + 4 g + i, columns 16 d + r
-    v4f S[NA][4];
-    {
-        const float* e = q.enter ? q.enter + seg * q.eseg + (int64_t)bh * X * Y : nullptr;
+    // The state's columns are dealt out so that a lane's results of four column tiles lie side by side: tile d, column r is 64 (d / 4) + 16 (r / 4) + 4 (d % 4) + r % 4
+    const int yr = 16 * (r >> 2) + (r & 3);
+    v4f S[NA][ND];
+    la_state_in<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, S);
+    // Every wavefront has its rows of the state, and a tile of 16 tokens by 64 columns (`half` of eight wavefronts' 128) of the output
+    const int wq = w & 3, half = w >> 2;
+    // Weights g^(t-s) of pairs s = 16 st + 4 g + i, t = 16 w + r: on the diagonal their own, below it near[i] far[st], of which neither is a negative power;
+    // and of token s in the state behind the chunk, tail[i] block[st]
+    const int t = 16 * wq + r;
+    float diag[4], near[4], far[3], tail[4], block[4];
 #pragma unroll
-        for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int x = 16 * (NA * w + ta) + 4 * g + i, y = y0 + 16 * d + r;
-                    S[ta][d][i] = e && x < X && y < Y ? e[x * q.ex + y * q.ey] : 0.0f;
-                }
+    for (int i = 0; i < 4; ++i) {
+        const int s = 4 * g + i;
+        diag[i] = s <= r ? decay_pow(lg, r - s) * (q.pair * q.scale) : 0.0f;
+        near[i] = decay_pow(lg, r - s + 15) * (q.pair * q.scale);
+        tail[i] = decay_pow(lg, 15 - s) * q.pair;
+        block[i] = everywhere(decay_pow(lg, 48 - 16 * i + back));
     }
-    // tables of a whole chunk: weights of pairs (tokens s = 16 st + 4 g + i, t = 16 w + r), of the state for token t, of token s for the state
-    float dec[4][4], kw[4][4];
-    const int t = 16 * w + r;
-    float qw = decay_pow(lg, t + 1 - back);
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = 16 * st + 4 * g + i;
-            dec[st][i] = s <= t ? decay_pow(lg, t - s) * q.pair : 0.0f;
-            kw[st][i] = decay_pow(lg, LC - 1 - s + back) * q.pair;
-        }
+    for (int st = 0; st < 3; ++st) far[st] = everywhere(decay_pow(lg, max(16 * (wq - st) - 15, 0)));
+    float qw = decay_pow(lg, max(t - gap, 0) + 1 - back) * q.scale, sd = everywhere(decay_pow(lg, LC - gap));      // (the first chunk's)
     float left = 1.0f;                                        // of the segment's first state
 
-    u32x4 vb[L::BV], vc[L::CV];
+    const int brow = tid / (DX / 8), bcol = tid % (DX / 8) * 8, crow = tid / (L::YW / 8), ccol = tid % (L::YW / 8) * 8;
+    constexpr int BR = 512 * NW / DX, CR = 512 * NW / L::YW;             // rows from one vector of a lane to its next
+    u32x4 vb[L::BV], vc[L::CV], va[OUT ? L::KX : 1];
     uint32_t cut = 0;
-    auto token = [&](int64_t i) { return back ? n - 1 - i : i; };
-    auto fetch = [&](int64_t base) {
+    // Pointers of a lane's rows, which go on by a chunk with every fetch.  In the first chunk rows that are not there count as the first that is.
+    const T *lb = pb + brow * tb + bcol, *lc = pc + crow * tc + ccol, *la = pa + t * ta_ + 8 * g;
+    auto fetch = [&](int c, auto first) {
+        constexpr bool FIRST = decltype(first)::value;
 #pragma unroll
         for (int k = 0; k < L::BV; ++k) {
-            const int v = tid + 256 * k, row = v / (DX / L::VE), col = v % (DX / L::VE) * L::VE;
-            const int64_t i = base + row;
-            vb[k] = row_vec(pb + (i < i1 ? token(i) * q.b.st + col : 0), i < i1 ? X - col : 0);
+            const T* f = lb + k * BR * tb;
+            if constexpr (FIRST) f += max(gap - brow - k * BR, 0) * tb;
+            vb[k] = FULL ? *(const u32x4_at2*)f : row_vec(bcol < X ? f : pb + gap * tb, X - bcol);
         }
 #pragma unroll
         for (int k = 0; k < L::CV; ++k) {
-            const int v = tid + 256 * k, row = v / (LY / L::VE), col = v % (LY / L::VE) * L::VE;
-            const int64_t i = base + row;
-            vc[k] = row_vec(pc + (i < i1 ? token(i) * q.c.st + col : 0), i < i1 ? yw - col : 0);
+            const T* f = lc + k * CR * tc;
+            if constexpr (FIRST) f += max(gap - crow - k * CR, 0) * tc;
+            vc[k] = FULL ? *(const u32x4_at2*)f : row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol);
         }
-        // does token i = base + lane start from nothing?  (backwards: does the token before it in this order, the one behind it)
+        lb += LC * tb;
+        lc += LC * tc;
+        // does the token of this lane start from nothing?  (backwards: does the one behind it in time)
         cut = 0;
         if (p.reset) {
-            const int64_t i = base + lane, at = back ? n - i : i;
-            if (i < i1 && !(back && i == 0)) cut = p.reset[b * p.rb + at * p.rt];
+            const int64_t i = base0 + (int64_t)c * LC + lane, tok = back ? n - i : i;
+            if (i >= i0 && !(back && i == 0)) cut = p.reset[b * p.rb + tok * p.rt];
         }
     };
-    auto stage = [&]() {
-        uint32_t top = 0;
-        auto put = [&](E* to, u32x4 v) {
-            if constexpr (__is_same(T, F16)) {
-                float f[8];
+    // this wavefront's 16 tokens of a, straight from memory
+    auto fetch_a = [&](auto first) {
+        if constexpr (OUT) {
+            const T* f = la;
+            if constexpr (decltype(first)::value) f += max(gap - t, 0) * ta_;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) el_pair<F16>(v[j], f[2 * j], f[2 * j + 1]);
+            for (int k = 0; k < L::KX; ++k) va[k] = FULL ? *(const u32x4_at2*)(f + 32 * k) : row_vec(8 * g + 32 * k < X ? f + 32 * k : f - 8 * g, X - 32 * k - 8 * g);
+            la += LC * ta_;
+        }
+    };
+    const std::true_type is_first;
+    const std::false_type later;
+    auto stage = [&](int c) {
+        if (c == 0 && gap) {
+            const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) keep_top<false>(top, __float_as_uint(f[j]));
-                *(v4f*)to = v4f{f[0], f[1], f[2], f[3]};
-                *(v4f*)(to + 4) = v4f{f[4], f[5], f[6], f[7]};
-            } else {
+            for (int k = 0; k < L::BV; ++k) if (brow + k * BR < gap) vb[k] = none;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) keep_top<HALF>(top, v[j]);
-                *(u32x4*)to = v;
-            }
+            for (int k = 0; k < L::CV; ++k) if (crow + k * CR < gap) vc[k] = none;
+        }
+        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+        us2 top = {0, 0};
+        auto look = [&](u32x4 v) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
         };
 #pragma unroll
         for (int k = 0; k < L::BV; ++k) {
-            const int v = tid + 256 * k;
-            put(sb + v / (DX / L::VE) * L::BP + v % (DX / L::VE) * L::VE, vb[k]);
+            look(vb[k]);
+            *(u32x4*)(sb + (brow + k * BR) * L::BP + bcol) = vb[k];
         }
 #pragma unroll
         for (int k = 0; k < L::CV; ++k) {
-            const int v = tid + 256 * k;
-            put(sc + v / (LY / L::VE) * L::CP + v % (LY / L::VE) * L::VE, vc[k]);
+            look(vc[k]);
+            uint16_t* o = sc + (crow + k * CR) * L::CP + ccol;
+            if constexpr (L::SPLIT) {
+                float x[8];
+                v8bf part[2];
+                unpack8<T>(vc[k], x);
+                parts8<2>(x, part);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 v = __builtin_bit_cast(u32x4, part[i]);
+                    *(u32x2*)(o + i * L::CT) = u32x2{v[0], v[1]};
+                    *(u32x2*)(o + i * L::CT + 4) = u32x2{v[2], v[3]};
+                }
+            } else {
+                *(u32x2*)o = u32x2{vc[k][0], vc[k][1]};
+                *(u32x2*)(o + 4) = u32x2{vc[k][2], vc[k][3]};
+            }
         }
-        const bool any = __ballot(not_finite<HALF>(top)) != 0;
+        const bool any = __ballot(max((uint32_t)top[0], (uint32_t)top[1]) >= L::INF) != 0;
+        if (lane == 0) odd[w] = any;
+    };
+    auto publish = [&](int first) {
+        if constexpr (OUT && L::SPLIT) {
+            // (an infinity has no second part; a state that the chunk's first token ends may be anything)
+            uint32_t top = 0;
+            if (__ballot(cut != 0) >> first & 1)
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(S[ta][d][i]) & 0x7fffffffu);
+            if (__ballot(top >= 0x7f800000u) && lane == 0) odd[w] = 1;
+        }
+        if constexpr (OUT)
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta) {
+                const int tile = NA * w + ta, quad = 4 * (tile & 1) + g;    // rows 4 quad .. of the 32 of a fragment belong to lane group quad / 2
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    uint16_t* o = ss + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
+                    const v4f s = S[ta][d];
+                    if constexpr (L::SPLIT) {
+                        *(u32x2*)o = u32x2{high_halves(s[0], s[1]), high_halves(s[2], s[3])};
+                        *(u32x2*)(o + L::SF) = u32x2{f32_pair<BF16>(s[0] - cut16(s[0]), s[1] - cut16(s[1])), f32_pair<BF16>(s[2] - cut16(s[2]), s[3] - cut16(s[3]))};
+                    } else {
+                        *(u32x2*)o = u32x2{f32_pair<BF16>(s[0], s[1]), f32_pair<BF16>(s[2], s[3])};
+                    }
+                }
+            }
+    };
+    // Four rows of four columns each are turned by a read of 16 lanes: each has a column, down four tokens; two reads make the eight of a fragment of 32 tokens
+    typedef __attribute__((address_space(3))) v4s lds4;
+    auto down = [&](const uint16_t* from, int rows16) {
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(from + rows16));
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const uint16_t* down_b = sb + (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w;
+    const uint16_t* down_c = sc + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
+
+    if (chunks) { fetch(0, is_first); fetch_a(is_first); stage(0); publish(gap); }
+    for (int c = 0; c < chunks; ++c) {
+        const uint64_t cuts = __ballot(cut != 0);
+        __syncthreads();
+        const bool more = c + 1 < chunks;
+        // (kept as they are: their products, worked out ahead of the loop, would take 28 registers)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
+        if (more) fetch(c + 1, later);
+        __builtin_amdgcn_sched_barrier(0);
+        int seen = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) seen |= odd[i];
+        const bool plain = !seen;
+        const int last_cut = cuts ? 63 - __builtin_clzll(cuts) : -1;
+
+        if (plain) {
+            v4f O[4];
+            v8bf pt[2][L::PARTS];                             // weights of pairs as the product with c reads them
+            if constexpr (OUT) {
+                v4f P[4];
+#pragma unroll
+                for (int st = 0; st < 4; ++st) P[st] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < L::KX; ++k) {
+                    v8bf fa[L::PARTS];
+                    if constexpr (L::SPLIT) {
+                        float x[8];
+                        unpack8<T>(va[k], x);
+                        parts8<2>(x, fa);
+                    } else {
+                        fa[0] = __builtin_bit_cast(v8bf, va[k]);
+                    }
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const uint16_t* f = ss + (((4 * half + d) * L::KX + k) * 64 + lane) * 8;
+                        if constexpr (L::SPLIT) {
+                            O[d] = mma(*(const v8bf*)(f + L::SF), fa[0], O[d]);
+                            O[d] = mma(*(const v8bf*)f, fa[1], O[d]);
+                        }
+                        O[d] = mma(*(const v8bf*)f, fa[0], O[d]);
+                    }
+                }
+#pragma unroll
+                for (int st = 0; st < 4; ++st)
+                    if (st <= wq)
+#pragma unroll
+                        for (int k = 0; k < L::KX; ++k) P[st] = mma_as<T>(*(const u32x4*)(sb + (16 * st + r) * L::BP + 32 * k + 8 * g), va[k], P[st]);
+                if (more) fetch_a(later);
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) O[d][i] *= qw;
+                float wt[4][4];
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wt[st][i] = 0.0f;
+                    if (st == wq) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * diag[i];
+                    } else if (st < wq) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * (near[i] * far[st < 3 ? st : 0]);
+                    }
+                }
+                if (cuts) {
+                    const uint64_t before = cuts & ((2ull << t) - 1);
+                    const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
+                    // (selected, not multiplied by 0: the state of the episode before may hold anything)
+                    if (first >= 0)
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
+#pragma unroll
+                    for (int st = 0; st < 4; ++st)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (16 * st + 4 * g + i < first) wt[st][i] = 0.0f;
+                }
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    const float* x = wt[2 * ks];
+                    if constexpr (L::SPLIT) parts8<2>(x, pt[ks]);
+                    else pt[ks][0] = __builtin_bit_cast(v8bf, u32x4{f32_pair<BF16>(x[0], x[1]), f32_pair<BF16>(x[2], x[3]), f32_pair<BF16>(x[4], x[5]), f32_pair<BF16>(x[6], x[7])});
+                }
+            }
+            if constexpr (OUT) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (2 * ks <= wq)
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) {
+                            v8bf fc[L::PARTS];
+#pragma unroll
+                            for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * half + 4 * d, 16 * L::CP));
+                            if constexpr (L::SPLIT) {
+                                O[d] = mma(fc[1], pt[ks][0], O[d]);
+                                O[d] = mma(fc[0], pt[ks][1], O[d]);
+                            }
+                            O[d] = mma(fc[0], pt[ks][0], O[d]);
+                        }
+                if (c || t >= gap) {
+                    const int64_t o = po + ((int64_t)c * LC + t) * to + 64 * half + 16 * g;
+                    float v[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = O[j / 4][j % 4];
+                    if (q.out_f32) {
+                        float* f = (float*)q.out + o;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) {
+                            if (FULL || 64 * half + 16 * g + 4 * d + 4 <= yw) *(u32x4_at4*)(f + 4 * d) = __builtin_bit_cast(u32x4, v4f{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]});
+                            else
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) if (64 * half + 16 * g + 4 * d + i < yw) f[4 * d + i] = v[4 * d + i];
+                        }
+                    } else {
+                        T* f = (T*)q.out + o;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float* x = v + 8 * e;
+                            if (FULL || 64 * half + 16 * g + 8 * e + 8 <= yw)
+                                *(u32x4_at2*)(f + 8 * e) = u32x4{f32_pair<T>(x[0], x[1]), f32_pair<T>(x[2], x[3]), f32_pair<T>(x[4], x[5]), f32_pair<T>(x[6], x[7])};
+                            else
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) if (64 * half + 16 * g + 8 * e + i < yw) f[8 * e + i] = f32_el<T>(x[i]);
+                        }
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // what enters the next chunk
+            if (cuts) {
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+            } else {
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) S[ta][d][i] *= sd;
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                float kw[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) kw[j] = tail[j % 4] * block[2 * ks + j / 4];
+                if (cuts)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) if (32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut) kw[j] = 0.0f;
+                // b weighted in fp32 and taken apart without loss: the state is a sum of fp32 terms
+                v8bf fb[NA][3];
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta) {
+                    float x[8];
+                    unpack8<T>(down(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] *= kw[j];
+                    parts8<3>(x, fb[ta]);
+                }
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    v8bf fc[L::PARTS];
+#pragma unroll
+                    for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * (d / 4) + 4 * (d % 4), 16 * L::CP));
+#pragma unroll
+                    for (int ta = 0; ta < NA; ++ta) {
+                        S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
+                        if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
+                        S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
+                        if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
+                        S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+                    }
+                }
+            }
+        } else {
+            // A NaN or an infinity in the chunk (fp16: or in the state): in the products above a weight of 0 would carry it to tokens before it and to other episodes.  Token by token,
+            // as the formula says.
+            const float ge = pow2(lg);
+            int r = lane & 15, g = lane >> 4, tid = threadIdx.x;
+            asm("" : "+v"(r), "+v"(g), "+v"(tid));            // (its addresses are made here, not kept through the chunks that do without them)
+            const int yr = 16 * (r >> 2) + (r & 3);
+            for (int s = c ? 0 : gap; s < LC; ++s) {
+                const bool anew = cuts >> s & 1;
+                const int64_t row = (int64_t)c * LC + s;
+                float part[ND] = {};
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int x = 16 * (NA * w + ta) + 4 * g + j;
+                        const float eb = el_f32(T{sb[s * L::BP + x]}) * q.pair;
+                        float ea = 0.0f;
+                        if constexpr (OUT) if (x < X) ea = el_f32(pa[row * ta_ + x]);
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) {
+                            const uint16_t* f = sc + s * L::CP + yr + 64 * (d / 4) + 4 * (d % 4);
+                            float ec = L::SPLIT ? el_f32(BF16{f[0]}) : el_f32(T{f[0]});
+                            if constexpr (L::SPLIT) { const float lo = el_f32(BF16{f[L::CT]}); if (lo == lo) ec += lo; }    // (of an infinity the second part is a NaN)
+                            float e = anew ? 0.0f : back ? S[ta][d][j] : S[ta][d][j] * ge;
+                            e += eb * ec;
+                            if (x < X) part[d] += ea * e;
+                            S[ta][d][j] = back ? e * ge : e;
+                        }
+                    }
+                if constexpr (OUT) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        part[d] += __shfl_xor(part[d], 16);
+                        part[d] += __shfl_xor(part[d], 32);
+                        if (g == 0) red[w][yr + 64 * (d / 4) + 4 * (d % 4)] = part[d];
+                    }
+                    __syncthreads();
+                    if (tid < yw) {
+                        float v = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < NW; ++i) v += red[i][tid];
+                        v *= q.scale;
+                        const int64_t o = po + row * to + tid;
+                        if (q.out_f32) ((float*)q.out)[o] = v;
+                        else ((T*)q.out)[o] = f32_el<T>(v);
+                    }
+                    __syncthreads();
+                }
+            }
+            if (more) fetch_a(later);
+        }
+        left = cuts ? 0.0f : left * sd;
+        qw = decay_pow(lg, t + 1 - back) * q.scale;
+        sd = everywhere(decay_pow(lg, LC));
+        __syncthreads();
+        if (more) { stage(c + 1); publish(0); }
+    }
+
+    if (q.last) {
+        // backwards the state that enters the unroll has no gradient if its first token resets
+        const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
+        if (gone) left = 0.0f;
+        la_state_out<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, gone, S);
+        if (q.keep && at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = left;
+    }
+    if constexpr (OUT) la_behind<T, NW>(p, q, at, n, i0, y0, yw);
+}
+
+// ---------------------------------------------------------------- tokens of fp32
+// The same walk on fp32 matrix instructions, which are what bounds it: 376 of 32 cycles for a chunk of a head of 128, at 64 columns.
+template <int DX>
+struct LaFloat {
+    // rows 16 bytes further on in the banks, for 16-byte reads of 16 rows and for reads of four rows that lie four apart
+    static constexpr int BP = DX + 4, CP = LY + 4;
+    static constexpr int BV = DX / 16, CV = LY / 16;          // vectors of a lane
+    static constexpr int KX = DX / 16;
+};
+
+template <int DX, bool OUT, bool FULL>
+__global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const LaParams p) {
+    typedef LaFloat<DX> L;
+    constexpr int NA = DX / 64;                               // tiles of 16 rows of the state for a wavefront
+
+    __shared__ __attribute__((aligned(16))) float sb[LC * L::BP];
+    __shared__ __attribute__((aligned(16))) float sc[LC * L::CP];
+    __shared__ __attribute__((aligned(16))) float ss[OUT ? DX * LY : 4];      // the state's fragments: [column tile][depth][lane][4]
+    __shared__ int odd[4];                                    // whether a wavefront has seen a NaN or an infinity in b or c
+    __shared__ float red[4][LY];
+
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const LaPlace at = la_place(p);
+    if (!at.mine) return;
+    const LaRole& q = p.role[at.which];
+    const int X = FULL ? DX : q.X, Y = q.Y, y0 = at.slice * LY, yw = FULL ? LY : min(Y - y0, LY), back = q.back;
+    const uint32_t seg = at.seg, bh = at.bh, b = bh / p.H, h = bh % p.H;
+    int64_t n = p.T;
+    if (p.lengths) n = min(max((int64_t)p.lengths[b], (int64_t)0), n);
+    const int64_t i0 = seg * p.seg_len, i1 = min(n, i0 + p.seg_len);
+    const int chunks = i1 > i0 ? (int)((i1 - i0 + LC - 1) / LC) : 0;
+    const int64_t base0 = i1 - (int64_t)chunks * LC;          // of the first chunk; its tokens from `gap` on are there
+    const int gap = (int)(i0 - base0);
+    const float lg = p.log_decay[h] * LOG2E;
+    const int64_t tb = back ? -q.b.st : q.b.st, tc = back ? -q.c.st : q.c.st, ta_ = back ? -q.a.st : q.a.st, to = back ? -q.ot : q.ot;
+    const int64_t t0 = back ? n - 1 : 0;
+    const float* pb = (const float*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh + t0 * q.b.st + base0 * tb;
+    const float* pc = (const float*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + t0 * q.c.st + base0 * tc + y0;
+    const float* pa = (const float*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh + t0 * q.a.st + base0 * ta_;
+    float* po = (float*)q.out + b * q.ob + (int64_t)h * q.oh + t0 * q.ot + base0 * to + y0;
+
+    // the state: rows 16 (NA w + ta) + 4 g + i, columns 16 d + r
+    v4f S[NA][4];
+    la_state_in<NA, 4, 16, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, r, X, yw, S);
+    // weights as in the kernel above
+    const int t = 16 * w + r;
+    float diag[4], near[4], far[3], tail[4], block[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int s = 4 * g + i;
+        diag[i] = s <= r ? decay_pow(lg, r - s) * q.pair : 0.0f;
+        near[i] = decay_pow(lg, r - s + 15) * q.pair;
+        tail[i] = decay_pow(lg, 15 - s) * q.pair;
+        block[i] = decay_pow(lg, 48 - 16 * i + back);
+    }
+#pragma unroll
+    for (int st = 0; st < 3; ++st) far[st] = decay_pow(lg, max(16 * (w - st) - 15, 0));
+    float qw = decay_pow(lg, max(t - gap, 0) + 1 - back), sd = decay_pow(lg, LC - gap);      // (the first chunk's)
+    float left = 1.0f;                                        // of the segment's first state
+
+    const int brow = tid / (DX / 4), bcol = tid % (DX / 4) * 4, crow = tid / (LY / 4), ccol = tid % (LY / 4) * 4;
+    constexpr int BR = 1024 / DX, CR = 1024 / LY;             // rows from one vector of a lane to its next
+    u32x4 vb[L::BV], vc[L::CV];
+    uint32_t cut = 0;
+    auto fetch = [&](int c) {
+        const int skip = c ? 0 : gap;
+#pragma unroll
+        for (int k = 0; k < L::BV; ++k) {
+            const float* f = pb + ((int64_t)c * LC + max(brow + k * BR, skip)) * tb + bcol;
+            vb[k] = FULL ? *(const u32x4_at4*)f : row_vec(bcol < X ? f : pb + gap * tb, X - bcol);
+        }
+#pragma unroll
+        for (int k = 0; k < L::CV; ++k) {
+            const float* f = pc + ((int64_t)c * LC + max(crow + k * CR, skip)) * tc + ccol;
+            vc[k] = FULL ? *(const u32x4_at4*)f : row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol);
+        }
+        cut = 0;
+        if (p.reset) {
+            const int64_t i = base0 + (int64_t)c * LC + lane, tok = back ? n - i : i;
+            if (i >= i0 && !(back && i == 0)) cut = p.reset[b * p.rb + tok * p.rt];
+        }
+    };
+    auto stage = [&](int c) {
+        uint32_t top = 0;
+        const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < L::BV; ++k) {
+            if (c == 0 && brow + k * BR < gap) vb[k] = none;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, vb[k][j] & 0x7fffffffu);
+            *(u32x4*)(sb + (brow + k * BR) * L::BP + bcol) = vb[k];
+        }
+#pragma unroll
+        for (int k = 0; k < L::CV; ++k) {
+            if (c == 0 && crow + k * CR < gap) vc[k] = none;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, vc[k][j] & 0x7fffffffu);
+            *(u32x4*)(sc + (crow + k * CR) * L::CP + ccol) = vc[k];
+        }
+        const bool any = __ballot(top >= 0x7f800000u) != 0;
         if (lane == 0) odd[w] = any;
     };
     auto publish = [&]() {
         if constexpr (OUT)
 #pragma unroll
-            for (int ta = 0; ta < NA; ++ta) {
-                const int at = NA * w + ta;
+            for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    if constexpr (HALF) {                     // depth 32: rows 4 quad .. of the 32 belong to lane group quad / 2
-                        const int quad = 4 * (at & 1) + g;
-                        u32x2 two = {f32_pair<BF16>(S[ta][d][0], S[ta][d][1]), f32_pair<BF16>(S[ta][d][2], S[ta][d][3])};
-                        *(u32x2*)(ss + ((d * L::KX + (at >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1)) = two;
-                    } else {
-                        *(v4f*)(ss + ((d * L::KX + at) * 64 + lane) * 4) = S[ta][d];
-                    }
-                }
-            }
+                for (int d = 0; d < 4; ++d) *(v4f*)(ss + ((d * L::KX + NA * w + ta) * 64 + lane) * 4) = S[ta][d];
     };
-    auto out_at = [&](int64_t i) { return b * q.ob + (int64_t)h * q.oh + token(i) * q.ot + y0; };
 
-    if (i0 < i1) { fetch(i0); stage(); publish(); }
-    for (int64_t base = i0; base < i1; base += LC) {
-        const int m = (int)min((int64_t)LC, i1 - base);
+    if (chunks) { fetch(0); stage(0); publish(); }
+    for (int c = 0; c < chunks; ++c) {
         const uint64_t cuts = __ballot(cut != 0);
         __syncthreads();
-        const bool more = base + LC < i1;
-        if (more) fetch(base + LC);
+        const bool more = c + 1 < chunks;
+        // (kept as they are: their products, worked out ahead of the loop, would take 28 registers)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
+        if (more) fetch(c + 1);
         const bool plain = !(odd[0] | odd[1] | odd[2] | odd[3]);
-        if (m < LC) {
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int s = 16 * st + 4 * g + i;
-                    kw[st][i] = s < m ? decay_pow(lg, m - 1 - s + back) * q.pair : 0.0f;
-                }
-        }
         const int last_cut = cuts ? 63 - __builtin_clzll(cuts) : -1;
-        const uint64_t before = cuts & ((2ull << t) - 1);
-        const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
 
         if (plain) {
             v4f O[4];
-            E pt[4][4];                                       // weights of pairs as the product with c reads them
+            float wt[4][4];
             if constexpr (OUT) {
-                // this wavefront's 16 tokens of a, straight from memory
-                const bool have = t < m;
-                const T* ra = pa + (have ? token(base + t) * q.a.st : 0);
-#pragma unroll
-                for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
+                const float* ra = pa + ((int64_t)c * LC + max(t, c ? 0 : gap)) * ta_ + 4 * g;
                 v4f P[4];
 #pragma unroll
-                for (int st = 0; st < 4; ++st) P[st] = v4f{0, 0, 0, 0};
-                if constexpr (HALF) {
-                    v8bf fa[L::KX];
-#pragma unroll
-                    for (int k = 0; k < L::KX; ++k) fa[k] = __builtin_bit_cast(v8bf, row_vec(ra + (have ? 32 * k + 8 * g : 0), have ? X - 32 * k - 8 * g : 0));
+                for (int st = 0; st < 4; ++st) O[st] = P[st] = v4f{0, 0, 0, 0};
+#pragma unroll 4
+                for (int k = 0; k < L::KX; ++k) {
+                    const v4f fa = __builtin_bit_cast(v4f, FULL ? *(const u32x4_at4*)(ra + 16 * k) : row_vec(4 * g + 16 * k < X ? ra + 16 * k : ra - 4 * g, X - 16 * k - 4 * g));
 #pragma unroll
                     for (int st = 0; st < 4; ++st)
-                        if (st <= w)
+                        if (st <= w) {
+                            const v4f fb = *(const v4f*)(sb + (16 * st + r) * L::BP + 16 * k + 4 * g);
 #pragma unroll
-                            for (int k = 0; k < L::KX; ++k)
-                                P[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const v8bf*)(sb + (16 * st + r) * L::BP + 32 * k + 8 * g), fa[k], P[st], 0, 0, 0);
-#pragma unroll
-                    for (int k = 0; k < L::KX; ++k)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d)
-                            O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const v8bf*)(ss + ((d * L::KX + k) * 64 + lane) * 8), fa[k], O[d], 0, 0, 0);
-                } else {
-                    for (int k = 0; k < L::KX; ++k) {
-                        v4f fa = {0, 0, 0, 0};
-                        const int in = have ? X - 16 * k - 4 * g : 0;
-                        const T* rk = ra + (in > 0 ? 16 * k + 4 * g : 0);
-                        if constexpr (sizeof(T) == 4) fa = __builtin_bit_cast(v4f, row_vec(rk, in));
-                        else
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) if (j < in) fa[j] = el_f32(rk[j]);
-#pragma unroll
-                        for (int st = 0; st < 4; ++st)
-                            if (st <= w) {
-                                const v4f fb = *(const v4f*)(sb + (16 * st + r) * L::BP + 16 * k + 4 * g);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) P[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j], fa[j], P[st], 0, 0, 0);
-                            }
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            const v4f fs = *(const v4f*)(ss + ((d * L::KX + k) * 64 + lane) * 4);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fs[j], fa[j], O[d], 0, 0, 0);
+                            for (int j = 0; j < 4; ++j) P[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j], fa[j], P[st], 0, 0, 0);
                         }
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const v4f fs = *(const v4f*)(ss + ((d * L::KX + k) * 64 + lane) * 4);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fs[j], fa[j], O[d], 0, 0, 0);
                     }
                 }
-                // (selected, not multiplied by 0: the state of the episode before may hold anything)
-                const float f = qw;
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) O[d][i] = first >= 0 ? 0.0f : O[d][i] * f;
+                    for (int i = 0; i < 4; ++i) O[d][i] *= qw;
 #pragma unroll
-                for (int st = 0; st < 4; ++st)
+                for (int st = 0; st < 4; ++st) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int s = 16 * st + 4 * g + i;
-                        pt[st][i] = f32_el<E>(s <= t && s >= first ? P[st][i] * dec[st][i] : 0.0f);
+                    for (int i = 0; i < 4; ++i) wt[st][i] = 0.0f;
+                    if (st == w) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * diag[i];
+                    } else if (st < w) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * (near[i] * far[st < 3 ? st : 0]);
                     }
+                }
+                if (cuts) {
+                    const uint64_t before = cuts & ((2ull << t) - 1);
+                    const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
+                    // (selected, not multiplied by 0: the state of the episode before may hold anything)
+                    if (first >= 0)
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
+#pragma unroll
+                    for (int st = 0; st < 4; ++st)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (16 * st + 4 * g + i < first) wt[st][i] = 0.0f;
+                }
             }
             // what enters the next chunk
-            const float sd = decay_pow(lg, m);
 #pragma unroll
             for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) S[ta][d][i] = cuts ? 0.0f : S[ta][d][i] * sd;
-            if constexpr (HALF) {
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    // four rows of four columns each are turned by a read: the columns of 16 lanes, down four tokens
-                    typedef __attribute__((address_space(3))) v4s lds4;
-                    auto down = [&](const E* tile, int pitch, int col) {
-                        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + (32 * ks + 4 * g + (r >> 2)) * pitch + col + 4 * (r & 3)));
-                        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + (32 * ks + 16 + 4 * g + (r >> 2)) * pitch + col + 4 * (r & 3)));
-                        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    };
-                    v8bf fc[4];
+            for (int st = 0; st < 4; ++st) {
+                v4f fc[4];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) fc[d] = __builtin_bit_cast(v8bf, down(sc, L::CP, 16 * d));
-                    if constexpr (OUT) if (2 * ks <= w) {
-                        v8s pp;
+                for (int d = 0; d < 4; ++d)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) pp[j] = (short)pt[2 * ks + j / 4][j % 4].u;
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[d], __builtin_bit_cast(v8bf, pp), O[d], 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int ta = 0; ta < NA; ++ta) {
-                        // b weighted in fp32 and split in two bf16 parts: the state keeps 2^-17 of every term
-                        const v8s fb = down(sb, L::BP, 16 * (NA * w + ta));
-                        v8s hi, lo;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int s = 32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4;
-                            const float x = el_f32(BF16{(uint16_t)fb[j]}) * kw[2 * ks + j / 4][j % 4];
-                            const float xw = s < last_cut ? 0.0f : x;
-                            const BF16 xh = f32_el<BF16>(xw);
-                            hi[j] = (short)xh.u;
-                            lo[j] = (short)f32_el<BF16>(xw - el_f32(xh)).u;
-                        }
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, lo), fc[d], S[ta][d], 0, 0, 0);
-                            S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, hi), fc[d], S[ta][d], 0, 0, 0);
-                        }
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    v4f fc[4];
+                    for (int i = 0; i < 4; ++i) fc[d][i] = sc[(16 * st + 4 * g + i) * L::CP + 16 * d + r];
+                if constexpr (OUT) if (st <= w) {
 #pragma unroll
                     for (int d = 0; d < 4; ++d)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) fc[d][i] = sc[(16 * st + 4 * g + i) * L::CP + 16 * d + r];
-                    if constexpr (OUT) if (st <= w) {
+                        for (int i = 0; i < 4; ++i) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[d][i], wt[st][i], O[d], 0, 0, 0);
+                }
 #pragma unroll
-                        for (int d = 0; d < 4; ++d)
+                for (int i = 0; i < 4; ++i) {
+                    const int s = 16 * st + 4 * g + i;
+                    const float kw = s < last_cut ? 0.0f : tail[i] * block[st];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[d][i], pt[st][i], O[d], 0, 0, 0);
+                    for (int ta = 0; ta < NA; ++ta) {
+                        const float x = sb[s * L::BP + 16 * (NA * w + ta) + r] * kw;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, fc[d][i], S[ta][d], 0, 0, 0);
                     }
-#pragma unroll
-                    for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int s = 16 * st + 4 * g + i;
-                            const float x = sb[s * L::BP + 16 * (NA * w + ta) + r] * kw[st][i];
-                            const float xw = s < last_cut ? 0.0f : x;
-#pragma unroll
-                            for (int d = 0; d < 4; ++d) S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(xw, fc[d][i], S[ta][d], 0, 0, 0);
-                        }
                 }
             }
             if constexpr (OUT) {
-                if (t < m) {
-                    const int64_t o = out_at(base + t);
+                if (c || t >= gap) {
+                    float* f = po + ((int64_t)c * LC + t) * to;
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
                         const int y = 16 * d + 4 * g;
                         v4f v = O[d];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v[i] *= q.scale;
-                        if (q.out_f32) {
-                            float* to = (float*)q.out + o + y;
-                            if (y + 4 <= yw) *(u32x4_at4*)to = __builtin_bit_cast(u32x4, v);
-                            else
+                        if (FULL || y + 4 <= yw) *(u32x4_at4*)(f + y) = __builtin_bit_cast(u32x4, v);
+                        else
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) if (y + i < yw) to[i] = v[i];
-                        } else {
-                            T* to = (T*)q.out + o + y;
-                            if (y + 4 <= yw) {
-                                if constexpr (sizeof(T) == 4) *(u32x4_at4*)to = __builtin_bit_cast(u32x4, v);
-                                else *(u32x2_at2*)to = u32x2{f32_pair<T>(v[0], v[1]), f32_pair<T>(v[2], v[3])};
-                            } else
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) if (y + i < yw) to[i] = f32_el<T>(v[i]);
-                        }
+                            for (int i = 0; i < 4; ++i) if (y + i < yw) f[y + i] = v[i];
                     }
                 }
             }
         } else {
-            // A NaN or an infinity in the chunk: in the products above a weight of 0 would carry it to tokens before it and to other episodes.  Token by token,
-            // as the formula says.
+            // a NaN or an infinity in the chunk: token by token, as in the kernel above
             const float ge = pow2(lg);
-            for (int s = 0; s < m; ++s) {
+            int r = lane & 15, g = lane >> 4, tid = threadIdx.x;
+            asm("" : "+v"(r), "+v"(g), "+v"(tid));
+            for (int s = c ? 0 : gap; s < LC; ++s) {
                 const bool anew = cuts >> s & 1;
+                const int64_t i = (int64_t)c * LC + s;
                 float part[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int x = 16 * (NA * w + ta) + 4 * g + i;
-                        const float eb = el_f32(sb[s * L::BP + x]) * q.pair;
+                    for (int j = 0; j < 4; ++j) {
+                        const int x = 16 * (NA * w + ta) + 4 * g + j;
+                        const float eb = sb[s * L::BP + x] * q.pair;
                         float ea = 0.0f;
-                        if constexpr (OUT) if (x < X) ea = el_f32(pa[token(base + s) * q.a.st + x]);
+                        if constexpr (OUT) if (x < X) ea = pa[i * ta_ + x];
 #pragma unroll
                         for (int d = 0; d < 4; ++d) {
-                            float e = anew ? 0.0f : back ? S[ta][d][i] : S[ta][d][i] * ge;
-                            e += eb * el_f32(sc[s * L::CP + 16 * d + r]);
+                            float e = anew ? 0.0f : back ? S[ta][d][j] : S[ta][d][j] * ge;
+                            e += eb * sc[s * L::CP + 16 * d + r];
                             if (x < X) part[d] += ea * e;
-                            S[ta][d][i] = back ? e * ge : e;
+                            S[ta][d][j] = back ? e * ge : e;
                         }
                     }
                 if constexpr (OUT) {
@@ -463,47 +868,25 @@ __global__ __launch_bounds__(256, LaCompute<T>::HALF ? 2 : 1) void la_chunks_ker
                         if (g == 0) red[w][16 * d + r] = part[d];
                     }
                     __syncthreads();
-                    if (tid < yw) {
-                        const float v = (red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]) * q.scale;
-                        const int64_t o = out_at(base + s) + tid;
-                        if (q.out_f32) ((float*)q.out)[o] = v;
-                        else ((T*)q.out)[o] = f32_el<T>(v);
-                    }
+                    if (tid < yw) po[i * to + tid] = (red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]) * q.scale;
                     __syncthreads();
                 }
             }
         }
-        left = cuts ? 0.0f : left * decay_pow(lg, m);
+        left = cuts ? 0.0f : left * sd;
+        qw = decay_pow(lg, t + 1 - back);
+        sd = decay_pow(lg, LC);
         __syncthreads();
-        if (more) { stage(); publish(); }
+        if (more) { stage(c + 1); publish(); }
     }
 
     if (q.last) {
-        // backwards the state that enters the unroll has no gradient if its first token resets
         const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
         if (gone) left = 0.0f;
-        float* e = q.last + seg * q.lseg + (int64_t)bh * X * Y;
-#pragma unroll
-        for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int x = 16 * (NA * w + ta) + 4 * g + i, y = y0 + 16 * d + r;
-                    if (x < X && y < Y) e[x * q.lx + y * q.ly] = gone ? 0.0f : S[ta][d][i];
-                }
-        if (q.keep && slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = left;
+        la_state_out<NA, 4, 16, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, r, X, yw, gone, S);
+        if (q.keep && at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = left;
     }
-    if constexpr (OUT) {
-        // tokens behind the sequence's end
-        for (int64_t i = max(i0, n) + w; i < min(p.T, i0 + p.seg_len); i += 4) {
-            const int64_t o = b * q.ob + (int64_t)h * q.oh + i * q.ot + y0;
-            if (lane < yw) {
-                if (q.out_f32) ((float*)q.out)[o + lane] = 0.0f;
-                else ((T*)q.out)[o + lane] = T{};
-            }
-        }
-    }
+    if constexpr (OUT) la_behind<float, 4>(p, q, at, n, i0, y0, yw);
 }
 
 // The states that enter the segments, from what each segment adds: states [segment][B H][X Y] in place, the last one to `last`.
@@ -665,16 +1048,43 @@ int la_check_sizes(const char* who, int64_t B, int64_t T, int32_t H, int32_t Hk,
     return ACCERL_OK;
 }
 
+template <typename T, int DX, bool OUT>
+void la_go(const LaParams& p, bool wide, bool full, dim3 grid, hipStream_t s) {
+    const dim3 block(256);
+    if constexpr (__is_same(T, float)) {
+        if (full) la_float_kernel<DX, OUT, true><<<grid, block, 0, s>>>(p);
+        else la_float_kernel<DX, OUT, false><<<grid, block, 0, s>>>(p);
+    } else {
+        if constexpr (DX == 128 || (DX == 256 && __is_same(T, BF16))) {
+            if (wide) {
+                if (full) la_half_kernel<T, DX, 8, OUT, true><<<grid, dim3(512), 0, s>>>(p);
+                else la_half_kernel<T, DX, 8, OUT, false><<<grid, dim3(512), 0, s>>>(p);
+                return;
+            }
+        }
+        if (full) la_half_kernel<T, DX, 4, OUT, true><<<grid, block, 0, s>>>(p);
+        else la_half_kernel<T, DX, 4, OUT, false><<<grid, block, 0, s>>>(p);
+    }
+}
 template <typename T, bool OUT>
-int la_launch(const char* who, const LaParams& p, int X, hipStream_t s) {
-    int slices = 0;
-    for (const LaRole& r : p.role) slices += r.slices;
+int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
+    int slices = 0, most = 0;
+    for (const LaRole& r : p.role) if (r.slices) most = std::max(most, r.Y);
+    const bool wide = !__is_same(T, float) && X > 64 && most > LY && !(__is_same(T, F16) && X == 256);
+    const int cols = wide ? 2 * LY : LY;
+    bool full = true;
+    for (LaRole& r : p.role) {
+        if (!r.slices) continue;
+        r.slices = (r.Y + cols - 1) / cols;
+        slices += r.slices;
+        if (r.X != X || r.Y % cols) full = false;
+    }
     const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * slices;
     if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
-    const dim3 grid((uint32_t)blocks), block(256);
-    if (X <= 64) la_chunks_kernel<T, 64, OUT><<<grid, block, 0, s>>>(p);
-    else if (X <= 128) la_chunks_kernel<T, 128, OUT><<<grid, block, 0, s>>>(p);
-    else la_chunks_kernel<T, 256, OUT><<<grid, block, 0, s>>>(p);
+    const dim3 grid((uint32_t)blocks);
+    if (X == 64) la_go<T, 64, OUT>(p, wide, full, grid, s);
+    else if (X == 128) la_go<T, 128, OUT>(p, wide, full, grid, s);
+    else la_go<T, 256, OUT>(p, wide, full, grid, s);
     return la_launched(who);
 }
 int la_pad(int x) { return x <= 64 ? 64 : x <= 128 ? 128 : 256; }
