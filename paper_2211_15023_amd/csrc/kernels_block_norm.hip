@@ -1,8 +1,9 @@
 // The norms around a block with its gate and its residual, and their gradients.
 //
-// A row is read once and stays in the registers of its lanes, eight neighbouring elements at a time: all statistics are taken from there, the mean
-// first and then the squares around it.  Bound by memory: the gradients' six sums over a row lie between one row's loads and its stores, so that several
-// rows have to be under way on a compute unit.  Rows of up to 1024 elements belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
+// A row is read once and stays in the registers of its lanes, eight neighbouring elements at a time: all statistics are taken from there, the mean first and then
+// the squares around it.  Bound by memory where the row's eights fill its lanes: 65536 x 2048 bf16 with an fp32 stream 390 us (4.8 TB/s; a large copy reaches
+// 4.9), gradients of 32768 x 4096 bf16 520 (4.1; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
+// (gradients: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
 #include <algorithm>
 #include <cstdio>
 
@@ -18,7 +19,7 @@ struct NormParams {
     void *u, *h, *dy, *dx, *dg;
     int64_t ldy, ldx, ldg, ldgu, ldgh, ldu, ldh, lddy, lddx, lddg;
     const float *after, *before;
-    float *da, *db;                       // partial sums of the weights' gradients, [slot][D of a group]
+    float *da, *db;                       // partial sums of the weights' gradients, [record][D of a group]
     int64_t rows;                         // rows x groups
     int64_t step;                         // from a slot's row to its next: a multiple of the groups, so that a slot keeps its weights
     int D, groups, lanes;                 // of a group's row; lanes a row has
@@ -26,25 +27,31 @@ struct NormParams {
     float eps, skip, branch, inv_d;
 };
 
-// eight elements of a row, of which `left` are inside (the others 0)
-template <typename T> __device__ __forceinline__ void load8(const T* p, int left, float* o) {
-    if (left >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            const v4f a = __builtin_bit_cast(v4f, *(const u32x4_at4*)p), b = __builtin_bit_cast(v4f, *(const u32x4_at4*)(p + 4));
+// Eight elements of a row as they lie in memory, and as numbers.  TINY: rows of less than eight, of which `left` are there (the others 0).
+template <typename T> struct Eight { u32x4 w[sizeof(T) / 2]; };
+template <bool TINY, typename T> __device__ __forceinline__ void load8(const T* p, int left, Eight<T>& o) {
+    if constexpr (TINY) {
+        T e[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { o[j] = a[j]; o[4 + j] = b[j]; }
-        } else {
-            const u32x4 w = *(const u32x4_at2*)p;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) el_pair<T>(w[j], o[2 * j], o[2 * j + 1]);
-        }
+        for (int j = 0; j < 8; ++j) e[j] = j < left ? p[j] : T{};
+        __builtin_memcpy(&o, e, sizeof o);
+    } else if constexpr (sizeof(T) == 4) {
+        o.w[0] = *(const u32x4_at4*)p;
+        o.w[1] = *(const u32x4_at4*)(p + 4);
     } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = j < left ? el_f32(p[j]) : 0.0f;
+        o.w[0] = *(const u32x4_at2*)p;
     }
 }
-template <typename T> __device__ __forceinline__ void store8(T* p, int left, const float* v) {
-    if (left >= 8) {
+template <typename T> __device__ __forceinline__ void numbers8(const Eight<T>& v, float* o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) { o[j] = __uint_as_float(v.w[0][j]); o[4 + j] = __uint_as_float(v.w[1][j]); }
+        else el_pair<T>(v.w[0][j], o[2 * j], o[2 * j + 1]);
+    }
+}
+// elements from .. to - 1 of eight
+template <typename T> __device__ __forceinline__ void store8(T* p, int from, int to, const float* v) {
+    if (to - from == 8) {
         if constexpr (sizeof(T) == 4) {
             *(u32x4_at4*)p = __builtin_bit_cast(u32x4, v4f{v[0], v[1], v[2], v[3]});
             *(u32x4_at4*)(p + 4) = __builtin_bit_cast(u32x4, v4f{v[4], v[5], v[6], v[7]});
@@ -56,7 +63,7 @@ template <typename T> __device__ __forceinline__ void store8(T* p, int left, con
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) if (j < left) p[j] = f32_el<T>(v[j]);
+        for (int j = 0; j < 8; ++j) if (j >= from && j < to) p[j] = f32_el<T>(v[j]);
     }
 }
 
@@ -82,17 +89,18 @@ template <bool GROUP> struct RowSum {
     __device__ __forceinline__ float operator()(float a) { float b = 0.0f; (*this)(a, b); return a; }
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+// (the reciprocal instruction is off by one in the last place, as the exponential is)
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
-// z -> (z - mean) and the reciprocal root; elements behind the row's end stay 0
-template <int N, bool GROUP> __device__ __forceinline__ float normed(const NormParams& p, RowSum<GROUP>& sum, float* z, const int* left) {
+// z -> (z - mean) and the reciprocal root; elements that are not the lane's stay 0
+template <int N, bool GROUP, typename Mine> __device__ __forceinline__ float normed(const NormParams& p, RowSum<GROUP>& sum, float* z, const Mine& mine) {
     if (p.layer) {
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) s += z[i];
         const float mean = sum(s) * p.inv_d;
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = i % 8 < left[i / 8] ? z[i] - mean : 0.0f;
+        for (int i = 0; i < N; ++i) z[i] = mine(i, z[i] - mean);
     }
     float s = 0.0f;
 #pragma unroll
@@ -114,145 +122,238 @@ template <int N, bool GROUP> __device__ __forceinline__ void through(const NormP
     for (int i = 0; i < N; ++i) t[i] = r * (t[i] - b - z[i] * a);
 }
 
-template <typename T, typename S, int NC, bool GROUP, bool GRAD>
-__global__ __launch_bounds__(GROUP ? 1024 : 256) void block_norm_kernel(const NormParams p) {
+// What a row reads, as it lies in memory.
+template <typename T, typename S, int NC> struct NormRow { Eight<T> y[NC], gate[NC], gh[NC]; Eight<S> x[NC], gu[NC]; };
+
+// MOST: threads of a workgroup at most.  While a row is worked on the next one's loads are under way, where registers allow it (AHEAD).
+template <typename T, typename S, int NC, int MOST, bool GROUP, bool GRAD, bool TINY>
+__global__ __launch_bounds__(MOST, MOST == 1024 ? 4 : MOST == 512 || NC == 2 ? 2 : 3) void block_norm_kernel(const NormParams p) {
     constexpr int N = 8 * NC;
-    __shared__ float red[2][16][2];
+    constexpr bool AHEAD = NC <= 2 && MOST <= 512 && sizeof(NormRow<T, S, NC>) <= 160;
+    __shared__ float red[GROUP ? 2 : 1][16][2];
+    // The widest rows: the weights' sums are in LDS, and the weights come from the caches for every row
+    constexpr bool LEAN = GRAD && NC == 4;
+    __shared__ float sums[LEAN ? 2 * MOST * N : GRAD && !GROUP ? 256 * N : 1];
     RowSum<GROUP> sum{red, p.lanes};
     const int lane = GROUP ? threadIdx.x : threadIdx.x & (p.lanes - 1);
     const int64_t slot = GROUP ? blockIdx.x : (int64_t)blockIdx.x * (256 / p.lanes) + threadIdx.x / p.lanes;
-    const int part = (int)(slot % p.groups);
-    int at[NC], left[NC];
+    const int part = (int)(slot % p.groups), off = part * p.D;
+    // A lane's eights begin at `at`.  The row's last one ends with the row and so begins inside the one before, whose elements it reads too but leaves alone:
+    // its own are those from `from` to `to` - 1 (none where the row has no eight for the lane, which reads the first).
+    int at[NC], from[NC], to[NC];
+    bool whole = true;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        at[c] = (c * p.lanes + lane) * 8;
-        left[c] = min(max(p.D - at[c], 0), 8);
-        if (!left[c]) at[c] = 0;
+        const int k = (c * p.lanes + lane) * 8, in = min(max(p.D - k, 0), 8);
+        at[c] = in == 0 ? 0 : TINY ? k : min(k, p.D - 8);
+        from[c] = TINY ? 0 : 8 - in;
+        to[c] = TINY ? in : 8;
     }
-    float wa[N], wb[N], sa[N], sb[N];
+    whole = !TINY && p.D == 8 * NC * p.lanes;
+    auto mine = [&](int i, float v) { return whole || (i % 8 >= from[i / 8] && i % 8 < to[i / 8]) ? v : 0.0f; };
+    constexpr int KEPT = LEAN ? 1 : N;
+    float wa[KEPT], wb[KEPT], sa[KEPT], sb[KEPT];
+    auto weight = [&](const float* w, int c, int j) { return w && (!TINY || j < to[c]) ? w[at[c] + j] : 0.0f; };
+    const float* after = p.after ? p.after + off : nullptr;
+    if constexpr (LEAN) {
+        for (int i = 0; i < 2 * N; ++i) sums[i * MOST + threadIdx.x] = 0.0f;
+    } else {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            wa[8 * c + j] = p.after && j < left[c] ? p.after[part * p.D + at[c] + j] : 0.0f;
-            wb[8 * c + j] = p.before && j < left[c] ? p.before[at[c] + j] : 0.0f;
-            sa[8 * c + j] = sb[8 * c + j] = 0.0f;
+        for (int i = 0; i < N; ++i) {
+            wa[i] = weight(after, i / 8, i % 8);
+            wb[i] = weight(p.before, i / 8, i % 8);
+            sa[i] = sb[i] = 0.0f;
         }
     }
-    for (int64_t row = slot; row < p.rows; row += p.step) {
-        const int64_t n = p.groups == 1 ? row : row / p.groups;
-        const int off = part * p.D;
-        float y[N], gt[N], u[N];
+    auto wa_of = [&](int i) { if constexpr (LEAN) return weight(after, i / 8, i % 8); else return wa[i]; };
+    auto wb_of = [&](int i) { if constexpr (LEAN) return weight(p.before, i / 8, i % 8); else return wb[i]; };
+    auto add_a = [&](int i, float v) { if constexpr (LEAN) sums[i * MOST + threadIdx.x] += v; else sa[i] += v; };
+    auto add_b = [&](int i, float v) { if constexpr (LEAN) sums[(N + i) * MOST + threadIdx.x] += v; else sb[i] += v; };
+    // a lane's places in the row it reads and the row it writes, which go on with the rows
+    const int64_t n0 = slot / p.groups, rows_on = p.step / p.groups;
+    const T *y_at = (const T*)p.y + n0 * p.ldy + off, *gate_at = (const T*)p.gate + n0 * p.ldg + off, *gh_at = (const T*)p.gh + n0 * p.ldgh + off;
+    const S *x_at = (const S*)p.x + n0 * p.ldx + off, *gu_at = (const S*)p.gu + n0 * p.ldgu + off;
+    T *h_at = (T*)p.h + n0 * p.ldh + off, *dy_at = (T*)p.dy + n0 * p.lddy + off, *dg_at = (T*)p.dg + n0 * p.lddg + off;
+    S *u_at = (S*)p.u + n0 * p.ldu + off, *dx_at = (S*)p.dx + n0 * p.lddx + off;
+    auto load_values = [&](NormRow<T, S, NC>& v) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            load8((const T*)p.y + n * p.ldy + off + at[c], left[c], y + 8 * c);
-            if (p.gate_kind) load8((const T*)p.gate + n * p.ldg + off + at[c], left[c], gt + 8 * c);
-            if (p.x) load8((const S*)p.x + n * p.ldx + off + at[c], left[c], u + 8 * c);
+            load8<TINY>(y_at + at[c], to[c], v.y[c]);
+            if (p.gate_kind) load8<TINY>(gate_at + at[c], to[c], v.gate[c]);
+            if (p.x) load8<TINY>(x_at + at[c], to[c], v.x[c]);
         }
-        float gu[N], gh[N];
+        y_at += rows_on * p.ldy;
+        gate_at += rows_on * p.ldg;
+        x_at += rows_on * p.ldx;
+    };
+    auto load_gradients = [&](NormRow<T, S, NC>& v) {
         if constexpr (GRAD) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                if (p.gu) load8((const S*)p.gu + n * p.ldgu + off + at[c], left[c], gu + 8 * c);
-                if (p.gh) load8((const T*)p.gh + n * p.ldgh + off + at[c], left[c], gh + 8 * c);
+                if (p.gh) load8<TINY>(gh_at + at[c], to[c], v.gh[c]);
+                if (p.gu) load8<TINY>(gu_at + at[c], to[c], v.gu[c]);
             }
-#pragma unroll
-            for (int i = 0; i < N; ++i) { if (!p.gu) gu[i] = 0.0f; if (!p.gh) gh[i] = 0.0f; }
+            gh_at += rows_on * p.ldgh;
+            gu_at += rows_on * p.ldgu;
         }
+    };
+    NormRow<T, S, NC> now, next;
+    if (AHEAD && slot < p.rows) { load_values(next); load_gradients(next); }
+    for (int64_t row = slot; row < p.rows; row += p.step) {
+        if constexpr (AHEAD) {
+            now = next;
+            if (row + p.step < p.rows) { load_values(next); load_gradients(next); }
+        } else {
+            load_values(now);
+            if constexpr (!LEAN) load_gradients(now);
+        }
+        float y[N], u[N], e[N];                               // e: the gate's sigmoid
+#pragma unroll
+        for (int c = 0; c < NC; ++c) numbers8(now.y[c], y + 8 * c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = mine(i, y[i]);
         float ry = 1.0f;
-        if (p.after) ry = normed<N, GROUP>(p, sum, y, left);
-        // u, and with gradients the gate's value (in gt) and its slope
-        float slope[N];
+        if (p.after) ry = normed<N, GROUP>(p, sum, y, mine);
+        auto each = [&](auto&& f) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float m = p.after ? y[i] * wa[i] : y[i];
-            float s = 1.0f;
-            slope[i] = 0.0f;
-            if (p.gate_kind) {
-                const float e = sigmoid(gt[i]);
-                s = p.gate_kind == ACCERL_GATE_SIGMOID ? e : gt[i] * e;
-                slope[i] = p.gate_kind == ACCERL_GATE_SIGMOID ? e * (1.0f - e) : e * (1.0f + gt[i] * (1.0f - e));
-            }
-            gt[i] = s;
-            u[i] = p.branch * s * m + (p.x ? p.skip * u[i] : 0.0f);
-            if (i % 8 >= left[i / 8]) u[i] = 0.0f;
+            for (int i = 0; i < N; ++i) f(i);
+        };
+        each([&](int i) { u[i] = p.after ? y[i] * wa_of(i) : y[i]; });
+        float gate[N];
+        if (p.gate_kind) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) numbers8(now.gate[c], gate + 8 * c);
+            each([&](int i) { e[i] = sigmoid(gate[i]); u[i] *= e[i]; });
+            if (p.gate_kind == ACCERL_GATE_SILU) each([&](int i) { u[i] *= gate[i]; });
         }
+        each([&](int i) { u[i] *= p.branch; });
+        if (p.x)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                float x[8];
+                numbers8(now.x[c], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[8 * c + j] += mine(8 * c + j, p.skip * x[j]);
+            }
         if constexpr (!GRAD) {
             if (p.u)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) store8((S*)p.u + n * p.ldu + off + at[c], left[c], u + 8 * c);
+                for (int c = 0; c < NC; ++c) store8(u_at + at[c], from[c], to[c], u + 8 * c);
             if (p.before) {
-                normed<N, GROUP>(p, sum, u, left);
+                normed<N, GROUP>(p, sum, u, mine);
 #pragma unroll
-                for (int i = 0; i < N; ++i) u[i] *= wb[i];
+                for (int i = 0; i < N; ++i) u[i] *= wb_of(i);
 #pragma unroll
-                for (int c = 0; c < NC; ++c) store8((T*)p.h + n * p.ldh + off + at[c], left[c], u + 8 * c);
+                for (int c = 0; c < NC; ++c) store8(h_at + at[c], from[c], to[c], u + 8 * c);
             }
+            u_at += rows_on * p.ldu;
+            h_at += rows_on * p.ldh;
         } else {
+            float g[N];                                       // the gradient by u
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[i] = 0.0f;
+            if constexpr (LEAN) load_gradients(now);
             if (p.before) {
-                const float ru = normed<N, GROUP>(p, sum, u, left);
-                float t[N];
+                const float ru = normed<N, GROUP>(p, sum, u, mine);
+                if (p.gh) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    sb[i] += gh[i] * u[i];
-                    t[i] = gh[i] * wb[i];
+                    for (int c = 0; c < NC; ++c) numbers8(now.gh[c], g + 8 * c);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        g[i] = mine(i, g[i]);
+                        add_b(i, g[i] * u[i]);
+                        g[i] *= wb_of(i);
+                    }
+                    through<N, GROUP>(p, sum, g, u, ru);
                 }
-                through<N, GROUP>(p, sum, t, u, ru);
-#pragma unroll
-                for (int i = 0; i < N; ++i) gu[i] += t[i];
             }
-            float o[N];
-            if (p.dx) {
+            if (p.gu)
 #pragma unroll
-                for (int i = 0; i < N; ++i) o[i] = p.skip * gu[i];
+                for (int c = 0; c < NC; ++c) {
+                    float o[8];
+                    numbers8(now.gu[c], o);
 #pragma unroll
-                for (int c = 0; c < NC; ++c) store8((S*)p.dx + n * p.lddx + off + at[c], left[c], o + 8 * c);
-            }
+                    for (int j = 0; j < 8; ++j) g[8 * c + j] += o[j];
+                }
+            if (p.dx)
 #pragma unroll
-            for (int i = 0; i < N; ++i) gu[i] *= p.branch;
-            if (p.dg) {
+                for (int c = 0; c < NC; ++c) {
+                    float o[8];
 #pragma unroll
-                for (int i = 0; i < N; ++i) o[i] = gu[i] * (p.after ? y[i] * wa[i] : y[i]) * slope[i];
+                    for (int j = 0; j < 8; ++j) o[j] = p.skip * g[8 * c + j];
+                    store8(dx_at + at[c], from[c], to[c], o);
+                }
+            each([&](int i) { g[i] = mine(i, g[i] * p.branch); });
+            if (p.gate_kind) {
+                float o[N];
+                each([&](int i) { o[i] = g[i] * (p.after ? y[i] * wa_of(i) : y[i]); g[i] *= e[i]; });
+                if (p.gate_kind == ACCERL_GATE_SILU) each([&](int i) { o[i] *= e[i] * (1.0f + gate[i] * (1.0f - e[i])); g[i] *= gate[i]; });
+                else each([&](int i) { o[i] *= e[i] * (1.0f - e[i]); });
+                if (p.dg)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) store8((T*)p.dg + n * p.lddg + off + at[c], left[c], o + 8 * c);
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                gu[i] *= gt[i];
-                if (i % 8 >= left[i / 8]) gu[i] = 0.0f;
+                    for (int c = 0; c < NC; ++c) store8(dg_at + at[c], from[c], to[c], o + 8 * c);
             }
             if (p.after) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    sa[i] += gu[i] * y[i];
-                    gu[i] *= wa[i];
+                    add_a(i, g[i] * y[i]);
+                    g[i] *= wa_of(i);
                 }
-                if (p.dy) through<N, GROUP>(p, sum, gu, y, ry);
+                if (p.dy) through<N, GROUP>(p, sum, g, y, ry);
             }
             if (p.dy)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) store8((T*)p.dy + n * p.lddy + off + at[c], left[c], gu + 8 * c);
+                for (int c = 0; c < NC; ++c) store8(dy_at + at[c], from[c], to[c], g + 8 * c);
+            dx_at += rows_on * p.lddx;
+            dg_at += rows_on * p.lddg;
+            dy_at += rows_on * p.lddy;
         }
     }
     if constexpr (GRAD) {
-        // a slot without rows has zeros
+        // a slot without rows has zeros; slots of a workgroup that have the same weights are added up first
+        auto keep = [&](float* out, const float* s, int which) {
+            if (!out) return;
+            if constexpr (LEAN) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            if (p.da) store8(p.da + slot * p.D + at[c], left[c], sa + 8 * c);
-            if (p.db) store8(p.db + slot * p.D + at[c], left[c], sb + 8 * c);
-        }
+                for (int c = 0; c < NC; ++c) {
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = sums[(which * N + 8 * c + j) * MOST + threadIdx.x];
+                    store8(out + slot * p.D + at[c], from[c], to[c], v);
+                }
+            } else if constexpr (GROUP) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) store8(out + slot * p.D + at[c], from[c], to[c], s + 8 * c);
+            } else {
+                const int slots = 256 / p.lanes, nth = threadIdx.x / p.lanes;
+                const bool fold = slots % p.groups == 0;
+                __syncthreads();
+#pragma unroll
+                for (int c = 0; c < NC; ++c) store8((fold ? sums + nth * p.D : out + slot * p.D) + at[c], from[c], to[c], s + 8 * c);
+                __syncthreads();
+                if (fold)
+                    for (int i = threadIdx.x; i < p.groups * p.D; i += 256) {
+                        float t = 0.0f;
+                        for (int k = i / p.D; k < slots; k += p.groups) t += sums[k * p.D + i % p.D];
+                        out[(int64_t)blockIdx.x * p.groups * p.D + i] = t;
+                    }
+            }
+        };
+        keep(p.da, sa, 0);
+        keep(p.db, sb, 1);
     }
 }
 
-// The weights' gradients from the slots' sums: 64 columns a workgroup, 16 wavefronts take slots in turn, joined in 64 bits.
-struct NormJoinParams { const float* part[2]; float* out[2]; int64_t slots; int D, groups; };
+// The weights' gradients from the workgroups' sums: 64 columns a workgroup, 16 wavefronts take records in turn, joined in 64 bits.
+struct NormJoinParams { const float* part[2]; float* out[2]; int64_t records; int D, groups; };
 __global__ __launch_bounds__(1024) void block_norm_join_kernel(const NormJoinParams p) {
     __shared__ double red[16][64];
     const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
     const float* from = p.part[blockIdx.y];
     double s = 0.0;
     if (from && c < p.D * p.groups)
-        for (int64_t k = c / p.D + (int64_t)w * p.groups; k < p.slots; k += 16 * p.groups) s += from[k * p.D + c % p.D];
+#pragma unroll 4
+        for (int64_t k = c / p.D + (int64_t)w * p.groups; k < p.records; k += 16 * p.groups) s += from[k * p.D + c % p.D];
     red[w][threadIdx.x & 63] = s;
     __syncthreads();
     if (from && w == 0 && c < p.D * p.groups) {
@@ -272,26 +373,29 @@ int bn_launched(const char* who) {
 }
 bool bn_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-// How rows of d elements (of a group) lie on lanes: nc eights for each of `lanes`; rows a workgroup works on at a time.
-struct NormShape { int nc, lanes, threads, at_once; bool group; int64_t blocks; };
-NormShape bn_shape(int64_t rows, int d, int groups) {
+// How rows of d elements (of a group) lie on lanes: nc eights for each of `lanes`; rows a workgroup works on at a time; partial sums of weights it leaves.
+struct NormShape { int nc, lanes, threads, at_once; bool group; int64_t blocks, records; };
+NormShape bn_shape(int64_t rows, int d, int groups, bool grad) {
     NormShape s{};
-    if (d <= 1024) {
+    if (d <= (grad ? 512 : 1024)) {
         s.nc = d <= 512 ? 1 : 2;
         s.lanes = 1;
         while (s.lanes * 8 * s.nc < d) s.lanes *= 2;
         s.threads = 256;
         s.at_once = 256 / s.lanes;
     } else {
+        // (gradients of rows of 600 and 1024 bf16: 470 and 249 us for 2^26 elements with one eight a lane, 496 and 266 with two in a wavefront; of 3000 and 4096:
+        // 396 and 250 with two, 656 and 369 with one)
         s.group = true;
-        s.nc = 2;
-        s.threads = s.lanes = (d + 1023) / 1024 * 64;
+        s.nc = !grad ? 2 : d <= 1024 ? 1 : d <= 8192 ? 2 : 4;
+        s.threads = s.lanes = (d + 512 * s.nc - 1) / (512 * s.nc) * 64;
         s.at_once = 1;
     }
-    // two workgroups of 1024 lanes a compute unit; the slots in all are a multiple of the groups
-    int64_t most = 256 * 2048 / s.threads;
+    // as many workgroups as are on the chip at once; the slots in all are a multiple of the groups
+    const int64_t most = 256 * std::max<int64_t>(1, (grad ? s.nc == 1 ? 768 : 512 : 2048) / s.threads);
     s.blocks = std::max<int64_t>(1, std::min(most, (rows + s.at_once - 1) / s.at_once));
     while (s.blocks * s.at_once % groups) ++s.blocks;
+    s.records = s.blocks * (s.at_once % groups == 0 ? groups : s.at_once);
     return s;
 }
 
@@ -304,9 +408,19 @@ int bn_sizes(const char* who, int64_t N, int32_t D, int32_t groups) {
 
 template <typename T, typename S, bool GRAD> void bn_go(const NormParams& p, const NormShape& s, hipStream_t st) {
     const dim3 grid((uint32_t)s.blocks), block(s.threads);
-    if (s.group) block_norm_kernel<T, S, 2, true, GRAD><<<grid, block, 0, st>>>(p);
-    else if (s.nc == 2) block_norm_kernel<T, S, 2, false, GRAD><<<grid, block, 0, st>>>(p);
-    else block_norm_kernel<T, S, 1, false, GRAD><<<grid, block, 0, st>>>(p);
+    if (p.D < 8) block_norm_kernel<T, S, 1, 256, false, GRAD, true><<<grid, block, 0, st>>>(p);
+    else if (!s.group) {
+        if (s.nc == 2) block_norm_kernel<T, S, 2, 256, false, false, false><<<grid, block, 0, st>>>(p);
+        else block_norm_kernel<T, S, 1, 256, false, GRAD, false><<<grid, block, 0, st>>>(p);
+    } else if (s.nc == 4) {
+        block_norm_kernel<T, S, GRAD ? 4 : 2, 512, true, GRAD, false><<<grid, block, 0, st>>>(p);
+    } else if (s.nc == 2) {
+        if (s.threads <= 256) block_norm_kernel<T, S, 2, 256, true, GRAD, false><<<grid, block, 0, st>>>(p);
+        else if (s.threads <= 512) block_norm_kernel<T, S, 2, 512, true, GRAD, false><<<grid, block, 0, st>>>(p);
+        else if constexpr (!GRAD) block_norm_kernel<T, S, 2, 1024, true, GRAD, false><<<grid, block, 0, st>>>(p);
+    } else {
+        block_norm_kernel<T, S, 1, 256, true, GRAD, false><<<grid, block, 0, st>>>(p);
+    }
 }
 template <bool GRAD> int bn_run(const char* who, const accerl_block_norm_args& a, NormParams& p, const NormShape& s, hipStream_t st) {
     const bool wide = a.stream_dtype == ACCERL_DT_F32;
@@ -358,7 +472,7 @@ NormParams bn_params(const accerl_block_norm_args& a, const NormShape& s) {
     p.inv_d = (float)(1.0 / p.D);
     return p;
 }
-int64_t bn_part(const NormShape& s, int d) { return (s.blocks * s.at_once * d + 3) / 4 * 4; }
+int64_t bn_part(const NormShape& s, int d) { return (s.records * d + 3) / 4 * 4; }
 }  // namespace
 }  // namespace accerl
 
@@ -368,7 +482,7 @@ extern "C" {
 
 int64_t accerl_block_norm_workspace(int64_t N, int32_t D, int32_t groups) {
     if (int rc = bn_sizes("block_norm_workspace", N, D, groups)) return rc;
-    return 2 * 4 * bn_part(bn_shape(N * groups, D / groups, groups), D / groups);
+    return 2 * 4 * bn_part(bn_shape(N * groups, D / groups, groups, true), D / groups);
 }
 
 int accerl_block_norm(const accerl_block_norm_args* a, void* stream) {
@@ -383,7 +497,7 @@ int accerl_block_norm(const accerl_block_norm_args* a, void* stream) {
     if (int rc = bn_check(who, a, t, 5, &done)) return rc;
     if (done) return ACCERL_OK;
     if (a->before ? !a->out_h : !a->out_u) return bn_fail(ACCERL_EINVAL, who, "NULL output");
-    const NormShape s = bn_shape(a->N * a->groups, a->D / a->groups, a->groups);
+    const NormShape s = bn_shape(a->N * a->groups, a->D / a->groups, a->groups, false);
     NormParams p = bn_params(*a, s);
     p.u = a->out_u; p.ldu = a->ld_u;
     p.h = a->out_h; p.ldh = a->ld_h;
@@ -405,7 +519,7 @@ int accerl_block_norm_grad(const accerl_block_norm_args* a, void* stream) {
         return bn_fail(ACCERL_EINVAL, who, "a gradient by what the call does not have");
     if (!bn_aligned(a->grad_after, 4) || !bn_aligned(a->grad_before, 4)) return bn_fail(ACCERL_EINVAL, who, "misaligned argument");
     const bool sums = a->grad_after || a->grad_before;
-    const NormShape s = bn_shape(a->N * a->groups, a->D / a->groups, a->groups);
+    const NormShape s = bn_shape(a->N * a->groups, a->D / a->groups, a->groups, true);
     const int64_t part = bn_part(s, a->D / a->groups);
     float* ws = (float*)a->workspace;
     if (sums) {
@@ -426,7 +540,7 @@ int accerl_block_norm_grad(const accerl_block_norm_args* a, void* stream) {
     NormJoinParams j{};
     j.part[0] = p.da; j.out[0] = a->grad_after;
     j.part[1] = p.db; j.out[1] = a->grad_before;
-    j.slots = s.blocks * s.at_once; j.D = p.D; j.groups = a->groups;
+    j.records = s.records; j.D = p.D; j.groups = a->groups;
     block_norm_join_kernel<<<dim3((a->D + 63) / 64, 2), dim3(1024), 0, (hipStream_t)stream>>>(j);
     return bn_launched(who);
 }

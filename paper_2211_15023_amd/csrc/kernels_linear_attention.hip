@@ -147,8 +147,10 @@ struct LaHalf {
     static constexpr int BV = DX / 8 / NW, CV = YW / 8 / NW;  // vectors of a lane
     static constexpr int NA = DX / 16 / NW, ND = NW;          // tiles of 16 rows and 16 columns of the state for a wavefront
     static constexpr int KX = DX / 32;                        // depth of the products over X in matrix instructions
-    static constexpr int WAVES = NW == 8 ? 2 : SPLIT ? (DX == 256 ? 1 : 2) : DX == 64 ? 3 : DX == 128 ? 2 : 1;      // of a SIMD
-    static constexpr int CT = LC * CP, SF = DX * YW;          // elements of a part of c's tile and of the state's fragments
+    static constexpr int WAVES = NW == 8 ? 2 : SPLIT ? (DX == 256 ? 1 : 2) : DX == 64 ? 2 : 1;      // of a SIMD
+    // Two of each tile, where they fit: the next chunk is staged and the next state handed out while this one is read, and a chunk has one barrier
+    static constexpr bool TWO = !SPLIT && DX <= 128;
+    static constexpr int CT = LC * CP, SF = DX * YW, BT = LC * BP;          // elements of a part of c's tile and of the state's fragments
 };
 
 __device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
@@ -169,6 +171,11 @@ template <int N> __device__ __forceinline__ void parts8(const float* x, v8bf* to
 #pragma unroll
     for (int k = 0; k < N; ++k) to[k] = __builtin_bit_cast(v8bf, p[k]);
 }
+// the same rounded to nearest: one part or two
+template <int N> __device__ __forceinline__ void rounded8(const float* x, v8bf* to) {
+    if constexpr (N == 2) parts8<2>(x, to);
+    else to[0] = __builtin_bit_cast(v8bf, u32x4{f32_pair<BF16>(x[0], x[1]), f32_pair<BF16>(x[2], x[3]), f32_pair<BF16>(x[4], x[5]), f32_pair<BF16>(x[6], x[7])});
+}
 template <typename T> __device__ __forceinline__ void unpack8(u32x4 w, float* x) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) el_pair<T>(w[j], x[2 * j], x[2 * j + 1]);
@@ -182,16 +189,17 @@ template <typename T> __device__ __forceinline__ v4f mma_as(u32x4 a, u32x4 b, v4
 
 // FULL: heads of exactly DX and slices of exactly LY elements, whose loads need no look at where a row ends.  OUT: the mixing; else the state behind the
 // segment alone.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its end) and the tables hold for all.
-template <typename T, int DX, int NW, bool OUT, bool FULL>
-__global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_kernel(const LaParams p) {
+// EXACT: the state is wanted; else b's weighted copy has one part only, rounded as the state's copy is.
+template <typename T, int DX, int NW, bool OUT, bool FULL, bool EXACT>
+__global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAVES : NW == 8 ? 4 : 3)) void la_half_kernel(const LaParams p) {
     typedef LaHalf<T, DX, NW> L;
-    constexpr int NA = L::NA, ND = L::ND;
+    constexpr int NA = L::NA, ND = L::ND, NB = L::TWO ? 2 : 1, TERMS = EXACT ? 3 : L::PARTS;
 
-    __shared__ __attribute__((aligned(16))) uint16_t sb[LC * L::BP];
-    __shared__ __attribute__((aligned(16))) uint16_t sc[L::PARTS * L::CT];
+    __shared__ __attribute__((aligned(16))) uint16_t sb[NB * L::BT];
+    __shared__ __attribute__((aligned(16))) uint16_t sc[NB * L::PARTS * L::CT];
     // the state as the fragments that the product with a reads: [part][column tile][depth][lane][8]
-    __shared__ __attribute__((aligned(16))) uint16_t ss[OUT ? L::PARTS * L::SF : 8];
-    __shared__ int odd[NW];                                   // whether a wavefront has seen a NaN or an infinity in b or c
+    __shared__ __attribute__((aligned(16))) uint16_t ss[OUT ? NB * L::PARTS * L::SF : 8];
+    __shared__ int odd[NB][NW];                                 // whether a wavefront has seen a NaN or an infinity in b or c
     __shared__ float red[NW][L::YW];
 
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
@@ -221,20 +229,36 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
     la_state_in<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, S);
     // Every wavefront has its rows of the state, and a tile of 16 tokens by 64 columns (`half` of eight wavefronts' 128) of the output
     const int wq = w & 3, half = w >> 2;
-    // Weights g^(t-s) of pairs s = 16 st + 4 g + i, t = 16 w + r: on the diagonal their own, below it near[i] far[st], of which neither is a negative power;
-    // and of token s in the state behind the chunk, tail[i] block[st]
+    // Weights g^(t-s) of pairs s = 16 st + 4 g + i, and g^(63-s) of token s in the state behind the chunk.  Where registers are short (LEAN) they are made of two
+    // factors, of which neither is a negative power: below the diagonal of 16 x 16 near[i] far[st], and tail[i] block[st].
+    constexpr bool LEAN = !OUT || DX == 256;
     const int t = 16 * wq + r;
-    float diag[4], near[4], far[3], tail[4], block[4];
+    float dec[LEAN ? 1 : 4][4], kw[LEAN ? 1 : 4][4], diag[4], near[4], tail[4], far[4], block[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int s = 4 * g + i;
-        diag[i] = s <= r ? decay_pow(lg, r - s) * (q.pair * q.scale) : 0.0f;
-        near[i] = decay_pow(lg, r - s + 15) * (q.pair * q.scale);
-        tail[i] = decay_pow(lg, 15 - s) * q.pair;
-        block[i] = everywhere(decay_pow(lg, 48 - 16 * i + back));
-    }
+        if constexpr (LEAN) {
+            diag[i] = s <= r ? decay_pow(lg, r - s) * (q.pair * q.scale) : 0.0f;
+            near[i] = decay_pow(lg, r - s + 15) * (q.pair * q.scale);
+            tail[i] = decay_pow(lg, 15 - s) * q.pair;
+            far[i] = everywhere(i < wq ? decay_pow(lg, 16 * (wq - i) - 15) : 0.0f);
+            block[i] = everywhere(decay_pow(lg, 48 - 16 * i + back));
+        } else {
 #pragma unroll
-    for (int st = 0; st < 3; ++st) far[st] = everywhere(decay_pow(lg, max(16 * (wq - st) - 15, 0)));
+            for (int st = 0; st < 4; ++st) {
+                dec[st][i] = 16 * st + s <= t ? decay_pow(lg, t - 16 * st - s) * (q.pair * q.scale) : 0.0f;
+                kw[st][i] = decay_pow(lg, LC - 1 - 16 * st - s + back) * q.pair;
+            }
+        }
+    }
+    auto dec_of = [&](int st, int i) {
+        if constexpr (LEAN) return st == wq ? diag[i] : near[i] * far[st];
+        else return dec[st][i];
+    };
+    auto kw_of = [&](int st, int i) {
+        if constexpr (LEAN) return tail[i] * block[st];
+        else return kw[st][i];
+    };
     float qw = decay_pow(lg, max(t - gap, 0) + 1 - back) * q.scale, sd = everywhere(decay_pow(lg, LC - gap));      // (the first chunk's)
     float left = 1.0f;                                        // of the segment's first state
 
@@ -242,6 +266,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
     constexpr int BR = 512 * NW / DX, CR = 512 * NW / L::YW;             // rows from one vector of a lane to its next
     u32x4 vb[L::BV], vc[L::CV], va[OUT ? L::KX : 1];
     uint32_t cut = 0;
+    uint64_t cuts = 0;                                        // tokens of a chunk that start from nothing
     // Pointers of a lane's rows, which go on by a chunk with every fetch.  In the first chunk rows that are not there count as the first that is.
     const T *lb = pb + brow * tb + bcol, *lc = pc + crow * tc + ccol, *la = pa + t * ta_ + 8 * g;
     auto fetch = [&](int c, auto first) {
@@ -280,6 +305,8 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
     const std::true_type is_first;
     const std::false_type later;
     auto stage = [&](int c) {
+        const int at = L::TWO ? c & 1 : 0;
+        uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT;
         if (c == 0 && gap) {
             const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
@@ -296,12 +323,12 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
 #pragma unroll
         for (int k = 0; k < L::BV; ++k) {
             look(vb[k]);
-            *(u32x4*)(sb + (brow + k * BR) * L::BP + bcol) = vb[k];
+            *(u32x4*)(tb_ + (brow + k * BR) * L::BP + bcol) = vb[k];
         }
 #pragma unroll
         for (int k = 0; k < L::CV; ++k) {
             look(vc[k]);
-            uint16_t* o = sc + (crow + k * CR) * L::CP + ccol;
+            uint16_t* o = tc_ + (crow + k * CR) * L::CP + ccol;
             if constexpr (L::SPLIT) {
                 float x[8];
                 v8bf part[2];
@@ -319,13 +346,15 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
             }
         }
         const bool any = __ballot(max((uint32_t)top[0], (uint32_t)top[1]) >= L::INF) != 0;
-        if (lane == 0) odd[w] = any;
+        if (lane == 0) odd[at][w] = any;
+        cuts = __ballot(cut != 0);
     };
-    auto publish = [&](int first) {
+    auto publish = [&](int c, int first) {
+        uint16_t* const ts = ss + (L::TWO ? c & 1 : 0) * L::PARTS * L::SF;
         if constexpr (OUT && L::SPLIT) {
             // (an infinity has no second part; a state that the chunk's first token ends may be anything)
             uint32_t top = 0;
-            if (__ballot(cut != 0) >> first & 1)
+            if (cuts >> first & 1)
 #pragma unroll
                 for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
@@ -336,7 +365,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
                 for (int d = 0; d < ND; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(S[ta][d][i]) & 0x7fffffffu);
-            if (__ballot(top >= 0x7f800000u) && lane == 0) odd[w] = 1;
+            if (__ballot(top >= 0x7f800000u) && lane == 0) odd[0][w] = 1;
         }
         if constexpr (OUT)
 #pragma unroll
@@ -344,7 +373,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
                 const int tile = NA * w + ta, quad = 4 * (tile & 1) + g;    // rows 4 quad .. of the 32 of a fragment belong to lane group quad / 2
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    uint16_t* o = ss + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
+                    uint16_t* o = ts + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
                     const v4f s = S[ta][d];
                     if constexpr (L::SPLIT) {
                         *(u32x2*)o = u32x2{high_halves(s[0], s[1]), high_halves(s[2], s[3])};
@@ -361,196 +390,200 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
         const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(from + rows16));
         return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    const uint16_t* down_b = sb + (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w;
-    const uint16_t* down_c = sc + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
-
-    if (chunks) { fetch(0, is_first); fetch_a(is_first); stage(0); publish(gap); }
-    for (int c = 0; c < chunks; ++c) {
-        const uint64_t cuts = __ballot(cut != 0);
-        __syncthreads();
-        const bool more = c + 1 < chunks;
-        // (kept as they are: their products, worked out ahead of the loop, would take 28 registers)
+    // One chunk, without and with borders of episodes in it (LEAN: one form for both).  The order lets the loads of what comes next run behind all products.
+    auto chunk = [&](int c, bool more, uint64_t here, auto bordered) {
+        constexpr bool CUTS = decltype(bordered)::value;
+        const int at = L::TWO ? c & 1 : 0;
+        const uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT, *const ts = ss + at * L::PARTS * L::SF;
+        const uint16_t* down_b = tb_ + (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w;
+        const uint16_t* down_c = tc_ + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
+        if constexpr (LEAN) {
+            // (kept as they are: the products, worked out ahead of the loop, would take the registers)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
-        if (more) fetch(c + 1, later);
-        __builtin_amdgcn_sched_barrier(0);
-        int seen = 0;
+            for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
+        }
+        const int last_cut = here ? 63 - __builtin_clzll(here) : -1;
+        if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (OUT) {
+            v4f O[4], P[4];
 #pragma unroll
-        for (int i = 0; i < NW; ++i) seen |= odd[i];
-        const bool plain = !seen;
-        const int last_cut = cuts ? 63 - __builtin_clzll(cuts) : -1;
-
-        if (plain) {
-            v4f O[4];
-            v8bf pt[2][L::PARTS];                             // weights of pairs as the product with c reads them
-            if constexpr (OUT) {
-                v4f P[4];
+            for (int d = 0; d < 4; ++d) O[d] = P[d] = v4f{0, 0, 0, 0};
 #pragma unroll
-                for (int st = 0; st < 4; ++st) P[st] = v4f{0, 0, 0, 0};
-#pragma unroll
-                for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < L::KX; ++k) {
-                    v8bf fa[L::PARTS];
-                    if constexpr (L::SPLIT) {
-                        float x[8];
-                        unpack8<T>(va[k], x);
-                        parts8<2>(x, fa);
-                    } else {
-                        fa[0] = __builtin_bit_cast(v8bf, va[k]);
-                    }
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const uint16_t* f = ss + (((4 * half + d) * L::KX + k) * 64 + lane) * 8;
-                        if constexpr (L::SPLIT) {
-                            O[d] = mma(*(const v8bf*)(f + L::SF), fa[0], O[d]);
-                            O[d] = mma(*(const v8bf*)f, fa[1], O[d]);
-                        }
-                        O[d] = mma(*(const v8bf*)f, fa[0], O[d]);
-                    }
+            for (int k = 0; k < L::KX; ++k) {
+                v8bf fa[L::PARTS];
+                if constexpr (L::SPLIT) {
+                    float x[8];
+                    unpack8<T>(va[k], x);
+                    parts8<2>(x, fa);
+                } else {
+                    fa[0] = __builtin_bit_cast(v8bf, va[k]);
                 }
 #pragma unroll
-                for (int st = 0; st < 4; ++st)
-                    if (st <= wq)
+                for (int d = 0; d < 4; ++d) {
+                    const uint16_t* f = ts + (((4 * half + d) * L::KX + k) * 64 + lane) * 8;
+                    if constexpr (L::SPLIT) {
+                        O[d] = mma(*(const v8bf*)(f + L::SF), fa[0], O[d]);
+                        O[d] = mma(*(const v8bf*)f, fa[1], O[d]);
+                    }
+                    O[d] = mma(*(const v8bf*)f, fa[0], O[d]);
+                }
 #pragma unroll
-                        for (int k = 0; k < L::KX; ++k) P[st] = mma_as<T>(*(const u32x4*)(sb + (16 * st + r) * L::BP + 32 * k + 8 * g), va[k], P[st]);
-                if (more) fetch_a(later);
+                for (int st = 0; st < 4; ++st) P[st] = mma_as<T>(*(const u32x4*)(tb_ + (16 * st + r) * L::BP + 32 * k + 8 * g), va[k], P[st]);
+            }
+            if (more) fetch_a(later);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) O[d][i] *= qw;
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) P[st][i] *= dec_of(st, i);
+            if constexpr (CUTS) {
+                const uint64_t before = here & ((2ull << t) - 1);
+                const int first = before ? 63 - __builtin_clzll(before) : -1;            // the token that t's episode begins with, if it begins in this chunk
+                // (selected, not multiplied by 0: the state of the episode before may hold anything)
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) O[d][i] *= qw;
-                float wt[4][4];
+                    for (int i = 0; i < 4; ++i) O[d][i] = first >= 0 ? 0.0f : O[d][i];
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
+                for (int st = 0; st < 4; ++st)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) wt[st][i] = 0.0f;
-                    if (st == wq) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * diag[i];
-                    } else if (st < wq) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * (near[i] * far[st < 3 ? st : 0]);
-                    }
-                }
-                if (cuts) {
-                    const uint64_t before = cuts & ((2ull << t) - 1);
-                    const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
-                    // (selected, not multiplied by 0: the state of the episode before may hold anything)
-                    if (first >= 0)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
-#pragma unroll
-                    for (int st = 0; st < 4; ++st)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) if (16 * st + 4 * g + i < first) wt[st][i] = 0.0f;
-                }
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    const float* x = wt[2 * ks];
-                    if constexpr (L::SPLIT) parts8<2>(x, pt[ks]);
-                    else pt[ks][0] = __builtin_bit_cast(v8bf, u32x4{f32_pair<BF16>(x[0], x[1]), f32_pair<BF16>(x[2], x[3]), f32_pair<BF16>(x[4], x[5]), f32_pair<BF16>(x[6], x[7])});
-                }
-            }
-            if constexpr (OUT) {
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks)
-                    if (2 * ks <= wq)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            v8bf fc[L::PARTS];
-#pragma unroll
-                            for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * half + 4 * d, 16 * L::CP));
-                            if constexpr (L::SPLIT) {
-                                O[d] = mma(fc[1], pt[ks][0], O[d]);
-                                O[d] = mma(fc[0], pt[ks][1], O[d]);
-                            }
-                            O[d] = mma(fc[0], pt[ks][0], O[d]);
-                        }
-                if (c || t >= gap) {
-                    const int64_t o = po + ((int64_t)c * LC + t) * to + 64 * half + 16 * g;
-                    float v[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = O[j / 4][j % 4];
-                    if (q.out_f32) {
-                        float* f = (float*)q.out + o;
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            if (FULL || 64 * half + 16 * g + 4 * d + 4 <= yw) *(u32x4_at4*)(f + 4 * d) = __builtin_bit_cast(u32x4, v4f{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]});
-                            else
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) if (64 * half + 16 * g + 4 * d + i < yw) f[4 * d + i] = v[4 * d + i];
-                        }
-                    } else {
-                        T* f = (T*)q.out + o;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float* x = v + 8 * e;
-                            if (FULL || 64 * half + 16 * g + 8 * e + 8 <= yw)
-                                *(u32x4_at2*)(f + 8 * e) = u32x4{f32_pair<T>(x[0], x[1]), f32_pair<T>(x[2], x[3]), f32_pair<T>(x[4], x[5]), f32_pair<T>(x[6], x[7])};
-                            else
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) if (64 * half + 16 * g + 8 * e + i < yw) f[8 * e + i] = f32_el<T>(x[i]);
-                        }
-                    }
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            // what enters the next chunk
-            if (cuts) {
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
-            } else {
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) S[ta][d][i] *= sd;
+                    for (int i = 0; i < 4; ++i) P[st][i] = 16 * st + 4 * g + i < first ? 0.0f : P[st][i];
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                float kw[8];
+                v8bf pt[L::PARTS];                            // weights of pairs as the product with c reads them
+                const float x[8] = {P[2 * ks][0], P[2 * ks][1], P[2 * ks][2], P[2 * ks][3], P[2 * ks + 1][0], P[2 * ks + 1][1], P[2 * ks + 1][2], P[2 * ks + 1][3]};
+                rounded8<L::PARTS>(x, pt);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) kw[j] = tail[j % 4] * block[2 * ks + j / 4];
-                if (cuts)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) if (32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut) kw[j] = 0.0f;
-                // b weighted in fp32 and taken apart without loss: the state is a sum of fp32 terms
-                v8bf fb[NA][3];
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta) {
-                    float x[8];
-                    unpack8<T>(down(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] *= kw[j];
-                    parts8<3>(x, fb[ta]);
-                }
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
+                for (int d = 0; d < 4; ++d) {
                     v8bf fc[L::PARTS];
 #pragma unroll
-                    for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * (d / 4) + 4 * (d % 4), 16 * L::CP));
+                    for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * half + 4 * d, 16 * L::CP));
+                    if constexpr (L::SPLIT) {
+                        O[d] = mma(fc[1], pt[0], O[d]);
+                        O[d] = mma(fc[0], pt[1], O[d]);
+                    }
+                    O[d] = mma(fc[0], pt[0], O[d]);
+                }
+            }
+            if (c || t >= gap) {
+                const int64_t o = po + ((int64_t)c * LC + t) * to + 64 * half + 16 * g;
+                float v[16];
 #pragma unroll
-                    for (int ta = 0; ta < NA; ++ta) {
-                        S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
-                        if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
-                        S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
-                        if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
-                        S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+                for (int j = 0; j < 16; ++j) v[j] = O[j / 4][j % 4];
+                if (q.out_f32) {
+                    float* f = (float*)q.out + o;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        if (FULL || 64 * half + 16 * g + 4 * d + 4 <= yw) *(u32x4_at4*)(f + 4 * d) = __builtin_bit_cast(u32x4, v4f{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]});
+                        else
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) if (64 * half + 16 * g + 4 * d + i < yw) f[4 * d + i] = v[4 * d + i];
+                    }
+                } else {
+                    T* f = (T*)q.out + o;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float* x = v + 8 * e;
+                        if (FULL || 64 * half + 16 * g + 8 * e + 8 <= yw)
+                            *(u32x4_at2*)(f + 8 * e) = u32x4{f32_pair<T>(x[0], x[1]), f32_pair<T>(x[2], x[3]), f32_pair<T>(x[4], x[5]), f32_pair<T>(x[6], x[7])};
+                        else
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) if (64 * half + 16 * g + 8 * e + i < yw) f[8 * e + i] = f32_el<T>(x[i]);
                     }
                 }
             }
+        }
+        if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
+        // what enters the next chunk
+        if (CUTS && (!LEAN || here)) {
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) S[ta][d][i] *= sd;
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
+            v8bf fb[NA][TERMS];
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta) {
+                // b weighted in fp32 and, where the state is wanted, taken apart without loss: it is a sum of fp32 terms
+                float x[8];
+                unpack8<T>(down(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[j] *= kw_of(2 * ks + j / 4, j % 4);
+                    if constexpr (CUTS) x[j] = 32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut ? 0.0f : x[j];
+                }
+                if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
+                else rounded8<TERMS>(x, fb[ta]);
+                if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                v8bf fc[L::PARTS];
+#pragma unroll
+                for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * (d / 4) + 4 * (d % 4), 16 * L::CP));
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta) {
+                    if constexpr (TERMS == 3) S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
+                    if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
+                    if constexpr (TERMS >= 2) S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
+                    if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
+                    S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+                }
+            }
+        }
+        left = CUTS && (!LEAN || here) ? 0.0f : left * sd;
+    };
+
+    if (chunks) {
+        fetch(0, is_first);
+        fetch_a(is_first);
+        stage(0);
+        publish(0, gap);
+        if (L::TWO && chunks > 1) fetch(1, later);
+    }
+    for (int c = 0; c < chunks; ++c) {
+        __syncthreads();
+        const bool more = c + 1 < chunks;
+        int seen = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) seen |= odd[L::TWO ? c & 1 : 0][i];
+        const uint64_t here = cuts;                           // of this chunk: staging the next one replaces them
+        if (more) {
+            if constexpr (L::TWO) {
+                stage(c + 1);
+                if (c + 2 < chunks) fetch(c + 2, later);
+            } else {
+                fetch(c + 1, later);
+            }
+        }
+        if (!seen) {
+            if (LEAN || here) chunk(c, more, here, std::true_type{});
+            else chunk(c, more, here, std::false_type{});
         } else {
             // A NaN or an infinity in the chunk (fp16: or in the state): in the products above a weight of 0 would carry it to tokens before it and to other episodes.  Token by token,
             // as the formula says.
             const float ge = pow2(lg);
+            const int at = L::TWO ? c & 1 : 0;
+            const uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT;
             int r = lane & 15, g = lane >> 4, tid = threadIdx.x;
             asm("" : "+v"(r), "+v"(g), "+v"(tid));            // (its addresses are made here, not kept through the chunks that do without them)
             const int yr = 16 * (r >> 2) + (r & 3);
             for (int s = c ? 0 : gap; s < LC; ++s) {
-                const bool anew = cuts >> s & 1;
+                const bool anew = here >> s & 1;
                 const int64_t row = (int64_t)c * LC + s;
                 float part[ND] = {};
 #pragma unroll
@@ -558,12 +591,12 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int x = 16 * (NA * w + ta) + 4 * g + j;
-                        const float eb = el_f32(T{sb[s * L::BP + x]}) * q.pair;
+                        const float eb = el_f32(T{tb_[s * L::BP + x]}) * q.pair;
                         float ea = 0.0f;
                         if constexpr (OUT) if (x < X) ea = el_f32(pa[row * ta_ + x]);
 #pragma unroll
                         for (int d = 0; d < ND; ++d) {
-                            const uint16_t* f = sc + s * L::CP + yr + 64 * (d / 4) + 4 * (d % 4);
+                            const uint16_t* f = tc_ + s * L::CP + yr + 64 * (d / 4) + 4 * (d % 4);
                             float ec = L::SPLIT ? el_f32(BF16{f[0]}) : el_f32(T{f[0]});
                             if constexpr (L::SPLIT) { const float lo = el_f32(BF16{f[L::CT]}); if (lo == lo) ec += lo; }    // (of an infinity the second part is a NaN)
                             float e = anew ? 0.0f : back ? S[ta][d][j] : S[ta][d][j] * ge;
@@ -593,12 +626,15 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::WAVES)) void la_half_k
                 }
             }
             if (more) fetch_a(later);
+            left = here ? 0.0f : left * sd;
         }
-        left = cuts ? 0.0f : left * sd;
         qw = decay_pow(lg, t + 1 - back) * q.scale;
         sd = everywhere(decay_pow(lg, LC));
-        __syncthreads();
-        if (more) { stage(c + 1); publish(0); }
+        if constexpr (!L::TWO) {
+            __syncthreads();
+            if (more) stage(c + 1);
+        }
+        if (more) publish(c + 1, 0);
     }
 
     if (q.last) {
@@ -1048,22 +1084,21 @@ int la_check_sizes(const char* who, int64_t B, int64_t T, int32_t H, int32_t Hk,
     return ACCERL_OK;
 }
 
+template <typename T, int DX, int NW, bool OUT, bool FULL>
+void la_half(const LaParams& p, bool exact, dim3 grid, hipStream_t s) {
+    if (!OUT || exact) la_half_kernel<T, DX, NW, OUT, FULL, true><<<grid, dim3(64 * NW), 0, s>>>(p);
+    else if constexpr (OUT) la_half_kernel<T, DX, NW, OUT, FULL, false><<<grid, dim3(64 * NW), 0, s>>>(p);
+}
 template <typename T, int DX, bool OUT>
-void la_go(const LaParams& p, bool wide, bool full, dim3 grid, hipStream_t s) {
-    const dim3 block(256);
+void la_go(const LaParams& p, bool wide, bool full, bool exact, dim3 grid, hipStream_t s) {
     if constexpr (__is_same(T, float)) {
-        if (full) la_float_kernel<DX, OUT, true><<<grid, block, 0, s>>>(p);
-        else la_float_kernel<DX, OUT, false><<<grid, block, 0, s>>>(p);
+        if (full) la_float_kernel<DX, OUT, true><<<grid, dim3(256), 0, s>>>(p);
+        else la_float_kernel<DX, OUT, false><<<grid, dim3(256), 0, s>>>(p);
     } else {
         if constexpr (DX == 128 || (DX == 256 && __is_same(T, BF16))) {
-            if (wide) {
-                if (full) la_half_kernel<T, DX, 8, OUT, true><<<grid, dim3(512), 0, s>>>(p);
-                else la_half_kernel<T, DX, 8, OUT, false><<<grid, dim3(512), 0, s>>>(p);
-                return;
-            }
+            if (wide) return full ? la_half<T, DX, 8, OUT, true>(p, exact, grid, s) : la_half<T, DX, 8, OUT, false>(p, exact, grid, s);
         }
-        if (full) la_half_kernel<T, DX, 4, OUT, true><<<grid, block, 0, s>>>(p);
-        else la_half_kernel<T, DX, 4, OUT, false><<<grid, block, 0, s>>>(p);
+        return full ? la_half<T, DX, 4, OUT, true>(p, exact, grid, s) : la_half<T, DX, 4, OUT, false>(p, exact, grid, s);
     }
 }
 template <typename T, bool OUT>
@@ -1072,9 +1107,10 @@ int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
     for (const LaRole& r : p.role) if (r.slices) most = std::max(most, r.Y);
     const bool wide = !__is_same(T, float) && X > 64 && most > LY && !(__is_same(T, F16) && X == 256);
     const int cols = wide ? 2 * LY : LY;
-    bool full = true;
+    bool full = true, exact = false;
     for (LaRole& r : p.role) {
         if (!r.slices) continue;
+        if (r.last) exact = true;
         r.slices = (r.Y + cols - 1) / cols;
         slices += r.slices;
         if (r.X != X || r.Y % cols) full = false;
@@ -1082,9 +1118,9 @@ int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
     const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * slices;
     if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
     const dim3 grid((uint32_t)blocks);
-    if (X == 64) la_go<T, 64, OUT>(p, wide, full, grid, s);
-    else if (X == 128) la_go<T, 128, OUT>(p, wide, full, grid, s);
-    else la_go<T, 256, OUT>(p, wide, full, grid, s);
+    if (X == 64) la_go<T, 64, OUT>(p, wide, full, exact, grid, s);
+    else if (X == 128) la_go<T, 128, OUT>(p, wide, full, exact, grid, s);
+    else la_go<T, 256, OUT>(p, wide, full, exact, grid, s);
     return la_launched(who);
 }
 int la_pad(int x) { return x <= 64 ? 64 : x <= 128 ? 128 : 256; }
