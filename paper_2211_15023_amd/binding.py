@@ -258,8 +258,8 @@ def accerl_policy_destroy(handle):
 # Marshalling is most of what a small call costs the host (32 states of the 64-unit MLP, time between calls: 5.8 us through ctypes from
 # the code below, 3.6 through accerl_args; the kernel takes 2.5).  A policy's forwards, V-trace and the KL indicators go through
 # accerl_args and come here where it returns None, because an argument is not a plain tensor: an error to raise, a subclass of torch.Tensor,
-# a stream object.  The mixture and the distillation loss always come here.  DenseInt8 and PolicyLoss go through accerl_args, which makes their
-# outputs too, on the current stream.
+# a stream object.  The mixture and the distillation loss always come here.  DenseInt8, PolicyLoss, LinearAttention and BlockNorm go through accerl_args,
+# which makes their outputs too, on the current stream.
 def _ptr(t, dtype=None):
     if t is None:
         return None
@@ -959,6 +959,8 @@ class LinearAttention:
             raise ValueError(f"q, k and v must be CUDA/HIP tensors of {dims} dimensions, q of {self.H} heads")
 
     def _workspace(self, q, k, v, grad, raw):
+        if q.dim() != 4 or k.dim() != 4 or v.dim() != 4 or q.shape[2] != self.H:
+            return None                              # (refused by what comes next)
         n = accerl_linear_attention_workspace(q.shape[0], q.shape[1], self.H, k.shape[2], q.shape[3], v.shape[3], grad)
         return self._work.get(n, raw, q.device) if n else None
 
@@ -967,6 +969,13 @@ class LinearAttention:
 
         state: the one before the first token (None: zeros); reset: bytes [B, T], not 0 where a token begins an episode; lengths: int32 [B], tokens a
         sequence has; out_state: where the state goes, the given one too (None: a new tensor)."""
+        if stream is None and out is None and out_state is None and q.is_cuda:
+            raw = torch._C._cuda_getCurrentRawStream(q.get_device())
+            t = (_args or _loaded()).linear_attention(q, k, v, self.log_decay, state, reset, lengths, self.scale, self._workspace(q, k, v, False, raw), raw)
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                return t[1], t[2]
         self._heads(q, k, v, 4)
         q, k, v = q.detach(), k.detach(), v.detach()
         with _On(stream, q.device) as raw:
@@ -980,9 +989,19 @@ class LinearAttention:
     def backward(self, grad_out, q, k, v, state=None, reset=None, lengths=None, grad_state=None, stream=None):
         """Gradients by q, k, v and (if it was given) the state, of what `forward` of these arguments returns: grad_out by its output, grad_state by
         the state it returns (None: zeros).  `torch.autograd.backward([q, k, v], [r.q, r.k, r.v])` continues them."""
+        r = self.Result()
+        if stream is None and q.is_cuda:
+            raw = torch._C._cuda_getCurrentRawStream(q.get_device())
+            t = (_args or _loaded()).linear_attention_grad(q, k, v, self.log_decay, state, reset, lengths, grad_out, grad_state, self.scale,
+                                                           self._workspace(q, k, v, True, raw), raw)
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                _, r.q, r.k, r.v, *s = t
+                r.state = s[0] if s else None
+                return r
         self._heads(q, k, v, 4)
         q, k, v = q.detach(), k.detach(), v.detach()
-        r = self.Result()
         with _On(stream, q.device) as raw:
             r.q, r.k, r.v = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
             r.state = None if state is None else torch.empty(state.shape, dtype=torch.float32, device=q.device)
@@ -992,6 +1011,13 @@ class LinearAttention:
 
     def step(self, q, k, v, state, reset=None, out=None, out_state=None, stream=None):
         """One token of each environment: q [B, H, Dk], k [B, Hk, Dk], v [B, Hk, Dv] -> out [B, H, Dv].  The state is updated in place, or goes to out_state."""
+        if stream is None and out is None and q.is_cuda:
+            t = (_args or _loaded()).linear_attention_step(q, k, v, self.log_decay, state, reset, None, state if out_state is None else out_state, self.scale,
+                                                           torch._C._cuda_getCurrentRawStream(q.get_device()))
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                return t[1]
         self._heads(q, k, v, 3)
         q, k, v = q.detach(), k.detach(), v.detach()
         with _On(stream, q.device) as raw:
@@ -1022,6 +1048,7 @@ class BlockNorm:
             raise ValueError("unknown kind of norm or gate")
         self.D = D
         self.how = dict(kind=kind, gate_kind=gate, groups=groups, eps=float(eps), skip=float(skip), branch=float(branch))
+        self._how = (NORM_KINDS[kind], GATE_KINDS[gate], groups, float(eps), float(skip), float(branch))
         for n, w in (("after", after), ("before", before)):
             if w is not None and tuple(w.shape) != (D,):
                 raise ValueError(f"{n} must be a vector of {D}")
@@ -1037,6 +1064,11 @@ class BlockNorm:
             if w is not None:
                 getattr(self, n).copy_(w.detach())
 
+    def _sums(self, y, raw):
+        if self.after is None and self.before is None:
+            return None
+        return self._work.get(accerl_block_norm_workspace(y.shape[0], self.D, self.how["groups"]), raw, y.device)
+
     def _input(self, y):
         if not y.is_cuda or y.dim() != 2 or y.shape[1] != self.D:
             raise ValueError(f"y must be a CUDA/HIP matrix of {self.D} columns")
@@ -1044,6 +1076,12 @@ class BlockNorm:
 
     def forward(self, y, x=None, gate=None, u=None, h=None, stream=None):
         """y, x, gate [N, D] -> (u, h): u of x's type (of y's without x), h of y's, None without `before`.  u, h: tables to write to, x and y themselves too."""
+        if stream is None and u is None and h is None and y.is_cuda and y.shape[-1] == self.D:
+            t = (_args or _loaded()).block_norm(y, x, gate, self.after, self.before, *self._how, torch._C._cuda_getCurrentRawStream(y.get_device()))
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                return t[1], t[2] if self.before is not None else None
         y = self._input(y)
         x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
         with _On(stream, y.device) as raw:
@@ -1057,18 +1095,23 @@ class BlockNorm:
     def backward(self, y, x=None, gate=None, grad_u=None, grad_h=None, stream=None):
         """Gradients of what `forward` of these arguments returns, by y, x, gate and the weights (fp32), None where there is nothing to have one; grad_u by
         u, grad_h by h (None: zeros)."""
-        y = self._input(y)
-        x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
         if grad_h is not None and self.before is None:
             raise ValueError("grad_h belongs to the norm before the next block")
         r = self.Result()
+        if stream is None and y.is_cuda and y.dim() == 2 and y.shape[1] == self.D:
+            raw = torch._C._cuda_getCurrentRawStream(y.get_device())
+            t = (_args or _loaded()).block_norm_grad(y, x, gate, self.after, self.before, *self._how, grad_u, grad_h, self._sums(y, raw), raw)
+            if t is not None:
+                if t[0]:
+                    _check(t[0])
+                _, r.y, r.x, r.gate, r.after, r.before = t
+                return r
+        y = self._input(y)
+        x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
         with _On(stream, y.device) as raw:
             like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
             r.y, r.x, r.gate, r.after, r.before = like(y), like(x), like(gate), like(self.after), like(self.before)
-            ws = None
-            if r.after is not None or r.before is not None:
-                ws = self._work.get(accerl_block_norm_workspace(y.shape[0], self.D, self.how["groups"]), raw, y.device)
-            accerl_block_norm_grad(y, ws, x, gate, self.after, self.before, grad_u, grad_h, r.y, r.x, r.gate, r.after, r.before, stream=raw, **self.how)
+            accerl_block_norm_grad(y, self._sums(y, raw), x, gate, self.after, self.before, grad_u, grad_h, r.y, r.x, r.gate, r.after, r.before, stream=raw, **self.how)
         return r
 
 

@@ -1,4 +1,4 @@
-// Argument marshalling of a policy's forwards, V-trace, the KL indicators and the operators of wide policies, as a CPython module: tensors are checked and taken to pointers here, and
+// Argument marshalling of a policy's forwards, V-trace, the KL indicators and the operators of wide policies and of those with a memory, as a CPython module: tensors are checked and taken to pointers here, and
 // the library is called without the interpreter's lock.  A call of 32 states on the 64-unit MLP costs the host what the checks, the
 // conversions of eight ctypes arguments and the launch cost; the kernel takes 2.5 us.
 //
@@ -333,6 +333,213 @@ PyObject* policy_loss(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     });
 }
 
+// ---------------------------------------------------------------- operators of policies with a memory
+struct Tokens { const void* p = nullptr; accerl_token_stride stride{}; int64_t size[4] = {}; };
+accerl_token_stride token_stride(const at::Tensor& t, int dims) {
+    auto of = [&](int i) { return t.size(i) == 1 ? (int64_t)0 : t.stride(i); };
+    return dims == 4 ? accerl_token_stride{of(0), of(1), of(2)} : accerl_token_stride{of(0), 0, of(1)};
+}
+// [B, T, heads, D] or, `dims` 3, [B, heads, D] with contiguous heads
+Tokens tokens(Args& a, c10::ScalarType* type, int dims) {
+    Tokens r;
+    PyObject* o = *a.at++;
+    if (!a.plain || Py_TYPE(o) != (PyTypeObject*)THPVariableClass) { a.plain = false; return r; }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!a.here(t) || t.dim() != dims || (*type != c10::ScalarType::Undefined && t.scalar_type() != *type) || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) { a.plain = false; return r; }
+    *type = t.scalar_type();
+    r.p = t.data_ptr();
+    r.stride = token_stride(t, dims);
+    r.size[0] = t.size(0); r.size[1] = dims == 4 ? t.size(1) : 1; r.size[2] = t.size(dims - 2); r.size[3] = t.size(dims - 1);
+    return r;
+}
+// a dense tensor of this shape, or None
+void* dense(Args& a, c10::ScalarType type, c10::IntArrayRef shape) {
+    if (*a.at == Py_None) { ++a.at; return nullptr; }
+    return a.shaped(type, shape);
+}
+
+// (q, k, v, log_decay, state, reset, lengths): what all calls begin with
+bool attention(Args& a, accerl_linear_attention_args& p, c10::ScalarType* type, int dims) {
+    const Tokens q = tokens(a, type, dims), k = tokens(a, type, dims), v = tokens(a, type, dims);
+    p.B = q.size[0]; p.T = q.size[1]; p.H = (int32_t)q.size[2]; p.Dk = (int32_t)q.size[3];
+    p.Hk = (int32_t)k.size[2]; p.Dv = (int32_t)v.size[3];
+    p.dtype = dtype_code(*type);
+    p.q = q.p; p.k = k.p; p.v = v.p;
+    p.q_stride = q.stride; p.k_stride = k.stride; p.v_stride = v.stride;
+    for (int i = 0; i < 2; ++i) if (k.size[i] != q.size[i] || v.size[i] != q.size[i]) a.plain = false;
+    if (k.size[3] != q.size[3] || v.size[2] != k.size[2] || p.dtype < 0 || p.B < 1 || p.T < 1) a.plain = false;
+    p.log_decay = (const float*)a.vector(c10::kFloat, p.H);
+    p.state = (const float*)dense(a, c10::kFloat, {p.B, p.H, p.Dk, p.Dv});
+    if (*a.at == Py_None) ++a.at;
+    else {
+        PyObject* o = *a.at++;
+        if (!a.plain || Py_TYPE(o) != (PyTypeObject*)THPVariableClass) { a.plain = false; return false; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!a.here(t) || t.scalar_type() != c10::kByte || t.dim() != dims - 2 || t.size(0) != p.B || (dims == 4 && t.size(1) != p.T)) { a.plain = false; return false; }
+        p.reset = (const uint8_t*)t.data_ptr();
+        p.reset_batch = t.stride(0);
+        p.reset_token = dims == 4 ? t.stride(1) : 0;
+    }
+    p.lengths = (const int32_t*)a.vector(c10::kInt, p.B);
+    if (!p.log_decay) a.plain = false;
+    return a.plain;
+}
+// the workspace argument: a tensor of bytes, or None
+void attention_workspace(Args& a, accerl_linear_attention_args& p) {
+    if (*a.at == Py_None) { ++a.at; return; }
+    const at::Tensor* ws = a.tensor();
+    if (!a.plain) return;
+    p.workspace = ws->data_ptr();
+    p.workspace_bytes = ws->numel();
+}
+void* made_state(std::vector<at::Tensor>& outs, const accerl_linear_attention_args& p) {
+    outs.push_back(made({p.B, p.H, p.Dk, p.Dv}, c10::kFloat));
+    return outs.back().data_ptr();
+}
+
+// (q, k, v, log_decay, state, reset, lengths, scale, workspace, stream) -> (status, out, state)
+PyObject* linear_attention(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return call_out(argv, n, 10, [](Args& a, std::vector<at::Tensor>& outs) {
+        accerl_linear_attention_args p{};
+        c10::ScalarType type = c10::ScalarType::Undefined;
+        attention(a, p, &type, 4);
+        if (a.plain) {
+            p.scale = a.number();
+            attention_workspace(a, p);
+            if (p.workspace_bytes < accerl_linear_attention_workspace(p.B, p.T, p.H, p.Hk, p.Dk, p.Dv, 0)) a.plain = false;
+        }
+        void* s = a.plain ? a.stream() : nullptr;
+        if (a.plain) {
+            outs.push_back(made({p.B, p.T, p.H, p.Dv}, type));
+            p.out = outs[0].data_ptr();
+            p.out_stride = token_stride(outs[0], 4);
+            p.out_state = (float*)made_state(outs, p);
+        }
+        return [=] { return accerl_linear_attention(&p, s); };
+    });
+}
+
+// (q, k, v, log_decay, state, reset, lengths, grad_out, grad_state, scale, workspace, stream) -> (status, grad_q, grad_k, grad_v[, the state's])
+PyObject* linear_attention_grad(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return call_out(argv, n, 12, [](Args& a, std::vector<at::Tensor>& outs) {
+        accerl_linear_attention_args p{};
+        c10::ScalarType type = c10::ScalarType::Undefined;
+        attention(a, p, &type, 4);
+        if (a.plain) {
+            const Tokens go = tokens(a, &type, 4);
+            if (go.size[0] != p.B || go.size[1] != p.T || go.size[2] != p.H || go.size[3] != p.Dv) a.plain = false;
+            p.grad_out = go.p;
+            p.grad_out_stride = go.stride;
+            p.grad_out_state = (const float*)dense(a, c10::kFloat, {p.B, p.H, p.Dk, p.Dv});
+            p.scale = a.number();
+            attention_workspace(a, p);
+            if (a.plain && p.workspace_bytes < accerl_linear_attention_workspace(p.B, p.T, p.H, p.Hk, p.Dk, p.Dv, 1)) a.plain = false;
+        }
+        void* s = a.plain ? a.stream() : nullptr;
+        if (a.plain) {
+            outs.push_back(made({p.B, p.T, p.H, p.Dk}, type));
+            outs.push_back(made({p.B, p.T, p.Hk, p.Dk}, type));
+            outs.push_back(made({p.B, p.T, p.Hk, p.Dv}, type));
+            p.grad_q = outs[0].data_ptr(); p.grad_q_stride = token_stride(outs[0], 4);
+            p.grad_k = outs[1].data_ptr(); p.grad_k_stride = token_stride(outs[1], 4);
+            p.grad_v = outs[2].data_ptr(); p.grad_v_stride = token_stride(outs[2], 4);
+            if (p.state) p.grad_state = (float*)made_state(outs, p);
+        }
+        return [=] { return accerl_linear_attention_grad(&p, s); };
+    });
+}
+
+// (q, k, v, log_decay, state, reset, None, out_state, scale, stream) -> (status, out)
+PyObject* linear_attention_step(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return call_out(argv, n, 10, [](Args& a, std::vector<at::Tensor>& outs) {
+        accerl_linear_attention_args p{};
+        c10::ScalarType type = c10::ScalarType::Undefined;
+        attention(a, p, &type, 3);
+        if (a.plain) {
+            p.out_state = (float*)dense(a, c10::kFloat, {p.B, p.H, p.Dk, p.Dv});
+            p.scale = a.number();
+            if (!p.state || !p.out_state) a.plain = false;
+        }
+        void* s = a.plain ? a.stream() : nullptr;
+        if (a.plain) {
+            outs.push_back(made({p.B, p.H, p.Dv}, type));
+            p.out = outs[0].data_ptr();
+            p.out_stride = token_stride(outs[0], 3);
+        }
+        return [=] { return accerl_linear_attention_step(&p, s); };
+    });
+}
+
+// (y, x, gate, after, before, kind, kind of gate, groups, eps, skip, branch): what both calls begin with
+void block_norm_of(Args& a, accerl_block_norm_args& p, c10::ScalarType* type, c10::ScalarType* flow) {
+    int64_t N = -1, D = -1;
+    p.y = a.rows(type, &N, &D, &p.ld_y);
+    p.x = a.rows(flow, &N, &D, &p.ld_x, true);
+    if (!p.x) *flow = *type;
+    p.gate = a.rows(type, &N, &D, &p.ld_gate, true);
+    p.after = (const float*)a.vector(c10::kFloat, D);
+    p.before = (const float*)a.vector(c10::kFloat, D);
+    p.kind = (int32_t)a.integer();
+    p.gate_kind = (int32_t)a.integer();
+    p.groups = (int32_t)a.integer();
+    p.eps = a.number(); p.skip = a.number(); p.branch = a.number();
+    p.N = N; p.D = (int32_t)D;
+    p.dtype = dtype_code(*type);
+    p.stream_dtype = dtype_code(*flow);
+    if (p.dtype < 0 || p.stream_dtype < 0 || N < 1 || D < 1 || (p.gate_kind != 0) != (p.gate != nullptr)) a.plain = false;
+}
+
+// (.., stream) -> (status, u[, h])
+PyObject* block_norm(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return call_out(argv, n, 12, [](Args& a, std::vector<at::Tensor>& outs) {
+        accerl_block_norm_args p{};
+        c10::ScalarType type = c10::ScalarType::Undefined, flow = c10::ScalarType::Undefined;
+        block_norm_of(a, p, &type, &flow);
+        void* s = a.stream();
+        if (a.plain) {
+            p.ld_u = p.ld_h = p.D;
+            outs.push_back(made({p.N, p.D}, flow));
+            p.out_u = outs[0].data_ptr();
+            if (p.before) {
+                outs.push_back(made({p.N, p.D}, type));
+                p.out_h = outs[1].data_ptr();
+            }
+        }
+        return [=] { return accerl_block_norm(&p, s); };
+    });
+}
+
+// (.., grad_u, grad_h, workspace, stream) -> (status, grad_y, grad_x, grad_gate, grad_after, grad_before), None where there is nothing to have one
+PyObject* block_norm_grad(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return call_out(argv, n, 15, [](Args& a, std::vector<at::Tensor>& outs) {
+        accerl_block_norm_args p{};
+        c10::ScalarType type = c10::ScalarType::Undefined, flow = c10::ScalarType::Undefined;
+        block_norm_of(a, p, &type, &flow);
+        int64_t N = p.N, D = p.D;
+        p.grad_u = a.plain ? a.rows(&flow, &N, &D, &p.ld_grad_u, true) : nullptr;
+        p.grad_h = a.plain ? a.rows(&type, &N, &D, &p.ld_grad_h, true) : nullptr;
+        if (a.plain) {
+            if (*a.at == Py_None) ++a.at;
+            else if (const at::Tensor* ws = a.tensor(); a.plain) { p.workspace = ws->data_ptr(); p.workspace_bytes = ws->numel(); }
+        }
+        void* s = a.plain ? a.stream() : nullptr;
+        if (a.plain && (p.after || p.before) && p.workspace_bytes < accerl_block_norm_workspace(p.N, p.D, p.groups)) a.plain = false;
+        if (a.plain) {
+            p.ld_grad_y = p.ld_grad_x = p.ld_grad_gate = p.D;
+            auto next = [&](bool wanted, c10::IntArrayRef shape, c10::ScalarType t) -> void* {
+                outs.push_back(wanted ? made(shape, t) : at::Tensor());
+                return wanted ? outs.back().data_ptr() : nullptr;
+            };
+            p.grad_y = next(true, {p.N, p.D}, type);
+            p.grad_x = next(p.x != nullptr, {p.N, p.D}, flow);
+            p.grad_gate = next(p.gate != nullptr, {p.N, p.D}, type);
+            p.grad_after = (float*)next(p.after != nullptr, {p.D}, c10::kFloat);
+            p.grad_before = (float*)next(p.before != nullptr, {p.D}, c10::kFloat);
+        }
+        return [=] { return accerl_block_norm_grad(&p, s); };
+    });
+}
+
 PyObject* init(PyObject*, PyObject* type) {
     if (!PyType_Check(type)) { PyErr_SetString(PyExc_TypeError, "expected ctypes.c_void_p"); return nullptr; }
     Py_INCREF(type);
@@ -352,6 +559,11 @@ PyMethodDef methods[] = {
     {"dense_dynamic", FAST(dense_dynamic)},
     {"action_logprob", FAST(action_logprob)},
     {"policy_loss", FAST(policy_loss)},
+    {"linear_attention", FAST(linear_attention)},
+    {"linear_attention_grad", FAST(linear_attention_grad)},
+    {"linear_attention_step", FAST(linear_attention_step)},
+    {"block_norm", FAST(block_norm)},
+    {"block_norm_grad", FAST(block_norm_grad)},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "accerl_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
