@@ -59,6 +59,20 @@ __device__ __forceinline__ float decay_pow(float lg, int n) { return n == 0 ? 1.
 // the same number of all lanes, in a scalar register
 __device__ __forceinline__ float everywhere(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
+// How the vectors of a row are read.  EXACT: the row is as wide as the tile.  EDGE: the row has a vector at least; the last one is read so that it ends with the
+// row and moved down, those behind it are zeros.  SHORT: element by element where need be.
+enum LaEdge { EXACT = 0, EDGE = 1, SHORT = 2 };
+// eight elements of 16 bits moved down by n (8 and more: all gone), zeros moved in
+__device__ __forceinline__ u32x4 move_down(u32x4 w, int n) {
+    if (n > 0) {
+        if (n & 4) w = u32x4{w[2], w[3], 0, 0};
+        if (n & 2) w = u32x4{w[1], w[2], w[3], 0};
+        if (n & 1) w = u32x4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16), __builtin_amdgcn_alignbit(w[3], w[2], 16), w[3] >> 16};
+        if (n >= 8) w = u32x4{0, 0, 0, 0};
+    }
+    return w;
+}
+
 // 16 bytes of a row of which `left` elements are inside; the others are zeros
 template <typename T> __device__ __forceinline__ u32x4 row_vec(const T* p, int left) {
     constexpr int N = 16 / sizeof(T);
@@ -107,7 +121,14 @@ __device__ __forceinline__ void la_state_in(const LaRole& q, uint32_t seg, uint3
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (FULL || (x + 16 * ta + i < X && y + la_column<STEP>(d) < yw)) S[ta][d][i] = e[(16 * ta + i) * q.ex + la_column<STEP>(d) * q.ey];
+                if constexpr (FULL) {
+                    S[ta][d][i] = e[(16 * ta + i) * q.ex + la_column<STEP>(d) * q.ey];
+                } else {
+                    // (those that are not there read the last one that is)
+                    const int xs = min(x + 16 * ta + i, X - 1) - x, ys = min(y + la_column<STEP>(d), yw - 1) - y;
+                    const float v = e[xs * q.ex + ys * q.ey];
+                    S[ta][d][i] = xs == 16 * ta + i && ys == la_column<STEP>(d) ? v : 0.0f;
+                }
 }
 template <int NA, int ND, int STEP, bool FULL>
 __device__ __forceinline__ void la_state_out(const LaRole& q, uint32_t seg, uint32_t bh, int x, int y0, int y, int X, int yw, bool gone, const v4f (&S)[NA][ND]) {
@@ -187,13 +208,14 @@ template <typename T> __device__ __forceinline__ v4f mma_as(u32x4 a, u32x4 b, v4
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
-// FULL: heads of exactly DX and slices of exactly LY elements, whose loads need no look at where a row ends.  OUT: the mixing; else the state behind the
+// HOW: EXACT for heads of DX and slices of YW elements.  OUT: the mixing; else the state behind the
 // segment alone.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its end) and the tables hold for all.
-// EXACT: the state is wanted; else b's weighted copy has one part only, rounded as the state's copy is.
-template <typename T, int DX, int NW, bool OUT, bool FULL, bool EXACT>
+// WANTED: the state behind the last token is; else b's weighted copy has one part only, rounded as the state's copy is.
+template <typename T, int DX, int NW, bool OUT, LaEdge HOW, bool WANTED>
 __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAVES : NW == 8 ? 4 : 3)) void la_half_kernel(const LaParams p) {
     typedef LaHalf<T, DX, NW> L;
-    constexpr int NA = L::NA, ND = L::ND, NB = L::TWO ? 2 : 1, TERMS = EXACT ? 3 : L::PARTS;
+    constexpr int NA = L::NA, ND = L::ND, NB = L::TWO ? 2 : 1, TERMS = WANTED ? 3 : L::PARTS;
+    constexpr bool FULL = HOW == EXACT;
 
     __shared__ __attribute__((aligned(16))) uint16_t sb[NB * L::BT];
     __shared__ __attribute__((aligned(16))) uint16_t sc[NB * L::PARTS * L::CT];
@@ -265,6 +287,7 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
     const int brow = tid / (DX / 8), bcol = tid % (DX / 8) * 8, crow = tid / (L::YW / 8), ccol = tid % (L::YW / 8) * 8;
     constexpr int BR = 512 * NW / DX, CR = 512 * NW / L::YW;             // rows from one vector of a lane to its next
     u32x4 vb[L::BV], vc[L::CV], va[OUT ? L::KX : 1];
+    const int b_to = HOW == EDGE ? min(0, X - 8 - bcol) : 0, c_to = HOW == EDGE ? min(0, yw - 8 - ccol) : 0;      // (where a lane's vector is read, and to be moved from)
     uint32_t cut = 0;
     uint64_t cuts = 0;                                        // tokens of a chunk that start from nothing
     // Pointers of a lane's rows, which go on by a chunk with every fetch.  In the first chunk rows that are not there count as the first that is.
@@ -275,13 +298,13 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
         for (int k = 0; k < L::BV; ++k) {
             const T* f = lb + k * BR * tb;
             if constexpr (FIRST) f += max(gap - brow - k * BR, 0) * tb;
-            vb[k] = FULL ? *(const u32x4_at2*)f : row_vec(bcol < X ? f : pb + gap * tb, X - bcol);
+            vb[k] = HOW == SHORT ? row_vec(bcol < X ? f : pb + gap * tb, X - bcol) : *(const u32x4_at2*)(f + b_to);
         }
 #pragma unroll
         for (int k = 0; k < L::CV; ++k) {
             const T* f = lc + k * CR * tc;
             if constexpr (FIRST) f += max(gap - crow - k * CR, 0) * tc;
-            vc[k] = FULL ? *(const u32x4_at2*)f : row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol);
+            vc[k] = HOW == SHORT ? row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol) : *(const u32x4_at2*)(f + c_to);
         }
         lb += LC * tb;
         lc += LC * tc;
@@ -298,7 +321,10 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
             const T* f = la;
             if constexpr (decltype(first)::value) f += max(gap - t, 0) * ta_;
 #pragma unroll
-            for (int k = 0; k < L::KX; ++k) va[k] = FULL ? *(const u32x4_at2*)(f + 32 * k) : row_vec(8 * g + 32 * k < X ? f + 32 * k : f - 8 * g, X - 32 * k - 8 * g);
+            for (int k = 0; k < L::KX; ++k) {
+                if constexpr (HOW == SHORT) va[k] = row_vec(8 * g + 32 * k < X ? f + 32 * k : f - 8 * g, X - 32 * k - 8 * g);
+                else va[k] = *(const u32x4_at2*)(f + (HOW == EDGE ? min(32 * k, X - 8 - 8 * g) : 32 * k));
+            }
             la += LC * ta_;
         }
     };
@@ -313,6 +339,12 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
             for (int k = 0; k < L::BV; ++k) if (brow + k * BR < gap) vb[k] = none;
 #pragma unroll
             for (int k = 0; k < L::CV; ++k) if (crow + k * CR < gap) vc[k] = none;
+        }
+        if constexpr (HOW == EDGE) {
+#pragma unroll
+            for (int k = 0; k < L::BV; ++k) vb[k] = move_down(vb[k], -b_to);
+#pragma unroll
+            for (int k = 0; k < L::CV; ++k) vc[k] = move_down(vc[k], -c_to);
         }
         typedef unsigned short us2 __attribute__((ext_vector_type(2)));
         us2 top = {0, 0};
@@ -411,6 +443,7 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
 #pragma unroll
             for (int k = 0; k < L::KX; ++k) {
                 v8bf fa[L::PARTS];
+                if constexpr (HOW == EDGE) va[k] = move_down(va[k], max(0, 32 * k + 8 * g + 8 - X));
                 if constexpr (L::SPLIT) {
                     float x[8];
                     unpack8<T>(va[k], x);
@@ -934,10 +967,21 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaJoinParams p) {
     if (i >= p.n) return;
     const int64_t bh = i / p.per, all = p.n / p.per;
     float e = j.enter ? j.enter[i] : 0.0f;
-    for (int s = 0; s < p.segs; ++s) {
-        const float add = j.states[s * p.n + i], f = j.keep[s * all + bh];
-        j.states[s * p.n + i] = e;
-        e = (f == 0.0f ? 0.0f : f * e) + add;
+    constexpr int AT_ONCE = 8;                                // loads under way together
+    for (int s0 = 0; s0 < p.segs; s0 += AT_ONCE) {
+        float add[AT_ONCE], f[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int s = min(s0 + k, p.segs - 1);
+            add[k] = j.states[s * p.n + i];
+            f[k] = j.keep[s * all + bh];
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (s0 + k < p.segs) {
+                j.states[(s0 + k) * p.n + i] = e;
+                e = (f[k] == 0.0f ? 0.0f : f[k] * e) + add[k];
+            }
     }
     if (j.last) j.last[i] = e;
 }
@@ -973,50 +1017,56 @@ struct LaStep {
 };
 
 // A workgroup has 64 columns of a state: 16 lanes of four columns, 16 rows at a time, all rows asked for before the first is used.  Bound by memory: the state
-// is read and written once.
-template <typename T, int ROWS>
-__global__ __launch_bounds__(256) void la_step_kernel(const LaStep p) {
+// is read and written once.  FULL: 16 ROWS rows, and columns in whole workgroups.  ONCE: states that are more than the caches hold go by them.
+template <typename T, int ROWS, bool FULL, bool ONCE>
+__global__ __launch_bounds__(256, ROWS <= 4 ? 8 : ROWS == 8 ? 6 : 4) void la_step_kernel(const LaStep p) {
     __shared__ v4f red[4][16];
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, r = lane & 15, x0 = tid >> 4;
     const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, b = bh / p.H, h = bh % p.H;
-    const int y = slice * 64 + 4 * r, in = min(max(p.Y - y, 0), 4);
+    const int y = slice * 64 + 4 * r, in = FULL ? 4 : min(max(p.Y - y, 0), 4), X = FULL ? 16 * ROWS : p.X;
     const bool anew = p.reset && p.reset[b * p.rb] != 0;
-    const T* pq = (const T*)p.q.p + b * p.q.sb + h * p.q.sh;
-    const T* pk = (const T*)p.k.p + b * p.k.sb + (h / p.k.div) * p.k.sh;
-    const T* pv = (const T*)p.v.p + b * p.v.sb + (h / p.v.div) * p.v.sh + y;
-    const float* s = p.state + (int64_t)bh * p.X * p.Y;
-    float* so = p.out_state + (int64_t)bh * p.X * p.Y;
+    const T* pq = (const T*)p.q.p + b * p.q.sb + h * p.q.sh + x0;
+    const T* pk = (const T*)p.k.p + b * p.k.sb + (h / p.k.div) * p.k.sh + x0;
+    const T* pv = (const T*)p.v.p + b * p.v.sb + (h / p.v.div) * p.v.sh + (in ? y : 0);
+    const int64_t at = (int64_t)bh * X * p.Y + (int64_t)x0 * p.Y + (in ? y : 0);
+    const float* s = p.state + at;
+    float* so = p.out_state + at;
+    const int rows16 = 16 * p.Y;
     v4f S[ROWS];
-    float k[ROWS], q[ROWS];
+    T k[ROWS], q[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const int x = x0 + 16 * i;
         S[i] = v4f{0, 0, 0, 0};
-        k[i] = q[i] = 0.0f;
-        if (x < p.X) {
-            if (!anew) S[i] = __builtin_bit_cast(v4f, row_vec(s + (int64_t)x * p.Y + (in ? y : 0), in));
-            k[i] = el_f32(pk[x]);
-            q[i] = el_f32(pq[x]);
+        if (!anew && (FULL || x0 + 16 * i < X)) {
+            if constexpr (FULL && ONCE) S[i] = __builtin_nontemporal_load((const v4f*)(s + i * rows16));
+            else if constexpr (FULL) S[i] = *(const v4f*)(s + i * rows16);
+            else S[i] = __builtin_bit_cast(v4f, row_vec(s + i * rows16, in));
         }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const bool there = FULL || x0 + 16 * i < X;
+        k[i] = there ? pk[16 * i] : T{};
+        q[i] = there ? pq[16 * i] : T{};
     }
     v4f v = {0, 0, 0, 0}, o = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (j < in) v[j] = el_f32(pv[j]);
-    const float ge = pow2(p.log_decay[h] * LOG2E);
+    const float ge = anew ? 0.0f : pow2(p.log_decay[h] * LOG2E);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const int x = x0 + 16 * i;
-        if (x < p.X) {
+        const float kx = el_f32(k[i]), qx = el_f32(q[i]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                S[i][j] = (anew ? 0.0f : ge * S[i][j]) + k[i] * v[j];
-                o[j] += q[i] * S[i][j];
-            }
-            float* to = so + (int64_t)x * p.Y + y;
-            if (in == 4) *(u32x4_at4*)to = __builtin_bit_cast(u32x4, S[i]);
+        for (int j = 0; j < 4; ++j) {
+            S[i][j] = ge * S[i][j] + kx * v[j];
+            o[j] += qx * S[i][j];
+        }
+        if (FULL || x0 + 16 * i < X) {
+            if constexpr (FULL && ONCE) __builtin_nontemporal_store(S[i], (v4f*)(so + i * rows16));
+            else if (in == 4) *(u32x4_at4*)(so + i * rows16) = __builtin_bit_cast(u32x4, S[i]);
             else
 #pragma unroll
-                for (int j = 0; j < 4; ++j) if (j < in) to[j] = S[i][j];
+                for (int j = 0; j < 4; ++j) if (j < in) so[i * rows16 + j] = S[i][j];
         }
     }
 #pragma unroll
@@ -1047,15 +1097,18 @@ int la_launched(const char* who) {
 bool la_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 constexpr int LA_MAX_D = 256;
+constexpr int64_t ONCE_BYTES = 96 << 20;
 
+constexpr int64_t SEG_BLOCKS = 1024;
+constexpr uint32_t WIDE_GROUPS = 512;
+constexpr int64_t TOGETHER_BLOCKS = 512;
 struct LaPlan { int segs; int64_t seg_len; };
 // Segments of a sequence, worked on side by side: what each adds to the state is summed first (keys and values are read twice), where sequences, heads and
 // columns alone leave compute units without work.
 LaPlan la_plan(int64_t B, int64_t T, int H, int slices) {
-    const int64_t blocks = B * H * slices;
+    const int64_t blocks = B * H * slices, chunks = (T + LC - 1) / LC;
     int64_t segs = 1;
-    if (blocks > 0 && blocks < 512 && T > 4 * LC) segs = std::max<int64_t>(1, std::min<int64_t>((1024 + blocks - 1) / blocks, T / (2 * LC)));
-    const int64_t chunks = (T + LC - 1) / LC;
+    if (blocks > 0 && blocks < 512 && chunks >= 4) segs = std::max<int64_t>(1, std::min<int64_t>((SEG_BLOCKS + blocks - 1) / blocks, chunks));
     const int64_t per = std::max<int64_t>(1, (chunks + segs - 1) / segs);
     return {(int)std::max<int64_t>(1, (chunks + per - 1) / per), per * LC};
 }
@@ -1084,54 +1137,69 @@ int la_check_sizes(const char* who, int64_t B, int64_t T, int32_t H, int32_t Hk,
     return ACCERL_OK;
 }
 
-template <typename T, int DX, int NW, bool OUT, bool FULL>
-void la_half(const LaParams& p, bool exact, dim3 grid, hipStream_t s) {
-    if (!OUT || exact) la_half_kernel<T, DX, NW, OUT, FULL, true><<<grid, dim3(64 * NW), 0, s>>>(p);
-    else if constexpr (OUT) la_half_kernel<T, DX, NW, OUT, FULL, false><<<grid, dim3(64 * NW), 0, s>>>(p);
+template <typename T, int DX, int NW, bool OUT, LaEdge HOW>
+void la_half(const LaParams& p, bool wanted, dim3 grid, hipStream_t s) {
+    if (!OUT || wanted) la_half_kernel<T, DX, NW, OUT, HOW, true><<<grid, dim3(64 * NW), 0, s>>>(p);
+    else if constexpr (OUT) la_half_kernel<T, DX, NW, OUT, HOW, false><<<grid, dim3(64 * NW), 0, s>>>(p);
 }
 template <typename T, int DX, bool OUT>
-void la_go(const LaParams& p, bool wide, bool full, bool exact, dim3 grid, hipStream_t s) {
+void la_go(const LaParams& p, bool wide, LaEdge how, bool wanted, dim3 grid, hipStream_t s) {
     if constexpr (__is_same(T, float)) {
-        if (full) la_float_kernel<DX, OUT, true><<<grid, dim3(256), 0, s>>>(p);
+        if (how == EXACT) la_float_kernel<DX, OUT, true><<<grid, dim3(256), 0, s>>>(p);
         else la_float_kernel<DX, OUT, false><<<grid, dim3(256), 0, s>>>(p);
     } else {
         if constexpr (DX == 128 || (DX == 256 && __is_same(T, BF16))) {
-            if (wide) return full ? la_half<T, DX, 8, OUT, true>(p, exact, grid, s) : la_half<T, DX, 8, OUT, false>(p, exact, grid, s);
+            if (wide) return how == EXACT ? la_half<T, DX, 8, OUT, EXACT>(p, wanted, grid, s) : la_half<T, DX, 8, OUT, EDGE>(p, wanted, grid, s);
         }
-        return full ? la_half<T, DX, 4, OUT, true>(p, exact, grid, s) : la_half<T, DX, 4, OUT, false>(p, exact, grid, s);
+        if (how == EXACT) la_half<T, DX, 4, OUT, EXACT>(p, wanted, grid, s);
+        else if (how == EDGE) la_half<T, DX, 4, OUT, EDGE>(p, wanted, grid, s);
+        else la_half<T, DX, 4, OUT, SHORT>(p, wanted, grid, s);
     }
 }
 template <typename T, bool OUT>
 int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
-    int slices = 0, most = 0;
-    for (const LaRole& r : p.role) if (r.slices) most = std::max(most, r.Y);
-    const bool wide = !__is_same(T, float) && X > 64 && most > LY && !(__is_same(T, F16) && X == 256);
+    int slices = 0, most = 0, least = LA_MAX_D;
+    for (const LaRole& r : p.role)
+        if (r.slices) {
+            most = std::max(most, r.Y);
+            least = std::min(least, std::min(r.X, r.Y));
+        }
+    // (fewer and wider workgroups where there are enough of them to go round)
+    const bool wide = !__is_same(T, float) && X > 64 && most > LY && least >= 8 && !(__is_same(T, F16) && X == 256) && p.groups >= WIDE_GROUPS;
     const int cols = wide ? 2 * LY : LY;
-    bool full = true, exact = false;
+    LaEdge how = least < 8 ? SHORT : EXACT;
+    bool wanted = false;
     for (LaRole& r : p.role) {
         if (!r.slices) continue;
-        if (r.last) exact = true;
+        if (r.last) wanted = true;
         r.slices = (r.Y + cols - 1) / cols;
         slices += r.slices;
-        if (r.X != X || r.Y % cols) full = false;
+        if (how == EXACT && (r.X != X || r.Y % cols)) how = EDGE;
     }
     const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * slices;
     if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
     const dim3 grid((uint32_t)blocks);
-    if (X == 64) la_go<T, 64, OUT>(p, wide, full, exact, grid, s);
-    else if (X == 128) la_go<T, 128, OUT>(p, wide, full, exact, grid, s);
-    else la_go<T, 256, OUT>(p, wide, full, exact, grid, s);
+    if (X == 64) la_go<T, 64, OUT>(p, wide, how, wanted, grid, s);
+    else if (X == 128) la_go<T, 128, OUT>(p, wide, how, wanted, grid, s);
+    else la_go<T, 256, OUT>(p, wide, how, wanted, grid, s);
     return la_launched(who);
 }
 int la_pad(int x) { return x <= 64 ? 64 : x <= 128 ? 128 : 256; }
 
-// launches of the roles, those of one width together
+// Launches of the roles, those of one width together; all in the widest one's where they leave compute units without work one by one.
 template <typename T, bool OUT>
 int la_run(const char* who, const LaParams& common, const LaRole* roles, int count, hipStream_t s) {
+    int64_t blocks = 0;
+    int widest = 0;
+    for (int i = 0; i < count; ++i) {
+        blocks += (int64_t)common.groups * roles[i].slices;
+        widest = std::max(widest, la_pad(roles[i].X));
+    }
+    const bool together = blocks <= TOGETHER_BLOCKS;
     for (int x : {64, 128, 256}) {
         LaParams p = common;
         int n = 0;
-        for (int i = 0; i < count; ++i) if (la_pad(roles[i].X) == x) p.role[n++] = roles[i];
+        for (int i = 0; i < count; ++i) if ((together ? widest : la_pad(roles[i].X)) == x) p.role[n++] = roles[i];
         if (n) if (int rc = la_launch<T, OUT>(who, p, x, s)) return rc;
     }
     return ACCERL_OK;
@@ -1383,12 +1451,19 @@ int accerl_linear_attention_step(const accerl_linear_attention_args* a, void* st
     const int64_t blocks = a->B * a->H * p.slices;
     if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads and columns than one launch takes");
     const dim3 grid((uint32_t)blocks), block(256);
+    const bool whole = a->Dv % 64 == 0, once = 4 * a->B * a->H * (int64_t)a->Dk * a->Dv >= ONCE_BYTES;
     auto go = [&](auto type) {
         typedef decltype(type) T;
-        if (a->Dk <= 32) la_step_kernel<T, 2><<<grid, block, 0, s>>>(p);
-        else if (a->Dk <= 64) la_step_kernel<T, 4><<<grid, block, 0, s>>>(p);
-        else if (a->Dk <= 128) la_step_kernel<T, 8><<<grid, block, 0, s>>>(p);
-        else la_step_kernel<T, 16><<<grid, block, 0, s>>>(p);
+        auto rows = [&](auto n) {
+            constexpr int ROWS = decltype(n)::value;
+            if (!(whole && a->Dk == 16 * ROWS)) la_step_kernel<T, ROWS, false, false><<<grid, block, 0, s>>>(p);
+            else if (once) la_step_kernel<T, ROWS, true, true><<<grid, block, 0, s>>>(p);
+            else la_step_kernel<T, ROWS, true, false><<<grid, block, 0, s>>>(p);
+        };
+        if (a->Dk <= 32) rows(std::integral_constant<int, 2>());
+        else if (a->Dk <= 64) rows(std::integral_constant<int, 4>());
+        else if (a->Dk <= 128) rows(std::integral_constant<int, 8>());
+        else rows(std::integral_constant<int, 16>());
     };
     if (a->dtype == ACCERL_DT_F32) go(0.0f);
     else if (a->dtype == ACCERL_DT_BF16) go(BF16{});
