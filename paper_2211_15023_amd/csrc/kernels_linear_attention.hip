@@ -142,6 +142,65 @@ __device__ __forceinline__ void la_state_out(const LaRole& q, uint32_t seg, uint
                 if (FULL || (x + 16 * ta + i < X && y + la_column<STEP>(d) < yw)) e[(16 * ta + i) * q.lx + la_column<STEP>(d) * q.ly] = gone ? 0.0f : S[ta][d][i];
 }
 
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+// A segment in which a NaN or an infinity of b or c was seen, again, token by token as the formula says: in the products a weight of 0 would carry it to tokens
+// before it and to other episodes.  A lane has the rows x + 16 ta + j and columns y + la_column(d) of the state; with outputs (red) wavefront `w` of the state's
+// leaves its part of a token's there, and meets those that take it.
+template <typename T, int NA, int ND, int STEP, bool OUT, typename F>
+__device__ __forceinline__ void la_tokens(const LaParams& p, const LaRole& q, uint32_t b, uint32_t h, int64_t n, int64_t i0, int64_t i1, float lg, int x, int y, int y0, int X, int yw,
+                                          float* red, v4f (&S)[NA][ND], F taken) {
+    const float ge = pow2(lg);
+    const T* pa = (const T*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh;
+    const T* pb = (const T*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh;
+    const T* pc = (const T*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + y0;
+    for (int64_t i = i0; i < i1; ++i) {
+        const int64_t t = q.back ? n - 1 - i : i;
+        const bool anew = p.reset && (!q.back || i > 0) && p.reset[b * p.rb + (q.back ? t + 1 : t) * p.rt] != 0;
+        float part[ND] = {};
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int xx = x + 16 * ta + j;
+                const float eb = xx < X ? el_f32(pb[t * q.b.st + xx]) * q.pair : 0.0f, ea = OUT && xx < X ? el_f32(pa[t * q.a.st + xx]) : 0.0f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const int yy = y + la_column<STEP>(d);
+                    float e = anew ? 0.0f : q.back ? S[ta][d][j] : S[ta][d][j] * ge;
+                    e += eb * (yy < yw ? el_f32(pc[t * q.c.st + yy]) : 0.0f);
+                    if (OUT && xx < X) part[d] += ea * e;
+                    S[ta][d][j] = q.back ? e * ge : e;
+                }
+            }
+        if constexpr (OUT) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                part[d] += __shfl_xor(part[d], 16);
+                part[d] += __shfl_xor(part[d], 32);
+                if ((threadIdx.x & 63) < 16) red[y + la_column<STEP>(d)] = part[d];
+            }
+            meet();
+            taken(i);
+            meet();
+        }
+    }
+}
+// the other side of it: column y of token i from the parts of `ws` wavefronts, each LY apart
+template <typename T>
+__device__ __forceinline__ void la_token_out(const LaRole& q, uint32_t b, uint32_t h, int64_t n, int64_t i, int y, int y0, int yw, int ws, const float* red) {
+    if (y >= yw) return;
+    float v = 0.0f;
+    for (int k = 0; k < ws; ++k) v += red[k * LY + y];
+    v *= q.scale;
+    const int64_t o = b * q.ob + (int64_t)h * q.oh + (q.back ? n - 1 - i : i) * q.ot + y0 + y;
+    if (q.out_f32) ((float*)q.out)[o] = v;
+    else ((T*)q.out)[o] = f32_el<T>(v);
+}
+
 // outputs of tokens behind the sequence's end
 template <typename T, int NW> __device__ __forceinline__ void la_behind(const LaParams& p, const LaRole& q, const LaPlace& at, int64_t n, int64_t i0, int y0, int yw) {
     const int lane = threadIdx.x & 63;
@@ -161,17 +220,12 @@ template <typename T, int DX, int NW>
 struct LaHalf {
     static constexpr bool SPLIT = __is_same(T, F16);
     static constexpr int PARTS = SPLIT ? 2 : 1;
-    static constexpr uint32_t INF = SPLIT ? 0x7c00u : 0x7f80u;
     // rows 16 bytes further on in the banks: a quarter wavefront's 16-byte reads of 16 rows meet no bank twice; and c's rows 8 bytes, for reads down its columns
     static constexpr int YW = 16 * NW;                        // columns of a workgroup
     static constexpr int BP = DX + 8, CP = YW + 4;
-    static constexpr int BV = DX / 8 / NW, CV = YW / 8 / NW;  // vectors of a lane
     static constexpr int NA = DX / 16 / NW, ND = NW;          // tiles of 16 rows and 16 columns of the state for a wavefront
     static constexpr int KX = DX / 32;                        // depth of the products over X in matrix instructions
-    static constexpr int WAVES = NW == 8 ? 2 : SPLIT ? (DX == 256 ? 1 : 2) : DX == 64 ? 2 : 1;      // of a SIMD
-    // Two of each tile, where they fit: the next chunk is staged and the next state handed out while this one is read, and a chunk has one barrier
-    static constexpr bool TWO = !SPLIT && DX <= 128;
-    static constexpr int CT = LC * CP, SF = DX * YW, BT = LC * BP;          // elements of a part of c's tile and of the state's fragments
+    static constexpr int CT = LC * CP, SF = DX * YW, BT = LC * BP;    // elements of a tile (c: of a part) and of the state's fragments
 };
 
 __device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
@@ -210,19 +264,202 @@ template <typename T> __device__ __forceinline__ v4f mma_as(u32x4 a, u32x4 b, v4
 
 // HOW: EXACT for heads of DX and slices of YW elements.  OUT: the mixing; else the state behind the
 // segment alone.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its end) and the tables hold for all.
-// WANTED: the state behind the last token is; else b's weighted copy has one part only, rounded as the state's copy is.
-template <typename T, int DX, int NW, bool OUT, LaEdge HOW, bool WANTED>
-__global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAVES : NW == 8 ? 4 : 3)) void la_half_kernel(const LaParams p) {
+// Weights g^(63-s) of tokens s = 16 st + 4 g + i in the state behind a chunk: tail[i] block[st], neither a negative power.
+struct LaTail {
+    float tail[4], block[4];
+    __device__ __forceinline__ LaTail(float lg, int back, float pair, int g) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            tail[i] = decay_pow(lg, 15 - 4 * g - i) * pair;
+            block[i] = everywhere(decay_pow(lg, 48 - 16 * i + back));
+        }
+    }
+};
+
+// What NS wavefronts bring into LDS: the tiles of b and c, a chunk's tokens by DX and YW elements.
+template <typename T, int DX, int YW, int NS, LaEdge HOW>
+struct LaTiles {
+    static constexpr bool SPLIT = __is_same(T, F16);
+    static constexpr int BV = DX / 8 / NS, CV = YW / 8 / NS;                  // vectors of a lane
+    static constexpr int BR = 512 * NS / DX, CR = 512 * NS / YW;              // rows from one vector of a lane to its next
+    static constexpr int BP = DX + 8, CP = YW + 4;
+    const LaParams& p;
+    uint16_t *const sb, *const sc;
+    const int bt, ct;                                         // from one tile to its twin
+    const T *const pb, *const pc;                             // (SHORT) the first chunk's tiles
+    const int64_t tb, tc;
+    const int X, yw, gap;
+    const int brow, bcol, crow, ccol, b_to, c_to;             // a lane's first vectors, and (EDGE) how far ahead they are read and to be moved from
+    const T *lb, *lc;                                         // where they are in the chunk to be fetched
+    const uint8_t* reset = nullptr;                           // of this lane's token there
+    int64_t rt = 0, i, i0;
+    int back;
+    u32x4 vb[BV], vc[CV];
+    uint32_t cut = 0, odd = 0;
+    uint64_t cuts = 0;                                        // tokens of the staged chunk that start from nothing
+
+    __device__ __forceinline__ LaTiles(const LaParams& p, const LaRole& q, uint16_t* sb, uint16_t* sc, int bt, int ct, const T* pb, const T* pc, int64_t tb, int64_t tc, int X, int yw, int gap,
+                                       int tid)
+        : p(p), sb(sb), sc(sc), bt(bt), ct(ct), pb(pb), pc(pc), tb(tb), tc(tc), X(X), yw(yw), gap(gap), brow(tid / (DX / 8)), bcol(tid % (DX / 8) * 8), crow(tid / (YW / 8)),
+          ccol(tid % (YW / 8) * 8), b_to(HOW == EDGE ? min(0, X - 8 - bcol) : 0), c_to(HOW == EDGE ? min(0, yw - 8 - ccol) : 0), lb(pb + brow * tb + bcol), lc(pc + crow * tc + ccol) {}
+    __device__ __forceinline__ void at(uint32_t b, int64_t n, int64_t first, int64_t base0, int backwards) {
+        back = backwards;
+        i = base0 + (threadIdx.x & 63);
+        i0 = first;
+        if (p.reset) reset = p.reset + b * p.rb + (back ? n - i : i) * p.rt;
+        rt = (back ? -p.rt : p.rt) * LC;
+    }
+    // chunks in turn; rows of the first one that are not there count as the first that is
+    template <typename F> __device__ __forceinline__ void fetch(int, F) {
+        constexpr bool FIRST = F::value;
+#pragma unroll
+        for (int k = 0; k < BV; ++k) {
+            const T* f = lb + k * BR * tb;
+            if constexpr (FIRST) f += max(gap - brow - k * BR, 0) * tb;
+            vb[k] = HOW == SHORT ? row_vec(bcol < X ? f : pb + gap * tb, X - bcol) : *(const u32x4_at2*)(f + b_to);
+        }
+#pragma unroll
+        for (int k = 0; k < CV; ++k) {
+            const T* f = lc + k * CR * tc;
+            if constexpr (FIRST) f += max(gap - crow - k * CR, 0) * tc;
+            vc[k] = HOW == SHORT ? row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol) : *(const u32x4_at2*)(f + c_to);
+        }
+        lb += LC * tb;
+        lc += LC * tc;
+        // does the token of this lane start from nothing?  (backwards: does the one behind it in time)
+        cut = 0;
+        if (reset) {
+            if (i >= i0 && !(back && i == 0)) cut = *reset;
+            reset += rt;
+            i += LC;
+        }
+    }
+    template <typename F> __device__ __forceinline__ void stage(int tile, F) {
+        uint16_t *const to_b = sb + tile * bt, *const to_c = sc + tile * ct;
+        if constexpr (F::value) {
+            const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < BV; ++k) if (brow + k * BR < gap) vb[k] = none;
+#pragma unroll
+            for (int k = 0; k < CV; ++k) if (crow + k * CR < gap) vc[k] = none;
+        }
+        if constexpr (HOW == EDGE) {
+#pragma unroll
+            for (int k = 0; k < BV; ++k) vb[k] = move_down(vb[k], -b_to);
+#pragma unroll
+            for (int k = 0; k < CV; ++k) vc[k] = move_down(vc[k], -c_to);
+        }
+        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+        us2 top = {0, 0};
+        auto look = [&](u32x4 v) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
+        };
+#pragma unroll
+        for (int k = 0; k < BV; ++k) {
+            look(vb[k]);
+            *(u32x4*)(to_b + (brow + k * BR) * BP + bcol) = vb[k];
+        }
+#pragma unroll
+        for (int k = 0; k < CV; ++k) {
+            look(vc[k]);
+            uint16_t* o = to_c + (crow + k * CR) * CP + ccol;
+            if constexpr (SPLIT) {
+                float x[8];
+                v8bf part[2];
+                unpack8<T>(vc[k], x);
+                parts8<2>(x, part);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const u32x4 v = __builtin_bit_cast(u32x4, part[j]);
+                    *(u32x2*)(o + j * LC * CP) = u32x2{v[0], v[1]};
+                    *(u32x2*)(o + j * LC * CP + 4) = u32x2{v[2], v[3]};
+                }
+            } else {
+                *(u32x2*)o = u32x2{vc[k][0], vc[k][1]};
+                *(u32x2*)(o + 4) = u32x2{vc[k][2], vc[k][3]};
+            }
+        }
+        odd |= __ballot(max((uint32_t)top[0], (uint32_t)top[1]) >= (SPLIT ? 0x7c00u : 0x7f80u)) != 0;
+        cuts = __ballot(cut != 0);
+    }
+};
+
+typedef __attribute__((address_space(3))) v4s la_lds4;
+// Four rows of four columns each are turned by a read of 16 lanes: each has a column, down four tokens; two reads, 16 rows apart, make the eight of a fragment of 32
+// tokens.
+__device__ __forceinline__ u32x4 down32(const uint16_t* from, int rows16) {
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4*)(from + rows16));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The state behind a chunk: TERMS parts of b's weighted copy, three (without loss: it is a sum of fp32 terms) where the state is wanted.
+template <typename T, typename L, int NA, int ND, int TERMS>
+__device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, const uint16_t* down_b, const uint16_t* down_c, int g, v4f (&S)[NA][ND]) {
+    const int last_cut = here ? 63 - __builtin_clzll(here) : -1;
+    // (kept as they are: the products, worked out ahead of the loop, would take the registers)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("" : "+v"(t.tail[i]));
+    if (here) {
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+    } else {
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[ta][d][i] *= sd;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        float k8[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k8[j] = t.tail[j % 4] * t.block[2 * ks + j / 4];
+        if (here)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) k8[j] = 32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut ? 0.0f : k8[j];
+        v8bf fb[NA][TERMS];
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta) {
+            float x[8];
+            unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= k8[j];
+            if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
+            else rounded8<TERMS>(x, fb[ta]);
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            v8bf fc[L::PARTS];
+#pragma unroll
+            for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down32(down_c + 32 * ks * L::CP + k * L::CT + la_column<4>(d), 16 * L::CP));
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta) {
+                if constexpr (TERMS == 3) S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
+                if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
+                if constexpr (TERMS >= 2) S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
+                if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
+                S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+            }
+        }
+    }
+}
+
+// The state behind a segment alone: what it adds, from nothing.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its
+// end) and the weights hold for all.  Two of each tile: the next chunk is staged while this one is read, and a chunk has one barrier.
+// HOW: EXACT for heads of DX and slices of YW elements.
+template <typename T, int DX, int NW, LaEdge HOW>
+__global__ __launch_bounds__(64 * NW, (DX == 256 ? 2 : NW == 8 ? 4 : 3)) void la_sum_kernel(const LaParams p) {
     typedef LaHalf<T, DX, NW> L;
-    constexpr int NA = L::NA, ND = L::ND, NB = L::TWO ? 2 : 1, TERMS = WANTED ? 3 : L::PARTS;
+    constexpr int NA = L::NA, ND = L::ND, NB = DX == 256 ? 1 : 2;
     constexpr bool FULL = HOW == EXACT;
 
     __shared__ __attribute__((aligned(16))) uint16_t sb[NB * L::BT];
     __shared__ __attribute__((aligned(16))) uint16_t sc[NB * L::PARTS * L::CT];
-    // the state as the fragments that the product with a reads: [part][column tile][depth][lane][8]
-    __shared__ __attribute__((aligned(16))) uint16_t ss[OUT ? NB * L::PARTS * L::SF : 8];
-    __shared__ int odd[NB][NW];                                 // whether a wavefront has seen a NaN or an infinity in b or c
-    __shared__ float red[NW][L::YW];
+    __shared__ int odd[NW];                                   // whether a wavefront has seen a NaN or an infinity in b or c
 
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const LaPlace at = la_place(p);
@@ -238,205 +475,145 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
     const int gap = (int)(i0 - base0);
     const float lg = p.log_decay[h] * LOG2E;
     // tokens in this order: token i lies i strides behind the first
-    const int64_t tb = back ? -q.b.st : q.b.st, tc = back ? -q.c.st : q.c.st, ta_ = back ? -q.a.st : q.a.st, to = back ? -q.ot : q.ot;
-    const int64_t t0 = back ? n - 1 : 0;
+    const int64_t tb = back ? -q.b.st : q.b.st, tc = back ? -q.c.st : q.c.st, t0 = back ? n - 1 : 0;
     const T* pb = (const T*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh + t0 * q.b.st + base0 * tb;
     const T* pc = (const T*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + t0 * q.c.st + base0 * tc + y0;
-    const T* pa = (const T*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh + t0 * q.a.st + base0 * ta_;
-    const int64_t po = b * q.ob + (int64_t)h * q.oh + t0 * q.ot + base0 * to + y0;
-
-    // The state's columns are dealt out so that a lane's results of four column tiles lie side by side: tile d, column r is 64 (d / 4) + 16 (r / 4) + 4 (d % 4) + r % 4
+    // the state's columns, dealt out as the kernel below needs them: tile d, column r is 64 (d / 4) + 16 (r / 4) + 4 (d % 4) + r % 4
     const int yr = 16 * (r >> 2) + (r & 3);
     v4f S[NA][ND];
-    la_state_in<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, S);
-    // Every wavefront has its rows of the state, and a tile of 16 tokens by 64 columns (`half` of eight wavefronts' 128) of the output
-    const int wq = w & 3, half = w >> 2;
-    // Weights g^(t-s) of pairs s = 16 st + 4 g + i, and g^(63-s) of token s in the state behind the chunk.  Where registers are short (LEAN) they are made of two
-    // factors, of which neither is a negative power: below the diagonal of 16 x 16 near[i] far[st], and tail[i] block[st].
-    constexpr bool LEAN = !OUT || DX == 256;
-    const int t = 16 * wq + r;
-    float dec[LEAN ? 1 : 4][4], kw[LEAN ? 1 : 4][4], diag[4], near[4], tail[4], far[4], block[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int s = 4 * g + i;
-        if constexpr (LEAN) {
-            diag[i] = s <= r ? decay_pow(lg, r - s) * (q.pair * q.scale) : 0.0f;
-            near[i] = decay_pow(lg, r - s + 15) * (q.pair * q.scale);
-            tail[i] = decay_pow(lg, 15 - s) * q.pair;
-            far[i] = everywhere(i < wq ? decay_pow(lg, 16 * (wq - i) - 15) : 0.0f);
-            block[i] = everywhere(decay_pow(lg, 48 - 16 * i + back));
-        } else {
+    for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                dec[st][i] = 16 * st + s <= t ? decay_pow(lg, t - 16 * st - s) * (q.pair * q.scale) : 0.0f;
-                kw[st][i] = decay_pow(lg, LC - 1 - 16 * st - s + back) * q.pair;
+        for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+    LaTail tail(lg, back, q.pair, g);
+    float sd = everywhere(decay_pow(lg, LC - gap)), left = 1.0f;              // (the first chunk's); what is left of a state before the segment
+    LaTiles<T, DX, L::YW, NW, HOW> tiles(p, q, sb, sc, L::BT, L::PARTS * L::CT, pb, pc, tb, tc, X, yw, gap, tid);
+    tiles.at(b, n, i0, base0, back);
+    const int down_b = (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w, down_c = (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
+    if (chunks) {
+        tiles.fetch(0, std::true_type{});
+        tiles.stage(0, std::true_type{});
+        if (NB == 2 && chunks > 1) tiles.fetch(1, std::false_type{});
+    }
+    for (int c = 0; c < chunks; ++c) {
+        __syncthreads();
+        const int now = NB == 2 ? c & 1 : 0;
+        const uint64_t here = tiles.cuts;
+        if constexpr (NB == 2) {
+            if (c + 1 < chunks) {
+                tiles.stage((c + 1) & 1, std::false_type{});
+                if (c + 2 < chunks) tiles.fetch(c + 2, std::false_type{});
             }
+        } else {
+            if (c + 1 < chunks) tiles.fetch(c + 1, std::false_type{});
+        }
+        la_state_on<T, L, NA, ND, 3>(here, sd, tail, sb + now * L::BT + down_b, sc + now * L::PARTS * L::CT + down_c, g, S);
+        left = here ? 0.0f : left * sd;
+        sd = everywhere(decay_pow(lg, LC));
+        if constexpr (NB == 1) {
+            __syncthreads();
+            if (c + 1 < chunks) tiles.stage(0, std::false_type{});
         }
     }
-    auto dec_of = [&](int st, int i) {
-        if constexpr (LEAN) return st == wq ? diag[i] : near[i] * far[st];
-        else return dec[st][i];
-    };
-    auto kw_of = [&](int st, int i) {
-        if constexpr (LEAN) return tail[i] * block[st];
-        else return kw[st][i];
-    };
-    float qw = decay_pow(lg, max(t - gap, 0) + 1 - back) * q.scale, sd = everywhere(decay_pow(lg, LC - gap));      // (the first chunk's)
-    float left = 1.0f;                                        // of the segment's first state
+    if (lane == 0) odd[w] = tiles.odd;
+    __syncthreads();
+    int seen = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) seen |= odd[i];
+    if (seen) {
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+        la_tokens<T, NA, ND, 4, false>(p, q, b, h, n, i0, i1, lg, 16 * NA * w + 4 * g, yr, y0, X, yw, nullptr, S, [](int64_t) {});
+    }
+    // backwards the state that enters the unroll has no gradient if its first token resets
+    const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
+    la_state_out<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, gone, S);
+    if (at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = gone ? 0.0f : left;
+}
 
-    const int brow = tid / (DX / 8), bcol = tid % (DX / 8) * 8, crow = tid / (L::YW / 8), ccol = tid % (L::YW / 8) * 8;
-    constexpr int BR = 512 * NW / DX, CR = 512 * NW / L::YW;             // rows from one vector of a lane to its next
-    u32x4 vb[L::BV], vc[L::CV], va[OUT ? L::KX : 1];
-    const int b_to = HOW == EDGE ? min(0, X - 8 - bcol) : 0, c_to = HOW == EDGE ? min(0, yw - 8 - ccol) : 0;      // (where a lane's vector is read, and to be moved from)
-    uint32_t cut = 0;
-    uint64_t cuts = 0;                                        // tokens of a chunk that start from nothing
-    // Pointers of a lane's rows, which go on by a chunk with every fetch.  In the first chunk rows that are not there count as the first that is.
-    const T *lb = pb + brow * tb + bcol, *lc = pc + crow * tc + ccol, *la = pa + t * ta_ + 8 * g;
-    auto fetch = [&](int c, auto first) {
-        constexpr bool FIRST = decltype(first)::value;
+// The mixing itself.  Four wavefronts work out the outputs of a chunk, 16 tokens by 64 columns each, from the tiles and the state before it, while the others bring the
+// state behind it and the next tiles: on every SIMD one kind's matrix instructions run beside the other's conversions, and either needs half of the registers
+// that one wavefront doing both does, so that two workgroups are on a compute unit.
+template <typename T, int DX>
+struct LaPair {
+    typedef LaHalf<T, DX, 4> L;
+    static constexpr int NS = DX == 256 ? 8 : 4;              // wavefronts of the state, of NA tiles of 16 rows each
+    static constexpr int NA = DX / 16 / NS;
+    static constexpr int THREADS = 64 * (4 + NS);
+    static constexpr int WAVES = L::SPLIT ? 2 : DX == 256 ? 3 : 4;    // of a SIMD
+};
+// WANTED: the state behind the last token is; else b's weighted copy has one part only, rounded as the state's copy is.
+template <typename T, int DX, LaEdge HOW, bool WANTED>
+__global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) void la_pair_kernel(const LaParams p) {
+    typedef LaPair<T, DX> Q;
+    typedef typename Q::L L;
+    constexpr int NS = Q::NS, NA = Q::NA, TERMS = WANTED ? 3 : L::PARTS;
+    constexpr bool FULL = HOW == EXACT;
+
+    __shared__ __attribute__((aligned(16))) uint16_t sb[L::BT];
+    __shared__ __attribute__((aligned(16))) uint16_t sc[L::PARTS * L::CT];
+    // the state as the fragments that the product with a reads: [part][column tile][depth][lane][8]
+    __shared__ __attribute__((aligned(16))) uint16_t ss[L::PARTS * L::SF];
+    __shared__ int odd[NS];                                   // whether a wavefront has seen a NaN or an infinity in b or c (fp16: or in the state)
+    __shared__ uint64_t cut_mask;                             // tokens of the chunk that start from nothing
+    __shared__ float red[NS][LY];
+
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const LaPlace at = la_place(p);
+    if (!at.mine) return;
+    const LaRole& q = p.role[at.which];
+    const int X = FULL ? DX : q.X, Y = q.Y, y0 = at.slice * LY, yw = FULL ? LY : min(Y - y0, LY), back = q.back;
+    const uint32_t seg = at.seg, bh = at.bh, b = bh / p.H, h = bh % p.H;
+    int64_t n = p.T;
+    if (p.lengths) n = min(max((int64_t)p.lengths[b], (int64_t)0), n);
+    const int64_t i0 = seg * p.seg_len, i1 = min(n, i0 + p.seg_len);
+    const int chunks = i1 > i0 ? (int)((i1 - i0 + LC - 1) / LC) : 0;
+    const int64_t base0 = i1 - (int64_t)chunks * LC;          // of the first chunk; its tokens from `gap` on are there
+    const int gap = (int)(i0 - base0);
+    const float lg = p.log_decay[h] * LOG2E;
+    const int64_t t0 = back ? n - 1 : 0;
+    const int yr = 16 * (r >> 2) + (r & 3);                   // (columns dealt out as in the kernel above)
+    const uint16_t* down_c = sc + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
+    // at the end: has any wavefront seen a NaN or an infinity?
+    auto strange = [&]() {
+        int seen = 0;
 #pragma unroll
-        for (int k = 0; k < L::BV; ++k) {
-            const T* f = lb + k * BR * tb;
-            if constexpr (FIRST) f += max(gap - brow - k * BR, 0) * tb;
-            vb[k] = HOW == SHORT ? row_vec(bcol < X ? f : pb + gap * tb, X - bcol) : *(const u32x4_at2*)(f + b_to);
-        }
-#pragma unroll
-        for (int k = 0; k < L::CV; ++k) {
-            const T* f = lc + k * CR * tc;
-            if constexpr (FIRST) f += max(gap - crow - k * CR, 0) * tc;
-            vc[k] = HOW == SHORT ? row_vec(ccol < yw ? f : pc + gap * tc, yw - ccol) : *(const u32x4_at2*)(f + c_to);
-        }
-        lb += LC * tb;
-        lc += LC * tc;
-        // does the token of this lane start from nothing?  (backwards: does the one behind it in time)
-        cut = 0;
-        if (p.reset) {
-            const int64_t i = base0 + (int64_t)c * LC + lane, tok = back ? n - i : i;
-            if (i >= i0 && !(back && i == 0)) cut = p.reset[b * p.rb + tok * p.rt];
-        }
+        for (int i = 0; i < NS; ++i) seen |= odd[i];
+        return __builtin_amdgcn_readfirstlane(seen) != 0;
     };
-    // this wavefront's 16 tokens of a, straight from memory
-    auto fetch_a = [&](auto first) {
-        if constexpr (OUT) {
-            const T* f = la;
-            if constexpr (decltype(first)::value) f += max(gap - t, 0) * ta_;
+
+    if (w < 4) {
+        // ------------------------------------------------ outputs
+        const int64_t ta_ = back ? -q.a.st : q.a.st, to = back ? -q.ot : q.ot;
+        const int t = 16 * w + r;
+        const T* pa = (const T*)q.a.p + b * q.a.sb + (h / q.a.div) * q.a.sh + t0 * q.a.st + base0 * ta_;
+        const T* la = pa + t * ta_ + 8 * g;
+        const int64_t po = b * q.ob + (int64_t)h * q.oh + t0 * q.ot + base0 * to + y0;
+        float dec[4][4];                                      // weights g^(t-s) of pairs s = 16 st + 4 g + i
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * st + 4 * g + i;
+                dec[st][i] = s <= t ? decay_pow(lg, t - s) * (q.pair * q.scale) : 0.0f;
+            }
+        float qw = decay_pow(lg, max(t - gap, 0) + 1 - back) * q.scale;       // (the first chunk's)
+        u32x4 va[L::KX];
+        auto fetch_a = [&](int more) {
+            const T* f = la + more * ta_;
 #pragma unroll
             for (int k = 0; k < L::KX; ++k) {
                 if constexpr (HOW == SHORT) va[k] = row_vec(8 * g + 32 * k < X ? f + 32 * k : f - 8 * g, X - 32 * k - 8 * g);
                 else va[k] = *(const u32x4_at2*)(f + (HOW == EDGE ? min(32 * k, X - 8 - 8 * g) : 32 * k));
             }
             la += LC * ta_;
-        }
-    };
-    const std::true_type is_first;
-    const std::false_type later;
-    auto stage = [&](int c) {
-        const int at = L::TWO ? c & 1 : 0;
-        uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT;
-        if (c == 0 && gap) {
-            const u32x4 none = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < L::BV; ++k) if (brow + k * BR < gap) vb[k] = none;
-#pragma unroll
-            for (int k = 0; k < L::CV; ++k) if (crow + k * CR < gap) vc[k] = none;
-        }
-        if constexpr (HOW == EDGE) {
-#pragma unroll
-            for (int k = 0; k < L::BV; ++k) vb[k] = move_down(vb[k], -b_to);
-#pragma unroll
-            for (int k = 0; k < L::CV; ++k) vc[k] = move_down(vc[k], -c_to);
-        }
-        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-        us2 top = {0, 0};
-        auto look = [&](u32x4 v) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
         };
-#pragma unroll
-        for (int k = 0; k < L::BV; ++k) {
-            look(vb[k]);
-            *(u32x4*)(tb_ + (brow + k * BR) * L::BP + bcol) = vb[k];
-        }
-#pragma unroll
-        for (int k = 0; k < L::CV; ++k) {
-            look(vc[k]);
-            uint16_t* o = tc_ + (crow + k * CR) * L::CP + ccol;
-            if constexpr (L::SPLIT) {
-                float x[8];
-                v8bf part[2];
-                unpack8<T>(vc[k], x);
-                parts8<2>(x, part);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const u32x4 v = __builtin_bit_cast(u32x4, part[i]);
-                    *(u32x2*)(o + i * L::CT) = u32x2{v[0], v[1]};
-                    *(u32x2*)(o + i * L::CT + 4) = u32x2{v[2], v[3]};
-                }
-            } else {
-                *(u32x2*)o = u32x2{vc[k][0], vc[k][1]};
-                *(u32x2*)(o + 4) = u32x2{vc[k][2], vc[k][3]};
-            }
-        }
-        const bool any = __ballot(max((uint32_t)top[0], (uint32_t)top[1]) >= L::INF) != 0;
-        if (lane == 0) odd[at][w] = any;
-        cuts = __ballot(cut != 0);
-    };
-    auto publish = [&](int c, int first) {
-        uint16_t* const ts = ss + (L::TWO ? c & 1 : 0) * L::PARTS * L::SF;
-        if constexpr (OUT && L::SPLIT) {
-            // (an infinity has no second part; a state that the chunk's first token ends may be anything)
-            uint32_t top = 0;
-            if (cuts >> first & 1)
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(S[ta][d][i]) & 0x7fffffffu);
-            if (__ballot(top >= 0x7f800000u) && lane == 0) odd[0][w] = 1;
-        }
-        if constexpr (OUT)
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta) {
-                const int tile = NA * w + ta, quad = 4 * (tile & 1) + g;    // rows 4 quad .. of the 32 of a fragment belong to lane group quad / 2
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    uint16_t* o = ts + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
-                    const v4f s = S[ta][d];
-                    if constexpr (L::SPLIT) {
-                        *(u32x2*)o = u32x2{high_halves(s[0], s[1]), high_halves(s[2], s[3])};
-                        *(u32x2*)(o + L::SF) = u32x2{f32_pair<BF16>(s[0] - cut16(s[0]), s[1] - cut16(s[1])), f32_pair<BF16>(s[2] - cut16(s[2]), s[3] - cut16(s[3]))};
-                    } else {
-                        *(u32x2*)o = u32x2{f32_pair<BF16>(s[0], s[1]), f32_pair<BF16>(s[2], s[3])};
-                    }
-                }
-            }
-    };
-    // Four rows of four columns each are turned by a read of 16 lanes: each has a column, down four tokens; two reads make the eight of a fragment of 32 tokens
-    typedef __attribute__((address_space(3))) v4s lds4;
-    auto down = [&](const uint16_t* from, int rows16) {
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(from + rows16));
-        return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    // One chunk, without and with borders of episodes in it (LEAN: one form for both).  The order lets the loads of what comes next run behind all products.
-    auto chunk = [&](int c, bool more, uint64_t here, auto bordered) {
-        constexpr bool CUTS = decltype(bordered)::value;
-        const int at = L::TWO ? c & 1 : 0;
-        const uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT, *const ts = ss + at * L::PARTS * L::SF;
-        const uint16_t* down_b = tb_ + (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w;
-        const uint16_t* down_c = tc_ + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
-        if constexpr (LEAN) {
-            // (kept as they are: the products, worked out ahead of the loop, would take the registers)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
-        }
-        const int last_cut = here ? 63 - __builtin_clzll(here) : -1;
-        if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
-        if constexpr (OUT) {
+        if (chunks) fetch_a(max(gap - t, 0));                 // (rows of the first chunk that are not there: the first that is)
+        for (int c = 0; c < chunks; ++c) {
+            meet();
+            const uint64_t here = cut_mask;
             v4f O[4], P[4];
 #pragma unroll
             for (int d = 0; d < 4; ++d) O[d] = P[d] = v4f{0, 0, 0, 0};
@@ -453,57 +630,61 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
                 }
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const uint16_t* f = ts + (((4 * half + d) * L::KX + k) * 64 + lane) * 8;
+                    const uint16_t* f = ss + ((d * L::KX + k) * 64 + lane) * 8;
                     if constexpr (L::SPLIT) {
                         O[d] = mma(*(const v8bf*)(f + L::SF), fa[0], O[d]);
                         O[d] = mma(*(const v8bf*)f, fa[1], O[d]);
                     }
                     O[d] = mma(*(const v8bf*)f, fa[0], O[d]);
                 }
-#pragma unroll
-                for (int st = 0; st < 4; ++st) P[st] = mma_as<T>(*(const u32x4*)(tb_ + (16 * st + r) * L::BP + 32 * k + 8 * g), va[k], P[st]);
             }
-            if (more) fetch_a(later);
+            __builtin_amdgcn_sched_barrier(0);            // (reads ahead of their products would take the registers)
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+                if (st <= w)
+#pragma unroll
+                    for (int k = 0; k < L::KX; ++k) P[st] = mma_as<T>(*(const u32x4*)(sb + (16 * st + r) * L::BP + 32 * k + 8 * g), va[k], P[st]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (c + 1 < chunks) fetch_a(0);
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) O[d][i] *= qw;
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) P[st][i] *= dec_of(st, i);
-            if constexpr (CUTS) {
+                for (int i = 0; i < 4; ++i) {
+                    O[d][i] *= qw;
+                    P[d][i] *= dec[d][i];
+                }
+            if (here) {
                 const uint64_t before = here & ((2ull << t) - 1);
-                const int first = before ? 63 - __builtin_clzll(before) : -1;            // the token that t's episode begins with, if it begins in this chunk
+                const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
                 // (selected, not multiplied by 0: the state of the episode before may hold anything)
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) O[d][i] = first >= 0 ? 0.0f : O[d][i];
-#pragma unroll
-                for (int st = 0; st < 4; ++st)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) P[st][i] = 16 * st + 4 * g + i < first ? 0.0f : P[st][i];
-            }
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                v8bf pt[L::PARTS];                            // weights of pairs as the product with c reads them
-                const float x[8] = {P[2 * ks][0], P[2 * ks][1], P[2 * ks][2], P[2 * ks][3], P[2 * ks + 1][0], P[2 * ks + 1][1], P[2 * ks + 1][2], P[2 * ks + 1][3]};
-                rounded8<L::PARTS>(x, pt);
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    v8bf fc[L::PARTS];
-#pragma unroll
-                    for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * half + 4 * d, 16 * L::CP));
-                    if constexpr (L::SPLIT) {
-                        O[d] = mma(fc[1], pt[0], O[d]);
-                        O[d] = mma(fc[0], pt[1], O[d]);
+                    for (int i = 0; i < 4; ++i) {
+                        O[d][i] = first >= 0 ? 0.0f : O[d][i];
+                        P[d][i] = 16 * d + 4 * g + i < first ? 0.0f : P[d][i];
                     }
-                    O[d] = mma(fc[0], pt[0], O[d]);
-                }
             }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+                if (2 * ks <= w) {
+                    v8bf pt[L::PARTS];                    // weights of pairs as the product with c reads them
+                    const float x[8] = {P[2 * ks][0], P[2 * ks][1], P[2 * ks][2], P[2 * ks][3], P[2 * ks + 1][0], P[2 * ks + 1][1], P[2 * ks + 1][2], P[2 * ks + 1][3]};
+                    rounded8<L::PARTS>(x, pt);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        v8bf fc[L::PARTS];
+#pragma unroll
+                        for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down32(down_c + 32 * ks * L::CP + k * L::CT + 4 * d, 16 * L::CP));
+                        if constexpr (L::SPLIT) {
+                            O[d] = mma(fc[1], pt[0], O[d]);
+                            O[d] = mma(fc[0], pt[1], O[d]);
+                        }
+                        O[d] = mma(fc[0], pt[0], O[d]);
+                    }
+                }
             if (c || t >= gap) {
-                const int64_t o = po + ((int64_t)c * LC + t) * to + 64 * half + 16 * g;
+                const int64_t o = po + ((int64_t)c * LC + t) * to + 16 * g;
                 float v[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] = O[j / 4][j % 4];
@@ -511,173 +692,113 @@ __global__ __launch_bounds__(64 * NW, (OUT || DX == 256 ? LaHalf<T, DX, NW>::WAV
                     float* f = (float*)q.out + o;
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
-                        if (FULL || 64 * half + 16 * g + 4 * d + 4 <= yw) *(u32x4_at4*)(f + 4 * d) = __builtin_bit_cast(u32x4, v4f{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]});
+                        if (FULL || 16 * g + 4 * d + 4 <= yw) *(u32x4_at4*)(f + 4 * d) = __builtin_bit_cast(u32x4, v4f{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]});
                         else
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) if (64 * half + 16 * g + 4 * d + i < yw) f[4 * d + i] = v[4 * d + i];
+                            for (int i = 0; i < 4; ++i) if (16 * g + 4 * d + i < yw) f[4 * d + i] = v[4 * d + i];
                     }
                 } else {
                     T* f = (T*)q.out + o;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float* x = v + 8 * e;
-                        if (FULL || 64 * half + 16 * g + 8 * e + 8 <= yw)
+                        if (FULL || 16 * g + 8 * e + 8 <= yw)
                             *(u32x4_at2*)(f + 8 * e) = u32x4{f32_pair<T>(x[0], x[1]), f32_pair<T>(x[2], x[3]), f32_pair<T>(x[4], x[5]), f32_pair<T>(x[6], x[7])};
                         else
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) if (64 * half + 16 * g + 8 * e + i < yw) f[8 * e + i] = f32_el<T>(x[i]);
+                            for (int i = 0; i < 8; ++i) if (16 * g + 8 * e + i < yw) f[8 * e + i] = f32_el<T>(x[i]);
                     }
                 }
             }
+            qw = decay_pow(lg, t + 1 - back) * q.scale;
+            meet();
         }
-        if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
-        // what enters the next chunk
-        if (CUTS && (!LEAN || here)) {
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
-        } else {
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) S[ta][d][i] *= sd;
-        }
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
-            v8bf fb[NA][TERMS];
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta) {
-                // b weighted in fp32 and, where the state is wanted, taken apart without loss: it is a sum of fp32 terms
-                float x[8];
-                unpack8<T>(down(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] *= kw_of(2 * ks + j / 4, j % 4);
-                    if constexpr (CUTS) x[j] = 32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut ? 0.0f : x[j];
-                }
-                if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
-                else rounded8<TERMS>(x, fb[ta]);
-                if constexpr (LEAN) __builtin_amdgcn_sched_barrier(0);
+        meet();
+        if (strange())
+            for (int64_t i = i0; i < i1; ++i) {
+                meet();
+                la_token_out<T>(q, b, h, n, i, threadIdx.x, y0, yw, NS, &red[0][0]);
+                meet();
             }
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                v8bf fc[L::PARTS];
-#pragma unroll
-                for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down(down_c + 32 * ks * L::CP + k * L::CT + 64 * (d / 4) + 4 * (d % 4), 16 * L::CP));
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta) {
-                    if constexpr (TERMS == 3) S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
-                    if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
-                    if constexpr (TERMS >= 2) S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
-                    if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
-                    S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
-                }
-            }
-        }
-        left = CUTS && (!LEAN || here) ? 0.0f : left * sd;
-    };
-
-    if (chunks) {
-        fetch(0, is_first);
-        fetch_a(is_first);
-        stage(0);
-        publish(0, gap);
-        if (L::TWO && chunks > 1) fetch(1, later);
+        la_behind<T, 4>(p, q, at, n, i0, y0, yw);
+        return;
     }
-    for (int c = 0; c < chunks; ++c) {
-        __syncthreads();
-        const bool more = c + 1 < chunks;
-        int seen = 0;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) seen |= odd[L::TWO ? c & 1 : 0][i];
-        const uint64_t here = cuts;                           // of this chunk: staging the next one replaces them
-        if (more) {
-            if constexpr (L::TWO) {
-                stage(c + 1);
-                if (c + 2 < chunks) fetch(c + 2, later);
-            } else {
-                fetch(c + 1, later);
-            }
-        }
-        if (!seen) {
-            if (LEAN || here) chunk(c, more, here, std::true_type{});
-            else chunk(c, more, here, std::false_type{});
-        } else {
-            // A NaN or an infinity in the chunk (fp16: or in the state): in the products above a weight of 0 would carry it to tokens before it and to other episodes.  Token by token,
-            // as the formula says.
-            const float ge = pow2(lg);
-            const int at = L::TWO ? c & 1 : 0;
-            const uint16_t *const tb_ = sb + at * L::BT, *const tc_ = sc + at * L::PARTS * L::CT;
-            int r = lane & 15, g = lane >> 4, tid = threadIdx.x;
-            asm("" : "+v"(r), "+v"(g), "+v"(tid));            // (its addresses are made here, not kept through the chunks that do without them)
-            const int yr = 16 * (r >> 2) + (r & 3);
-            for (int s = c ? 0 : gap; s < LC; ++s) {
-                const bool anew = here >> s & 1;
-                const int64_t row = (int64_t)c * LC + s;
-                float part[ND] = {};
+
+    // ---------------------------------------------------- the state and the tiles
+    const int ws = w - 4, tid = threadIdx.x - 256;
+    const int64_t tb = back ? -q.b.st : q.b.st, tc = back ? -q.c.st : q.c.st;
+    const T* pb = (const T*)q.b.p + b * q.b.sb + (h / q.b.div) * q.b.sh + t0 * q.b.st + base0 * tb;
+    const T* pc = (const T*)q.c.p + b * q.c.sb + (h / q.c.div) * q.c.sh + t0 * q.c.st + base0 * tc + y0;
+    v4f S[NA][4];
+    la_state_in<NA, 4, 4, FULL>(q, seg, bh, 16 * NA * ws + 4 * g, y0, yr, X, yw, S);
+    LaTail tail(lg, back, q.pair, g);
+    float sd = everywhere(decay_pow(lg, LC - gap));           // (the first chunk's)
+    LaTiles<T, DX, LY, NS, HOW> tiles(p, q, sb, sc, 0, 0, pb, pc, tb, tc, X, yw, gap, tid);
+    tiles.at(b, n, i0, base0, back);
+    // the next tiles, and the state handed out
+    auto hand_out = [&](auto first) {
+        tiles.stage(0, first);
+        if constexpr (L::SPLIT) {
+            // (an infinity has no second part; a state that the chunk's first token ends may be anything)
+            if (tiles.cuts >> (decltype(first)::value ? gap : 0) & 1)
 #pragma unroll
                 for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int x = 16 * (NA * w + ta) + 4 * g + j;
-                        const float eb = el_f32(T{tb_[s * L::BP + x]}) * q.pair;
-                        float ea = 0.0f;
-                        if constexpr (OUT) if (x < X) ea = el_f32(pa[row * ta_ + x]);
+                    for (int d = 0; d < 4; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+            uint32_t most = 0;
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) {
-                            const uint16_t* f = tc_ + s * L::CP + yr + 64 * (d / 4) + 4 * (d % 4);
-                            float ec = L::SPLIT ? el_f32(BF16{f[0]}) : el_f32(T{f[0]});
-                            if constexpr (L::SPLIT) { const float lo = el_f32(BF16{f[L::CT]}); if (lo == lo) ec += lo; }    // (of an infinity the second part is a NaN)
-                            float e = anew ? 0.0f : back ? S[ta][d][j] : S[ta][d][j] * ge;
-                            e += eb * ec;
-                            if (x < X) part[d] += ea * e;
-                            S[ta][d][j] = back ? e * ge : e;
-                        }
-                    }
-                if constexpr (OUT) {
+            for (int ta = 0; ta < NA; ++ta)
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        part[d] += __shfl_xor(part[d], 16);
-                        part[d] += __shfl_xor(part[d], 32);
-                        if (g == 0) red[w][yr + 64 * (d / 4) + 4 * (d % 4)] = part[d];
-                    }
-                    __syncthreads();
-                    if (tid < yw) {
-                        float v = 0.0f;
+                for (int d = 0; d < 4; ++d)
 #pragma unroll
-                        for (int i = 0; i < NW; ++i) v += red[i][tid];
-                        v *= q.scale;
-                        const int64_t o = po + row * to + tid;
-                        if (q.out_f32) ((float*)q.out)[o] = v;
-                        else ((T*)q.out)[o] = f32_el<T>(v);
-                    }
-                    __syncthreads();
+                    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(S[ta][d][i]) & 0x7fffffffu);
+            tiles.odd |= __ballot(most >= 0x7f800000u) != 0;
+        }
+        if (ws == 0 && lane == 0) cut_mask = tiles.cuts;
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta) {
+            const int tile = NA * ws + ta, quad = 4 * (tile & 1) + g;       // rows 4 quad .. of the 32 of a fragment belong to lane group quad / 2
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                uint16_t* o = ss + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
+                const v4f s = S[ta][d];
+                if constexpr (L::SPLIT) {
+                    *(u32x2*)o = u32x2{high_halves(s[0], s[1]), high_halves(s[2], s[3])};
+                    *(u32x2*)(o + L::SF) = u32x2{f32_pair<BF16>(s[0] - cut16(s[0]), s[1] - cut16(s[1])), f32_pair<BF16>(s[2] - cut16(s[2]), s[3] - cut16(s[3]))};
+                } else {
+                    *(u32x2*)o = u32x2{f32_pair<BF16>(s[0], s[1]), f32_pair<BF16>(s[2], s[3])};
                 }
             }
-            if (more) fetch_a(later);
-            left = here ? 0.0f : left * sd;
         }
-        qw = decay_pow(lg, t + 1 - back) * q.scale;
-        sd = everywhere(decay_pow(lg, LC));
-        if constexpr (!L::TWO) {
-            __syncthreads();
-            if (more) stage(c + 1);
-        }
-        if (more) publish(c + 1, 0);
-    }
+    };
+    const uint16_t* down_b = sb + (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * ws;
 
+    if (chunks) {
+        tiles.fetch(0, std::true_type{});
+        hand_out(std::true_type{});
+        if (chunks > 1) tiles.fetch(1, std::false_type{});
+    }
+    for (int c = 0; c < chunks; ++c) {
+        meet();
+        la_state_on<T, L, NA, 4, TERMS>(tiles.cuts, sd, tail, down_b, down_c, g, S);
+        sd = everywhere(decay_pow(lg, LC));
+        meet();
+        if (c + 1 < chunks) {
+            hand_out(std::false_type{});
+            if (c + 2 < chunks) tiles.fetch(c + 2, std::false_type{});
+        }
+    }
+    if (lane == 0) odd[ws] = tiles.odd;
+    meet();
+    if (strange()) {
+        la_state_in<NA, 4, 4, FULL>(q, seg, bh, 16 * NA * ws + 4 * g, y0, yr, X, yw, S);
+        la_tokens<T, NA, 4, 4, true>(p, q, b, h, n, i0, i1, lg, 16 * NA * ws + 4 * g, yr, y0, X, yw, red[ws], S, [](int64_t) {});
+    }
     if (q.last) {
         // backwards the state that enters the unroll has no gradient if its first token resets
         const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
-        if (gone) left = 0.0f;
-        la_state_out<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, gone, S);
-        if (q.keep && at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = left;
+        la_state_out<NA, 4, 4, FULL>(q, seg, bh, 16 * NA * ws + 4 * g, y0, yr, X, yw, gone, S);
     }
-    if constexpr (OUT) la_behind<T, NW>(p, q, at, n, i0, y0, yw);
 }
 
 // ---------------------------------------------------------------- tokens of fp32
@@ -744,6 +865,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     constexpr int BR = 1024 / DX, CR = 1024 / LY;             // rows from one vector of a lane to its next
     u32x4 vb[L::BV], vc[L::CV];
     uint32_t cut = 0;
+    int seen = 0;                                             // a NaN or an infinity in b or c
     auto fetch = [&](int c) {
         const int skip = c ? 0 : gap;
 #pragma unroll
@@ -780,7 +902,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
             *(u32x4*)(sc + (crow + k * CR) * L::CP + ccol) = vc[k];
         }
         const bool any = __ballot(top >= 0x7f800000u) != 0;
-        if (lane == 0) odd[w] = any;
+        seen |= any;
     };
     auto publish = [&]() {
         if constexpr (OUT)
@@ -799,149 +921,110 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("" : "+v"(near[i]), "+v"(tail[i]));
         if (more) fetch(c + 1);
-        const bool plain = !(odd[0] | odd[1] | odd[2] | odd[3]);
         const int last_cut = cuts ? 63 - __builtin_clzll(cuts) : -1;
 
-        if (plain) {
-            v4f O[4];
-            float wt[4][4];
-            if constexpr (OUT) {
-                const float* ra = pa + ((int64_t)c * LC + max(t, c ? 0 : gap)) * ta_ + 4 * g;
-                v4f P[4];
+        v4f O[4];
+        float wt[4][4];
+        if constexpr (OUT) {
+            const float* ra = pa + ((int64_t)c * LC + max(t, c ? 0 : gap)) * ta_ + 4 * g;
+            v4f P[4];
 #pragma unroll
-                for (int st = 0; st < 4; ++st) O[st] = P[st] = v4f{0, 0, 0, 0};
+            for (int st = 0; st < 4; ++st) O[st] = P[st] = v4f{0, 0, 0, 0};
 #pragma unroll 4
-                for (int k = 0; k < L::KX; ++k) {
-                    const v4f fa = __builtin_bit_cast(v4f, FULL ? *(const u32x4_at4*)(ra + 16 * k) : row_vec(4 * g + 16 * k < X ? ra + 16 * k : ra - 4 * g, X - 16 * k - 4 * g));
+            for (int k = 0; k < L::KX; ++k) {
+                const v4f fa = __builtin_bit_cast(v4f, FULL ? *(const u32x4_at4*)(ra + 16 * k) : row_vec(4 * g + 16 * k < X ? ra + 16 * k : ra - 4 * g, X - 16 * k - 4 * g));
 #pragma unroll
-                    for (int st = 0; st < 4; ++st)
-                        if (st <= w) {
-                            const v4f fb = *(const v4f*)(sb + (16 * st + r) * L::BP + 16 * k + 4 * g);
+                for (int st = 0; st < 4; ++st)
+                    if (st <= w) {
+                        const v4f fb = *(const v4f*)(sb + (16 * st + r) * L::BP + 16 * k + 4 * g);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) P[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j], fa[j], P[st], 0, 0, 0);
-                        }
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const v4f fs = *(const v4f*)(ss + ((d * L::KX + k) * 64 + lane) * 4);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fs[j], fa[j], O[d], 0, 0, 0);
+                        for (int j = 0; j < 4; ++j) P[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j], fa[j], P[st], 0, 0, 0);
                     }
-                }
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+                for (int d = 0; d < 4; ++d) {
+                    const v4f fs = *(const v4f*)(ss + ((d * L::KX + k) * 64 + lane) * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) O[d][i] *= qw;
-#pragma unroll
-                for (int st = 0; st < 4; ++st) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) wt[st][i] = 0.0f;
-                    if (st == w) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * diag[i];
-                    } else if (st < w) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * (near[i] * far[st < 3 ? st : 0]);
-                    }
-                }
-                if (cuts) {
-                    const uint64_t before = cuts & ((2ull << t) - 1);
-                    const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
-                    // (selected, not multiplied by 0: the state of the episode before may hold anything)
-                    if (first >= 0)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
-#pragma unroll
-                    for (int st = 0; st < 4; ++st)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) if (16 * st + 4 * g + i < first) wt[st][i] = 0.0f;
+                    for (int j = 0; j < 4; ++j) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fs[j], fa[j], O[d], 0, 0, 0);
                 }
             }
-            // what enters the next chunk
 #pragma unroll
-            for (int ta = 0; ta < NA; ++ta)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) S[ta][d][i] = cuts ? 0.0f : S[ta][d][i] * sd;
+                for (int i = 0; i < 4; ++i) O[d][i] *= qw;
 #pragma unroll
             for (int st = 0; st < 4; ++st) {
-                v4f fc[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wt[st][i] = 0.0f;
+                if (st == w) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * diag[i];
+                } else if (st < w) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wt[st][i] = P[st][i] * (near[i] * far[st < 3 ? st : 0]);
+                }
+            }
+            if (cuts) {
+                const uint64_t before = cuts & ((2ull << t) - 1);
+                const int first = before ? 63 - __builtin_clzll(before) : -1;        // the token that t's episode begins with, if it begins in this chunk
+                // (selected, not multiplied by 0: the state of the episode before may hold anything)
+                if (first >= 0)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) O[d] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int st = 0; st < 4; ++st)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (16 * st + 4 * g + i < first) wt[st][i] = 0.0f;
+            }
+        }
+        // what enters the next chunk
+#pragma unroll
+        for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[ta][d][i] = cuts ? 0.0f : S[ta][d][i] * sd;
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+            v4f fc[4];
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fc[d][i] = sc[(16 * st + 4 * g + i) * L::CP + 16 * d + r];
+            if constexpr (OUT) if (st <= w) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) fc[d][i] = sc[(16 * st + 4 * g + i) * L::CP + 16 * d + r];
-                if constexpr (OUT) if (st <= w) {
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[d][i], wt[st][i], O[d], 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int s = 16 * st + 4 * g + i;
-                    const float kw = s < last_cut ? 0.0f : tail[i] * block[st];
-#pragma unroll
-                    for (int ta = 0; ta < NA; ++ta) {
-                        const float x = sb[s * L::BP + 16 * (NA * w + ta) + r] * kw;
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, fc[d][i], S[ta][d], 0, 0, 0);
-                    }
-                }
+                    for (int i = 0; i < 4; ++i) O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(fc[d][i], wt[st][i], O[d], 0, 0, 0);
             }
-            if constexpr (OUT) {
-                if (c || t >= gap) {
-                    float* f = po + ((int64_t)c * LC + t) * to;
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const int y = 16 * d + 4 * g;
-                        v4f v = O[d];
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * st + 4 * g + i;
+                const float kw = s < last_cut ? 0.0f : tail[i] * block[st];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] *= q.scale;
-                        if (FULL || y + 4 <= yw) *(u32x4_at4*)(f + y) = __builtin_bit_cast(u32x4, v);
-                        else
+                for (int ta = 0; ta < NA; ++ta) {
+                    const float x = sb[s * L::BP + 16 * (NA * w + ta) + r] * kw;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) if (y + i < yw) f[y + i] = v[i];
-                    }
-                }
-            }
-        } else {
-            // a NaN or an infinity in the chunk: token by token, as in the kernel above
-            const float ge = pow2(lg);
-            int r = lane & 15, g = lane >> 4, tid = threadIdx.x;
-            asm("" : "+v"(r), "+v"(g), "+v"(tid));
-            for (int s = c ? 0 : gap; s < LC; ++s) {
-                const bool anew = cuts >> s & 1;
-                const int64_t i = (int64_t)c * LC + s;
-                float part[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int x = 16 * (NA * w + ta) + 4 * g + j;
-                        const float eb = sb[s * L::BP + x] * q.pair;
-                        float ea = 0.0f;
-                        if constexpr (OUT) if (x < X) ea = pa[i * ta_ + x];
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            float e = anew ? 0.0f : back ? S[ta][d][j] : S[ta][d][j] * ge;
-                            e += eb * sc[s * L::CP + 16 * d + r];
-                            if (x < X) part[d] += ea * e;
-                            S[ta][d][j] = back ? e * ge : e;
-                        }
-                    }
-                if constexpr (OUT) {
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        part[d] += __shfl_xor(part[d], 16);
-                        part[d] += __shfl_xor(part[d], 32);
-                        if (g == 0) red[w][16 * d + r] = part[d];
-                    }
-                    __syncthreads();
-                    if (tid < yw) po[i * to + tid] = (red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]) * q.scale;
-                    __syncthreads();
+                    for (int d = 0; d < 4; ++d) S[ta][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, fc[d][i], S[ta][d], 0, 0, 0);
                 }
             }
         }
+        if constexpr (OUT) {
+            if (c || t >= gap) {
+                float* f = po + ((int64_t)c * LC + t) * to;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int y = 16 * d + 4 * g;
+                    v4f v = O[d];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] *= q.scale;
+                    if (FULL || y + 4 <= yw) *(u32x4_at4*)(f + y) = __builtin_bit_cast(u32x4, v);
+                    else
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (y + i < yw) f[y + i] = v[i];
+                }
+            }
+        }
+
         left = cuts ? 0.0f : left * sd;
         qw = decay_pow(lg, t + 1 - back);
         sd = decay_pow(lg, LC);
@@ -949,6 +1032,18 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
         if (more) { stage(c + 1); publish(); }
     }
 
+    if (lane == 0) odd[w] = seen;
+    __syncthreads();
+    if (odd[0] | odd[1] | odd[2] | odd[3]) {
+        if constexpr (OUT) la_state_in<NA, 4, 16, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, r, X, yw, S);
+        else
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) S[ta][d] = v4f{0, 0, 0, 0};
+        la_tokens<float, NA, 4, 16, OUT>(p, q, b, h, n, i0, i1, lg, 16 * NA * w + 4 * g, r, y0, X, yw, red[w], S,
+                                         [&](int64_t i) { la_token_out<float>(q, b, h, n, i, tid, y0, yw, 4, &red[0][0]); });
+    }
     if (q.last) {
         const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
         if (gone) left = 0.0f;
@@ -1137,35 +1232,34 @@ int la_check_sizes(const char* who, int64_t B, int64_t T, int32_t H, int32_t Hk,
     return ACCERL_OK;
 }
 
-template <typename T, int DX, int NW, bool OUT, LaEdge HOW>
-void la_half(const LaParams& p, bool wanted, dim3 grid, hipStream_t s) {
-    if (!OUT || wanted) la_half_kernel<T, DX, NW, OUT, HOW, true><<<grid, dim3(64 * NW), 0, s>>>(p);
-    else if constexpr (OUT) la_half_kernel<T, DX, NW, OUT, HOW, false><<<grid, dim3(64 * NW), 0, s>>>(p);
-}
 template <typename T, int DX, bool OUT>
 void la_go(const LaParams& p, bool wide, LaEdge how, bool wanted, dim3 grid, hipStream_t s) {
-    if constexpr (__is_same(T, float)) {
-        if (how == EXACT) la_float_kernel<DX, OUT, true><<<grid, dim3(256), 0, s>>>(p);
-        else la_float_kernel<DX, OUT, false><<<grid, dim3(256), 0, s>>>(p);
-    } else {
-        if constexpr (DX == 128 || (DX == 256 && __is_same(T, BF16))) {
-            if (wide) return how == EXACT ? la_half<T, DX, 8, OUT, EXACT>(p, wanted, grid, s) : la_half<T, DX, 8, OUT, EDGE>(p, wanted, grid, s);
+    auto go = [&](auto kind) {
+        constexpr LaEdge HOW = decltype(kind)::value;
+        if constexpr (__is_same(T, float)) la_float_kernel<DX, OUT, HOW == EXACT><<<grid, dim3(256), 0, s>>>(p);
+        else if constexpr (OUT) {
+            const dim3 block(LaPair<T, DX>::THREADS);
+            if (wanted) la_pair_kernel<T, DX, HOW, true><<<grid, block, 0, s>>>(p);
+            else la_pair_kernel<T, DX, HOW, false><<<grid, block, 0, s>>>(p);
+        } else {
+            if constexpr (DX > 64) if (wide) return la_sum_kernel<T, DX, 8, HOW><<<grid, dim3(512), 0, s>>>(p);
+            la_sum_kernel<T, DX, 4, HOW><<<grid, dim3(256), 0, s>>>(p);
         }
-        if (how == EXACT) la_half<T, DX, 4, OUT, EXACT>(p, wanted, grid, s);
-        else if (how == EDGE) la_half<T, DX, 4, OUT, EDGE>(p, wanted, grid, s);
-        else la_half<T, DX, 4, OUT, SHORT>(p, wanted, grid, s);
-    }
+    };
+    if (how == EXACT) go(std::integral_constant<LaEdge, EXACT>());
+    else if (how == EDGE || __is_same(T, float)) go(std::integral_constant<LaEdge, EDGE>());
+    else go(std::integral_constant<LaEdge, SHORT>());
 }
 template <typename T, bool OUT>
 int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
+    // (the segments' sums: fewer and wider workgroups where there are enough of them to go round)
     int slices = 0, most = 0, least = LA_MAX_D;
     for (const LaRole& r : p.role)
         if (r.slices) {
             most = std::max(most, r.Y);
             least = std::min(least, std::min(r.X, r.Y));
         }
-    // (fewer and wider workgroups where there are enough of them to go round)
-    const bool wide = !__is_same(T, float) && X > 64 && most > LY && least >= 8 && !(__is_same(T, F16) && X == 256) && p.groups >= WIDE_GROUPS;
+    const bool wide = !OUT && !__is_same(T, float) && X > 64 && most > LY && least >= 8 && p.groups >= WIDE_GROUPS;
     const int cols = wide ? 2 * LY : LY;
     LaEdge how = least < 8 ? SHORT : EXACT;
     bool wanted = false;
