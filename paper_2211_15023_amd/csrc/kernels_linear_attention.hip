@@ -92,7 +92,8 @@ template <typename T> __device__ __forceinline__ u32x4 row_vec(const T* p, int l
     return v;
 }
 
-// Which work a workgroup has.  Workgroups go round the eight XCDs: the slices of a sequence, which read the same a and b, lie eight apart.
+// Which work a workgroup has.  Workgroups go round the eight XCDs: the slices of a sequence, which read the same a and b, lie eight apart.  Heads go before segments:
+// those of one token lie side by side in memory (65536 tokens of 16 heads of 128, bf16: 398 us, 449 the other way round).
 struct LaPlace { bool mine; uint32_t which, slice, seg, bh; };
 __device__ __forceinline__ LaPlace la_place(const LaParams& p) {
     LaPlace a;
@@ -101,8 +102,9 @@ __device__ __forceinline__ LaPlace la_place(const LaParams& p) {
     a.slice = id / 8 % slices;
     a.which = 0;
     while (a.slice >= (uint32_t)p.role[a.which].slices) a.slice -= p.role[a.which++].slices;
-    a.seg = grp % p.segs;
-    a.bh = grp / p.segs;
+    const uint32_t heads = p.groups / p.segs;
+    a.seg = grp / heads;
+    a.bh = grp % heads;
     return a;
 }
 // A lane's part of a state: rows x + 16 ta + i, columns y0 + y + the tile's first, which is 16 d or, dealt out by fours (STEP 4), 64 (d / 4) + 4 (d % 4).
@@ -421,28 +423,56 @@ __device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, 
         if (here)
 #pragma unroll
             for (int j = 0; j < 8; ++j) k8[j] = 32 * ks + (j < 4 ? 0 : 16) + 4 * g + j % 4 < last_cut ? 0.0f : k8[j];
-        v8bf fb[NA][TERMS];
+        if constexpr (ND == 4 && TERMS == 3) {
+            // (one tile of b's parts after the other: both at once, and reads ahead of them, would take the registers)
+            v8bf fc[ND][L::PARTS];
 #pragma unroll
-        for (int ta = 0; ta < NA; ++ta) {
-            float x[8];
-            unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= k8[j];
-            if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
-            else rounded8<TERMS>(x, fb[ta]);
-        }
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            v8bf fc[L::PARTS];
-#pragma unroll
-            for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down32(down_c + 32 * ks * L::CP + k * L::CT + la_column<4>(d), 16 * L::CP));
+                for (int k = 0; k < L::PARTS; ++k) fc[d][k] = __builtin_bit_cast(v8bf, down32(down_c + 32 * ks * L::CP + k * L::CT + la_column<4>(d), 16 * L::CP));
 #pragma unroll
             for (int ta = 0; ta < NA; ++ta) {
-                if constexpr (TERMS == 3) S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
-                if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
-                if constexpr (TERMS >= 2) S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
-                if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
-                S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+                float x[8];
+                v8bf fb[TERMS];
+                unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= k8[j];
+                if constexpr (TERMS == 3) parts8<3>(x, fb);
+                else rounded8<TERMS>(x, fb);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    if constexpr (TERMS == 3) S[ta][d] = mma(fb[2], fc[d][0], S[ta][d]);
+                    if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[1], fc[d][1], S[ta][d]);
+                    if constexpr (TERMS >= 2) S[ta][d] = mma(fb[1], fc[d][0], S[ta][d]);
+                    if constexpr (L::SPLIT) S[ta][d] = mma(fb[0], fc[d][1], S[ta][d]);
+                    S[ta][d] = mma(fb[0], fc[d][0], S[ta][d]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            v8bf fb[NA][TERMS];
+#pragma unroll
+            for (int ta = 0; ta < NA; ++ta) {
+                float x[8];
+                unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= k8[j];
+                if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
+                else rounded8<TERMS>(x, fb[ta]);
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                v8bf fc[L::PARTS];
+#pragma unroll
+                for (int k = 0; k < L::PARTS; ++k) fc[k] = __builtin_bit_cast(v8bf, down32(down_c + 32 * ks * L::CP + k * L::CT + la_column<4>(d), 16 * L::CP));
+#pragma unroll
+                for (int ta = 0; ta < NA; ++ta) {
+                    if constexpr (TERMS == 3) S[ta][d] = mma(fb[ta][2], fc[0], S[ta][d]);
+                    if constexpr (TERMS == 3 && L::SPLIT) S[ta][d] = mma(fb[ta][1], fc[1], S[ta][d]);
+                    if constexpr (TERMS >= 2) S[ta][d] = mma(fb[ta][1], fc[0], S[ta][d]);
+                    if constexpr (L::SPLIT) S[ta][d] = mma(fb[ta][0], fc[1], S[ta][d]);
+                    S[ta][d] = mma(fb[ta][0], fc[0], S[ta][d]);
+                }
             }
         }
     }
@@ -450,9 +480,11 @@ __device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, 
 
 // The state behind a segment alone: what it adds, from nothing.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its
 // end) and the weights hold for all.  Two of each tile: the next chunk is staged while this one is read, and a chunk has one barrier.
+// b and its weight are multiplied in fp32 and handed to the matrix instructions in three bf16 parts, which hold all 24 bits: the state is as exact as in fp32.
+// Bound by the splitting of b, not by memory: 65536 tokens of 16 heads of 128, bf16, 134 us, 4.0 TB/s of keys and values.
 // HOW: EXACT for heads of DX and slices of YW elements.
 template <typename T, int DX, int NW, LaEdge HOW>
-__global__ __launch_bounds__(64 * NW, (DX == 256 ? 2 : NW == 8 ? 4 : 3)) void la_sum_kernel(const LaParams p) {
+__global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2 : NW == 8 ? 4 : 3)) void la_sum_kernel(const LaParams p) {
     typedef LaHalf<T, DX, NW> L;
     constexpr int NA = L::NA, ND = L::ND, NB = DX == 256 ? 1 : 2;
     constexpr bool FULL = HOW == EXACT;
@@ -536,6 +568,8 @@ __global__ __launch_bounds__(64 * NW, (DX == 256 ? 2 : NW == 8 ? 4 : 3)) void la
 // The mixing itself.  Four wavefronts work out the outputs of a chunk, 16 tokens by 64 columns each, from the tiles and the state before it, while the others bring the
 // state behind it and the next tiles: on every SIMD one kind's matrix instructions run beside the other's conversions, and either needs half of the registers
 // that one wavefront doing both does, so that two workgroups are on a compute unit.
+// A pair's product, its weight and the state's copy go into the second product as bf16, half a step each (fp16: as two bf16 parts).  The tokens' traffic is 3.6 TB/s
+// of the 4.9 that a copy reaches where it is bound by memory (no state wanted: 92 us); what is left is a chunk's chain of products, barrier and state.
 template <typename T, int DX>
 struct LaPair {
     typedef LaHalf<T, DX, 4> L;
@@ -574,7 +608,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
     const int gap = (int)(i0 - base0);
     const float lg = p.log_decay[h] * LOG2E;
     const int64_t t0 = back ? n - 1 : 0;
-    const int yr = 16 * (r >> 2) + (r & 3);                   // (columns dealt out as in the kernel above)
+    const int yr = 16 * (r >> 2) + (r & 3);                   // (columns dealt out as in the sums)
     const uint16_t* down_c = sc + (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
     // at the end: has any wavefront seen a NaN or an infinity?
     auto strange = [&]() {
@@ -845,7 +879,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     // the state: rows 16 (NA w + ta) + 4 g + i, columns 16 d + r
     v4f S[NA][4];
     la_state_in<NA, 4, 16, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, r, X, yw, S);
-    // weights as in the kernel above
+    // weights of pairs, products of non-negative powers only: inside a tile of 16 tokens, of neighbouring tiles, of those further apart
     const int t = 16 * w + r;
     float diag[4], near[4], far[3], tail[4], block[4];
 #pragma unroll
@@ -1192,18 +1226,29 @@ int la_launched(const char* who) {
 bool la_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 constexpr int LA_MAX_D = 256;
-constexpr int64_t ONCE_BYTES = 96 << 20;
-
-constexpr int64_t SEG_BLOCKS = 1024;
+// What the caches hold.  One token's states of 16 heads of 128, read and written: 192 MB 61 us, and 70 by the caches; 512 MB 208 us, and 189 by the caches.
+constexpr int64_t ONCE_BYTES = 256 << 20;
+// From here on the segments' sums take 128 columns a workgroup, which read b half as often (65536 tokens, 16 heads of 128, bf16: 397 us in all, 422 with 64 columns).
 constexpr uint32_t WIDE_GROUPS = 512;
-constexpr int64_t TOGETHER_BLOCKS = 512;
+// Up to here the gradients' roles of two widths share a launch (2 x 200 tokens, 4 heads of 48 and 72, bf16: 20 us, 28 one by one); with more the padding costs more
+// (8 x 256 tokens, 8 heads of 100 and 200, fp32: 202 us, 166 one by one).
+constexpr int64_t TOGETHER_BLOCKS = 256;
 struct LaPlan { int segs; int64_t seg_len; };
-// Segments of a sequence, worked on side by side: what each adds to the state is summed first (keys and values are read twice), where sequences, heads and
-// columns alone leave compute units without work.
-LaPlan la_plan(int64_t B, int64_t T, int H, int slices) {
+// Segments of a sequence, worked on side by side, where sequences, heads and columns alone leave compute units without work: what each adds to the state is summed
+// first, so keys and values are read twice, and states go through memory.  From how many chunks on that pays, by workgroups without it:
+//     heads of 128, us whole / in segments     8: 3 chunks, 8, 16          64: 8 chunks, 16, 32          128: 16 chunks, 64        256: 64 chunks
+//     bf16                                     11/16, 21/17, 36/20         23/31, 38/36, 71/46           41/46, 156/132            168/225
+//     fp16                                     14/18, 29/19, 54/22         31/38, 56/46, 106/64          58/64, 222/194            236/339
+//     fp32 (bound by its products)             34/26, 82/27, 161/30        91/54, 175/82, 346/144        177/146, 772/531          785/1009
+LaPlan la_plan(int64_t B, int64_t T, int H, int slices, bool f32) {
     const int64_t blocks = B * H * slices, chunks = (T + LC - 1) / LC;
     int64_t segs = 1;
-    if (blocks > 0 && blocks < 512 && chunks >= 4) segs = std::max<int64_t>(1, std::min<int64_t>((SEG_BLOCKS + blocks - 1) / blocks, chunks));
+    if (blocks > 0 && (f32 ? blocks < 192 && chunks >= std::max<int64_t>(3, blocks / 16) : blocks < 160 && chunks >= std::max<int64_t>(8, blocks * blocks / 256))) {
+        // as many as are on the chip at once; twice as many where each still has eight chunks (65536 tokens, 16 heads of 128, bf16: 398 us with 1024, 420 with 512,
+        // 425 with 2048; 3 x 1777 tokens, 6 heads of 80 and 100, fp16: 49 us with 512, 65 with 1024)
+        const int64_t most = blocks * chunks >= 8 * 1024 ? 1024 : 512;
+        segs = std::max<int64_t>(1, std::min<int64_t>((most + blocks - 1) / blocks, chunks));
+    }
     const int64_t per = std::max<int64_t>(1, (chunks + segs - 1) / segs);
     return {(int)std::max<int64_t>(1, (chunks + per - 1) / per), per * LC};
 }
@@ -1212,9 +1257,9 @@ int64_t la_up(int64_t n) { return (n + 15) / 16 * 16; }
 
 // floats of the workspace: the segments' states and what each keeps, for the state and (gradients) its gradient; the parts of shared gradients
 struct LaWork { LaPlan plan; int64_t states, keep, parts_k, parts_v, total; };
-LaWork la_work(int64_t B, int64_t T, int H, int Hk, int Dk, int Dv, bool grad) {
+LaWork la_work(int64_t B, int64_t T, int H, int Hk, int Dk, int Dv, bool grad, bool f32) {
     LaWork k{};
-    k.plan = la_plan(B, T, H, grad ? 2 * la_slices(Dk) + la_slices(Dv) : la_slices(Dv));
+    k.plan = la_plan(B, T, H, grad ? 2 * la_slices(Dk) + la_slices(Dv) : la_slices(Dv), f32);
     if (k.plan.segs > 1) {
         k.states = la_up(B * H * (int64_t)Dk * Dv * k.plan.segs);
         k.keep = la_up(B * H * k.plan.segs);
@@ -1280,7 +1325,8 @@ int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
 }
 int la_pad(int x) { return x <= 64 ? 64 : x <= 128 ? 128 : 256; }
 
-// Launches of the roles, those of one width together; all in the widest one's where they leave compute units without work one by one.
+// Launches of the roles, those of one width together (gradients of 32 x 512 tokens, 16 heads of 128, bf16: 219 us, 227 with those whose state is not wanted in a launch of
+// their own), and all in the widest one's where they leave compute units without work one by one.
 template <typename T, bool OUT>
 int la_run(const char* who, const LaParams& common, const LaRole* roles, int count, hipStream_t s) {
     int64_t blocks = 0;
@@ -1471,7 +1517,8 @@ extern "C" {
 
 int64_t accerl_linear_attention_workspace(int64_t B, int64_t T, int32_t H, int32_t Hk, int32_t Dk, int32_t Dv, int32_t grad) {
     if (int rc = la_check_sizes("linear_attention_workspace", B, T, H, Hk, Dk, Dv)) return rc;
-    return 4 * la_work(B, T, H, Hk, Dk, Dv, grad != 0).total;
+    // (of either kind of tokens)
+    return 4 * std::max(la_work(B, T, H, Hk, Dk, Dv, grad != 0, false).total, la_work(B, T, H, Hk, Dk, Dv, grad != 0, true).total);
 }
 
 int accerl_linear_attention(const accerl_linear_attention_args* a, void* stream) {
@@ -1487,7 +1534,7 @@ int accerl_linear_attention(const accerl_linear_attention_args* a, void* stream)
     for (const LaTensor& t : {LaTensor{a->q, a->q_stride, a->H, a->Dk}, LaTensor{a->k, a->k_stride, a->Hk, a->Dk}, LaTensor{a->v, a->v_stride, a->Hk, a->Dv}})
         if (la_overlap(out, t, a->B, a->T, e)) return la_fail(ACCERL_EINVAL, who, "out overlaps q, k or v");
     if (a->out_state != a->state && la_states_overlap(a->out_state, a->state, a)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
-    const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, false);
+    const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, false, a->dtype == ACCERL_DT_F32);
     if (int rc = la_workspace(who, a, k)) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_forward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1515,7 +1562,7 @@ int accerl_linear_attention_grad(const accerl_linear_attention_args* a, void* st
     }
     if (!la_state_ok(a->state) || !la_state_ok(a->grad_out_state) || !la_state_ok(a->grad_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
     if (la_states_overlap(a->grad_state, a->state, a) || la_states_overlap(a->grad_state, a->grad_out_state, a)) return la_fail(ACCERL_EINVAL, who, "grad_state overlaps another state");
-    const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, true);
+    const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, true, a->dtype == ACCERL_DT_F32);
     if (int rc = la_workspace(who, a, k)) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_backward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1545,7 +1592,7 @@ int accerl_linear_attention_step(const accerl_linear_attention_args* a, void* st
     const int64_t blocks = a->B * a->H * p.slices;
     if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads and columns than one launch takes");
     const dim3 grid((uint32_t)blocks), block(256);
-    const bool whole = a->Dv % 64 == 0, once = 4 * a->B * a->H * (int64_t)a->Dk * a->Dv >= ONCE_BYTES;
+    const bool whole = a->Dv % 64 == 0, once = 4 * a->B * a->H * (int64_t)a->Dk * a->Dv > ONCE_BYTES;
     auto go = [&](auto type) {
         typedef decltype(type) T;
         auto rows = [&](auto n) {
