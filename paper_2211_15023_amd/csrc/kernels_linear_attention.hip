@@ -1316,7 +1316,7 @@ int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
         if (how == EXACT && (r.X != X || r.Y % cols)) how = EDGE;
     }
     const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * slices;
-    if (blocks * 256 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
+    if (blocks * 768 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
     const dim3 grid((uint32_t)blocks);
     if (X == 64) la_go<T, 64, OUT>(p, wide, how, wanted, grid, s);
     else if (X == 128) la_go<T, 128, OUT>(p, wide, how, wanted, grid, s);
