@@ -422,7 +422,7 @@ int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
  * aligned.  1 <= Dk, Dv <= 256.  log_decay holds numbers <= 0 or -inf.  State and sums are fp32.  With bf16 tokens the weights of
  * pairs of tokens and the state's copy that queries are multiplied with are rounded to bf16, as their partners are (fp16 tokens: to two bf16 parts,
  * 2^-17).  A state that is handed out, and those that segments of a long unroll hand on, are as exact as fp32; inside an unroll whose last state is
- * not wanted a key or value times its decay is rounded in the same way as a weight of a pair.
+ * not wanted a key or value times its decay is held to 2^-17.
  * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others.
  * out_state may be the state; otherwise outputs overlap neither inputs nor each other.
  */

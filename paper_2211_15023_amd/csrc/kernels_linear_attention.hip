@@ -578,12 +578,13 @@ struct LaPair {
     static constexpr int THREADS = 64 * (4 + NS);
     static constexpr int WAVES = L::SPLIT ? 2 : DX == 256 ? 3 : 4;    // of a SIMD
 };
-// WANTED: the state behind the last token is; else b's weighted copy has one part only, rounded as the state's copy is.
+// WANTED: the state behind the last token is; else b's weighted copy has two parts only, 2^-17 off, which the state's copy, rounded to one, does not show
+// (gradients' states and those between segments: 65536 tokens, 16 heads of 128, bf16, 405 us; one part 397, and outputs a fifth further off).
 template <typename T, int DX, LaEdge HOW, bool WANTED>
 __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) void la_pair_kernel(const LaParams p) {
     typedef LaPair<T, DX> Q;
     typedef typename Q::L L;
-    constexpr int NS = Q::NS, NA = Q::NA, TERMS = WANTED ? 3 : L::PARTS;
+    constexpr int NS = Q::NS, NA = Q::NA, TERMS = WANTED ? 3 : 2;
     constexpr bool FULL = HOW == EXACT;
 
     __shared__ __attribute__((aligned(16))) uint16_t sb[L::BT];
@@ -1228,7 +1229,7 @@ bool la_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) 
 constexpr int LA_MAX_D = 256;
 // What the caches hold.  One token's states of 16 heads of 128, read and written: 192 MB 61 us, and 70 by the caches; 512 MB 208 us, and 189 by the caches.
 constexpr int64_t ONCE_BYTES = 256 << 20;
-// From here on the segments' sums take 128 columns a workgroup, which read b half as often (65536 tokens, 16 heads of 128, bf16: 397 us in all, 422 with 64 columns).
+// From here on the segments' sums take 128 columns a workgroup, which read b half as often (65536 tokens, 16 heads of 128, bf16: 405 us in all, a sixteenth more with 64 columns).
 constexpr uint32_t WIDE_GROUPS = 512;
 // Up to here the gradients' roles of two widths share a launch (2 x 200 tokens, 4 heads of 48 and 72, bf16: 20 us, 28 one by one); with more the padding costs more
 // (8 x 256 tokens, 8 heads of 100 and 200, fp32: 202 us, 166 one by one).
