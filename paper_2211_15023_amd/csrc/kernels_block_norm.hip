@@ -1,8 +1,8 @@
 // The norms around a block with its gate and its residual, and their gradients.
 //
 // A row is read once and stays in the registers of its lanes, eight neighbouring elements at a time: all statistics are taken from there, the mean first and then
-// the squares around it.  Bound by memory where the row's eights fill its lanes: 65536 x 2048 bf16 with an fp32 stream 390 us (4.8 TB/s; a large copy reaches
-// 4.9), gradients of 32768 x 4096 bf16 520 (4.1; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
+// the squares around it.  Bound by memory where the row's eights fill its lanes: 65536 x 2048 bf16 with an fp32 stream 376 us (5.0 TB/s; a large copy reaches
+// 4.9), gradients of 32768 x 4096 bf16 490 (4.4; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
 // (gradients: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
 #include <algorithm>
 #include <cstdio>

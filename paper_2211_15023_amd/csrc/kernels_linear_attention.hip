@@ -481,7 +481,8 @@ __device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, 
 // The state behind a segment alone: what it adds, from nothing.  A sequence's tokens end with a chunk, so that only the first one may be short (its tokens at its
 // end) and the weights hold for all.  Two of each tile: the next chunk is staged while this one is read, and a chunk has one barrier.
 // b and its weight are multiplied in fp32 and handed to the matrix instructions in three bf16 parts, which hold all 24 bits: the state is as exact as in fp32.
-// Bound by the splitting of b, not by memory: 65536 tokens of 16 heads of 128, bf16, 134 us, 4.0 TB/s of keys and values.
+// Bound by the splitting of b and by its chain, not by memory alone: 65536 tokens of 16 heads of 128, bf16, 137 us, 3.9 TB/s of keys and values.
+// Vector instructions 53 % of the time, matrix instructions 33 %.
 // HOW: EXACT for heads of DX and slices of YW elements.
 template <typename T, int DX, int NW, LaEdge HOW>
 __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2 : NW == 8 ? 4 : 3)) void la_sum_kernel(const LaParams p) {
@@ -568,8 +569,9 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2
 // The mixing itself.  Four wavefronts work out the outputs of a chunk, 16 tokens by 64 columns each, from the tiles and the state before it, while the others bring the
 // state behind it and the next tiles: on every SIMD one kind's matrix instructions run beside the other's conversions, and either needs half of the registers
 // that one wavefront doing both does, so that two workgroups are on a compute unit.
-// A pair's product, its weight and the state's copy go into the second product as bf16, half a step each (fp16: as two bf16 parts).  The tokens' traffic is 3.6 TB/s
-// of the 4.9 that a copy reaches where it is bound by memory (no state wanted: 92 us); what is left is a chunk's chain of products, barrier and state.
+// A pair's product, its weight and the state's copy go into the second product as bf16, half a step each (fp16: as two bf16 parts).  64 x 512 tokens, 16 heads of 128,
+// bf16, state wanted: 162 us, 4.1 TB/s of the 4.9 that a copy reaches; vector instructions 47 % of the time, matrix instructions 23 %.  What is left is a chunk's
+// chain of products, barriers and state, which two workgroups a compute unit do not hide altogether.
 template <typename T, int DX>
 struct LaPair {
     typedef LaHalf<T, DX, 4> L;
