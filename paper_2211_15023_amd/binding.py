@@ -1082,6 +1082,8 @@ class BlockNorm:
                 if t[0]:
                     _check(t[0])
                 return t[1], t[2] if self.before is not None else None
+        if h is not None and self.before is None:
+            raise ValueError("h belongs to the norm before the next block")
         y = self._input(y)
         x, gate = None if x is None else x.detach(), None if gate is None else gate.detach()
         with _On(stream, y.device) as raw:

@@ -2,7 +2,7 @@
 //
 // A row is read once and stays in the registers of its lanes, eight neighbouring elements at a time: all statistics are taken from there, the mean first and then
 // the squares around it.  Bound by memory where the row's eights fill its lanes: 65536 x 2048 bf16 with an fp32 stream 376 us (5.0 TB/s; a large copy reaches
-// 4.9), gradients of 32768 x 4096 bf16 490 (4.4; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
+// 4.9), gradients of 32768 x 4096 bf16 463 (4.6; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
 // (gradients: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
 #include <algorithm>
 #include <cstdio>
@@ -138,7 +138,8 @@ __global__ __launch_bounds__(MOST, MOST == 1024 ? 4 : MOST == 512 || NC == 2 ? 2
     const int lane = GROUP ? threadIdx.x : threadIdx.x & (p.lanes - 1);
     const int64_t slot = GROUP ? blockIdx.x : (int64_t)blockIdx.x * (256 / p.lanes) + threadIdx.x / p.lanes;
     const int part = (int)(slot % p.groups), off = part * p.D;
-    // A lane's eights begin at `at`.  The row's last one ends with the row and so begins inside the one before, whose elements it reads too but leaves alone:
+    // A lane's eights begin at `at`.  The row's last one ends with the row and so begins inside the one before, whose elements it reads too but leaves alone
+    // (they count as zeros in everything, so that an infinity there is no NaN here):
     // its own are those from `from` to `to` - 1 (none where the row has no eight for the lane, which reads the first).
     int at[NC], from[NC], to[NC];
     bool whole = true;
@@ -160,13 +161,13 @@ __global__ __launch_bounds__(MOST, MOST == 1024 ? 4 : MOST == 512 || NC == 2 ? 2
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            wa[i] = weight(after, i / 8, i % 8);
-            wb[i] = weight(p.before, i / 8, i % 8);
+            wa[i] = mine(i, weight(after, i / 8, i % 8));
+            wb[i] = mine(i, weight(p.before, i / 8, i % 8));
             sa[i] = sb[i] = 0.0f;
         }
     }
-    auto wa_of = [&](int i) { if constexpr (LEAN) return weight(after, i / 8, i % 8); else return wa[i]; };
-    auto wb_of = [&](int i) { if constexpr (LEAN) return weight(p.before, i / 8, i % 8); else return wb[i]; };
+    auto wa_of = [&](int i) { if constexpr (LEAN) return mine(i, weight(after, i / 8, i % 8)); else return wa[i]; };
+    auto wb_of = [&](int i) { if constexpr (LEAN) return mine(i, weight(p.before, i / 8, i % 8)); else return wb[i]; };
     auto add_a = [&](int i, float v) { if constexpr (LEAN) sums[i * MOST + threadIdx.x] += v; else sa[i] += v; };
     auto add_b = [&](int i, float v) { if constexpr (LEAN) sums[(N + i) * MOST + threadIdx.x] += v; else sb[i] += v; };
     // a lane's places in the row it reads and the row it writes, which go on with the rows
@@ -223,6 +224,7 @@ __global__ __launch_bounds__(MOST, MOST == 1024 ? 4 : MOST == 512 || NC == 2 ? 2
         if (p.gate_kind) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) numbers8(now.gate[c], gate + 8 * c);
+            if (!whole) each([&](int i) { gate[i] = mine(i, gate[i]); });
             each([&](int i) { e[i] = sigmoid(gate[i]); u[i] *= e[i]; });
             if (p.gate_kind == ACCERL_GATE_SILU) each([&](int i) { u[i] *= gate[i]; });
         }

@@ -1319,7 +1319,6 @@ int la_launch(const char* who, LaParams p, int X, hipStream_t s) {
         if (how == EXACT && (r.X != X || r.Y % cols)) how = EDGE;
     }
     const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * slices;
-    if (blocks * 768 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
     const dim3 grid((uint32_t)blocks);
     if (X == 64) la_go<T, 64, OUT>(p, wide, how, wanted, grid, s);
     else if (X == 128) la_go<T, 128, OUT>(p, wide, how, wanted, grid, s);
@@ -1339,6 +1338,8 @@ int la_run(const char* who, const LaParams& common, const LaRole* roles, int cou
         widest = std::max(widest, la_pad(roles[i].X));
     }
     const bool together = blocks <= TOGETHER_BLOCKS;
+    // (all of them with the widest workgroup's threads, groups rounded up to eight: nothing is enqueued of a call that a later launch would refuse)
+    if ((blocks + 8 * 12) * 768 > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more heads, segments and columns than one launch takes");
     for (int x : {64, 128, 256}) {
         LaParams p = common;
         int n = 0;
@@ -1377,6 +1378,7 @@ int la_forward(const char* who, const accerl_linear_attention_args& a, LaParams 
     return la_run<T, true>(who, p, &r, 1, s);
 }
 
+int64_t la_fold_items(const accerl_linear_attention_args& a) { return a.B * a.T * a.Hk * (int64_t)std::max(a.Dk, a.Dv); }
 template <typename T>
 int la_backward(const char* who, const accerl_linear_attention_args& a, LaParams p, const LaWork& k, float* ws, hipStream_t s) {
     const int share = a.H / a.Hk;
@@ -1427,9 +1429,7 @@ int la_backward(const char* who, const accerl_linear_attention_args& a, LaParams
         f.at[0] = {parts_k, a.grad_k, a.grad_k_stride.batch, a.grad_k_stride.token, a.grad_k_stride.head, a.Dk};
         f.at[1] = {parts_v, a.grad_v, a.grad_v_stride.batch, a.grad_v_stride.token, a.grad_v_stride.head, a.Dv};
         f.tokens = a.B * a.T; f.T = a.T; f.H = a.H; f.Hk = a.Hk;
-        const int64_t items = f.tokens * a.Hk * std::max(a.Dk, a.Dv);
-        if (items > MAX_LAUNCH_ITEMS) return la_fail(ACCERL_EUNSUPPORTED, who, "more gradients of shared heads than one launch takes");
-        la_fold_kernel<T><<<dim3((uint32_t)((items + 255) / 256), 2), dim3(256), 0, s>>>(f);
+        la_fold_kernel<T><<<dim3((uint32_t)((la_fold_items(a) + 255) / 256), 2), dim3(256), 0, s>>>(f);
         if (int rc = la_launched(who)) return rc;
     }
     return ACCERL_OK;
@@ -1564,6 +1564,7 @@ int accerl_linear_attention_grad(const accerl_linear_attention_args* a, void* st
             !la_spread(a->grad_v_stride, a->B, a->T, a->Hk, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of a gradient overlap");
     }
     if (!la_state_ok(a->state) || !la_state_ok(a->grad_out_state) || !la_state_ok(a->grad_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
+    if (a->H != a->Hk && la_fold_items(*a) > MAX_LAUNCH_ITEMS - 256) return la_fail(ACCERL_EUNSUPPORTED, who, "more gradients of shared heads than one launch takes");
     if (la_states_overlap(a->grad_state, a->state, a) || la_states_overlap(a->grad_state, a->grad_out_state, a)) return la_fail(ACCERL_EINVAL, who, "grad_state overlaps another state");
     const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, true, a->dtype == ACCERL_DT_F32);
     if (int rc = la_workspace(who, a, k)) return rc;

@@ -174,3 +174,27 @@ def test_rows_past_32_bits(A):
     assert all(torch.equal(p, q) for p, q in zip(got, want))
     r = norm.backward(y, x=x, gate=gate, grad_u=gu, grad_h=gh)
     assert all(torch.equal(getattr(r, n), getattr(wr, n)) for n in ("y", "x", "gate", "after", "before"))
+
+
+@pytest.mark.parametrize("D", [9, 20, 300, 515, 1030, 2050, 3001, 9000])
+@pytest.mark.parametrize("where", ["gate", "after"])
+def test_an_infinity_near_a_rows_end(A, D, where):
+    """As anywhere else in the row: the norm that follows makes zeros of the others and NaN of it, and the rows beside it are as they were."""
+    R = 6
+    y, gate = torch.rand((R, D), device="cuda") + 0.5, torch.rand((R, D), device="cuda") + 0.5
+    after = torch.ones(D)
+    clean = A.BlockNorm(D, after=after, before=torch.ones(D), gate="silu").forward(y, gate=gate)
+    for back in range(1, 10):
+        if where == "gate":
+            g, a, rows = gate.clone(), after, slice(2, 3)
+            g[2, D - back] = float("inf")
+        else:
+            g, a, rows = gate, after.clone(), slice(0, R)
+            a[D - back] = float("inf")
+        u, h = A.BlockNorm(D, after=a, before=torch.ones(D), gate="silu").forward(y, gate=g)
+        there = torch.zeros((R, D), dtype=torch.bool, device="cuda")
+        there[rows, D - back] = True
+        beside = torch.zeros((R, D), dtype=torch.bool, device="cuda")
+        beside[rows] = True
+        assert torch.isinf(u[there]).all() and torch.equal(u[~there], clean[0][~there]), back
+        assert torch.isnan(h[there]).all() and (h[beside & ~there] == 0).all() and torch.equal(h[~beside], clean[1][~beside]), back

@@ -50,3 +50,25 @@ def test_more_heads_than_a_launch_takes(A):
             assert f(C.byref(a), None) == EUNSUPPORTED and "one launch" in A.accerl_last_error()
         a = attention_args(at(9), dtype=dtype, **dict(big, state=at(20), out_state=at(20)))
         assert lib.accerl_linear_attention_step(C.byref(a), None) == EUNSUPPORTED and "one launch" in A.accerl_last_error()
+
+
+def test_more_shared_gradients_than_a_launch_takes(A):
+    """2^25 tokens of 128 elements whose heads are shared: refused before anything is enqueued."""
+    from paper_2211_15023_amd import binding
+    lib = A.load_library()
+    q, kv = binding._TokenStride(256 << 25, 256, 128), binding._TokenStride(128 << 25, 128, 128)
+    at = lambda i: (i + 1) << 40
+    a = attention_args(at(9), B=1, T=1 << 25, H=2, Hk=1, Dk=128, Dv=128, reset=None, lengths=None, q_stride=q, k_stride=kv, v_stride=kv, grad_out_stride=q, grad_q_stride=q, grad_k_stride=kv,
+                       grad_v_stride=kv, q=at(0), k=at(1), v=at(2), grad_out=at(4), grad_q=at(5), grad_k=at(6), grad_v=at(7), state=None, grad_state=None, grad_out_state=None,
+                       workspace=at(30), workspace_bytes=1 << 40)
+    assert lib.accerl_linear_attention_grad(C.byref(a), None) == EUNSUPPORTED and "shared heads" in A.accerl_last_error()
+
+
+def test_a_table_for_a_norm_that_is_not_there(A):
+    with torch._subclasses.fake_tensor.FakeTensorMode():
+        y = torch.empty((3, 8), device="cuda")
+        norm = A.BlockNorm(8, after=y[0])
+        with pytest.raises(ValueError, match="before the next block"):
+            norm.forward(y, h=torch.empty_like(y))
+        with pytest.raises(ValueError, match="before the next block"):
+            norm.backward(y, grad_h=y)
