@@ -840,6 +840,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
 
 // ---------------------------------------------------------------- tokens of fp32
 // The same walk on fp32 matrix instructions, which are what bounds it: 376 of 32 cycles for a chunk of a head of 128, at 64 columns.
+// 32 x 512 tokens, 16 heads of 128: 412 us.
 template <int DX>
 struct LaFloat {
     // rows 16 bytes further on in the banks, for 16-byte reads of 16 rows and for reads of four rows that lie four apart
@@ -1091,6 +1092,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
 }
 
 // The states that enter the segments, from what each segment adds: states [segment][B H][X Y] in place, the last one to `last`.
+// Bound by memory and by the chain of the segments (64 segments of 16 heads of 128 x 128: 12 us for 67 MB read and written).
 struct LaJoin { float* states; const float* keep; const float* enter; float* last; };
 struct LaJoinParams { LaJoin at[2]; int64_t n, per; int segs; };               // n = B H X Y, per = X Y
 __global__ __launch_bounds__(256) void la_join_kernel(const LaJoinParams p) {
@@ -1119,6 +1121,7 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaJoinParams p) {
 }
 
 // The gradients of shared keys and values: the heads' parts [B, T, H, D] in fp32, summed in the heads' order and rounded once.
+// Bound by memory, or a launch (5 x 333 tokens: 4 us).
 struct LaFold { const float* part; void* out; int64_t sb, st, sh; int D; };
 struct LaFoldParams { LaFold at[2]; int64_t tokens, T; int H, Hk; };
 template <typename T>
@@ -1150,6 +1153,7 @@ struct LaStep {
 
 // A workgroup has 64 columns of a state: 16 lanes of four columns, 16 rows at a time, all rows asked for before the first is used.  Bound by memory: the state
 // is read and written once.  FULL: 16 ROWS rows, and columns in whole workgroups.  ONCE: states that are more than the caches hold go by them.
+// 512 environments of 16 heads of 128, bf16 tokens: 190 us, 5.7 TB/s.
 template <typename T, int ROWS, bool FULL, bool ONCE>
 __global__ __launch_bounds__(256, ROWS <= 4 ? 8 : ROWS == 8 ? 6 : 4) void la_step_kernel(const LaStep p) {
     __shared__ v4f red[4][16];

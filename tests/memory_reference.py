@@ -69,8 +69,8 @@ def unroll_roundings(T, D, decay):
 
 
 def unroll_tolerance(ref, size, dtype, T, D, decay, state=False):
-    """size: the same result of magnitudes.  bf16: the weights of pairs and the state's copy are rounded once (half a step of the size); a state's terms are split in
-    two halves of which the second is rounded (half a step, squared).  Last the result's own rounding."""
+    """size: the same result of magnitudes.  bf16: the weights of pairs and the state's copy are rounded once (half a step of the size); a state's terms may be
+    held in two halves of which the second is rounded (half a step, squared).  Last the result's own rounding."""
     part = unroll_roundings(T, D, decay) * U
     if dtype == "bf16":
         part += HALF_STEP["bf16"] ** 2 if state else HALF_STEP["bf16"] * 1.01
