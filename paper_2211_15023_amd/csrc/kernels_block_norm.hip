@@ -3,7 +3,7 @@
 // A row is read once and stays in the registers of its lanes, eight neighbouring elements at a time: all statistics are taken from there, the mean first and then
 // the squares around it.  Bound by memory where the row's eights fill its lanes: 65536 x 2048 bf16 with an fp32 stream 376 us (5.0 TB/s; a large copy reaches
 // 4.9), gradients of 32768 x 4096 bf16 463 (4.6; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
-// (gradients: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
+// (gradients and few rows: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
 #include <algorithm>
 #include <cstdio>
 
@@ -379,7 +379,10 @@ bool bn_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) 
 struct NormShape { int nc, lanes, threads, at_once; bool group; int64_t blocks, records; };
 NormShape bn_shape(int64_t rows, int d, int groups, bool grad) {
     NormShape s{};
-    if (d <= (grad ? 512 : 1024)) {
+    // (forwards, few rows, which are latency alone: one eight a lane, in a workgroup where that takes more than a wavefront.  16 rows of 600, 1024 and 2048, bf16: 4.3, 4.4
+    // and 5.5 us, 6.7, 7.6 and 6.0 with two; 1024 rows 6.7, 8.3 and 13.2, and 7.4, 8.4 and 13.8)
+    const bool few = !grad && rows <= 1024 && d <= 2048;
+    if (d <= (grad || few ? 512 : 1024)) {
         s.nc = d <= 512 ? 1 : 2;
         s.lanes = 1;
         while (s.lanes * 8 * s.nc < d) s.lanes *= 2;
@@ -389,7 +392,7 @@ NormShape bn_shape(int64_t rows, int d, int groups, bool grad) {
         // (gradients of rows of 600 and 1024 bf16: 470 and 249 us for 2^26 elements with one eight a lane, 496 and 266 with two in a wavefront; of 3000 and 4096:
         // 396 and 250 with two, 656 and 369 with one)
         s.group = true;
-        s.nc = !grad ? 2 : d <= 1024 ? 1 : d <= 8192 ? 2 : 4;
+        s.nc = few ? 1 : !grad ? 2 : d <= 1024 ? 1 : d <= 8192 ? 2 : 4;
         s.threads = s.lanes = (d + 512 * s.nc - 1) / (512 * s.nc) * 64;
         s.at_once = 1;
     }

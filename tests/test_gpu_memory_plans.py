@@ -198,3 +198,22 @@ def test_an_infinity_near_a_rows_end(A, D, where):
         beside[rows] = True
         assert torch.isinf(u[there]).all() and torch.equal(u[~there], clean[0][~there]), back
         assert torch.isnan(h[there]).all() and (h[beside & ~there] == 0).all() and torch.equal(h[~beside], clean[1][~beside]), back
+
+
+@pytest.mark.parametrize("D,groups", [(600, 1), (1024, 1), (1201, 1), (2048, 1), (3000, 1), (3000, 5), (2048, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norms_of_few_and_many_rows(A, D, groups, dtype):
+    """A row's result does not depend on how many there are: sums of up to 3000 terms in other orders, 3000 2^-24 apart before the root, and a rounding to the type."""
+    R = 1100
+    g = torch.Generator(device="cuda").manual_seed(D)
+    y, gate, x = (torch.randn((R, D), generator=g, device="cuda").to(t) for t in (dtype, dtype, torch.float32))
+    norm = A.BlockNorm(D, after=torch.linspace(0.5, 1.5, D), before=torch.ones(D) if groups == 1 else None, gate="silu", groups=groups, kind="layer")
+    u, h = norm.forward(y, x=x, gate=gate)
+    for rows in (slice(0, 1), slice(5, 70), slice(76, R)):
+        us, hs = norm.forward(y[rows], x=x[rows], gate=gate[rows])
+        assert torch.allclose(us, u[rows], rtol=2e-4, atol=2e-4)
+        if groups == 1:
+            step = 2e-4 + (0 if dtype == torch.float32 else 2.0 ** -7)
+            assert torch.allclose(hs.float(), h[rows].float(), rtol=step, atol=2e-4)
+    want = x.double() + torch.nn.functional.layer_norm(y.double().view(R, groups, -1), (D // groups,), eps=1e-6).view(R, D) * norm.after.double() * torch.nn.functional.silu(gate.double())
+    assert torch.allclose(u.double(), want, rtol=2e-4, atol=2e-4)
