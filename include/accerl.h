@@ -424,7 +424,7 @@ int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
  * 2^-17).  A state that is handed out, and those that segments of a long unroll hand on, are as exact as fp32; inside an unroll whose last state is
  * not wanted a key or value times its decay is held to 2^-17.
  * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others.
- * out_state may be the state; otherwise outputs overlap neither inputs nor each other.
+ * out_state may be the state; otherwise outputs overlap neither inputs nor each other, and the workspace overlaps nothing (ACCERL_EINVAL, also of columns of one buffer's rows).
  */
 typedef struct { int64_t batch, token, head; } accerl_token_stride;
 

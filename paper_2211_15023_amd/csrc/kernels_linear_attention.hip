@@ -10,6 +10,7 @@
 // and the chunk's last state is g^64 E_before + sum_s g^{63-s} b_s c_s^T: four matrix products.
 #include <algorithm>
 #include <cstdio>
+#include <initializer_list>
 #include <type_traits>
 
 #include "wide_ops.h"
@@ -1471,37 +1472,42 @@ bool la_spread(const accerl_token_stride& s, int64_t B, int64_t T, int H, int D)
     return true;
 }
 
-// A tensor of tokens as a table of rows, if its dimensions fold into one (contiguous heads or tokens, one stride over the rest).
-bool la_table(const void* at, const accerl_token_stride& st, int64_t B, int64_t T, int64_t H, int D, int e, Table& t) {
-    struct Dim { int64_t n, step; } d[3] = {{B, st.batch}, {T, st.token}, {H, st.head}};
-    std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.step < y.step; });
-    int64_t run = D, rows = 1, apart = 0;
-    for (const Dim& x : d) {
-        if (x.n <= 1) continue;
-        if (x.step < 0) return false;
-        if (rows == 1 && x.step == run) run *= x.n;
-        else if (rows == 1) { if (x.step < run) return false; rows = x.n; apart = x.step; }
-        else if (x.step == apart * rows) rows *= x.n;
-        else return false;
+// What a call reads and writes, as runs of bytes.
+struct LaPlaces {
+    Strided q, k, v, log_decay, reset, lengths, state, out, out_state, grad_out, grad_out_state, grad_q, grad_k, grad_v, grad_state;
+    // (step: one token, and no lengths)
+    LaPlaces(const accerl_linear_attention_args& a, bool step)
+        : q(tokens(a, a.q, a.q_stride, a.H, a.Dk, step)), k(tokens(a, a.k, a.k_stride, a.Hk, a.Dk, step)), v(tokens(a, a.v, a.v_stride, a.Hk, a.Dv, step)),
+          log_decay(a.log_decay, 4 * (int64_t)a.H), reset(a.reset, a.B, a.reset_batch, step ? 1 : a.T, a.reset_token, 1, 0, 1), lengths(step ? nullptr : a.lengths, 4 * a.B),
+          state(states(a, a.state)), out(tokens(a, a.out, a.out_stride, a.H, a.Dv, step)), out_state(states(a, a.out_state)),
+          grad_out(tokens(a, a.grad_out, a.grad_out_stride, a.H, a.Dv, step)), grad_out_state(states(a, a.grad_out_state)), grad_q(tokens(a, a.grad_q, a.grad_q_stride, a.H, a.Dk, step)),
+          grad_k(tokens(a, a.grad_k, a.grad_k_stride, a.Hk, a.Dk, step)), grad_v(tokens(a, a.grad_v, a.grad_v_stride, a.Hk, a.Dv, step)), grad_state(states(a, a.grad_state)) {}
+    static Strided tokens(const accerl_linear_attention_args& a, const void* p, const accerl_token_stride& s, int H, int D, bool step) {
+        const int64_t e = dtype_bytes(a.dtype);
+        return Strided(p, a.B, s.batch * e, step ? 1 : a.T, s.token * e, H, s.head * e, D * e);
     }
-    t = {at, rows, (rows == 1 ? run : apart) * e, run * e};
-    return true;
+    static Strided states(const accerl_linear_attention_args& a, const void* p) { return Strided(p, 4 * a.B * a.H * a.Dk * a.Dv); }
+};
+typedef std::initializer_list<const Strided*> LaList;
+bool la_any_share(LaList outs, LaList others) {
+    for (const Strided* o : outs)
+        for (const Strided* t : others) if (share(*o, *t)) return true;
+    return false;
 }
-// Whether an output shares elements with another tensor: looked for where both fold into tables (or at all where they lie apart), else the caller's to avoid.
-struct LaTensor { const void* p; accerl_token_stride st; int H, D; };
-bool la_overlap(const LaTensor& o, const LaTensor& t, int64_t B, int64_t T, int e) {
-    Table a, b;
-    return o.p && t.p && la_table(o.p, o.st, B, T, o.H, o.D, e, a) && la_table(t.p, t.st, B, T, t.H, t.D, e, b) && share(a, b);
-}
-bool la_states_overlap(const void* a, const void* b, const accerl_linear_attention_args* s) {
-    const int64_t n = 4 * s->B * s->H * s->Dk * s->Dv;
-    return a && b && share(table(a, n), table(b, n));
+// an unroll's or a step's outputs; out_state may be the state
+int la_outputs_apart(const char* who, const accerl_linear_attention_args* a, const LaPlaces& at) {
+    if (la_any_share({&at.out, &at.out_state}, {&at.q, &at.k, &at.v, &at.log_decay, &at.reset, &at.lengths})) return la_fail(ACCERL_EINVAL, who, "an output overlaps an input");
+    if (la_any_share({&at.out}, {&at.state, &at.out_state})) return la_fail(ACCERL_EINVAL, who, "out overlaps a state");
+    if (a->out_state != a->state && share(at.out_state, at.state)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
+    return ACCERL_OK;
 }
 
-int la_workspace(const char* who, const accerl_linear_attention_args* a, const LaWork& k) {
+int la_workspace(const char* who, const accerl_linear_attention_args* a, const LaWork& k, LaList all) {
     if (k.total == 0) return ACCERL_OK;
     if (!a->workspace || !la_aligned(a->workspace, 16)) return la_fail(ACCERL_EINVAL, who, "workspace is NULL or misaligned");
     if (a->workspace_bytes < 4 * k.total) return la_fail(ACCERL_EINVAL, who, "workspace smaller than accerl_linear_attention_workspace says");
+    const Strided work(a->workspace, 4 * k.total);
+    if (la_any_share({&work}, all)) return la_fail(ACCERL_EINVAL, who, "the workspace overlaps an input or an output");
     return ACCERL_OK;
 }
 
@@ -1537,12 +1543,10 @@ int accerl_linear_attention(const accerl_linear_attention_args* a, void* stream)
     if (a->T > 0 && (!a->out || !la_aligned(a->out, e))) return la_fail(ACCERL_EINVAL, who, "out is NULL or misaligned");
     if (a->T > 0 && !la_spread(a->out_stride, a->B, a->T, a->H, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of the output overlap");
     if (!la_state_ok(a->state) || !la_state_ok(a->out_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
-    const LaTensor out = {a->out, a->out_stride, a->H, a->Dv};
-    for (const LaTensor& t : {LaTensor{a->q, a->q_stride, a->H, a->Dk}, LaTensor{a->k, a->k_stride, a->Hk, a->Dk}, LaTensor{a->v, a->v_stride, a->Hk, a->Dv}})
-        if (la_overlap(out, t, a->B, a->T, e)) return la_fail(ACCERL_EINVAL, who, "out overlaps q, k or v");
-    if (a->out_state != a->state && la_states_overlap(a->out_state, a->state, a)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
+    const LaPlaces at(*a, false);
+    if (int rc = la_outputs_apart(who, a, at)) return rc;
     const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, false, a->dtype == ACCERL_DT_F32);
-    if (int rc = la_workspace(who, a, k)) return rc;
+    if (int rc = la_workspace(who, a, k, {&at.q, &at.k, &at.v, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.out, &at.out_state})) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_forward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
     if (a->dtype == ACCERL_DT_BF16) return la_forward<BF16>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1558,20 +1562,19 @@ int accerl_linear_attention_grad(const accerl_linear_attention_args* a, void* st
     if (a->T > 0) {
         for (const void* p : {a->grad_out, (const void*)a->grad_q, (const void*)a->grad_k, (const void*)a->grad_v})
             if (!p || !la_aligned(p, e)) return la_fail(ACCERL_EINVAL, who, "a gradient is NULL or misaligned");
-        const LaTensor in[4] = {{a->q, a->q_stride, a->H, a->Dk}, {a->k, a->k_stride, a->Hk, a->Dk}, {a->v, a->v_stride, a->Hk, a->Dv}, {a->grad_out, a->grad_out_stride, a->H, a->Dv}};
-        const LaTensor to[3] = {{a->grad_q, a->grad_q_stride, a->H, a->Dk}, {a->grad_k, a->grad_k_stride, a->Hk, a->Dk}, {a->grad_v, a->grad_v_stride, a->Hk, a->Dv}};
-        for (int i = 0; i < 3; ++i) {
-            for (const LaTensor& t : in) if (la_overlap(to[i], t, a->B, a->T, e)) return la_fail(ACCERL_EINVAL, who, "a gradient overlaps an input");
-            for (int j = 0; j < i; ++j) if (la_overlap(to[i], to[j], a->B, a->T, e)) return la_fail(ACCERL_EINVAL, who, "two gradients overlap");
-        }
         if (!la_spread(a->grad_q_stride, a->B, a->T, a->H, a->Dk) || !la_spread(a->grad_k_stride, a->B, a->T, a->Hk, a->Dk) ||
             !la_spread(a->grad_v_stride, a->B, a->T, a->Hk, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of a gradient overlap");
     }
     if (!la_state_ok(a->state) || !la_state_ok(a->grad_out_state) || !la_state_ok(a->grad_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
     if (a->H != a->Hk && la_fold_items(*a) > MAX_LAUNCH_ITEMS - 256) return la_fail(ACCERL_EUNSUPPORTED, who, "more gradients of shared heads than one launch takes");
-    if (la_states_overlap(a->grad_state, a->state, a) || la_states_overlap(a->grad_state, a->grad_out_state, a)) return la_fail(ACCERL_EINVAL, who, "grad_state overlaps another state");
+    const LaPlaces at(*a, false);
+    if (la_any_share({&at.grad_q, &at.grad_k, &at.grad_v, &at.grad_state}, {&at.q, &at.k, &at.v, &at.grad_out, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.grad_out_state}))
+        return la_fail(ACCERL_EINVAL, who, "a gradient overlaps an input");
+    if (la_any_share({&at.grad_q}, {&at.grad_k, &at.grad_v, &at.grad_state}) || la_any_share({&at.grad_k}, {&at.grad_v, &at.grad_state}) || share(at.grad_v, at.grad_state))
+        return la_fail(ACCERL_EINVAL, who, "two gradients overlap");
     const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, true, a->dtype == ACCERL_DT_F32);
-    if (int rc = la_workspace(who, a, k)) return rc;
+    if (int rc = la_workspace(who, a, k, {&at.q, &at.k, &at.v, &at.grad_out, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.grad_out_state, &at.grad_q, &at.grad_k, &at.grad_v,
+                                          &at.grad_state})) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_backward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
     if (a->dtype == ACCERL_DT_BF16) return la_backward<BF16>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1587,7 +1590,7 @@ int accerl_linear_attention_step(const accerl_linear_attention_args* a, void* st
     if (!a->out || !la_aligned(a->out, e)) return la_fail(ACCERL_EINVAL, who, "out is NULL or misaligned");
     if (!la_spread({a->out_stride.batch, 0, a->out_stride.head}, a->B, 1, a->H, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of the output overlap");
     if (!a->state || !a->out_state || !la_state_ok(a->state) || !la_state_ok(a->out_state)) return la_fail(ACCERL_EINVAL, who, "a state is NULL or not 16-byte aligned");
-    if (a->out_state != a->state && la_states_overlap(a->out_state, a->state, a)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
+    if (int rc = la_outputs_apart(who, a, LaPlaces(*a, true))) return rc;
     LaStep p{};
     const int share = a->H / a->Hk;
     p.q = la_side(a->q, a->q_stride, 1); p.k = la_side(a->k, a->k_stride, share); p.v = la_side(a->v, a->v_stride, share);
