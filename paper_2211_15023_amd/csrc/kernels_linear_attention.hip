@@ -1429,7 +1429,7 @@ int la_backward(const char* who, const accerl_linear_attention_args& a, LaParams
     }
     LaRole roles[3] = {rq, rk, rv};
     if (int rc = la_run<T, true>(who, p, roles, 3, s)) return rc;
-    if (share > 1) {
+    if (share > 1 && a.T > 0) {                               // (no launch is of nothing)
         LaFoldParams f{};
         f.at[0] = {parts_k, a.grad_k, a.grad_k_stride.batch, a.grad_k_stride.token, a.grad_k_stride.head, a.Dk};
         f.at[1] = {parts_v, a.grad_v, a.grad_v_stride.batch, a.grad_v_stride.token, a.grad_v_stride.head, a.Dv};
