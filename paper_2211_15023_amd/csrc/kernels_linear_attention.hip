@@ -150,9 +150,10 @@ __device__ __forceinline__ void meet() {
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
-// A segment in which a NaN or an infinity of b or c was seen, again, token by token as the formula says: in the products a weight of 0 would carry it to tokens
-// before it and to other episodes.  A lane has the rows x + 16 ta + j and columns y + la_column(d) of the state; with outputs (red) wavefront `w` of the state's
-// leaves its part of a token's there, and meets those that take it.
+// A segment in which a NaN or an infinity was seen, in b, in c or in an output, again, token by token as the formula says: in the products a weight of 0 would carry it
+// to tokens before it and to other episodes, an infinity of a would meet pairs of either sign, and a pair's product that fp32 does not hold would be an infinity though
+// its weight is 0.  A lane has the rows x + 16 ta + j and columns y + la_column(d) of the state; with outputs (red) wavefront `w` of the state's leaves its part of a
+// token's there, and meets those that take it.
 template <typename T, int NA, int ND, int STEP, bool OUT, typename F>
 __device__ __forceinline__ void la_tokens(const LaParams& p, const LaRole& q, uint32_t b, uint32_t h, int64_t n, int64_t i0, int64_t i1, float lg, int x, int y, int y0, int X, int yw,
                                           float* red, v4f (&S)[NA][ND], F taken) {
@@ -594,7 +595,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
     __shared__ __attribute__((aligned(16))) uint16_t sc[L::PARTS * L::CT];
     // the state as the fragments that the product with a reads: [part][column tile][depth][lane][8]
     __shared__ __attribute__((aligned(16))) uint16_t ss[L::PARTS * L::SF];
-    __shared__ int odd[NS];                                   // whether a wavefront has seen a NaN or an infinity in b or c (fp16: or in the state)
+    __shared__ int odd[4 + NS];                               // whether a wavefront has seen a NaN or an infinity, in an output or in b or c
     __shared__ uint64_t cut_mask;                             // tokens of the chunk that start from nothing
     __shared__ float red[NS][LY];
 
@@ -618,7 +619,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
     auto strange = [&]() {
         int seen = 0;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) seen |= odd[i];
+        for (int i = 0; i < 4 + NS; ++i) seen |= odd[i];
         return __builtin_amdgcn_readfirstlane(seen) != 0;
     };
 
@@ -649,6 +650,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
             la += LC * ta_;
         };
         if (chunks) fetch_a(max(gap - t, 0));                 // (rows of the first chunk that are not there: the first that is)
+        float zero = 0.0f;                                    // NaN from an output on that is not finite
         for (int c = 0; c < chunks; ++c) {
             meet();
             const uint64_t here = cut_mask;
@@ -725,7 +727,10 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
                 const int64_t o = po + ((int64_t)c * LC + t) * to + 16 * g;
                 float v[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = O[j / 4][j % 4];
+                for (int j = 0; j < 16; ++j) {
+                    v[j] = O[j / 4][j % 4];
+                    zero = __builtin_fmaf(v[j], 0.0f, zero);
+                }
                 if (q.out_f32) {
                     float* f = (float*)q.out + o;
 #pragma unroll
@@ -751,6 +756,8 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
             qw = decay_pow(lg, t + 1 - back) * q.scale;
             meet();
         }
+        const bool any = __ballot(zero != 0.0f) != 0;
+        if (lane == 0) odd[w] = any;
         meet();
         if (strange())
             for (int64_t i = i0; i < i1; ++i) {
@@ -776,22 +783,6 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
     // the next tiles, and the state handed out
     auto hand_out = [&](auto first) {
         tiles.stage(0, first);
-        if constexpr (L::SPLIT) {
-            // (an infinity has no second part; a state that the chunk's first token ends may be anything)
-            if (tiles.cuts >> (decltype(first)::value ? gap : 0) & 1)
-#pragma unroll
-                for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) S[ta][d] = v4f{0, 0, 0, 0};
-            uint32_t most = 0;
-#pragma unroll
-            for (int ta = 0; ta < NA; ++ta)
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(S[ta][d][i]) & 0x7fffffffu);
-            tiles.odd |= __ballot(most >= 0x7f800000u) != 0;
-        }
         if (ws == 0 && lane == 0) cut_mask = tiles.cuts;
 #pragma unroll
         for (int ta = 0; ta < NA; ++ta) {
@@ -826,7 +817,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
             if (c + 2 < chunks) tiles.fetch(c + 2, std::false_type{});
         }
     }
-    if (lane == 0) odd[ws] = tiles.odd;
+    if (lane == 0) odd[w] = tiles.odd;
     meet();
     if (strange()) {
         la_state_in<NA, 4, 4, FULL>(q, seg, bh, 16 * NA * ws + 4 * g, y0, yr, X, yw, S);
@@ -858,7 +849,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     __shared__ __attribute__((aligned(16))) float sb[LC * L::BP];
     __shared__ __attribute__((aligned(16))) float sc[LC * L::CP];
     __shared__ __attribute__((aligned(16))) float ss[OUT ? DX * LY : 4];      // the state's fragments: [column tile][depth][lane][4]
-    __shared__ int odd[4];                                    // whether a wavefront has seen a NaN or an infinity in b or c
+    __shared__ int odd[4];                                    // whether a wavefront has seen a NaN or an infinity in b, c or an output
     __shared__ float red[4][LY];
 
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
@@ -905,6 +896,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     u32x4 vb[L::BV], vc[L::CV];
     uint32_t cut = 0;
     int seen = 0;                                             // a NaN or an infinity in b or c
+    float zero = 0.0f;                                        // NaN from an output on that is not finite
     auto fetch = [&](int c) {
         const int skip = c ? 0 : gap;
 #pragma unroll
@@ -1055,7 +1047,10 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
                     const int y = 16 * d + 4 * g;
                     v4f v = O[d];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] *= q.scale;
+                    for (int i = 0; i < 4; ++i) {
+                        v[i] *= q.scale;
+                        zero = __builtin_fmaf(v[i], 0.0f, zero);
+                    }
                     if (FULL || y + 4 <= yw) *(u32x4_at4*)(f + y) = __builtin_bit_cast(u32x4, v);
                     else
 #pragma unroll
@@ -1071,6 +1066,10 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
         if (more) { stage(c + 1); publish(); }
     }
 
+    if constexpr (OUT) {
+        const bool any = __ballot(zero != 0.0f) != 0;
+        seen |= any;
+    }
     if (lane == 0) odd[w] = seen;
     __syncthreads();
     if (odd[0] | odd[1] | odd[2] | odd[3]) {
