@@ -1472,20 +1472,16 @@ bool la_spread(const accerl_token_stride& s, int64_t B, int64_t T, int H, int D)
 }
 
 // What a call reads and writes, as runs of bytes.
-struct LaPlaces {
-    Strided q, k, v, log_decay, reset, lengths, state, out, out_state, grad_out, grad_out_state, grad_q, grad_k, grad_v, grad_state;
-    // (step: one token, and no lengths)
-    LaPlaces(const accerl_linear_attention_args& a, bool step)
-        : q(tokens(a, a.q, a.q_stride, a.H, a.Dk, step)), k(tokens(a, a.k, a.k_stride, a.Hk, a.Dk, step)), v(tokens(a, a.v, a.v_stride, a.Hk, a.Dv, step)),
-          log_decay(a.log_decay, 4 * (int64_t)a.H), reset(a.reset, a.B, a.reset_batch, step ? 1 : a.T, a.reset_token, 1, 0, 1), lengths(step ? nullptr : a.lengths, 4 * a.B),
-          state(states(a, a.state)), out(tokens(a, a.out, a.out_stride, a.H, a.Dv, step)), out_state(states(a, a.out_state)),
-          grad_out(tokens(a, a.grad_out, a.grad_out_stride, a.H, a.Dv, step)), grad_out_state(states(a, a.grad_out_state)), grad_q(tokens(a, a.grad_q, a.grad_q_stride, a.H, a.Dk, step)),
-          grad_k(tokens(a, a.grad_k, a.grad_k_stride, a.Hk, a.Dk, step)), grad_v(tokens(a, a.grad_v, a.grad_v_stride, a.Hk, a.Dv, step)), grad_state(states(a, a.grad_state)) {}
-    static Strided tokens(const accerl_linear_attention_args& a, const void* p, const accerl_token_stride& s, int H, int D, bool step) {
-        const int64_t e = dtype_bytes(a.dtype);
-        return Strided(p, a.B, s.batch * e, step ? 1 : a.T, s.token * e, H, s.head * e, D * e);
-    }
-    static Strided states(const accerl_linear_attention_args& a, const void* p) { return Strided(p, 4 * a.B * a.H * a.Dk * a.Dv); }
+Strided la_tokens_at(const accerl_linear_attention_args& a, const void* p, const accerl_token_stride& s, int H, int D, int64_t T) {
+    const int64_t e = dtype_bytes(a.dtype);
+    return Strided(p, a.B, s.batch * e, T, s.token * e, H, s.head * e, D * e);
+}
+Strided la_states_at(const accerl_linear_attention_args& a, const void* p) { return Strided(p, 4 * a.B * a.H * a.Dk * a.Dv); }
+struct LaInputs {
+    Strided q, k, v, log_decay, reset, lengths, state;
+    LaInputs(const accerl_linear_attention_args& a, int64_t T, const int32_t* lengths)
+        : q(la_tokens_at(a, a.q, a.q_stride, a.H, a.Dk, T)), k(la_tokens_at(a, a.k, a.k_stride, a.Hk, a.Dk, T)), v(la_tokens_at(a, a.v, a.v_stride, a.Hk, a.Dv, T)),
+          log_decay(a.log_decay, 4 * (int64_t)a.H), reset(a.reset, a.B, a.reset_batch, T, a.reset_token, 1, 0, 1), lengths(lengths, 4 * a.B), state(la_states_at(a, a.state)) {}
 };
 typedef std::initializer_list<const Strided*> LaList;
 bool la_any_share(LaList outs, LaList others) {
@@ -1494,10 +1490,10 @@ bool la_any_share(LaList outs, LaList others) {
     return false;
 }
 // an unroll's or a step's outputs; out_state may be the state
-int la_outputs_apart(const char* who, const accerl_linear_attention_args* a, const LaPlaces& at) {
-    if (la_any_share({&at.out, &at.out_state}, {&at.q, &at.k, &at.v, &at.log_decay, &at.reset, &at.lengths})) return la_fail(ACCERL_EINVAL, who, "an output overlaps an input");
-    if (la_any_share({&at.out}, {&at.state, &at.out_state})) return la_fail(ACCERL_EINVAL, who, "out overlaps a state");
-    if (a->out_state != a->state && share(at.out_state, at.state)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
+int la_outputs_apart(const char* who, const accerl_linear_attention_args* a, const LaInputs& in, const Strided& out, const Strided& out_state) {
+    if (la_any_share({&out, &out_state}, {&in.q, &in.k, &in.v, &in.log_decay, &in.reset, &in.lengths})) return la_fail(ACCERL_EINVAL, who, "an output overlaps an input");
+    if (la_any_share({&out}, {&in.state, &out_state})) return la_fail(ACCERL_EINVAL, who, "out overlaps a state");
+    if (a->out_state != a->state && share(out_state, in.state)) return la_fail(ACCERL_EINVAL, who, "out_state overlaps the state other than being it");
     return ACCERL_OK;
 }
 
@@ -1542,10 +1538,11 @@ int accerl_linear_attention(const accerl_linear_attention_args* a, void* stream)
     if (a->T > 0 && (!a->out || !la_aligned(a->out, e))) return la_fail(ACCERL_EINVAL, who, "out is NULL or misaligned");
     if (a->T > 0 && !la_spread(a->out_stride, a->B, a->T, a->H, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of the output overlap");
     if (!la_state_ok(a->state) || !la_state_ok(a->out_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
-    const LaPlaces at(*a, false);
-    if (int rc = la_outputs_apart(who, a, at)) return rc;
+    const LaInputs in(*a, a->T, a->lengths);
+    const Strided out = la_tokens_at(*a, a->out, a->out_stride, a->H, a->Dv, a->T), out_state = la_states_at(*a, a->out_state);
+    if (int rc = la_outputs_apart(who, a, in, out, out_state)) return rc;
     const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, false, a->dtype == ACCERL_DT_F32);
-    if (int rc = la_workspace(who, a, k, {&at.q, &at.k, &at.v, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.out, &at.out_state})) return rc;
+    if (int rc = la_workspace(who, a, k, {&in.q, &in.k, &in.v, &in.log_decay, &in.reset, &in.lengths, &in.state, &out, &out_state})) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_forward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
     if (a->dtype == ACCERL_DT_BF16) return la_forward<BF16>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1566,14 +1563,15 @@ int accerl_linear_attention_grad(const accerl_linear_attention_args* a, void* st
     }
     if (!la_state_ok(a->state) || !la_state_ok(a->grad_out_state) || !la_state_ok(a->grad_state)) return la_fail(ACCERL_EINVAL, who, "states must be 16-byte aligned");
     if (a->H != a->Hk && la_fold_items(*a) > MAX_LAUNCH_ITEMS - 256) return la_fail(ACCERL_EUNSUPPORTED, who, "more gradients of shared heads than one launch takes");
-    const LaPlaces at(*a, false);
-    if (la_any_share({&at.grad_q, &at.grad_k, &at.grad_v, &at.grad_state}, {&at.q, &at.k, &at.v, &at.grad_out, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.grad_out_state}))
+    const LaInputs in(*a, a->T, a->lengths);
+    const Strided go = la_tokens_at(*a, a->grad_out, a->grad_out_stride, a->H, a->Dv, a->T), gs = la_states_at(*a, a->grad_out_state);
+    const Strided gq = la_tokens_at(*a, a->grad_q, a->grad_q_stride, a->H, a->Dk, a->T), gk = la_tokens_at(*a, a->grad_k, a->grad_k_stride, a->Hk, a->Dk, a->T);
+    const Strided gv = la_tokens_at(*a, a->grad_v, a->grad_v_stride, a->Hk, a->Dv, a->T), gstate = la_states_at(*a, a->grad_state);
+    if (la_any_share({&gq, &gk, &gv, &gstate}, {&in.q, &in.k, &in.v, &go, &in.log_decay, &in.reset, &in.lengths, &in.state, &gs}))
         return la_fail(ACCERL_EINVAL, who, "a gradient overlaps an input");
-    if (la_any_share({&at.grad_q}, {&at.grad_k, &at.grad_v, &at.grad_state}) || la_any_share({&at.grad_k}, {&at.grad_v, &at.grad_state}) || share(at.grad_v, at.grad_state))
-        return la_fail(ACCERL_EINVAL, who, "two gradients overlap");
+    if (la_any_share({&gq}, {&gk, &gv, &gstate}) || la_any_share({&gk}, {&gv, &gstate}) || share(gv, gstate)) return la_fail(ACCERL_EINVAL, who, "two gradients overlap");
     const LaWork k = la_work(a->B, a->T, a->H, a->Hk, a->Dk, a->Dv, true, a->dtype == ACCERL_DT_F32);
-    if (int rc = la_workspace(who, a, k, {&at.q, &at.k, &at.v, &at.grad_out, &at.log_decay, &at.reset, &at.lengths, &at.state, &at.grad_out_state, &at.grad_q, &at.grad_k, &at.grad_v,
-                                          &at.grad_state})) return rc;
+    if (int rc = la_workspace(who, a, k, {&in.q, &in.k, &in.v, &go, &in.log_decay, &in.reset, &in.lengths, &in.state, &gs, &gq, &gk, &gv, &gstate})) return rc;
     const LaParams p = la_params(a, k.plan);
     if (a->dtype == ACCERL_DT_F32) return la_backward<float>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
     if (a->dtype == ACCERL_DT_BF16) return la_backward<BF16>(who, *a, p, k, (float*)a->workspace, (hipStream_t)stream);
@@ -1589,7 +1587,7 @@ int accerl_linear_attention_step(const accerl_linear_attention_args* a, void* st
     if (!a->out || !la_aligned(a->out, e)) return la_fail(ACCERL_EINVAL, who, "out is NULL or misaligned");
     if (!la_spread({a->out_stride.batch, 0, a->out_stride.head}, a->B, 1, a->H, a->Dv)) return la_fail(ACCERL_EINVAL, who, "heads of the output overlap");
     if (!a->state || !a->out_state || !la_state_ok(a->state) || !la_state_ok(a->out_state)) return la_fail(ACCERL_EINVAL, who, "a state is NULL or not 16-byte aligned");
-    if (int rc = la_outputs_apart(who, a, LaPlaces(*a, true))) return rc;
+    if (int rc = la_outputs_apart(who, a, LaInputs(*a, 1, nullptr), la_tokens_at(*a, a->out, a->out_stride, a->H, a->Dv, 1), la_states_at(*a, a->out_state))) return rc;
     LaStep p{};
     const int share = a->H / a->Hk;
     p.q = la_side(a->q, a->q_stride, 1); p.k = la_side(a->k, a->k_stride, share); p.v = la_side(a->v, a->v_stride, share);
