@@ -33,7 +33,7 @@ struct LaRole {
     int64_t ob, ot, oh;
     const float* enter;                   // the state before the first token of a segment, or NULL (zeros)
     float* last;                          // the state behind the last one, or NULL
-    float* keep;                          // what is left of a segment's first state behind it, [segment][B H] (sums only)
+    float* keep;                          // what is left of a segment's first state behind it, [segment][B H] (sums only); CUT: an episode ends in between
     int64_t ex, ey, lx, ly;               // strides of x and y in both
     int64_t eseg, lseg;                   // from one segment's states to the next one's
     int X, Y, slices;
@@ -53,6 +53,7 @@ struct LaParams {
     uint32_t groups;                      // B H segs
 };
 
+constexpr float CUT = -1.0f;
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 // g^n of lg = log2 g, which may be -inf
 __device__ __forceinline__ float decay_pow(float lg, int n) { return n == 0 ? 1.0f : pow2(lg * (float)n); }
@@ -522,6 +523,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2
         for (int d = 0; d < ND; ++d) S[ta][d] = v4f{0, 0, 0, 0};
     LaTail tail(lg, back, q.pair, g);
     float sd = everywhere(decay_pow(lg, LC - gap)), left = 1.0f;              // (the first chunk's); what is left of a state before the segment
+    bool ends = false;                                        // whether an episode does in it
     LaTiles<T, DX, L::YW, NW, HOW> tiles(p, q, sb, sc, L::BT, L::PARTS * L::CT, pb, pc, tb, tc, X, yw, gap, tid);
     tiles.at(b, n, i0, base0, back);
     const int down_b = (4 * g + (r >> 2)) * L::BP + 4 * (r & 3) + 16 * NA * w, down_c = (4 * g + (r >> 2)) * L::CP + 16 * (r & 3);
@@ -543,7 +545,8 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2
             if (c + 1 < chunks) tiles.fetch(c + 1, std::false_type{});
         }
         la_state_on<T, L, NA, ND, 3>(here, sd, tail, sb + now * L::BT + down_b, sc + now * L::PARTS * L::CT + down_c, g, S);
-        left = here ? 0.0f : left * sd;
+        left *= sd;
+        ends |= here != 0;
         sd = everywhere(decay_pow(lg, LC));
         if constexpr (NB == 1) {
             __syncthreads();
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2
     // backwards the state that enters the unroll has no gradient if its first token resets
     const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
     la_state_out<NA, ND, 4, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, yr, X, yw, gone, S);
-    if (at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = gone ? 0.0f : left;
+    if (at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = gone || ends ? CUT : left;
 }
 
 // The mixing itself.  Four wavefronts work out the outputs of a chunk, 16 tokens by 64 columns each, from the tiles and the state before it, while the others bring the
@@ -890,6 +893,7 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     for (int st = 0; st < 3; ++st) far[st] = decay_pow(lg, max(16 * (w - st) - 15, 0));
     float qw = decay_pow(lg, max(t - gap, 0) + 1 - back), sd = decay_pow(lg, LC - gap);      // (the first chunk's)
     float left = 1.0f;                                        // of the segment's first state
+    bool ends = false;                                        // whether an episode does in the segment
 
     const int brow = tid / (DX / 4), bcol = tid % (DX / 4) * 4, crow = tid / (LY / 4), ccol = tid % (LY / 4) * 4;
     constexpr int BR = 1024 / DX, CR = 1024 / LY;             // rows from one vector of a lane to its next
@@ -1059,7 +1063,8 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
             }
         }
 
-        left = cuts ? 0.0f : left * sd;
+        left *= sd;
+        ends |= cuts != 0;
         qw = decay_pow(lg, t + 1 - back);
         sd = decay_pow(lg, LC);
         __syncthreads();
@@ -1084,9 +1089,8 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
     }
     if (q.last) {
         const bool gone = back && seg == p.segs - 1 && n > 0 && p.reset && p.reset[b * p.rb] != 0;
-        if (gone) left = 0.0f;
         la_state_out<NA, 4, 16, FULL>(q, seg, bh, 16 * NA * w + 4 * g, y0, r, X, yw, gone, S);
-        if (q.keep && at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = left;
+        if (q.keep && at.slice == 0 && tid == 0) q.keep[(int64_t)seg * (p.groups / p.segs) + bh] = gone || ends ? CUT : left;
     }
     if constexpr (OUT) la_behind<float, 4>(p, q, at, n, i0, y0, yw);
 }
@@ -1094,13 +1098,15 @@ __global__ __launch_bounds__(256, DX == 64 ? 2 : 1) void la_float_kernel(const L
 // The states that enter the segments, from what each segment adds: states [segment][B H][X Y] in place, the last one to `last`.
 // Bound by memory and by the chain of the segments (64 segments of 16 heads of 128 x 128: 12 us for 67 MB read and written).
 struct LaJoin { float* states; const float* keep; const float* enter; float* last; };
-struct LaJoinParams { LaJoin at[2]; int64_t n, per; int segs; };               // n = B H X Y, per = X Y
+struct LaJoinParams { LaJoin at[2]; const float* log_decay; int64_t n, per; int H, segs; };     // n = B H X Y, per = X Y
 __global__ __launch_bounds__(256) void la_join_kernel(const LaJoinParams p) {
     const LaJoin& j = p.at[blockIdx.y];
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= p.n) return;
     const int64_t bh = i / p.per, all = p.n / p.per;
     float e = j.enter ? j.enter[i] : 0.0f;
+    // (an infinity stays one under any decay but 0, which makes it NaN, also where the power is 0 in fp32)
+    const float stays = p.log_decay[bh % p.H] == -INFINITY ? 0.0f : 1.0f;
     constexpr int AT_ONCE = 8;                                // loads under way together
     for (int s0 = 0; s0 < p.segs; s0 += AT_ONCE) {
         float add[AT_ONCE], f[AT_ONCE];
@@ -1114,7 +1120,8 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaJoinParams p) {
         for (int k = 0; k < AT_ONCE; ++k)
             if (s0 + k < p.segs) {
                 j.states[(s0 + k) * p.n + i] = e;
-                e = (f[k] == 0.0f ? 0.0f : f[k] * e) + add[k];
+                const float on = f[k] > 0.0f ? f[k] * e : isfinite(e) ? 0.0f : e * stays;
+                e = (f[k] == CUT ? 0.0f : on) + add[k];
             }
     }
     if (j.last) j.last[i] = e;
@@ -1370,7 +1377,7 @@ int la_forward(const char* who, const accerl_linear_attention_args& a, LaParams 
         if (int rc = la_run<T, false>(who, p, &sum, 1, s)) return rc;
         LaJoinParams j{};
         j.at[0] = {ws, ws + k.states, a.state, a.out_state};
-        j.n = n; j.per = per; j.segs = p.segs;
+        j.log_decay = p.log_decay; j.n = n; j.per = per; j.H = p.H; j.segs = p.segs;
         la_join_kernel<<<dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s>>>(j);
         if (int rc = la_launched(who)) return rc;
         r.enter = ws; r.eseg = n;
@@ -1407,7 +1414,7 @@ int la_backward(const char* who, const accerl_linear_attention_args& a, LaParams
         LaJoinParams j{};
         j.at[0] = {S, keep, a.state, nullptr};
         j.at[1] = {R, keep_back, a.grad_out_state, a.grad_state};
-        j.n = n; j.per = per; j.segs = p.segs;
+        j.log_decay = p.log_decay; j.n = n; j.per = per; j.H = p.H; j.segs = p.segs;
         la_join_kernel<<<dim3((uint32_t)((n + 255) / 256), 2), dim3(256), 0, s>>>(j);
         if (int rc = la_launched(who)) return rc;
         rq.enter = S; rk.enter = rv.enter = R;

@@ -70,3 +70,19 @@ def test_a_product_past_the_range_that_no_result_holds(A, dtype, early, late, de
     for name, (got, want) in both(A, a, decay, go).items():
         state = "state" in name
         check(name, got, want, ref.unroll_tolerance(want, sizes[name], dtype, T, max(D, E), np.array(decay), state=state))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [150, 700, 2000])
+@pytest.mark.parametrize("which", ["k", "v", "state"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("decay", [[0.1, 0.9], [0.0, 0.9]])
+def test_no_decay_ends_what_is_not_finite(A, dtype, T, which, what, decay):
+    """Between episodes' borders it goes on to the last token, also where a chunk's or a segment's decay is below what fp32 holds (0.1^64)."""
+    a = make(1, T, 2, 2, 48, 72, dtype)
+    if which == "state":
+        a["state"][0, 0, 5, 3] = what
+    else:
+        a[which][0, 37, 0, 5] = what
+    go = torch.randn((1, T, 2, 72), device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(DT[dtype])
+    alike(both(A, a, decay, go))
