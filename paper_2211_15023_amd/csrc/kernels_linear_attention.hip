@@ -1200,11 +1200,11 @@ __global__ __launch_bounds__(256, ROWS <= 4 ? 8 : ROWS == 8 ? 6 : 4) void la_ste
     for (int i = 0; i < ROWS; ++i) {
         const float kx = el_f32(k[i]), qx = el_f32(q[i]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            S[i][j] = ge * S[i][j] + kx * v[j];
-            o[j] += qx * S[i][j];
-        }
+        for (int j = 0; j < 4; ++j) S[i][j] = ge * S[i][j] + kx * v[j];
+        // (a row that is not there has no part in the output: an infinity of v times its key of 0 would be NaN)
         if (FULL || x0 + 16 * i < X) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] += qx * S[i][j];
             if constexpr (FULL && ONCE) __builtin_nontemporal_store(S[i], (v4f*)(so + i * rows16));
             else if (in == 4) *(u32x4_at4*)(so + i * rows16) = __builtin_bit_cast(u32x4, S[i]);
             else

@@ -86,3 +86,20 @@ def test_no_decay_ends_what_is_not_finite(A, dtype, T, which, what, decay):
         a[which][0, 37, 0, 5] = what
     go = torch.randn((1, T, 2, 72), device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(DT[dtype])
     alike(both(A, a, decay, go))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("Dk,Dv", [(1, 1), (17, 5), (33, 64), (40, 70), (64, 64), (100, 128), (130, 20), (256, 256)])
+@pytest.mark.parametrize("which", ["q", "k", "v"])
+def test_a_step_of_an_infinity(A, dtype, Dk, Dv, which):
+    """Everything positive, so that each sum that meets it is an infinity."""
+    B, H = 2, 2
+    g = torch.Generator(device="cuda").manual_seed(Dk)
+    draw = lambda *s: (torch.rand(s, generator=g, device="cuda") + 0.5)
+    x = dict(q=draw(B, H, Dk).to(DT[dtype]), k=draw(B, H, Dk).to(DT[dtype]), v=draw(B, H, Dv).to(DT[dtype]))
+    x[which][0, 1, -1] = float("inf")
+    state = draw(B, H, Dk, Dv)
+    beside = torch.empty_like(state)
+    out = A.LinearAttention([0.9, 0.5]).step(**x, state=state, out_state=beside)
+    o, s = ref.unroll(*(wide(x[n])[:, None] for n in "qkv"), np.array([0.9, 0.5]), 1.0, state=wide(state))
+    alike({"out": (out, o[:, 0]), "state": (beside, s)})
