@@ -476,8 +476,8 @@ typedef enum { ACCERL_GATE_NONE = 0, ACCERL_GATE_SIGMOID = 1, ACCERL_GATE_SILU =
  * groups is 1.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the gate.  1 <= D <= 16384.
  * y, gate, h and their gradients have `dtype`; x, u and theirs `stream_dtype`, which is `dtype` or fp32.  Weights and their
  * gradients are DEVICE fp32 [D].  Arithmetic is fp32; h is taken from u before u is rounded; results are rounded once.  Rows do not
- * touch each other: a NaN stays in its row (and in the weights' gradients).  An output may lie over an input of the same type and stride, whole, and
- * overlaps nothing else.
+ * touch each other: a NaN stays in its row (and in the weights' gradients).  Rows of an output may lie over rows of an input of the same type and stride, whole, and a
+ * weight's gradient over a weight; outputs and the workspace overlap nothing else (ACCERL_EINVAL).
  * Gradients: of sum(grad_u . u) + sum(grad_h . h), by y, x, gate and both weights (a pointer of NULL: not wanted; grad_u or grad_h NULL: zeros).
  * They start from the forward's inputs: nothing is kept from the forward.  The weights' sums over rows have a fixed order.
  * workspace: of accerl_block_norm_workspace's bytes, needed where gradients of weights are asked for; used as accerl_dense_i8_dynamic's.

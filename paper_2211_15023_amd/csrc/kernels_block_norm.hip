@@ -461,7 +461,25 @@ int bn_check(const char* who, const accerl_block_norm_args* a, const NormTable* 
             if (!over && share(table(o.p, a->N, o.ld, a->D, e[o.stream]), table(t.p, a->N, t.ld, a->D, e[t.stream])))
                 return bn_fail(ACCERL_EINVAL, who, "an output overlaps an input (other than lying over it) or another output");
         }
+    for (int i = 0; i < count; ++i) {
+        const Table o = table(tables[i].p, a->N, tables[i].ld, a->D, e[tables[i].stream]);
+        if (tables[i].out && o.at && (share(o, table(a->after, 4 * (int64_t)a->D)) || share(o, table(a->before, 4 * (int64_t)a->D)))) return bn_fail(ACCERL_EINVAL, who, "an output overlaps a weight");
+    }
     return ACCERL_OK;
+}
+// what the weights' gradients and the workspace (of `used` bytes) may lie over: a weight, whole, and nothing
+int bn_apart(const char* who, const accerl_block_norm_args& a, const NormTable* tables, int count, int64_t used) {
+    const int64_t bytes = 4 * (int64_t)a.D;
+    const Table work = table(a.workspace, used), after = table(a.after, bytes), before = table(a.before, bytes), grad_after = table(a.grad_after, bytes), grad_before = table(a.grad_before, bytes);
+    for (const Table& g : {grad_after, grad_before}) {
+        for (const Table& w : {after, before}) if (g.at != w.at && share(g, w)) return bn_fail(ACCERL_EINVAL, who, "a weight's gradient overlaps a weight (other than lying over it)");
+        for (int i = 0; i < count; ++i)
+            if (tables[i].p && share(g, table(tables[i].p, a.N, tables[i].ld, a.D, dtype_bytes(tables[i].stream ? a.stream_dtype : a.dtype)))) return bn_fail(ACCERL_EINVAL, who, "a weight's gradient overlaps rows");
+    }
+    if (share(grad_after, grad_before)) return bn_fail(ACCERL_EINVAL, who, "the weights' gradients overlap");
+    bool over = share(work, after) || share(work, before) || share(work, grad_after) || share(work, grad_before);
+    for (int i = 0; i < count; ++i) over = over || (tables[i].p && share(work, table(tables[i].p, a.N, tables[i].ld, a.D, dtype_bytes(tables[i].stream ? a.stream_dtype : a.dtype))));
+    return over ? bn_fail(ACCERL_EINVAL, who, "the workspace overlaps an input or an output") : ACCERL_OK;
 }
 NormParams bn_params(const accerl_block_norm_args& a, const NormShape& s) {
     NormParams p{};
@@ -530,6 +548,7 @@ int accerl_block_norm_grad(const accerl_block_norm_args* a, void* stream) {
     if (sums) {
         if (!ws || !bn_aligned(ws, 16)) return bn_fail(ACCERL_EINVAL, who, "workspace is NULL or misaligned");
         if (a->workspace_bytes < 8 * part) return bn_fail(ACCERL_EINVAL, who, "workspace smaller than accerl_block_norm_workspace says");
+        if (int rc = bn_apart(who, *a, t, 8, 8 * part)) return rc;
     }
     if (done && !sums) return ACCERL_OK;
     NormParams p = bn_params(*a, s);

@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from tests.test_memory_ops_cpu import EINVAL, attention_args
+from tests.test_memory_ops_cpu import EINVAL, attention_args, norm_args
 from tests.test_wide_ops_cpu import aligned
 
 SOURCE = r"""
@@ -143,3 +143,40 @@ def test_a_step_of_wide_heads_over_its_tokens(A):
     for n in "qkv":
         a = attention_args(p, **dict(good, out=good[n]))
         assert A.load_library().accerl_linear_attention_step(C.byref(a), None) == EINVAL and "overlap" in A.accerl_last_error()
+
+
+# ------------------------------------------------------------------ norms: places of norm_args (3 rows of 20: y 0, x 1024, gate 2048, out_u 4096, out_h 5120, grad_u 6144, grad_h 7168,
+# grad_y 8192, grad_x 9216, grad_gate 10240, grad_after 11264, grad_before 12288), the weights and the workspace apart
+NORM = dict(after=16384, before=17408, workspace=32768)
+
+
+def _norm_refused(A, name, **change):
+    p, own = aligned(1 << 17)
+    a = norm_args(p, workspace_bytes=1 << 16, **{k: p + v for k, v in {**NORM, **change}.items()})
+    assert getattr(A.load_library(), "accerl_" + name)(C.byref(a), None) == EINVAL
+    return A.accerl_last_error()
+
+
+@pytest.mark.parametrize("which", ["after", "before"])
+@pytest.mark.parametrize("at", [4096, 4096 + 160, 5120, 5120 + 40])
+def test_norms_over_their_weights(A, which, at):
+    assert "overlaps" in _norm_refused(A, "block_norm", **{which: at})
+
+
+@pytest.mark.parametrize("which", ["after", "before"])
+@pytest.mark.parametrize("at", [8192, 8192 + 116, 9216, 9216 + 236, 10240])
+def test_gradients_of_norms_over_the_weights(A, which, at):
+    assert "overlaps" in _norm_refused(A, "block_norm_grad", **{which: at})
+
+
+@pytest.mark.parametrize("which,own", [("grad_after", 11264), ("grad_before", 12288)])
+@pytest.mark.parametrize("at", [0, 1024, 2048 + 40, 6144, 7168, 8192, 9216 + 80, 10240, 11264, 11264 + 76, 12288, 12288 - 4, 16384 + 4, 17408 - 4])
+def test_weights_gradients_over_rows_and_weights_in_part(A, which, own, at):
+    if at in (own, {"grad_after": 11264 + 76, "grad_before": 12288 - 4}[which]):
+        pytest.skip("free")
+    assert "overlap" in _norm_refused(A, "block_norm_grad", **{which: at})
+
+
+@pytest.mark.parametrize("at", [0, 1024, 2048, 6144, 7168, 8192, 9216, 10240, 11264, 12288, 16384, 17408])
+def test_a_norms_workspace_over_what_a_call_has(A, at):
+    assert "workspace" in _norm_refused(A, "block_norm_grad", workspace=at)
