@@ -473,7 +473,7 @@ typedef enum { ACCERL_GATE_NONE = 0, ACCERL_GATE_SIGMOID = 1, ACCERL_GATE_SILU =
  *     u = skip x + branch act(gate) after(y),    h = before(u)
  *     norm(z)_i = weight_i (z_i - m) / sqrt(mean_j (z_j - m)^2 + eps),    m = 0 (RMS) or mean_j z_j (LAYER)
  * `after` works on each of `groups` equal parts of a row by itself (the heads of an attention); `before` on the whole row, and with it
- * groups is 1.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the gate.  1 <= D <= 16384.
+ * groups is 1.  eps is positive, 2^-126 at least.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the gate.  1 <= D <= 16384.
  * y, gate, h and their gradients have `dtype`; x, u and theirs `stream_dtype`, which is `dtype` or fp32.  Weights and their
  * gradients are DEVICE fp32 [D].  Arithmetic is fp32; h is taken from u before u is rounded; results are rounded once.  Rows do not
  * touch each other: a NaN stays in its row (and in the weights' gradients).  Rows of an output may lie over rows of an input of the same type and stride, whole, and a

@@ -5,6 +5,7 @@
 // 4.9), gradients of 32768 x 4096 bf16 463 (4.6; two sums over the row in each direction lie between a row's loads and its stores).  Rows of up to 1024 elements
 // (gradients and few rows: 512) belong to a part of a wavefront or to a whole one, longer rows to a workgroup.
 #include <algorithm>
+#include <cfloat>
 #include <cstdio>
 
 #include "wide_ops.h"
@@ -446,7 +447,7 @@ int bn_check(const char* who, const accerl_block_norm_args* a, const NormTable* 
     if (!dtype_known(a->dtype) || (a->stream_dtype != a->dtype && a->stream_dtype != ACCERL_DT_F32)) return bn_fail(ACCERL_EINVAL, who, "unknown types, or a residual stream that is neither of the rows' type nor fp32");
     if (a->kind < ACCERL_NORM_RMS || a->kind > ACCERL_NORM_LAYER || a->gate_kind < ACCERL_GATE_NONE || a->gate_kind > ACCERL_GATE_SILU) return bn_fail(ACCERL_EINVAL, who, "unknown kind of norm or gate");
     if (a->groups > 1 && a->before) return bn_fail(ACCERL_EINVAL, who, "groups are for calls without the norm before the next block");
-    if (!(a->eps > 0.0 && a->eps < 1e30) || !(a->skip > -1e30 && a->skip < 1e30) || !(a->branch > -1e30 && a->branch < 1e30)) return bn_fail(ACCERL_EINVAL, who, "eps must be positive, skip and branch finite");
+    if (!(a->eps >= FLT_MIN && a->eps < 1e30) || !(a->skip > -1e30 && a->skip < 1e30) || !(a->branch > -1e30 && a->branch < 1e30)) return bn_fail(ACCERL_EINVAL, who, "eps must be positive and normal in fp32, skip and branch finite");
     for (int i = 0; i < count; ++i) if (tables[i].p && tables[i].ld < a->D) return bn_fail(ACCERL_EINVAL, who, "rows overlap (stride < D)");
     if (a->N == 0) { *done = true; return ACCERL_OK; }
     if (!a->y || (a->gate_kind && !a->gate)) return bn_fail(ACCERL_EINVAL, who, "y or the gate is NULL");
