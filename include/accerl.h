@@ -420,9 +420,9 @@ int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
  * Tensors of tokens are [B, T, heads, D] with strides (elements) of their own for batch, token and head, of any alignment of whole elements;
  * elements of a head are contiguous: time-major tensors and parts of wider rows are taken as they are.  States are DEVICE fp32 [B, H, Dk, Dv], dense, 16-byte
  * aligned.  1 <= Dk, Dv <= 256.  log_decay holds numbers <= 0 or -inf.  State and sums are fp32.  With bf16 tokens the weights of
- * pairs of tokens and the state's copy that queries are multiplied with are rounded to bf16, as their partners are (fp16 tokens: to two bf16 parts,
- * 2^-17).  A state that is handed out, and those that segments of a long unroll hand on, are as exact as fp32; inside an unroll whose last state is
- * not wanted a key or value times its decay is held to 2^-17.
+ * pairs of tokens and the state's copy that queries are multiplied with are rounded to bf16, as their partners are (fp16 tokens: both go through two bf16
+ * parts each, and a term is 2^-15 off at most).  A state that is handed out, and those that segments of a long unroll hand on, are as exact as fp32; inside an unroll
+ * whose last state is not wanted a key or value times its decay is held to 2^-16 (fp16: 2^-15).
  * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others.
  * out_state may be the state; otherwise outputs overlap neither inputs nor each other, and the workspace overlaps nothing (ACCERL_EINVAL, also of columns of one buffer's rows).
  */

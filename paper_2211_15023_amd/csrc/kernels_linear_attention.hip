@@ -220,7 +220,7 @@ template <typename T, int NW> __device__ __forceinline__ void la_behind(const La
 
 // ---------------------------------------------------------------- tokens of 16 bits
 // bf16 tokens are operands as they are.  fp16 tokens are split into two bf16 parts where fp16 could not hold what they meet (weights of pairs, the state: any
-// size), and the first and second order products taken.
+// size), and the first and second order products taken: the product of both second parts, 2^-16 of a term at most, is left out, and a second part is 2^-17 off.
 template <typename T, int DX, int NW>
 struct LaHalf {
     static constexpr bool SPLIT = __is_same(T, F16);
@@ -235,25 +235,37 @@ struct LaHalf {
 
 __device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 __device__ __forceinline__ float cut16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-// eight values as the sum of N bf16 parts, each cut off behind 8 bits (N = 3: exactly) and the last of two rounded
-template <int N> __device__ __forceinline__ void parts8(const float* x, v8bf* to) {
+// a and b rounded to bf16, which are taken off them
+__device__ __forceinline__ uint32_t part_pair(float& a, float& b) {
+    const uint32_t p = f32_pair<BF16>(a, b);
+    a -= __uint_as_float(p << 16);
+    b -= __uint_as_float(p & 0xffff0000u);
+    return p;
+}
+// Eight values as the sum of N bf16 parts.  NEAREST: each rounded, 2^-8 of the one before at most, so that two are 2^-17 off.  Else each but the second of two is cut off
+// behind 8 bits, which costs less (64 x 512 tokens, 16 heads of 128, bf16: 162 us, 167 rounded; their gradients 219 and 228), and two are 2^-16 off.  Three hold all 24 bits.
+template <int N, bool NEAREST> __device__ __forceinline__ void parts8(const float* x, v8bf* to) {
     u32x4 p[N];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float a = x[2 * j], b = x[2 * j + 1];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            p[k][j] = k == 1 && N == 2 ? f32_pair<BF16>(a, b) : high_halves(a, b);
-            a -= cut16(a);
-            b -= cut16(b);
+            if constexpr (NEAREST) {
+                p[k][j] = part_pair(a, b);
+            } else {
+                p[k][j] = k == 1 && N == 2 ? f32_pair<BF16>(a, b) : high_halves(a, b);
+                a -= cut16(a);
+                b -= cut16(b);
+            }
         }
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) to[k] = __builtin_bit_cast(v8bf, p[k]);
 }
-// the same rounded to nearest: one part or two
-template <int N> __device__ __forceinline__ void rounded8(const float* x, v8bf* to) {
-    if constexpr (N == 2) parts8<2>(x, to);
+// one part, rounded, or more
+template <int N, bool NEAREST> __device__ __forceinline__ void rounded8(const float* x, v8bf* to) {
+    if constexpr (N > 1) parts8<N, NEAREST>(x, to);
     else to[0] = __builtin_bit_cast(v8bf, u32x4{f32_pair<BF16>(x[0], x[1]), f32_pair<BF16>(x[2], x[3]), f32_pair<BF16>(x[4], x[5]), f32_pair<BF16>(x[6], x[7])});
 }
 template <typename T> __device__ __forceinline__ void unpack8(u32x4 w, float* x) {
@@ -373,7 +385,7 @@ struct LaTiles {
                 float x[8];
                 v8bf part[2];
                 unpack8<T>(vc[k], x);
-                parts8<2>(x, part);
+                parts8<2, true>(x, part);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const u32x4 v = __builtin_bit_cast(u32x4, part[j]);
@@ -440,8 +452,7 @@ __device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, 
                 unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= k8[j];
-                if constexpr (TERMS == 3) parts8<3>(x, fb);
-                else rounded8<TERMS>(x, fb);
+                rounded8<TERMS, L::SPLIT>(x, fb);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
                     if constexpr (TERMS == 3) S[ta][d] = mma(fb[2], fc[d][0], S[ta][d]);
@@ -460,8 +471,7 @@ __device__ __forceinline__ void la_state_on(uint64_t here, float sd, LaTail& t, 
                 unpack8<T>(down32(down_b + 32 * ks * L::BP + 16 * ta, 16 * L::BP), x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= k8[j];
-                if constexpr (TERMS == 3) parts8<3>(x, fb[ta]);
-                else rounded8<TERMS>(x, fb[ta]);
+                rounded8<TERMS, L::SPLIT>(x, fb[ta]);
             }
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
@@ -667,7 +677,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
                 if constexpr (L::SPLIT) {
                     float x[8];
                     unpack8<T>(va[k], x);
-                    parts8<2>(x, fa);
+                    parts8<2, true>(x, fa);
                 } else {
                     fa[0] = __builtin_bit_cast(v8bf, va[k]);
                 }
@@ -713,7 +723,7 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
                 if (2 * ks <= w) {
                     v8bf pt[L::PARTS];                    // weights of pairs as the product with c reads them
                     const float x[8] = {P[2 * ks][0], P[2 * ks][1], P[2 * ks][2], P[2 * ks][3], P[2 * ks + 1][0], P[2 * ks + 1][1], P[2 * ks + 1][2], P[2 * ks + 1][3]};
-                    rounded8<L::PARTS>(x, pt);
+                    rounded8<L::PARTS, true>(x, pt);
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
                         v8bf fc[L::PARTS];
@@ -795,8 +805,9 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
                 uint16_t* o = ss + ((d * L::KX + (tile >> 1)) * 64 + 16 * (quad >> 1) + r) * 8 + 4 * (quad & 1);
                 const v4f s = S[ta][d];
                 if constexpr (L::SPLIT) {
-                    *(u32x2*)o = u32x2{high_halves(s[0], s[1]), high_halves(s[2], s[3])};
-                    *(u32x2*)(o + L::SF) = u32x2{f32_pair<BF16>(s[0] - cut16(s[0]), s[1] - cut16(s[1])), f32_pair<BF16>(s[2] - cut16(s[2]), s[3] - cut16(s[3]))};
+                    float x[4] = {s[0], s[1], s[2], s[3]};
+                    *(u32x2*)o = u32x2{part_pair(x[0], x[1]), part_pair(x[2], x[3])};
+                    *(u32x2*)(o + L::SF) = u32x2{f32_pair<BF16>(x[0], x[1]), f32_pair<BF16>(x[2], x[3])};
                 } else {
                     *(u32x2*)o = u32x2{f32_pair<BF16>(s[0], s[1]), f32_pair<BF16>(s[2], s[3])};
                 }
