@@ -423,8 +423,10 @@ int accerl_policy_loss(const accerl_policy_loss_args* args, void* stream);
  * pairs of tokens and the state's copy that queries are multiplied with are rounded to bf16, as their partners are (fp16 tokens: both go through two bf16
  * parts each, and a term is 2^-15 off at most).  A state that is handed out, and those that segments of a long unroll hand on, are as exact as fp32; inside an unroll
  * whose last state is not wanted a key or value times its decay is held to 2^-16 (fp16: 2^-15).
- * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others.
- * out_state may be the state; otherwise outputs overlap neither inputs nor each other, and the workspace overlaps nothing (ACCERL_EINVAL, also of columns of one buffer's rows).
+ * A NaN or an infinity of a key or a value reaches the tokens behind it, of its episode and head, and no others; results that are not finite are those of
+ * the recurrence in fp32, token by token.
+ * out_state may be the state; otherwise outputs overlap neither inputs nor each other, and the workspace overlaps nothing (ACCERL_EINVAL; columns of
+ * one buffer's rows that lie beside each other do not).
  */
 typedef struct { int64_t batch, token, head; } accerl_token_stride;
 
@@ -473,11 +475,13 @@ typedef enum { ACCERL_GATE_NONE = 0, ACCERL_GATE_SIGMOID = 1, ACCERL_GATE_SILU =
  *     u = skip x + branch act(gate) after(y),    h = before(u)
  *     norm(z)_i = weight_i (z_i - m) / sqrt(mean_j (z_j - m)^2 + eps),    m = 0 (RMS) or mean_j z_j (LAYER)
  * `after` works on each of `groups` equal parts of a row by itself (the heads of an attention); `before` on the whole row, and with it
- * groups is 1.  eps is positive, 2^-126 at least.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the gate.  1 <= D <= 16384.
+ * groups is 1.  eps is positive, 2^-126 at least.  A NULL weight leaves its norm out (after(y) = y; no h), x NULL the residual, gate_kind NONE the
+ * gate.  1 <= D <= 16384.
  * y, gate, h and their gradients have `dtype`; x, u and theirs `stream_dtype`, which is `dtype` or fp32.  Weights and their
- * gradients are DEVICE fp32 [D].  Arithmetic is fp32; h is taken from u before u is rounded; results are rounded once.  Rows do not
- * touch each other: a NaN stays in its row (and in the weights' gradients).  Rows of an output may lie over rows of an input of the same type and stride, whole, and a
- * weight's gradient over a weight; outputs and the workspace overlap nothing else (ACCERL_EINVAL).
+ * gradients are DEVICE fp32 [D].  Arithmetic is fp32 (finite rows whose sum of squares leaves its range have norms of 0); h is taken from u before u
+ * is rounded; results are rounded once.  Rows do not touch each other: a NaN stays in its row (and in the weights' gradients).  Rows of an output may
+ * lie over rows of an input of the same type and stride, whole, and a weight's gradient over a weight; outputs and the workspace overlap nothing
+ * else (ACCERL_EINVAL).
  * Gradients: of sum(grad_u . u) + sum(grad_h . h), by y, x, gate and both weights (a pointer of NULL: not wanted; grad_u or grad_h NULL: zeros).
  * They start from the forward's inputs: nothing is kept from the forward.  The weights' sums over rows have a fixed order.
  * workspace: of accerl_block_norm_workspace's bytes, needed where gradients of weights are asked for; used as accerl_dense_i8_dynamic's.

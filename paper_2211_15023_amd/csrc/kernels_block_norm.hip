@@ -90,7 +90,8 @@ template <bool GROUP> struct RowSum {
     __device__ __forceinline__ float operator()(float a) { float b = 0.0f; (*this)(a, b); return a; }
 };
 
-// (the reciprocal instruction is off by one in the last place, as the exponential is)
+// (the reciprocal instruction is off by one in the last place, and the exponential by about (1 + |x|) 2^-24 of itself, as its argument is multiplied by log2 e in fp32; what
+// the slopes take of 1 - sigmoid has the last places of 1)
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
 // z -> (z - mean) and the reciprocal root; elements that are not the lane's stay 0

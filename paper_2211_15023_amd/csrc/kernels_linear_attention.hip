@@ -585,7 +585,7 @@ __global__ __launch_bounds__(64 * NW, (LaHalf<T, DX, NW>::SPLIT || DX == 256 ? 2
 // state behind it and the next tiles: on every SIMD one kind's matrix instructions run beside the other's conversions, and either needs half of the registers
 // that one wavefront doing both does, so that two workgroups are on a compute unit.
 // A pair's product, its weight and the state's copy go into the second product as bf16, half a step each (fp16: as two bf16 parts).  64 x 512 tokens, 16 heads of 128,
-// bf16, state wanted: 162 us, 4.1 TB/s of the 4.9 that a copy reaches; vector instructions 47 % of the time, matrix instructions 23 %.  What is left is a chunk's
+// bf16, state wanted: 163 us, 4.1 TB/s of the 4.9 that a copy reaches; vector instructions 47 % of the time, matrix instructions 23 %.  What is left is a chunk's
 // chain of products, barriers and state, which two workgroups a compute unit do not hide altogether.
 template <typename T, int DX>
 struct LaPair {
@@ -845,8 +845,9 @@ __global__ __launch_bounds__((LaPair<T, DX>::THREADS), (LaPair<T, DX>::WAVES)) v
 }
 
 // ---------------------------------------------------------------- tokens of fp32
-// The same walk on fp32 matrix instructions, which are what bounds it: 376 of 32 cycles for a chunk of a head of 128, at 64 columns.
-// 32 x 512 tokens, 16 heads of 128: 412 us.
+// The same walk on fp32 matrix instructions, of 32 cycles each: 304 to 448 for a wavefront and a chunk of a head of 128, at 64 columns.  32 x 512 tokens, 16 heads of 128:
+// 415 us, of which matrix instructions are 38 % and vector instructions 14 %.  The rest is waiting: a comes from memory among the products of its own chunk, wavefronts
+// meet whose products are uneven, and no second workgroup is on the compute unit.
 template <int DX>
 struct LaFloat {
     // rows 16 bytes further on in the banks, for 16-byte reads of 16 rows and for reads of four rows that lie four apart
@@ -1262,9 +1263,9 @@ struct LaPlan { int segs; int64_t seg_len; };
 // Segments of a sequence, worked on side by side, where sequences, heads and columns alone leave compute units without work: what each adds to the state is summed
 // first, so keys and values are read twice, and states go through memory.  From how many chunks on that pays, by workgroups without it:
 //     heads of 128, us whole / in segments     8: 3 chunks, 8, 16          64: 8 chunks, 16, 32          128: 16 chunks, 64        256: 64 chunks
-//     bf16                                     11/16, 21/17, 36/20         23/31, 38/36, 71/46           41/46, 156/132            168/225
-//     fp16                                     14/18, 29/19, 54/22         31/38, 56/46, 106/64          58/64, 222/194            236/339
-//     fp32 (bound by its products)             34/26, 82/27, 161/30        91/54, 175/82, 346/144        177/146, 772/531          785/1009
+//     bf16                                     11/16, 20/17, 36/20         22/32, 37/37, 69/45           39/46, 139/118            156/221
+//     fp16                                     14/17, 30/19, 55/22         31/38, 56/46, 107/63          57/65, 212/193            231/341
+//     fp32 (bound by its chain)                33/25, 81/26, 157/29        84/53, 174/80, 343/135        175/136, 765/519          777/990
 LaPlan la_plan(int64_t B, int64_t T, int H, int slices, bool f32) {
     const int64_t blocks = B * H * slices, chunks = (T + LC - 1) / LC;
     int64_t segs = 1;

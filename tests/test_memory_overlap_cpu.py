@@ -88,23 +88,19 @@ def test_outputs_over_tokens_and_states(A, name, at):
         assert "overlap" in _refused(A, name, out_state=at // 16 * 16)
 
 
-@pytest.mark.parametrize("name", ["linear_attention", "linear_attention_step"])
-@pytest.mark.parametrize("which", ["log_decay", "reset", "lengths"])
+@pytest.mark.parametrize("name,which", [("linear_attention", "log_decay"), ("linear_attention", "reset"), ("linear_attention", "lengths"), ("linear_attention_step", "log_decay"),
+                                        ("linear_attention_step", "reset")])
 def test_outputs_over_what_else_a_call_reads(A, name, which):
-    if which == "lengths" and name == "linear_attention_step":
-        pytest.skip("not looked at")
     assert "overlap" in _refused(A, name, **{which: 20480 + 16})
     assert "overlap" in _refused(A, name, **{which: 24576 + 32})
 
 
-GRADS = ["grad_q", "grad_k", "grad_v", "grad_state"]
+GRADS = {"grad_q": 45056, "grad_k": 49152, "grad_v": 53248, "grad_state": 57344}
 
 
-@pytest.mark.parametrize("which", GRADS)
-@pytest.mark.parametrize("at", [0, 4096, 8192, 12288, 12288 + STATES - 32, 32768, 36864, 36864 + 128, 45056, 49152, 53248, 57344, 57344 + STATES - 32])
+@pytest.mark.parametrize("which,at", [(w, at) for w in GRADS for at in (0, 4096, 8192, 12288, 12288 + STATES - 32, 32768, 36864, 36864 + 128, *GRADS.values(), 57344 + STATES - 32)
+                                      if at // 4096 != GRADS[w] // 4096])
 def test_gradients_over_tokens_states_and_each_other(A, which, at):
-    if at // 4096 == {"grad_q": 11, "grad_k": 12, "grad_v": 13, "grad_state": 14}[which]:
-        pytest.skip("its own place")
     assert "overlap" in _refused(A, "linear_attention_grad", **{which: at})
 
 
@@ -169,11 +165,9 @@ def test_gradients_of_norms_over_the_weights(A, which, at):
     assert "overlaps" in _norm_refused(A, "block_norm_grad", **{which: at})
 
 
-@pytest.mark.parametrize("which,own", [("grad_after", 11264), ("grad_before", 12288)])
-@pytest.mark.parametrize("at", [0, 1024, 2048 + 40, 6144, 7168, 8192, 9216 + 80, 10240, 11264, 11264 + 76, 12288, 12288 - 4, 16384 + 4, 17408 - 4])
-def test_weights_gradients_over_rows_and_weights_in_part(A, which, own, at):
-    if at in (own, {"grad_after": 11264 + 76, "grad_before": 12288 - 4}[which]):
-        pytest.skip("free")
+@pytest.mark.parametrize("which,at", [(w, at) for w in ("grad_after", "grad_before") for at in (0, 1024, 2048 + 40, 6144, 7168, 8192, 9216 + 80, 10240, 16384 + 4, 17408 - 4)] +
+                         [("grad_after", 12288), ("grad_after", 12288 - 4), ("grad_before", 11264), ("grad_before", 11264 + 76)])
+def test_weights_gradients_over_rows_and_weights_in_part(A, which, at):
     assert "overlap" in _norm_refused(A, "block_norm_grad", **{which: at})
 
 
